@@ -413,6 +413,74 @@ gnnk_status gat_aggregate_backward(gnnk_graph_t g, const gnnk_tensor* feat, cons
                                    const gnnk_tensor* grad_out, gnnk_tensor* grad_feat, gnnk_tensor* grad_el,
                                    gnnk_tensor* grad_er, hipStream_t stream);
 /* ------------------------------------------------------------------------ */
+/* Queries and keys of dot-product attention: norms of heads and rotation by
+ * the nodes' positions. */
+
+typedef enum { GNNK_POS_F32 = 0, GNNK_POS_I32 = 1 } gnnk_postype;
+
+/* Positions of the rows of a node tensor on 1 to 4 axes (points in space;
+ * height and width of an image's patches; time, height and width of a video's
+ * cells) and the rotation they make: the first P = pairs[0] + ... pairs of
+ * columns of each head are turned, the first pairs[0] of them by the first
+ * axis, the next pairs[1] by the second and so on.  Pair i is columns
+ * (2i, 2i + 1) with interleaved != 0, else (i, i + P); columns 2P and on stay
+ * as they are.  Row n turns pair i by the angle
+ *   theta = pos[n, axis of i] * freq[i]
+ * (formed and reduced in fp64).  No gradient is formed for positions and
+ * frequencies. */
+typedef struct {
+    const void* pos;      /* (rows, axes), device, of pos_type */
+    int64_t rows;
+    int64_t pos_stride;   /* row stride in elements, >= axes */
+    const float* freq;    /* P values, device */
+    int32_t pos_type;     /* gnnk_postype */
+    int32_t axes;
+    int32_t pairs[4];
+    int32_t interleaved;
+    int32_t reserved;
+} gnnk_rotary;
+
+/* out = x with its pairs turned by their angles (inverse != 0: by the
+ * opposite angles, which is also the gradient).  x and out: (rows, H, F), F at
+ * most 2,048.  Errors: GNNK_EINVAL on shapes, pairs or dtypes. */
+gnnk_status node_rotary(const gnnk_rotary* rot, const gnnk_tensor* x, int32_t inverse, gnnk_tensor* out,
+                        hipStream_t stream);
+
+/* Each head x of a row divided by its root mean square, times a weight per
+ * column, then turned, in one pass:
+ *   out = R(theta) (w * x / sqrt(mean(x^2) + eps))
+ * of q and, unless it is NULL, of k in the same launch.  q: (rows, H, F), wq
+ * (nullable: all ones) one row of (H, F) or (1, F), out_q like q; k may have
+ * other rows and heads but the same F.  rot_q / rot_k (nullable, both or
+ * neither: no rotation) have q's and k's rows and the same pairs and layout.
+ * The sum of a head's squares is fp32.  F is at most 2,048, eps >= 0.
+ * Errors: GNNK_EINVAL. */
+gnnk_status node_norm_rotary(const gnnk_tensor* q, const gnnk_tensor* wq, const gnnk_rotary* rot_q,
+                             gnnk_tensor* out_q, const gnnk_tensor* k, const gnnk_tensor* wk,
+                             const gnnk_rotary* rot_k, gnnk_tensor* out_k, float eps, hipStream_t stream);
+
+/* Gradients of node_norm_rotary.  With r = 1 / sqrt(mean(x^2) + eps) and
+ * g = R(-theta) grad_out,
+ *   grad_x = r (g w - x r^2 mean(g w x))
+ *   grad_w = sum over rows (and heads, for a weight of (1, F)) of g x r
+ * the latter in fp64, rounded once, in a fixed order.  grad_q / grad_wq /
+ * grad_k / grad_wk are nullable and take their operand's shape; grad_out_q and
+ * (with k) grad_out_k are required.  work: device memory of at least
+ * node_norm_rotary_work_bytes bytes, 256-byte aligned, for calls that ask for
+ * a weight gradient (else it may be NULL); it need not be initialised and is
+ * the caller's again once the work queued on `stream` is done. */
+gnnk_status node_norm_rotary_backward(const gnnk_tensor* q, const gnnk_tensor* wq, const gnnk_rotary* rot_q,
+                                      const gnnk_tensor* grad_out_q, gnnk_tensor* grad_q, gnnk_tensor* grad_wq,
+                                      const gnnk_tensor* k, const gnnk_tensor* wk, const gnnk_rotary* rot_k,
+                                      const gnnk_tensor* grad_out_k, gnnk_tensor* grad_k, gnnk_tensor* grad_wk,
+                                      float eps, void* work, size_t work_bytes, hipStream_t stream);
+
+/* Bytes of work that such a call needs for the weight gradients of these
+ * tensors (wq, k and wk nullable; only shapes are read). */
+gnnk_status node_norm_rotary_work_bytes(const gnnk_tensor* q, const gnnk_tensor* wq, const gnnk_tensor* k,
+                                        const gnnk_tensor* wk, size_t* bytes);
+
+/* ------------------------------------------------------------------------ */
 /* Tuning knobs, for schedule comparisons (forcing node- or edge-balanced
  * schedules; the paper's Table 1 states both are valid for commutative and
  * associative reducers).  Process-wide; "seg_edges" applies to graphs created

@@ -1320,3 +1320,273 @@ gnnk_status edge_leaky_relu_backward(const gnnk_tensor* x, const gnnk_tensor* dy
 }
 
 }  // extern "C"
+
+// ---------------------------------------------------------------------------
+// rotary positions and norms of heads
+
+namespace gnnk {
+namespace {
+
+constexpr int ROTARY_MAX_FEAT = 2048;
+constexpr size_t ROTARY_LDS = 32768;     // bytes of a block's cosines and sines, at most
+constexpr int ROTARY_BWD_BLOCKS = 1024;  // blocks that share a backward's rows, each leaving one partial row
+
+bool rotary_ok(const gnnk_rotary* r, int64_t rows, int F) {
+    if (r->rows != rows || r->axes < 1 || r->axes > 4 || (r->pos_type != GNNK_POS_F32 && r->pos_type != GNNK_POS_I32))
+        return false;
+    if (r->pos_stride < r->axes || (rows > 0 && (!r->pos || !r->freq))) return false;
+    int64_t P = 0;
+    for (int a = 0; a < r->axes; ++a) {
+        if (r->pairs[a] < 0) return false;
+        P += r->pairs[a];
+    }
+    return P >= 1 && 2 * P <= F;
+}
+
+bool same_pairs(const gnnk_rotary* a, const gnnk_rotary* b) {
+    if (a->axes != b->axes || (a->interleaved != 0) != (b->interleaved != 0)) return false;
+    for (int i = 0; i < a->axes; ++i)
+        if (a->pairs[i] != b->pairs[i]) return false;
+    return true;
+}
+
+// the geometry that both tensors of a call share; returns the pairs of a lane
+int rotary_geo(RotaryArgs& A, int F, const gnnk_rotary* rot, int dtype) {
+    A.F = F;
+    A.inv_F = 1.0f / (float)F;
+    A.P = 0;
+    for (int a = 0; a < 4; ++a) {
+        A.pairs[a] = rot && a < rot->axes ? rot->pairs[a] : 0;
+        A.P += A.pairs[a];
+    }
+    A.interleaved = rot ? rot->interleaved != 0 : 1;
+    // the widest vectors that divide both the pairs and the columns after
+    // them, 16 bytes (two of them a lane)
+    const int rest = F - 2 * A.P;
+    int V = dtype == 1 ? 8 : 4;
+    while (V > 1 && (A.P % V != 0 || rest % (2 * V) != 0)) V >>= 1;
+    A.NV = A.P / V + (rest + 2 * V - 1) / (2 * V);
+    A.L = std::min(64, pow2ceil(A.NV));
+    A.nchunk = (A.NV + 63) / 64;
+    A.log2L = 0;
+    while ((1 << A.log2L) < A.L) ++A.log2L;
+    return V;
+}
+
+// blocks of one tensor: a block's 256 / L lane groups take HB heads of RB rows
+// at once, and a tile of several such steps where the rows make more than
+// 2,048 blocks (the angles are computed once per tile; 16 steps at most)
+void rotary_blocks(const RotaryArgs& A, RotarySide& S, bool bwd) {
+    const int groups = 256 / A.L;
+    S.HB = std::min(S.H, groups);
+    S.hblocks = (S.H + S.HB - 1) / S.HB;
+    S.RB = groups / S.HB;
+    const int most = A.P > 0 ? (int)(ROTARY_LDS / 8) / A.P : 1 << 20;  // rows whose angles fit
+    S.RB = std::max(1, std::min(S.RB, most));
+    const int64_t steps = std::min<int64_t>(16, std::max<int64_t>(1, S.n * S.hblocks * A.nchunk / (2048 * S.RB)));
+    S.tile_rows = S.RB * (int)std::min<int64_t>(steps, std::max(1, most / S.RB));
+    const int64_t tiles = (S.n + S.tile_rows - 1) / S.tile_rows;
+    S.row_blocks = (int32_t)std::min<int64_t>(tiles, bwd ? ROTARY_BWD_BLOCKS : (1 << 20) / (S.hblocks * A.nchunk));
+    if (bwd) S.row_blocks = std::max(1, S.row_blocks);  // (weight gradients of no rows are written too)
+    S.blocks = S.row_blocks * S.hblocks * A.nchunk;
+    S.dw_parts = S.w_per_head ? S.row_blocks : (int64_t)S.row_blocks * S.hblocks;
+    S.dw_cols = S.w_per_head ? (int64_t)S.H * A.F : A.F;
+}
+
+size_t rotary_lds(const RotaryArgs& A, int V, bool bwd) {
+    size_t n = 0;
+    for (const RotarySide& S : A.side)
+        if (S.blocks) n = std::max(n, (size_t)S.tile_rows * A.P * 8);
+    return bwd ? std::max(n, (size_t)256 * 2 * V * 8) : n;
+}
+
+void rotary_positions(RotarySide& S, const gnnk_rotary* r) {
+    if (!r) return;
+    S.pos = r->pos;
+    S.pos_stride = r->pos_stride;
+    S.pos_i32 = r->pos_type == GNNK_POS_I32;
+    S.freq = r->freq;
+}
+
+// a weight of (H, F) or (1, F) in one row
+bool norm_weight_ok(const gnnk_tensor* w, const gnnk_tensor* x) {
+    return tensor_ok(w) && w->rows == 1 && w->feat == x->feat && (w->heads == x->heads || w->heads == 1);
+}
+
+bool same_shape(const gnnk_tensor* a, const gnnk_tensor* b) {
+    return a->rows == b->rows && a->heads == b->heads && a->feat == b->feat;
+}
+
+bool rotary_size_ok(const gnnk_tensor* x) {
+    return x->rows < ((int64_t)1 << 31) && x->heads <= 1024 && x->feat <= ROTARY_MAX_FEAT;
+}
+
+struct NormSide {
+    const gnnk_tensor *x, *w;
+    const gnnk_rotary* rot;
+    const gnnk_tensor* g;  // backward: the gradient of the output
+    gnnk_tensor *out, *dw; // the output, or the gradients (nullable)
+};
+
+gnnk_status norm_check(const NormSide& s, bool bwd, const char* name) {
+    if (!tensor_ok(s.x) || (s.w && !norm_weight_ok(s.w, s.x)))
+        return fail(GNNK_EINVAL, "%s must be (rows, H, F) and its weight one row of (H, F) or (1, F)", name);
+    if (bwd ? !tensor_ok(s.g) || !same_shape(s.g, s.x) : !s.out)
+        return fail(GNNK_EINVAL, "%s needs %s of its shape", name, bwd ? "a gradient of the output" : "an output");
+    if (s.out && (!tensor_ok(s.out) || !same_shape(s.out, s.x)))
+        return fail(GNNK_EINVAL, "the %s of %s must have its shape", bwd ? "gradient" : "output", name);
+    if (s.dw && (!s.w || !tensor_ok(s.dw) || !same_shape(s.dw, s.w)))
+        return fail(GNNK_EINVAL, "the weight gradient of %s must have its weight's shape", name);
+    if (s.rot && !rotary_ok(s.rot, s.x->rows, s.x->feat))
+        return fail(GNNK_EINVAL, "positions of %s: rows, 1 to 4 axes, and at least one pair within the head", name);
+    if (!rotary_size_ok(s.x))
+        return fail(GNNK_EINVAL, "%s: fewer than 2^31 rows, at most 1024 heads of at most %d columns", name,
+                    ROTARY_MAX_FEAT);
+    return GNNK_OK;
+}
+
+// the sides' arguments and blocks; bytes: of the partial weight gradients
+int norm_args(const NormSide* sides, int n, float eps, bool bwd, RotaryArgs& A, size_t& bytes) {
+    const int V = rotary_geo(A, sides[0].x->feat, sides[0].rot, dtype_code(sides[0].x));
+    A.sign = 1.0f;
+    A.eps = eps;
+    bytes = 0;
+    for (int i = 0; i < n; ++i) {
+        const NormSide& s = sides[i];
+        RotarySide& S = A.side[i];
+        S.x = s.x->data;
+        S.x_stride = s.x->row_stride;
+        S.n = s.x->rows;
+        S.H = s.x->heads;
+        if (s.w) {
+            S.w = s.w->data;
+            S.w_per_head = s.w->heads > 1;
+        }
+        if (s.g) {
+            S.g = s.g->data;
+            S.g_stride = s.g->row_stride;
+        }
+        if (s.out) {
+            S.out = s.out->data;
+            S.out_stride = s.out->row_stride;
+        }
+        rotary_positions(S, s.rot);
+        rotary_blocks(A, S, bwd);
+        if (s.dw) {
+            S.dw = s.dw->data;
+            bytes += ((size_t)S.dw_parts * S.dw_cols * 8 + 255) / 256 * 256;
+        }
+    }
+    return V;
+}
+
+gnnk_status norm_pair_check(const NormSide* sides, int n, float eps, bool bwd) {
+    for (int i = 0; i < n; ++i) {
+        const gnnk_status st = norm_check(sides[i], bwd, i ? "k" : "q");
+        if (st != GNNK_OK) return st;
+        if (!same_dtype({sides[0].x, sides[i].x, sides[i].w, sides[i].g, sides[i].out, sides[i].dw}))
+            return fail(GNNK_EINVAL, "all tensors must share one dtype");
+    }
+    if (!(eps >= 0.0f)) return fail(GNNK_EINVAL, "eps must not be negative");
+    if (n == 2) {
+        if (sides[0].x->feat != sides[1].x->feat) return fail(GNNK_EINVAL, "q and k must have heads of one width");
+        if (!sides[0].rot != !sides[1].rot || (sides[0].rot && !same_pairs(sides[0].rot, sides[1].rot)))
+            return fail(GNNK_EINVAL, "q and k must be turned by the same pairs");
+    }
+    return GNNK_OK;
+}
+
+}  // namespace
+}  // namespace gnnk
+
+extern "C" {
+
+gnnk_status node_rotary(const gnnk_rotary* rot, const gnnk_tensor* x, int32_t inverse, gnnk_tensor* out,
+                        hipStream_t stream) {
+    clear_error();
+    if (!rot || !tensor_ok(x) || !tensor_ok(out)) return fail(GNNK_EINVAL, "malformed tensor or NULL positions");
+    if (!same_shape(x, out) || !same_dtype({x, out})) return fail(GNNK_EINVAL, "out must have x's shape and dtype");
+    if (!rotary_ok(rot, x->rows, x->feat))
+        return fail(GNNK_EINVAL, "positions: x's rows, 1 to 4 axes, and at least one pair within the head");
+    if (!rotary_size_ok(x))
+        return fail(GNNK_EINVAL, "fewer than 2^31 rows, at most 1024 heads of at most %d columns", ROTARY_MAX_FEAT);
+    if (x->rows == 0) return GNNK_OK;
+    RotaryArgs A{};
+    const int V = rotary_geo(A, x->feat, rot, dtype_code(x));
+    A.sign = inverse ? -1.0f : 1.0f;
+    RotarySide& S = A.side[0];
+    S.x = x->data;
+    S.x_stride = x->row_stride;
+    S.out = out->data;
+    S.out_stride = out->row_stride;
+    S.n = x->rows;
+    S.H = x->heads;
+    rotary_positions(S, rot);
+    rotary_blocks(A, S, false);
+    return launch_status(launch_node_rotary(A, dtype_code(x), V, 0, rotary_lds(A, V, false), stream),
+                         "rotary launch");
+}
+
+gnnk_status node_norm_rotary(const gnnk_tensor* q, const gnnk_tensor* wq, const gnnk_rotary* rot_q,
+                             gnnk_tensor* out_q, const gnnk_tensor* k, const gnnk_tensor* wk,
+                             const gnnk_rotary* rot_k, gnnk_tensor* out_k, float eps, hipStream_t stream) {
+    clear_error();
+    const NormSide sides[2] = {{q, wq, rot_q, nullptr, out_q, nullptr}, {k, wk, rot_k, nullptr, out_k, nullptr}};
+    const int n = k ? 2 : 1;
+    gnnk_status st = norm_pair_check(sides, n, eps, false);
+    if (st != GNNK_OK) return st;
+    RotaryArgs A{};
+    size_t bytes;
+    const int V = norm_args(sides, n, eps, false, A, bytes);
+    return launch_status(launch_node_rotary(A, dtype_code(q), V, 1, rotary_lds(A, V, false), stream),
+                         "norm and rotary launch");
+}
+
+gnnk_status node_norm_rotary_backward(const gnnk_tensor* q, const gnnk_tensor* wq, const gnnk_rotary* rot_q,
+                                      const gnnk_tensor* grad_out_q, gnnk_tensor* grad_q, gnnk_tensor* grad_wq,
+                                      const gnnk_tensor* k, const gnnk_tensor* wk, const gnnk_rotary* rot_k,
+                                      const gnnk_tensor* grad_out_k, gnnk_tensor* grad_k, gnnk_tensor* grad_wk,
+                                      float eps, void* work, size_t work_bytes, hipStream_t stream) {
+    clear_error();
+    const NormSide sides[2] = {{q, wq, rot_q, grad_out_q, grad_q, grad_wq}, {k, wk, rot_k, grad_out_k, grad_k, grad_wk}};
+    const int n = k ? 2 : 1;
+    gnnk_status st = norm_pair_check(sides, n, eps, true);
+    if (st != GNNK_OK) return st;
+    RotaryArgs A{};
+    size_t bytes;
+    const int V = norm_args(sides, n, eps, true, A, bytes);
+    if (bytes > 0 && (!work || work_bytes < bytes))
+        return fail(GNNK_ENOMEM, "the weight gradients need %zu bytes of work, %zu given", bytes, work ? work_bytes : 0);
+    if (bytes > 0 && ((uintptr_t)work & 255)) return fail(GNNK_EINVAL, "work must be 256-byte aligned");
+    char* p = static_cast<char*>(work);
+    for (int i = 0; i < n; ++i) {
+        RotarySide& S = A.side[i];
+        if (!sides[i].dw) continue;
+        S.dw_part = reinterpret_cast<double*>(p);
+        p += ((size_t)S.dw_parts * S.dw_cols * 8 + 255) / 256 * 256;
+    }
+    return launch_status(launch_node_rotary(A, dtype_code(q), V, 2, rotary_lds(A, V, true), stream),
+                         "norm and rotary backward launch");
+}
+
+gnnk_status node_norm_rotary_work_bytes(const gnnk_tensor* q, const gnnk_tensor* wq, const gnnk_tensor* k,
+                                        const gnnk_tensor* wk, size_t* bytes) {
+    clear_error();
+    if (!bytes) return fail(GNNK_EINVAL, "NULL argument");
+    *bytes = 0;
+    const gnnk_tensor* x[2] = {q, k};
+    const gnnk_tensor* w[2] = {wq, wk};
+    if (!q) return fail(GNNK_EINVAL, "NULL argument");
+    for (int i = 0; i < 2; ++i) {
+        if (!x[i] || !w[i]) continue;
+        if (x[i]->heads < 1 || x[i]->feat < 1 || x[i]->rows < 0 || !rotary_size_ok(x[i]))
+            return fail(GNNK_EINVAL, "fewer than 2^31 rows, at most 1024 heads of at most %d columns", ROTARY_MAX_FEAT);
+        // a partial row per block that shares the rows, or per block and
+        // heads' block: never more than one of H * F columns per row of blocks
+        const size_t blocks = (size_t)std::min<int64_t>(ROTARY_BWD_BLOCKS, std::max<int64_t>(1, x[i]->rows));
+        *bytes += (blocks * x[i]->heads * x[i]->feat * 8 + 255) / 256 * 256;
+    }
+    return GNNK_OK;
+}
+
+}  // extern "C"

@@ -178,7 +178,7 @@ enum SpecId : int32_t {
     SP_VU = 7,       // a: own row; b: neighbour row            (edge gradient dZ[v] . X[u])
 };
 
-// ----- host-side launchers (spmm.hip, sddmm.hip, edge.hip, gat.hip, softmax.hip, misc.hip) -----
+// ----- host-side launchers (spmm.hip, sddmm.hip, edge.hip, gat.hip, rotary.hip, softmax.hip, misc.hip) -----
 // dtype: 0 fp32, 1 bf16; opk: 0 copy-a, 1 mul-ab, 2 generic; gc: lane groups
 // of a fast spec
 bool fast_vec(int dtype, int vec);
@@ -238,6 +238,40 @@ struct GatBwdArgs {
 };
 hipError_t launch_gat_backward(const EngineArgs& ain, const EngineArgs& aout, const GatBwdArgs& b, int dtype, int vec,
                                int gc, hipStream_t s);
+// rotary positions and norms of heads, rotary.hip: up to two tensors (queries
+// and keys) of one head width in one launch
+struct RotarySide {
+    const void* x;           // (n, H, F) T
+    int64_t x_stride;
+    const void* g;           // backward: gradient of the output
+    int64_t g_stride;
+    void* out;               // the output, or backward the gradient of x (nullable there)
+    int64_t out_stride;
+    const void* w;           // (H or 1, F) weight of the norm, nullable
+    const void* pos;         // (n, axes) fp32 or int32
+    int64_t pos_stride;
+    const float* freq;       // one per pair
+    void* dw;                // backward: gradient of w
+    double* dw_part;         // dw_parts x dw_cols sums of blocks, nullptr: dw not wanted
+    int64_t dw_parts, dw_cols;
+    int64_t n;
+    int32_t H, w_per_head, pos_i32;
+    int32_t HB, hblocks;     // heads per block, blocks per row
+    int32_t RB, tile_rows;   // rows of a block at once, rows of a tile
+    int32_t row_blocks;      // the tiles are dealt to that many blocks
+    int32_t blocks;          // row_blocks * hblocks * nchunk
+};
+struct RotaryArgs {
+    RotarySide side[2];
+    int32_t F, P;            // columns and pairs of a head
+    int32_t NV, L, log2L, nchunk;  // lanes' vectors of a head, lanes of a group, passes over a head
+    int32_t pairs[4];
+    int32_t interleaved;
+    float sign;              // of the angles (rotation alone)
+    float eps, inv_F;
+};
+// mode: 0 rotation alone, 1 norm and rotation, 2 the backward of that
+hipError_t launch_node_rotary(const RotaryArgs& a, int dtype, int vec, int mode, size_t lds, hipStream_t s);
 hipError_t launch_fill_rows(const void* ptr, int ptr64, int64_t n_rows, int64_t n_edges, int32_t* row,
                             hipStream_t s);
 hipError_t launch_sddmm(const EngineArgs& a, int dtype, int vec, int opk, int spec, int gc, hipStream_t s);

@@ -117,6 +117,11 @@ SYMBOLS = {
     "gat_aggregate_backward": [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_float,
                                ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p,
                                ctypes.c_void_p],
+    "node_rotary": [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int32, ctypes.c_void_p, ctypes.c_void_p],
+    "node_norm_rotary": [ctypes.c_void_p] * 8 + [ctypes.c_float, ctypes.c_void_p],
+    "node_norm_rotary_backward": [ctypes.c_void_p] * 12 + [ctypes.c_float, ctypes.c_void_p, ctypes.c_size_t,
+                                                           ctypes.c_void_p],
+    "node_norm_rotary_work_bytes": [ctypes.c_void_p] * 5,
     "graph_scratch_bytes": [ctypes.c_void_p, ctypes.c_int64, ctypes.c_int32, ctypes.c_void_p],
     "graph_attach_scratch": [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_size_t],
     "gnnk_scratch_needed": [ctypes.c_void_p],
@@ -538,3 +543,136 @@ def edge_leaky_relu_backward(x, dy, slope: float = 0.2, dx=None, stream=None):
         dx = torch.empty(x.shape, dtype=dy.dtype, device=dy.device)
     _check(load().edge_leaky_relu_backward(_desc(x), _desc(dy), _desc(dx), slope, _stream(stream)))
     return dx
+
+
+# ---------------------------------------------------------------------------
+# queries and keys of dot-product attention
+
+# gnnk_rotary (pos, rows, pos_stride, freq, pos_type, axes, pairs[4], interleaved, reserved) as bytes
+_ROTARY = struct.Struct("=QqqQIIIIIIII")
+
+
+def _here(*ts):
+    """Refuse tensors of another device than the current one, whose stream the call would run on."""
+    cur = _device() if _device is not None else torch.cuda.current_device()
+    for t in ts:
+        if t is not None and t.is_cuda and t.get_device() != cur:
+            raise ValueError(f"a tensor is on cuda:{t.get_device()}, the current device is cuda:{cur}")
+
+
+class Rotary:
+    """A rotation by positions on one to four axes: pairs[a] pairs of a head's columns are turned by axis a, pair i by
+    pos[row, axis of i] * freq[i].  freq: fp32 on the GPU, one value per pair.  interleaved: pair i is columns
+    (2i, 2i + 1), else (i, i + P), P being the number of pairs; columns from 2P on stay as they are."""
+
+    def __init__(self, freq: torch.Tensor, pairs, interleaved: bool = False):
+        self.pairs = tuple(int(p) for p in pairs)
+        if not 1 <= len(self.pairs) <= 4 or min(self.pairs) < 0 or sum(self.pairs) < 1:
+            raise ValueError("pairs must be one to four counts, not all 0")
+        if not freq.is_cuda:
+            raise ValueError("tensors must be on the GPU")
+        if freq.dtype is not torch.float32 or freq.shape != (sum(self.pairs),):
+            raise ValueError(f"freq must be float32 of shape ({sum(self.pairs)},)")
+        self.freq = freq.detach().contiguous()
+        self.interleaved = bool(interleaved)
+        self._tail = (len(self.pairs), *self.pairs, *(0,) * (4 - len(self.pairs)), int(self.interleaved), 0)
+
+    @classmethod
+    def geometric(cls, pairs, base: float = 10000.0, device="cuda", interleaved: bool = False) -> "Rotary":
+        """Frequencies base ** (-i / pairs[a]), i = 0..pairs[a] - 1, for each axis."""
+        f = [float(base) ** (-torch.arange(int(p), dtype=torch.float64) / max(int(p), 1)) for p in pairs]
+        return cls(torch.cat(f).float().to(device), pairs, interleaved)
+
+    def _desc(self, pos):
+        """gnnk_rotary bytes with the positions of a tensor's rows."""
+        if pos is None:
+            raise ValueError("a rotation needs positions")
+        if pos.dim() == 1:
+            pos = pos.unsqueeze(1)
+        if not pos.is_cuda:
+            raise ValueError("tensors must be on the GPU")
+        if pos.dtype is torch.float32:
+            kind = 0
+        elif pos.dtype is torch.int32:
+            kind = 1
+        else:
+            raise TypeError(f"positions must be float32 or int32, not {pos.dtype}")
+        rows, axes = pos.shape
+        if axes != len(self.pairs):
+            raise ValueError(f"positions have {axes} axes, the rotation {len(self.pairs)}")
+        if pos.requires_grad and torch.is_grad_enabled():
+            raise ValueError("no gradient is formed for positions: detach them")
+        stride = axes
+        if rows:
+            if axes > 1 and pos.stride(1) != 1:
+                raise ValueError("the positions of a row must be contiguous")
+            if rows > 1:
+                if pos.stride(0) < axes:
+                    raise ValueError("row stride of the positions smaller than their axes")
+                stride = pos.stride(0)
+        _here(pos, self.freq)
+        return _ROTARY.pack(pos.data_ptr(), rows, stride, self.freq.data_ptr(), kind, *self._tail)
+
+
+def node_rotary(rot: Rotary, x, pos, inverse: bool = False, out=None, stream=None):
+    """x (rows, H, F) with its pairs of columns turned by the angles of pos (rows, axes), float32 or int32; inverse: by
+    the opposite angles (the gradient)."""
+    x = _as3(x)
+    _here(x, out)
+    if out is None:
+        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+    _check(load().node_rotary(rot._desc(pos), _desc(x), int(inverse), _desc(out), _stream(stream)))
+    return out
+
+
+def _weight3(w):
+    """a weight as one row of (H, F): (F,), (H, F) or (1, H, F)"""
+    if w is None or w.dim() == 3:
+        return w
+    return w.view(1, 1, -1) if w.dim() == 1 else w.unsqueeze(0)
+
+
+def node_norm_rotary(q, wq=None, k=None, wk=None, rot: Rotary = None, pos_q=None, pos_k=None, eps: float = 1e-6,
+                     out_q=None, out_k=None, stream=None):
+    """Each head of q (rows, H, F) divided by its root mean square, times wq ((F,), (H, F) or None), then turned by
+    rot (None: not turned) at pos_q; the same of k, with wk and pos_k, in the same launch.  Returns out_q, or
+    (out_q, out_k) with k."""
+    q, wq, wk = _as3(q), _weight3(wq), _weight3(wk)
+    k = _as3(k) if k is not None else None
+    _here(q, wq, k, wk, out_q, out_k)
+    if out_q is None:
+        out_q = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    if k is not None and out_k is None:
+        out_k = torch.empty(k.shape, dtype=k.dtype, device=k.device)
+    rq = rot._desc(pos_q) if rot is not None else None
+    rk = rot._desc(pos_k) if rot is not None and k is not None else None
+    _check(load().node_norm_rotary(_desc(q), _desc(wq), rq, _desc(out_q), _desc(k), _desc(wk), rk, _desc(out_k), eps,
+                                   _stream(stream)))
+    return (out_q, out_k) if k is not None else out_q
+
+
+def node_norm_rotary_backward(q, wq, grad_q, k=None, wk=None, grad_k=None, rot: Rotary = None, pos_q=None, pos_k=None,
+                              eps: float = 1e-6, want_q: bool = True, want_wq: bool = True, want_k: bool = True,
+                              want_wk: bool = True, stream=None):
+    """Gradients of node_norm_rotary from those of its outputs: (dq, dwq), and with k (dq, dwq, dk, dwk); None where
+    not wanted or without a weight.  Weight gradients have their weight's shape."""
+    q, wq3, wk3, grad_q = _as3(q), _weight3(wq), _weight3(wk), _as3(grad_q)
+    k, grad_k = (_as3(k) if k is not None else None), (_as3(grad_k) if grad_k is not None else None)
+    _here(q, wq3, k, wk3, grad_q, grad_k)
+    like = lambda t, want: torch.empty(t.shape, dtype=t.dtype, device=t.device) if want and t is not None else None
+    dq, dwq, dk, dwk = like(q, want_q), like(wq3, want_wq), like(k, want_k), like(wk3, want_wk and k is not None)
+    rq = rot._desc(pos_q) if rot is not None else None
+    rk = rot._desc(pos_k) if rot is not None and k is not None else None
+    work, nbytes = None, 0
+    if dwq is not None or dwk is not None:
+        need = ctypes.c_size_t(0)
+        _check(load().node_norm_rotary_work_bytes(_desc(q), _desc(dwq), _desc(k), _desc(dwk), ctypes.byref(need)))
+        nbytes = need.value
+        with torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext():
+            work = torch.empty(nbytes, dtype=torch.uint8, device=q.device)
+    _check(load().node_norm_rotary_backward(_desc(q), _desc(wq3), rq, _desc(grad_q), _desc(dq), _desc(dwq), _desc(k),
+                                            _desc(wk3), rk, _desc(grad_k), _desc(dk), _desc(dwk), eps, _ptr(work),
+                                            nbytes, _stream(stream)))
+    dwq = dwq.view(wq.shape) if dwq is not None else None
+    dwk = dwk.view(wk.shape) if dwk is not None else None
+    return (dq, dwq, dk, dwk) if k is not None else (dq, dwq)

@@ -140,6 +140,43 @@ class _FusedGAT(torch.autograd.Function):
         return None, view(dfeat, feat), view(d_el, el), view(d_er, er), None
 
 
+class _Rotary(torch.autograd.Function):
+    """node_rotary; its gradient is the rotation by the opposite angles."""
+
+    @staticmethod
+    def forward(ctx, rot, x, pos):
+        ctx.rot = rot
+        ctx.save_for_backward(pos)
+        return gnnk.node_rotary(rot, x, pos).view(x.shape)
+
+    @staticmethod
+    def backward(ctx, dy):
+        (pos,) = ctx.saved_tensors
+        return None, gnnk.node_rotary(ctx.rot, _c(dy), pos, inverse=True).view(dy.shape), None
+
+
+class _NormRotary(torch.autograd.Function):
+    """node_norm_rotary of queries and keys; the backward takes the norms from
+    the inputs again."""
+
+    @staticmethod
+    def forward(ctx, q, wq, k, wk, rot, pos_q, pos_k, eps):
+        ctx.rot, ctx.eps = rot, eps
+        ctx.save_for_backward(q, wq, k, wk, pos_q, pos_k)
+        oq, ok = gnnk.node_norm_rotary(q, wq, k, wk, rot=rot, pos_q=pos_q, pos_k=pos_k, eps=eps)
+        return oq.view(q.shape), ok.view(k.shape)
+
+    @staticmethod
+    def backward(ctx, gq, gk):
+        q, wq, k, wk, pos_q, pos_k = ctx.saved_tensors
+        nf = ctx.needs_input_grad
+        dq, dwq, dk, dwk = gnnk.node_norm_rotary_backward(q, wq, _c(gq), k, wk, _c(gk), rot=ctx.rot, pos_q=pos_q,
+                                                          pos_k=pos_k, eps=ctx.eps, want_q=nf[0], want_wq=nf[1],
+                                                          want_k=nf[2], want_wk=nf[3])
+        view = lambda t, like: t.view(like.shape) if t is not None else None
+        return view(dq, q), dwq, view(dk, k), dwk, None, None, None, None
+
+
 # ---------------------------------------------------------------------------
 # functional API (same names and argument order as the C ABI)
 
@@ -167,6 +204,17 @@ def leaky_relu(x, slope: float = 0.2):
 def gat_aggregate(g, feat, el, er, slope: float = 0.2):
     """Differentiable fused attention aggregation (gat_aggregate)."""
     return _FusedGAT.apply(g, _c(feat), _c(el), _c(er), float(slope))
+
+
+def rotary(rot, x, pos):
+    """Differentiable rotation of x (rows, H, F) by the positions pos (rows, axes)."""
+    return _Rotary.apply(rot, _c(x), pos)
+
+
+def norm_rotary(q, wq, k, wk, rot=None, pos_q=None, pos_k=None, eps: float = 1e-6):
+    """Differentiable norms of the heads of queries and keys, with weights (F,), (H, F) or None, and their rotation by
+    positions (rot None: none)."""
+    return _NormRotary.apply(_c(q), _c(wq), _c(k), _c(wk), rot, pos_q, pos_k, float(eps))
 
 
 def degrees(g):
