@@ -243,8 +243,9 @@ gnnk_status graph_destroy(gnnk_graph_t g);
  * rows (g-SpMM sum/mean/max/min and their gradients, the fused attention),
  * the winner masks of the max/min backward, the per-(destination, head)
  * records of the fused attention backward, per-edge fp64 running sums of
- * reductions wider than one pass of a wavefront, and the partial rows of the
- * edge-parallel schedules.  The caller lends it, per stream: a call that
+ * reductions wider than one pass of a wavefront, the partial rows of the
+ * edge-parallel schedules, and the states of segments and the records of
+ * dot_aggregate and its backward.  The caller lends it, per stream: a call that
  * needs scratch uses the buffer attached to the handle for the stream it is
  * issued on, front to back; with none, or one too small, it returns
  * GNNK_ENOMEM before launching anything, and gnnk_scratch_needed() tells the
@@ -255,7 +256,8 @@ gnnk_status graph_destroy(gnnk_graph_t g);
 
 enum {
     GNNK_SCRATCH_ARGMAX = 1,     /* include the max/min backward (winner masks: E * ceil(cols / 32) * 4 bytes) */
-    GNNK_SCRATCH_WIDE_SUMS = 2   /* include sums over more than 64 lanes of a row (E * 8 bytes) */
+    GNNK_SCRATCH_WIDE_SUMS = 2   /* include sums over more than 64 lanes of a row (E * 8 bytes), and the gradient
+                                  * of an edge bias that the heads of dot_aggregate share (E * 4 bytes) */
 };
 
 /* Bytes of scratch that any call on this handle with messages of at most
@@ -412,6 +414,45 @@ gnnk_status gat_aggregate_backward(gnnk_graph_t g, const gnnk_tensor* feat, cons
                                    const gnnk_tensor* er, float slope, const gnnk_tensor* stats,
                                    const gnnk_tensor* grad_out, gnnk_tensor* grad_feat, gnnk_tensor* grad_el,
                                    gnnk_tensor* grad_er, hipStream_t stream);
+/* Dot-product attention over the edges: for every destination v and query
+ * head h, with j = h / (H / K) the key head that it shares,
+ *   s[e]      = scale * q[v, h, :] . k[u, j, :] + bias[e, h]
+ *   out[v, h] = sum over in-edges (u, e, v) of softmax_v(s)[e] * v[u, j, :]
+ * in one pass over each destination's in-edges, without writing the scores.
+ * q and out: (num_dst, H, F); k and v: (num_src, K, F), K dividing H; bias
+ * (nullable): (num_edges, H, 1), or (num_edges, 1, 1) for all heads.  A bias
+ * of -inf masks its edge: it weighs nothing, whatever k and v hold there.  A
+ * destination without in-edges, or with every score -inf, gets 0.  stats
+ * (nullable, (num_dst, H, 2), always fp32) receives the maximum score times
+ * log2(e) and the reciprocal of the sum of exp(s - max), (0, 0) where out is 0
+ * for want of edges; dot_aggregate_backward takes it.  Scores and weighted
+ * sums over the edges of one wavefront's share of a row are fp32, the joins of
+ * a long row's segments fp64.  F is at most 256 (fp32) or 512 (bf16) and H * F
+ * at most 65,536 (GNNK_EUNSUPPORTED beyond).  Scratch: partials of hub rows'
+ * segments.  Errors: GNNK_EINVAL on shapes or dtypes. */
+gnnk_status dot_aggregate(gnnk_graph_t g, const gnnk_tensor* q, const gnnk_tensor* k, const gnnk_tensor* v,
+                          const gnnk_tensor* bias, float scale, gnnk_tensor* out, gnnk_tensor* stats,
+                          hipStream_t stream);
+
+/* Gradients of dot_aggregate.  With a the attention recomputed from stats,
+ * da = grad_out[v, h] . v[u, j], S[v, h] = sum over in-edges of a * da and
+ * ds = a * (da - S),
+ *   grad_q[v, h] = scale * sum over in-edges of ds * k[u, j]
+ *   grad_k[u, j] = scale * sum over out-edges and the heads h of j of ds * q[v, h]
+ *   grad_v[u, j] = sum over out-edges and the heads h of j of a * grad_out[v, h]
+ *   grad_bias[e] = ds (its sum over the heads for a bias of (num_edges, 1, 1))
+ * q, k, v, bias and scale as passed to dot_aggregate, out and stats as written
+ * by it; grad_out (num_dst, H, F).  The gradients are nullable and take their
+ * operand's shape; grad_bias needs bias.  Masked edges get and give 0.
+ * Scratch: 16 bytes per (destination, head), partials of hub rows' segments,
+ * and 4 bytes per edge for the gradient of a bias that the heads share where
+ * they take several passes. */
+gnnk_status dot_aggregate_backward(gnnk_graph_t g, const gnnk_tensor* q, const gnnk_tensor* k, const gnnk_tensor* v,
+                                   const gnnk_tensor* bias, float scale, const gnnk_tensor* out,
+                                   const gnnk_tensor* stats, const gnnk_tensor* grad_out, gnnk_tensor* grad_q,
+                                   gnnk_tensor* grad_k, gnnk_tensor* grad_v, gnnk_tensor* grad_bias,
+                                   hipStream_t stream);
+
 /* ------------------------------------------------------------------------ */
 /* Queries and keys of dot-product attention: norms of heads and rotation by
  * the nodes' positions. */

@@ -17,8 +17,8 @@ LIB = os.path.join(HERE, "libgnnk.so")
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 ARCH = "gfx950"
 
-SOURCES = ["spmm.hip", "spmm_ov.hip", "sddmm.hip", "edge.hip", "gat.hip", "rotary.hip", "softmax.hip", "misc.hip",
-           "build.hip", "noalloc.hip", "graph.cpp", "api.cpp"]
+SOURCES = ["spmm.hip", "spmm_ov.hip", "sddmm.hip", "edge.hip", "gat.hip", "dot.hip", "rotary.hip",
+           "softmax.hip", "misc.hip", "build.hip", "noalloc.hip", "graph.cpp", "api.cpp"]
 
 COMMON = ["-O3", "-std=c++17", "-fPIC", "-Wall", "-I", os.path.join(ROOT, "include"), "-I", CSRC]
 # no hand-packed or compiler-packed fp32 math (v_pk_*_f32) on this target

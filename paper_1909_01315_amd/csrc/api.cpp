@@ -623,8 +623,12 @@ gnnk_status graph_scratch_bytes(gnnk_graph_t g, int64_t max_cols, int32_t flags,
                               al(std::max(si * 3 * C * 8, so * 2 * C * 8) + 8));
     if (flags & GNNK_SCRATCH_ARGMAX)  // winner masks, then the reverse pass's partials
         need = std::max(need, al(E * ((C + 31) / 32) * 4) + al(so * C * 8));
-    if (flags & GNNK_SCRATCH_WIDE_SUMS)  // running fp64 sum per edge between passes
-        need = std::max(need, al(E * 8));
+    // dot_aggregate and its backward: states and records as the fused
+    // attention's, in fp32
+    const size_t dot = al((size_t)g->n_dst * C * 16 + 16) + al(std::max(si * 4 * C, so * 2 * C) * 4 + 8);
+    need = std::max(need, dot);
+    if (flags & GNNK_SCRATCH_WIDE_SUMS)  // running sums per edge between passes
+        need = std::max({need, al(E * 8), dot + al(E * 4)});
     if (options().schedule >= 2) {
         // edge-parallel walks: two partial rows per sub-chunk of at least 64
         // positions, or one per row with atomics
@@ -1587,6 +1591,215 @@ gnnk_status node_norm_rotary_work_bytes(const gnnk_tensor* q, const gnnk_tensor*
         *bytes += (blocks * x[i]->heads * x[i]->feat * 8 + 255) / 256 * 256;
     }
     return GNNK_OK;
+}
+
+}  // extern "C"
+
+// ---------------------------------------------------------------------------
+// dot-product attention over the edges
+
+namespace gnnk {
+namespace {
+
+struct DotCall {
+    DotArgs D{};
+    Geo geo;
+    int dt = 0;
+};
+
+// a lane's vectors: the widest of a type, or for narrower heads the largest
+// power of two; a head's last vector starts where it ends with the head
+gnnk_status dot_geo(const gnnk_tensor* q, const gnnk_tensor* k, DotCall& c) {
+    const int F = q->feat;
+    c.dt = dtype_code(q);
+    Geo& geo = c.geo;
+    geo.vec = c.dt == 1 ? 8 : 4;
+    while (geo.vec > F) geo.vec >>= 1;
+    DotArgs& D = c.D;
+    D.H = q->heads;
+    D.K = k->heads;
+    D.R = D.H / D.K;
+    D.F = F;
+    D.FV = (F + geo.vec - 1) / geo.vec;
+    if (D.FV > 64 || (int64_t)D.H * F > 65536)
+        return fail(GNNK_EUNSUPPORTED, "heads of at most %d columns, rows of at most 65536", 64 * geo.vec);
+    const int lanes = pow2ceil(D.FV);
+    while ((1 << D.log2HL) < lanes) ++D.log2HL;
+    D.heads_slice = std::min(D.K, 64 / lanes);
+    D.slices = (D.K + D.heads_slice - 1) / D.heads_slice;
+    geo.F = F;
+    geo.H = D.K;
+    geo.D = (int64_t)D.K * F;
+    geo.L = pow2ceil(D.heads_slice * lanes);
+    while ((1 << geo.log2L) < geo.L) ++geo.log2L;
+    geo.G = 64 / geo.L;
+    geo.FV = D.FV;
+    geo.NV = D.heads_slice * lanes;
+    return GNNK_OK;
+}
+
+gnnk_status dot_check(gnnk_graph_t g, const gnnk_tensor* q, const gnnk_tensor* k, const gnnk_tensor* v,
+                      const gnnk_tensor* bias, const gnnk_tensor* out, const gnnk_tensor* stats) {
+    if (!g) return fail(GNNK_EINVAL, "NULL graph");
+    if (!tensor_ok(q) || !tensor_ok(k) || !tensor_ok(v) || !tensor_ok(out) || (bias && !tensor_ok(bias)))
+        return fail(GNNK_EINVAL, "malformed tensor");
+    if (!same_dtype({q, k, v, bias, out})) return fail(GNNK_EINVAL, "all tensors but stats must share one dtype");
+    if (q->rows != g->n_dst || out->rows != g->n_dst || k->rows != g->n_src || v->rows != g->n_src)
+        return fail(GNNK_EINVAL, "row counts must be num_dst (q, out) and num_src (k, v)");
+    if (k->feat != q->feat || v->feat != q->feat || v->heads != k->heads || q->heads % k->heads != 0 ||
+        !same_shape(q, out))
+        return fail(GNNK_EINVAL, "shapes must be q and out (H, F), k and v (K, F), K dividing H");
+    if (bias && (bias->rows != g->n_edges || bias->feat != 1 || (bias->heads != q->heads && bias->heads != 1)))
+        return fail(GNNK_EINVAL, "bias must be (num_edges, H, 1) or (num_edges, 1, 1)");
+    if (stats && !stats_ok(g, stats, q->heads)) return fail(GNNK_EINVAL, "stats must be (num_dst, H, 2) fp32");
+    return GNNK_OK;
+}
+
+void dot_operands(const gnnk_tensor* q, const gnnk_tensor* k, const gnnk_tensor* v, const gnnk_tensor* bias,
+                  float scale, const gnnk_tensor* stats, DotArgs& D) {
+    D.q = q->data;
+    D.q_stride = q->row_stride;
+    D.k = k->data;
+    D.k_stride = k->row_stride;
+    D.v = v->data;
+    D.v_stride = v->row_stride;
+    if (bias) {
+        D.bias = bias->data;
+        D.bias_stride = bias->row_stride;
+        D.bias_per_head = bias->heads == q->heads;
+    }
+    D.scale = scale;
+    D.scale2 = (float)((double)scale * 1.4426950408889634);
+    if (stats) {
+        D.stats = static_cast<float*>(stats->data);
+        D.stats_stride = stats->row_stride;
+    }
+}
+
+// a walk over d that gathers rows of a and b; returns the lane groups of its
+// compile-time layout, 0 for the runtime one (64-bit addresses)
+int dot_walk(const gnnk_graph* g, const Dir& d, const DotCall& c, const gnnk_tensor* a, const gnnk_tensor* b, bool ids,
+             EngineArgs& A) {
+    A.a = operand(a, K_FULL, T_NBR);
+    A.b = operand(b, K_FULL, T_NBR);
+    A.csr = csr_of(g, d, ids);
+    set_geo(A, c.geo);
+    A.sch = schedule(d, c.geo, true);
+    const int es = c.dt == 1 ? 2 : 4;
+    return !options().no_fast && fast_geo(c.geo, c.dt) && fits32(A.a, a->rows, es) && fits32(A.b, b->rows, es)
+               ? c.geo.G
+               : 0;
+}
+
+}  // namespace
+}  // namespace gnnk
+
+extern "C" {
+
+gnnk_status dot_aggregate(gnnk_graph_t g, const gnnk_tensor* q, const gnnk_tensor* k, const gnnk_tensor* v,
+                          const gnnk_tensor* bias, float scale, gnnk_tensor* out, gnnk_tensor* stats,
+                          hipStream_t stream) {
+    clear_error();
+    gnnk_status st = dot_check(g, q, k, v, bias, out, stats);
+    DotCall c;
+    if (st == GNNK_OK) st = dot_geo(q, k, c);
+    if (st != GNNK_OK || g->n_dst == 0) return st;
+    DotArgs& D = c.D;
+    dot_operands(q, k, v, bias, scale, stats, D);
+    D.out = out->data;
+    D.out_stride = out->row_stride;
+    EngineArgs A{};
+    const int gc = dot_walk(g, g->in_nbr, c, k, v, bias != nullptr, A);
+    D.part_stride = (int64_t)D.H * D.F + 2 * D.H;
+    if (A.sch.n_seg > 0) {
+        Scratch sc = scratch_of(g, stream);
+        D.part = static_cast<float*>(sc.take((size_t)A.sch.n_seg * D.part_stride * 4));
+        if (!D.part) return scratch_fail(sc);
+    }
+    return GNNK_LAUNCH(launch_dot(A, D, 0, c.dt, c.geo.vec, gc, stream), "dot-product attention launch");
+}
+
+static gnnk_status dot_backward(gnnk_graph_t g, const gnnk_tensor* q, const gnnk_tensor* k, const gnnk_tensor* v,
+                                const gnnk_tensor* bias, float scale, const gnnk_tensor* out,
+                                const gnnk_tensor* stats, const gnnk_tensor* grad_out, gnnk_tensor* grad_q,
+                                gnnk_tensor* grad_k, gnnk_tensor* grad_v, gnnk_tensor* grad_bias, hipStream_t stream) {
+    if (!stats) return fail(GNNK_EINVAL, "stats is NULL");
+    gnnk_status st = dot_check(g, q, k, v, bias, out, stats);
+    if (st != GNNK_OK) return st;
+    auto like = [](const gnnk_tensor* a, const gnnk_tensor* b) { return !a || (tensor_ok(a) && same_shape(a, b)); };
+    if (!tensor_ok(grad_out) || !same_shape(grad_out, q)) return fail(GNNK_EINVAL, "grad_out must have q's shape");
+    if (grad_bias && !bias) return fail(GNNK_EINVAL, "grad_bias without bias");
+    if (!like(grad_q, q) || !like(grad_k, k) || !like(grad_v, v) || (grad_bias && !like(grad_bias, bias)))
+        return fail(GNNK_EINVAL, "each gradient must have its operand's shape");
+    if (!same_dtype({q, grad_out, grad_q, grad_k, grad_v, grad_bias}))
+        return fail(GNNK_EINVAL, "all tensors but stats must share one dtype");
+    DotCall c;
+    st = dot_geo(q, k, c);
+    if (st != GNNK_OK) return st;
+    DotArgs& D = c.D;
+    dot_operands(q, k, v, bias, scale, stats, D);
+    D.o = out->data;
+    D.o_stride = out->row_stride;
+    D.dz = grad_out->data;
+    D.dz_stride = grad_out->row_stride;
+    auto grad = [](const gnnk_tensor* t, void*& p, int64_t& stride) {
+        p = t ? t->data : nullptr;
+        stride = t ? t->row_stride : 0;
+    };
+    grad(grad_q, D.d_q, D.d_q_stride);
+    grad(grad_k, D.d_k, D.d_k_stride);
+    grad(grad_v, D.d_v, D.d_v_stride);
+    grad(grad_bias, D.d_bias, D.d_bias_stride);
+    const int64_t W = (int64_t)D.H * D.F, KW = (int64_t)D.K * D.F;
+    EngineArgs ain{}, aout{};
+    const int gin = dot_walk(g, g->in_nbr, c, k, v, bias != nullptr, ain);
+    int gout = dot_walk(g, g->out_fine_nbr, c, q, grad_out, bias != nullptr, aout);
+    if ((int64_t)D.H * 16 >= (1 << 24) || (uint64_t)g->n_dst * D.H * 16 > 0xFFFFFFFFull) gout = 0;
+    // a bias that the heads share: one pass over the edges per slice and query head of it
+    const int passes = grad_bias && !D.bias_per_head ? D.slices * D.R : 1;
+    Scratch sc = scratch_of(g, stream);
+    D.rec = static_cast<float4*>(sc.take((size_t)g->n_dst * D.H * 16 + 16));
+    const size_t pa = (size_t)ain.sch.n_seg * (2 * W + 2 * D.H), pb = (size_t)aout.sch.n_seg * 2 * KW;
+    if (D.rec) D.part = static_cast<float*>(sc.take(std::max(pa, pb) * 4 + 8));
+    if (D.part && passes > 1) D.edge_acc = static_cast<float*>(sc.take((size_t)g->n_edges * 4));
+    if (!D.rec || !D.part || (passes > 1 && !D.edge_acc)) return scratch_fail(sc);
+    aout.x2 = D.rec;
+    aout.x2_stride = D.H;
+    D.part_stride = 2 * W + 2 * D.H;
+    st = GNNK_LAUNCH(launch_dot(ain, D, 1, c.dt, c.geo.vec, gin, stream), "dot-product attention backward launch");
+    if (st == GNNK_OK && (grad_k || grad_v)) {
+        D.part_stride = 2 * KW;
+        st = GNNK_LAUNCH(launch_dot(aout, D, 2, c.dt, c.geo.vec, gout, stream),
+                         "dot-product attention backward launch (sources)");
+    }
+    if (st != GNNK_OK || !grad_bias) return st;
+    const int slices = D.slices;
+    D.r1 = D.R;
+    for (int i = 0; i < passes && st == GNNK_OK; ++i) {
+        if (!D.bias_per_head) {
+            D.slices = 1;
+            D.slice0 = i % slices;
+            D.r0 = i / slices;
+            D.r1 = D.r0 + 1;
+            D.edge_first = i == 0;
+            D.edge_last = i == passes - 1;
+        }
+        st = GNNK_LAUNCH(launch_dot(ain, D, 3, c.dt, c.geo.vec, gin, stream),
+                         "dot-product attention backward launch (edges)");
+    }
+    return st;
+}
+
+gnnk_status dot_aggregate_backward(gnnk_graph_t g, const gnnk_tensor* q, const gnnk_tensor* k, const gnnk_tensor* v,
+                                   const gnnk_tensor* bias, float scale, const gnnk_tensor* out,
+                                   const gnnk_tensor* stats, const gnnk_tensor* grad_out, gnnk_tensor* grad_q,
+                                   gnnk_tensor* grad_k, gnnk_tensor* grad_v, gnnk_tensor* grad_bias,
+                                   hipStream_t stream) {
+    clear_error();
+    if (!g) return fail(GNNK_EINVAL, "NULL graph");
+    return planned(g, stream, [&] {
+        return dot_backward(g, q, k, v, bias, scale, out, stats, grad_out, grad_q, grad_k, grad_v, grad_bias, stream);
+    });
 }
 
 }  // extern "C"

@@ -1,0 +1,852 @@
+// Dot-product attention over a graph's edges, forward and backward:
+//
+//   s_e = scale q[v, h] . k[u, j] + bias[e, h]     (j the key head of query head h)
+//   out[v, h, :] = sum_e softmax(s)_e v[u, j, :]   over the in-edges e = (u, v)
+//
+// in one pass over each destination's in-edges, with the running maximum and
+// sum of the softmax, so no score is written.  An edge gathers one row of keys
+// and one of values; a lane holds VEC columns of a key head, the vectors of a
+// head in a power of two of neighbouring lanes, so that a head's dot product
+// is one shuffle-free reduction and every lane of the head gets it.  Heads
+// beyond one wavefront's lanes are slices of the grid.  Query heads that share
+// a key head are taken one after another by the same lanes.
+//
+// Scores are kept in base 2: the query is scaled by scale * log2(e) once per
+// row.  Dot products and the sums over the edges of one wavefront's share of a
+// row are fp32; the partial results of a long row's segments are joined in
+// fp64 in segment order.
+#include "walk.h"
+
+namespace gnnk {
+
+namespace {
+
+constexpr float LOG2E = 1.44269504088896341f;
+
+template <int CTRL>
+__device__ __forceinline__ float dpp_f(float x) {
+    return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), CTRL, 0xF, 0xF, false));
+}
+constexpr int DPP_HALF_MIRROR = 0x141, DPP_MIRROR = 0x140;
+
+// sums over the aligned run of `red` lanes (a power of two) that holds the
+// lane, of N values at once; every lane gets the totals
+template <int N>
+__device__ __forceinline__ void run_totals(float* v, int red) {
+    if (red >= 2)
+#pragma unroll
+        for (int u = 0; u < N; ++u) v[u] += dpp_f<DPP_QUAD_1032>(v[u]);
+    if (red >= 4)
+#pragma unroll
+        for (int u = 0; u < N; ++u) v[u] += dpp_f<DPP_QUAD_2301>(v[u]);
+    if (red >= 8)
+#pragma unroll
+        for (int u = 0; u < N; ++u) v[u] += dpp_f<DPP_HALF_MIRROR>(v[u]);
+    if (red >= 16)
+#pragma unroll
+        for (int u = 0; u < N; ++u) v[u] += dpp_f<DPP_MIRROR>(v[u]);
+    if (red >= 32)
+#pragma unroll
+        for (int u = 0; u < N; ++u) v[u] += __shfl_xor(v[u], 16, WAVE);
+    if (red >= 64)
+#pragma unroll
+        for (int u = 0; u < N; ++u) v[u] += __shfl_xor(v[u], 32, WAVE);
+}
+
+// a lane's place in the row of key heads (a slice of them)
+struct Place {
+    int j;     // key head
+    int c;     // first column within the head
+    int skip;  // columns that the vector before holds too
+    bool act;  // the lane holds a vector
+    bool first;  // and the head's first one
+};
+template <int VEC>
+__device__ __forceinline__ Place place_of(const DotArgs& D, int lig) {
+    const int hl = lig >> D.log2HL, f = lig & ((1 << D.log2HL) - 1);
+    const int j = (D.slice0 + (int)blockIdx.y) * D.heads_slice + hl;
+    Place p;
+    p.act = hl < D.heads_slice && j < D.K && f < D.FV;
+    p.j = p.act ? j : 0;
+    const int at = f * VEC, last = D.F - VEC;
+    p.c = p.act ? (at < last ? at : last) : 0;
+    p.skip = p.act && at > last ? at - last : 0;
+    p.first = p.act && f == 0;
+    return p;
+}
+
+// a lane's share of a dot product, without the columns it shares
+template <int VEC, bool OV>
+__device__ __forceinline__ float share(const float* x, const float* y, const Place& p) {
+    float s = 0.0f;
+#pragma unroll
+    for (int i = 0; i < VEC; ++i) {
+        if constexpr (OV) s = i < p.skip ? s : fmaf(x[i], y[i], s);
+        else s = fmaf(x[i], y[i], s);
+    }
+    return p.act ? s : 0.0f;
+}
+
+// the bias of an edge in base 2; false: the edge is masked (-inf)
+__device__ __forceinline__ bool bias2(float b, float& out) {
+    float v = b * LOG2E;
+    // (a finite bias stays finite: with a row of the lowest value everywhere
+    // the edges weigh the same, they are not masked)
+    if (fabsf(v) == INFINITY && fabsf(b) != INFINITY) v = copysignf(3.402823466e38f, b);
+    out = v;
+    return b != -INFINITY;
+}
+
+template <typename T>
+__device__ __forceinline__ float load_bias(const DotArgs& D, int32_t ed, int hq) {
+    return IO<T, 1>::load1(reinterpret_cast<const T*>(D.bias) + (uint64_t)(uint32_t)ed * (uint32_t)D.bias_stride +
+                           (D.bias_per_head ? hq : 0));
+}
+
+// scores of N slots of one query head (totals of the shares, plus the bias);
+// gone[u]: the slot lies outside the row or is masked
+template <typename T, int N, bool ALL>
+__device__ __forceinline__ void scores(const DotArgs& D, const float* bs, const bool* ok, float* s, bool* gone) {
+#pragma unroll
+    for (int u = 0; u < N; ++u) gone[u] = ALL ? false : !ok[u];
+    if (D.bias) {
+#pragma unroll
+        for (int u = 0; u < N; ++u) {
+            float b2;
+            gone[u] |= !bias2(bs[u], b2);
+            s[u] += b2;
+        }
+    }
+}
+
+// ---------------------------------------------------------------------------
+// forward
+
+template <typename T, int VEC, bool OV>
+struct Forward {
+    const DotArgs& D;
+    const Place& p;
+    int hq;
+    float q[VEC];
+    float m = -INFINITY, l = 0.0f, acc[VEC];
+
+    __device__ __forceinline__ Forward(const DotArgs& D_, const Place& p_, int hq_, int64_t row)
+        : D(D_), p(p_), hq(hq_) {
+        IO<T, VEC>::load(reinterpret_cast<const T*>(D.q) + row * D.q_stride + (int64_t)hq * D.F + p.c, q);
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) {
+            q[i] *= D.scale2;
+            acc[i] = 0.0f;
+        }
+    }
+    static constexpr bool kBatch = true, kSlots = true;
+    __device__ __forceinline__ void batch(const Raw<VEC>* rw, const int32_t* ed) { take<true>(rw, ed, nullptr); }
+    __device__ __forceinline__ void slots(const Raw<VEC>* rw, const int32_t* ed, const bool* ok) {
+        take<false>(rw, ed, ok);
+    }
+    template <bool ALL>
+    __device__ __forceinline__ void take(const Raw<VEC>* rw, const int32_t* ed, const bool* ok) {
+        float bs[UNR], s[UNR];
+        bool gone[UNR];
+        if (D.bias) {
+#pragma unroll
+            for (int u = 0; u < UNR; ++u) bs[u] = load_bias<T>(D, ed[u], hq);
+        }
+#pragma unroll
+        for (int u = 0; u < UNR; ++u) s[u] = share<VEC, OV>(q, rw[u].a, p);
+        run_totals<UNR>(s, 1 << D.log2HL);
+        scores<T, UNR, ALL>(D, bs, ok, s, gone);
+        float mn = m;
+#pragma unroll
+        for (int u = 0; u < UNR; ++u) {
+            s[u] = gone[u] ? -INFINITY : s[u];
+            mn = fmaxf(mn, s[u]);
+        }
+        const float at = mn == -INFINITY ? 0.0f : mn;
+        if (__ballot(mn > m) != 0ull) {
+            const float f = __builtin_amdgcn_exp2f(m - at);
+            l *= f;
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) acc[i] *= f;
+        }
+#pragma unroll
+        for (int u = 0; u < UNR; ++u) {
+            const float w = __builtin_amdgcn_exp2f(s[u] - at);
+            // (a slot that is gone adds nothing, whatever value it holds)
+            if (!gone[u]) {
+                l += w;
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) acc[i] = fmaf(w, rw[u].b[i], acc[i]);
+            }
+        }
+        m = mn;
+    }
+    // the states of the wavefront's lane groups, pairwise
+    __device__ __forceinline__ void join_groups(int L) {
+        for (int x = L; x < WAVE; x <<= 1) {
+            const float om = __shfl_xor(m, x, WAVE), ol = __shfl_xor(l, x, WAVE);
+            const float mn = fmaxf(m, om), at = mn == -INFINITY ? 0.0f : mn;
+            const float f = __builtin_amdgcn_exp2f(m - at), g = __builtin_amdgcn_exp2f(om - at);
+            l = l * f + ol * g;
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) acc[i] = acc[i] * f + __shfl_xor(acc[i], x, WAVE) * g;
+            m = mn;
+        }
+    }
+};
+
+// out and the statistics of a row's head: the maximum in base 2 and 1 / sum
+__device__ __forceinline__ void write_stats(const DotArgs& D, int64_t row, int hq, float m, float l) {
+    if (!D.stats) return;
+    float* st = D.stats + row * D.stats_stride + 2 * hq;
+    st[0] = l == 0.0f ? 0.0f : m;
+    st[1] = l == 0.0f ? 0.0f : 1.0f / l;
+}
+
+// the row of a wavefront's hub segment or big row (slot: its segment), or of
+// the lane group's small row
+struct Work {
+    int64_t r, b, e;
+    int slot;
+};
+__device__ __forceinline__ Work wave_work(const EngineArgs& A, int w) {
+    Work k;
+    if (w < A.sch.n_seg) {
+        const int4 s = A.csr.segw[w];
+        k = Work{s.x, s.y, s.z, s.w};
+    } else {
+        const int4 t = A.csr.rowt[A.sch.n_hub + (w - A.sch.n_seg)];
+        k = Work{t.x, t.y, t.z, -1};
+    }
+    return Work{uniform64(k.r), uniform64(k.b), uniform64(k.e), k.slot};
+}
+__device__ __forceinline__ Work lane_work(const EngineArgs& A, int w, int G, int g) {
+    const int64_t k = A.sch.n_big + (int64_t)(w - A.sch.w_big_end) * G + g;
+    if (k >= A.sch.n_nz) return Work{-1, 0, 0, -1};
+    const int4 t = A.csr.rowt[k];
+    return Work{t.x, t.y, t.z, -1};
+}
+// rows without edges: fn(row) for each row of this lane group
+template <class F>
+__device__ __forceinline__ void empty_rows(const EngineArgs& A, int w, int G, int g, F fn) {
+    const int64_t k0 = A.sch.n_nz + ((int64_t)(w - A.sch.w_small_end) * G + g) * A.sch.fill_rows_per_group;
+    for (int x = 0; x < A.sch.fill_rows_per_group; ++x)
+        if (k0 + x < A.sch.n_rows) fn((int64_t)A.csr.perm[k0 + x]);
+}
+
+template <typename T, int VEC, class S>
+__global__ __launch_bounds__(256) void dot_forward_kernel(EngineArgs A, DotArgs D) {
+    const int w = wave_id();
+    if (w >= A.sch.w_total) return;
+    const Lanes ln = lanes_of<S::GC>(A.geo);
+    const int G = S::GC > 0 ? S::GC : A.geo.G, L = WAVE / G;
+    const Place p = place_of<VEC>(D, ln.lig);
+    const int kcol = p.j * D.F + p.c;
+    const Pre<VEC> pre{};
+    auto store = [&](int64_t row, int hq, const float* v, float f) {
+        float o[VEC];
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) o[i] = v[i] * f;
+        IO<T, VEC>::store(reinterpret_cast<T*>(D.out) + row * D.out_stride + (int64_t)hq * D.F + p.c, o);
+    };
+    if (w < A.sch.w_big_end) {
+        const Work k = wave_work(A, w);
+        for (int r = 0; r < D.R; ++r) {
+            Forward<T, VEC, S::OV> st(D, p, p.j * D.R + r, k.r);
+            walk_row<T, VEC, 1, EXT_NONE, S>(A, (int32_t)k.r, k.b, k.e, ln.g, G, kcol, 0, pre, st);
+            st.join_groups(L);
+            if (ln.g != 0 || !p.act) continue;
+            if (k.slot >= 0) {
+                float* P = D.part + (int64_t)k.slot * D.part_stride;
+                for (int i = 0; i < VEC; ++i) P[(int64_t)st.hq * D.F + p.c + i] = st.acc[i];
+                if (p.first) {
+                    float* ml = P + (int64_t)D.H * D.F + 2 * st.hq;
+                    ml[0] = st.m;
+                    ml[1] = st.l;
+                }
+            } else {
+                store(k.r, st.hq, st.acc, st.l == 0.0f ? 0.0f : 1.0f / st.l);
+                if (p.first) write_stats(D, k.r, st.hq, st.m, st.l);
+            }
+        }
+    } else if (w < A.sch.w_small_end) {
+        const Work k = lane_work(A, w, G, ln.g);
+        const int64_t self = k.r >= 0 ? k.r : 0;
+        for (int r = 0; r < D.R; ++r) {
+            Forward<T, VEC, S::OV> st(D, p, p.j * D.R + r, self);
+            walk_lane<T, VEC, 1, EXT_NONE, S>(A, (int32_t)self, k.b, k.e, kcol, 0, pre, st);
+            if (k.r < 0 || !p.act) continue;
+            store(k.r, st.hq, st.acc, st.l == 0.0f ? 0.0f : 1.0f / st.l);
+            if (p.first) write_stats(D, k.r, st.hq, st.m, st.l);
+        }
+    } else {
+        empty_rows(A, w, G, ln.g, [&](int64_t row) {
+            const float zero[VEC] = {};
+            for (int r = 0; r < D.R && p.act; ++r) {
+                store(row, p.j * D.R + r, zero, 0.0f);
+                if (p.first) write_stats(D, row, p.j * D.R + r, 0.0f, 0.0f);
+            }
+        });
+    }
+}
+
+// Hub rows: the states of a row's segments joined.  A workgroup takes `cols`
+// columns of one row, its threads the columns of every (threads / cols)-th
+// segment; the runs are then joined in order.  A few columns and many runs
+// where rows have many segments (one node of 100,000 edges has 1,563).
+template <typename T>
+__global__ void dot_join_kernel(EngineArgs A, DotArgs D, int cols) {
+    __shared__ float sm[1024];
+    __shared__ double sl[1024], sa[1024];
+    const int t = threadIdx.x, runs = blockDim.x / cols, run = t / cols;
+    const int64_t W = (int64_t)D.H * D.F, col = (int64_t)blockIdx.y * cols + (t - run * cols);
+    const int64_t row = A.csr.perm[blockIdx.x];
+    const int s0 = A.csr.hub_off[blockIdx.x], s1 = A.csr.hub_off[blockIdx.x + 1];
+    const bool ok = col < W;
+    const int hq = ok ? (int)(col / D.F) : 0;
+    float m = -INFINITY;
+    double l = 0.0, a = 0.0;
+    auto add = [&](float om, double ol, double oa) {
+        const float mn = fmaxf(m, om), at = mn == -INFINITY ? 0.0f : mn;
+        const double f = (double)__builtin_amdgcn_exp2f(m - at), g = (double)__builtin_amdgcn_exp2f(om - at);
+        l = l * f + ol * g;
+        a = a * f + oa * g;
+        m = mn;
+    };
+    if (ok) {
+        constexpr int U = 4;
+        for (int s = s0 + run; s < s1; s += U * runs) {
+            float pm[U], pl[U], pa[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int x = s + u * runs;
+                const float* P = D.part + (int64_t)(x < s1 ? x : s) * D.part_stride;
+                pm[u] = P[W + 2 * hq];
+                pl[u] = P[W + 2 * hq + 1];
+                pa[u] = P[col];
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (s + u * runs < s1) add(pm[u], (double)pl[u], (double)pa[u]);
+        }
+    }
+    sm[t] = m;
+    sl[t] = l;
+    sa[t] = a;
+    __syncthreads();
+    if (run != 0 || !ok) return;
+    for (int k = 1; k < runs; ++k) add(sm[t + k * cols], sl[t + k * cols], sa[t + k * cols]);
+    IO<T, 1>::store1(reinterpret_cast<T*>(D.out) + row * D.out_stride + col, l == 0.0 ? 0.0f : (float)(a / l));
+    if (col % D.F == 0) write_stats(D, row, hq, m, (float)l);
+}
+
+// ---------------------------------------------------------------------------
+// backward
+//
+//   da_e = dout[v] . v[u],  S = sum_in a_e da_e,  ds_e = a_e (da_e - S)
+//   dq[v] = scale sum_in ds_e k[u]     dbias_e = ds_e
+//   dk[u] = scale sum_out ds_e q[v]    dv[u] = sum_out a_e dout[v]
+//
+// a_e is recomputed from the forward's statistics.  The destination pass
+// takes S0 = dout[v] . out[v], which is S but for the rounding of out, and
+// sums w = a (da - S0), w k and a k; with delta = sum w, S = S0 + delta and
+// dq = scale (sum w k - delta sum a k): what a bf16 out lost is put right, and
+// no large values cancel.  It leaves a record {max, 1 / sum, S} per
+// destination and head for the source pass, which walks the reverse graph's
+// CSR and gathers q, dout and the record.
+
+template <typename T, int VEC, bool OV>
+struct ToDst {
+    const DotArgs& D;
+    const Place& p;
+    int hq;
+    float q[VEC], dz[VEC], m, il, S0;
+    float e1[VEC], e2[VEC], delta = 0.0f;
+
+    __device__ __forceinline__ ToDst(const DotArgs& D_, const Place& p_, int hq_, int64_t row)
+        : D(D_), p(p_), hq(hq_) {
+        const int64_t c = (int64_t)hq * D.F + p.c;
+        float o[VEC];
+        IO<T, VEC>::load(reinterpret_cast<const T*>(D.q) + row * D.q_stride + c, q);
+        IO<T, VEC>::load(reinterpret_cast<const T*>(D.dz) + row * D.dz_stride + c, dz);
+        IO<T, VEC>::load(reinterpret_cast<const T*>(D.o) + row * D.o_stride + c, o);
+        m = D.stats[row * D.stats_stride + 2 * hq];
+        il = D.stats[row * D.stats_stride + 2 * hq + 1];
+        S0 = share<VEC, OV>(dz, o, p);
+        run_totals<1>(&S0, 1 << D.log2HL);
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) {
+            q[i] *= D.scale2;
+            e1[i] = e2[i] = 0.0f;
+        }
+    }
+    static constexpr bool kBatch = true, kSlots = true;
+    __device__ __forceinline__ void batch(const Raw<VEC>* rw, const int32_t* ed) { take<true>(rw, ed, nullptr); }
+    __device__ __forceinline__ void slots(const Raw<VEC>* rw, const int32_t* ed, const bool* ok) {
+        take<false>(rw, ed, ok);
+    }
+    template <bool ALL>
+    __device__ __forceinline__ void take(const Raw<VEC>* rw, const int32_t* ed, const bool* ok) {
+        float bs[UNR], s[2 * UNR];
+        bool gone[UNR];
+        if (D.bias) {
+#pragma unroll
+            for (int u = 0; u < UNR; ++u) bs[u] = load_bias<T>(D, ed[u], hq);
+        }
+#pragma unroll
+        for (int u = 0; u < UNR; ++u) {
+            s[u] = share<VEC, OV>(q, rw[u].a, p);
+            s[UNR + u] = share<VEC, OV>(dz, rw[u].b, p);
+        }
+        run_totals<2 * UNR>(s, 1 << D.log2HL);
+        scores<T, UNR, ALL>(D, bs, ok, s, gone);
+#pragma unroll
+        for (int u = 0; u < UNR; ++u) {
+            const float a = __builtin_amdgcn_exp2f(s[u] - m) * il, w = a * (s[UNR + u] - S0);
+            if (!gone[u]) {
+                delta += w;
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) {
+                    e1[i] = fmaf(w, rw[u].a[i], e1[i]);
+                    e2[i] = fmaf(a, rw[u].a[i], e2[i]);
+                }
+            }
+        }
+    }
+    __device__ __forceinline__ void join_groups(int L) {
+        for (int x = L; x < WAVE; x <<= 1) {
+            delta += __shfl_xor(delta, x, WAVE);
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) {
+                e1[i] += __shfl_xor(e1[i], x, WAVE);
+                e2[i] += __shfl_xor(e2[i], x, WAVE);
+            }
+        }
+    }
+    __device__ __forceinline__ void write(int64_t row) const {
+        if (D.d_q) {
+            float v[VEC];
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) v[i] = D.scale * (e1[i] - delta * e2[i]);
+            IO<T, VEC>::store(reinterpret_cast<T*>(D.d_q) + row * D.d_q_stride + (int64_t)hq * D.F + p.c, v);
+        }
+        if (p.first) D.rec[row * D.H + hq] = make_float4(m, il, S0 + delta, 0.0f);
+    }
+};
+
+// gradients of the bias, edge by edge, once the records are complete; of a
+// bias that the heads share, the sum over this pass's heads, added to those of
+// the passes before (their sums by edge id in D.edge_acc)
+template <typename T, int VEC, bool OV>
+struct ToEdge {
+    const DotArgs& D;
+    const Place& p;
+    int hq, L;
+    float q[VEC], dz[VEC];
+    float4 rec;
+
+    __device__ __forceinline__ ToEdge(const DotArgs& D_, const Place& p_, int hq_, int64_t row, int L_)
+        : D(D_), p(p_), hq(hq_), L(L_) {
+        const int64_t c = (int64_t)hq * D.F + p.c;
+        IO<T, VEC>::load(reinterpret_cast<const T*>(D.q) + row * D.q_stride + c, q);
+        IO<T, VEC>::load(reinterpret_cast<const T*>(D.dz) + row * D.dz_stride + c, dz);
+        rec = D.rec[row * D.H + hq];
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) q[i] *= D.scale2;
+    }
+    static constexpr bool kBatch = true, kSlots = true;
+    __device__ __forceinline__ void batch(const Raw<VEC>* rw, const int32_t* ed) { take<true>(rw, ed, nullptr); }
+    __device__ __forceinline__ void slots(const Raw<VEC>* rw, const int32_t* ed, const bool* ok) {
+        take<false>(rw, ed, ok);
+    }
+    template <bool ALL>
+    __device__ __forceinline__ void take(const Raw<VEC>* rw, const int32_t* ed, const bool* ok) {
+        float bs[UNR], s[2 * UNR], ds[UNR];
+        bool gone[UNR];
+#pragma unroll
+        for (int u = 0; u < UNR; ++u) bs[u] = load_bias<T>(D, ed[u], hq);
+#pragma unroll
+        for (int u = 0; u < UNR; ++u) {
+            s[u] = share<VEC, OV>(q, rw[u].a, p);
+            s[UNR + u] = share<VEC, OV>(dz, rw[u].b, p);
+        }
+        run_totals<2 * UNR>(s, 1 << D.log2HL);
+        scores<T, UNR, ALL>(D, bs, ok, s, gone);
+#pragma unroll
+        for (int u = 0; u < UNR; ++u) {
+            ds[u] = __builtin_amdgcn_exp2f(s[u] - rec.x) * rec.y * (s[UNR + u] - rec.z);
+            ds[u] = gone[u] ? 0.0f : ds[u];
+        }
+        if (D.bias_per_head) {
+#pragma unroll
+            for (int u = 0; u < UNR; ++u)
+                if (p.first && (ALL || ok[u]))
+                    IO<T, 1>::store1(reinterpret_cast<T*>(D.d_bias) +
+                                         (uint64_t)(uint32_t)ed[u] * (uint32_t)D.d_bias_stride + hq, ds[u]);
+            return;
+        }
+#pragma unroll
+        for (int u = 0; u < UNR; ++u) ds[u] = p.first ? ds[u] : 0.0f;
+        run_totals<UNR>(ds, L);
+        if (__lane_id() & (L - 1)) return;
+#pragma unroll
+        for (int u = 0; u < UNR; ++u) {
+            if (!ALL && !ok[u]) continue;
+            float x = ds[u];
+            if (!D.edge_first) x += D.edge_acc[(uint32_t)ed[u]];
+            if (D.edge_last)
+                IO<T, 1>::store1(reinterpret_cast<T*>(D.d_bias) +
+                                     (uint64_t)(uint32_t)ed[u] * (uint32_t)D.d_bias_stride, x);
+            else D.edge_acc[(uint32_t)ed[u]] = x;
+        }
+    }
+};
+
+template <typename T, int VEC, class S>
+__global__ __launch_bounds__(256) void dot_backward_dst_kernel(EngineArgs A, DotArgs D) {
+    const int w = wave_id();
+    if (w >= A.sch.w_total) return;
+    const Lanes ln = lanes_of<S::GC>(A.geo);
+    const int G = S::GC > 0 ? S::GC : A.geo.G, L = WAVE / G;
+    const Place p = place_of<VEC>(D, ln.lig);
+    const int kcol = p.j * D.F + p.c;
+    const Pre<VEC> pre{};
+    if (w < A.sch.w_big_end) {
+        const Work k = wave_work(A, w);
+        for (int r = 0; r < D.R; ++r) {
+            ToDst<T, VEC, S::OV> st(D, p, p.j * D.R + r, k.r);
+            walk_row<T, VEC, 1, EXT_NONE, S>(A, (int32_t)k.r, k.b, k.e, ln.g, G, kcol, 0, pre, st);
+            st.join_groups(L);
+            if (ln.g != 0 || !p.act) continue;
+            if (k.slot >= 0) {
+                float* P = D.part + (int64_t)k.slot * D.part_stride;
+                const int64_t W = (int64_t)D.H * D.F, c = (int64_t)st.hq * D.F + p.c;
+                for (int i = 0; i < VEC; ++i) {
+                    P[c + i] = st.e1[i];
+                    P[W + c + i] = st.e2[i];
+                }
+                if (p.first) {
+                    P[2 * W + 2 * st.hq] = st.delta;
+                    P[2 * W + 2 * st.hq + 1] = st.S0;
+                }
+            } else {
+                st.write(k.r);
+            }
+        }
+    } else if (w < A.sch.w_small_end) {
+        const Work k = lane_work(A, w, G, ln.g);
+        const int64_t self = k.r >= 0 ? k.r : 0;
+        for (int r = 0; r < D.R; ++r) {
+            ToDst<T, VEC, S::OV> st(D, p, p.j * D.R + r, self);
+            walk_lane<T, VEC, 1, EXT_NONE, S>(A, (int32_t)self, k.b, k.e, kcol, 0, pre, st);
+            if (k.r >= 0 && p.act) st.write(k.r);
+        }
+    } else if (D.d_q) {
+        empty_rows(A, w, G, ln.g, [&](int64_t row) {
+            const float zero[VEC] = {};
+            for (int r = 0; r < D.R && p.act; ++r)
+                IO<T, VEC>::store(reinterpret_cast<T*>(D.d_q) + row * D.d_q_stride +
+                                      (int64_t)(p.j * D.R + r) * D.F + p.c, zero);
+        });
+    }
+}
+
+// the destination pass's hub rows, laid out as in dot_join_kernel
+template <typename T>
+__global__ void dot_join_dst_kernel(EngineArgs A, DotArgs D, int cols) {
+    __shared__ double s1m[1024], s2m[1024], sdm[1024];
+    const int t = threadIdx.x, runs = blockDim.x / cols, run = t / cols;
+    const int64_t W = (int64_t)D.H * D.F, col = (int64_t)blockIdx.y * cols + (t - run * cols);
+    const int64_t row = A.csr.perm[blockIdx.x];
+    const int s0 = A.csr.hub_off[blockIdx.x], s1 = A.csr.hub_off[blockIdx.x + 1];
+    const bool ok = col < W;
+    const int hq = ok ? (int)(col / D.F) : 0;
+    double x1 = 0.0, x2 = 0.0, dl = 0.0;
+    if (ok) {
+        constexpr int U = 4;
+        for (int s = s0 + run; s < s1; s += U * runs) {
+            float p1[U], p2[U], pd[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int x = s + u * runs;
+                const float* P = D.part + (int64_t)(x < s1 ? x : s) * D.part_stride;
+                p1[u] = P[col];
+                p2[u] = P[W + col];
+                pd[u] = P[2 * W + 2 * hq];
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (s + u * runs < s1) {
+                    x1 += (double)p1[u];
+                    x2 += (double)p2[u];
+                    dl += (double)pd[u];
+                }
+        }
+    }
+    s1m[t] = x1;
+    s2m[t] = x2;
+    sdm[t] = dl;
+    __syncthreads();
+    if (run != 0 || !ok) return;
+    for (int k = 1; k < runs; ++k) {
+        x1 += s1m[t + k * cols];
+        x2 += s2m[t + k * cols];
+        dl += sdm[t + k * cols];
+    }
+    if (D.d_q)
+        IO<T, 1>::store1(reinterpret_cast<T*>(D.d_q) + row * D.d_q_stride + col,
+                         (float)((double)D.scale * (x1 - dl * x2)));
+    if (col % D.F == 0) {
+        const float* st = D.stats + row * D.stats_stride + 2 * hq;
+        const float S0 = D.part[(int64_t)s0 * D.part_stride + 2 * W + 2 * hq + 1];
+        D.rec[row * D.H + hq] = make_float4(st[0], st[1], (float)((double)S0 + dl), 0.0f);
+    }
+}
+
+// query heads r0 .. r1 - 1 of each key head
+template <typename T, int VEC, class S>
+__global__ __launch_bounds__(256) void dot_backward_edge_kernel(EngineArgs A, DotArgs D) {
+    const int w = wave_id();
+    if (w >= A.sch.w_small_end) return;
+    const Lanes ln = lanes_of<S::GC>(A.geo);
+    const int G = S::GC > 0 ? S::GC : A.geo.G, L = WAVE / G;
+    const Place p = place_of<VEC>(D, ln.lig);
+    const int kcol = p.j * D.F + p.c, r0 = D.r0, r1 = D.r1;
+    const Pre<VEC> pre{};
+    if (w < A.sch.w_big_end) {
+        const Work k = wave_work(A, w);
+        for (int r = r0; r < r1; ++r) {
+            ToEdge<T, VEC, S::OV> st(D, p, p.j * D.R + r, k.r, L);
+            walk_row<T, VEC, 1, EXT_NONE, S>(A, (int32_t)k.r, k.b, k.e, ln.g, G, kcol, 0, pre, st);
+        }
+    } else {
+        const Work k = lane_work(A, w, G, ln.g);
+        const int64_t self = k.r >= 0 ? k.r : A.csr.rowt[0].x;
+        for (int r = r0; r < r1; ++r) {
+            ToEdge<T, VEC, S::OV> st(D, p, p.j * D.R + r, self, L);
+            walk_lane<T, VEC, 1, EXT_NONE, S>(A, (int32_t)self, k.b, k.e, kcol, 0, pre, st);
+        }
+    }
+}
+
+// the source pass: dk and dv of a row over its out-edges
+template <typename T, int VEC, bool OV>
+struct ToSrc {
+    const DotArgs& D;
+    const Place& p;
+    int hq = 0;
+    float k[VEC], v[VEC];
+    float dk[VEC], dv[VEC];
+
+    __device__ __forceinline__ ToSrc(const DotArgs& D_, const Place& p_, int64_t row) : D(D_), p(p_) {
+        const int64_t c = (int64_t)p.j * D.F + p.c;
+        IO<T, VEC>::load(reinterpret_cast<const T*>(D.k) + row * D.k_stride + c, k);
+        IO<T, VEC>::load(reinterpret_cast<const T*>(D.v) + row * D.v_stride + c, v);
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) {
+            k[i] *= D.scale2;
+            dk[i] = dv[i] = 0.0f;
+        }
+    }
+    static constexpr bool kBatch = true, kSlots = true;
+    __device__ __forceinline__ void batch(const Raw<VEC>* rw, const int32_t* ed) { take<true>(rw, ed, nullptr); }
+    __device__ __forceinline__ void slots(const Raw<VEC>* rw, const int32_t* ed, const bool* ok) {
+        take<false>(rw, ed, ok);
+    }
+    template <bool ALL>
+    __device__ __forceinline__ void take(const Raw<VEC>* rw, const int32_t* ed, const bool* ok) {
+        float bs[UNR], s[2 * UNR];
+        bool gone[UNR];
+        if (D.bias) {
+#pragma unroll
+            for (int u = 0; u < UNR; ++u) bs[u] = load_bias<T>(D, ed[u], hq);
+        }
+#pragma unroll
+        for (int u = 0; u < UNR; ++u) {
+            s[u] = share<VEC, OV>(k, rw[u].a, p);
+            s[UNR + u] = share<VEC, OV>(v, rw[u].b, p);
+        }
+        run_totals<2 * UNR>(s, 1 << D.log2HL);
+        scores<T, UNR, ALL>(D, bs, ok, s, gone);
+#pragma unroll
+        for (int u = 0; u < UNR; ++u) {
+            const float a = __builtin_amdgcn_exp2f(s[u] - rw[u].rec.x) * rw[u].rec.y;
+            const float w = a * (s[UNR + u] - rw[u].rec.z);
+            if (!gone[u]) {
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) {
+                    dk[i] = fmaf(w, rw[u].a[i], dk[i]);
+                    dv[i] = fmaf(a, rw[u].b[i], dv[i]);
+                }
+            }
+        }
+    }
+    __device__ __forceinline__ void join_groups(int L) {
+        for (int x = L; x < WAVE; x <<= 1)
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) {
+                dk[i] += __shfl_xor(dk[i], x, WAVE);
+                dv[i] += __shfl_xor(dv[i], x, WAVE);
+            }
+    }
+    __device__ __forceinline__ void write(int64_t row) {
+        const int64_t c = (int64_t)p.j * D.F + p.c;
+#pragma unroll
+        for (int i = 0; i < VEC; ++i) dk[i] *= D.scale;
+        if (D.d_k) IO<T, VEC>::store(reinterpret_cast<T*>(D.d_k) + row * D.d_k_stride + c, dk);
+        if (D.d_v) IO<T, VEC>::store(reinterpret_cast<T*>(D.d_v) + row * D.d_v_stride + c, dv);
+    }
+};
+
+template <typename T, int VEC, class S>
+__global__ __launch_bounds__(256) void dot_backward_src_kernel(EngineArgs A, DotArgs D) {
+    const int w = wave_id();
+    if (w >= A.sch.w_total) return;
+    const Lanes ln = lanes_of<S::GC>(A.geo);
+    const int G = S::GC > 0 ? S::GC : A.geo.G, L = WAVE / G;
+    const Place p = place_of<VEC>(D, ln.lig);
+    const Pre<VEC> pre{};
+    if (w < A.sch.w_big_end) {
+        const Work k = wave_work(A, w);
+        ToSrc<T, VEC, S::OV> st(D, p, k.r);
+        for (int r = 0; r < D.R; ++r) {
+            st.hq = p.j * D.R + r;
+            walk_row<T, VEC, 1, EXT_REC, S>(A, (int32_t)k.r, k.b, k.e, ln.g, G, st.hq * D.F + p.c, st.hq, pre, st);
+        }
+        st.join_groups(L);
+        if (ln.g != 0 || !p.act) return;
+        if (k.slot >= 0) {
+            float* P = D.part + (int64_t)k.slot * D.part_stride;
+            const int64_t W = (int64_t)D.K * D.F, c = (int64_t)p.j * D.F + p.c;
+            for (int i = 0; i < VEC; ++i) {
+                P[c + i] = st.dk[i];
+                P[W + c + i] = st.dv[i];
+            }
+        } else {
+            st.write(k.r);
+        }
+    } else if (w < A.sch.w_small_end) {
+        const Work k = lane_work(A, w, G, ln.g);
+        const int64_t self = k.r >= 0 ? k.r : 0;
+        ToSrc<T, VEC, S::OV> st(D, p, self);
+        for (int r = 0; r < D.R; ++r) {
+            st.hq = p.j * D.R + r;
+            walk_lane<T, VEC, 1, EXT_REC, S>(A, (int32_t)self, k.b, k.e, st.hq * D.F + p.c, st.hq, pre, st);
+        }
+        if (k.r >= 0 && p.act) st.write(k.r);
+    } else {
+        empty_rows(A, w, G, ln.g, [&](int64_t row) {
+            const float zero[VEC] = {};
+            const int64_t c = (int64_t)p.j * D.F + p.c;
+            if (!p.act) return;
+            if (D.d_k) IO<T, VEC>::store(reinterpret_cast<T*>(D.d_k) + row * D.d_k_stride + c, zero);
+            if (D.d_v) IO<T, VEC>::store(reinterpret_cast<T*>(D.d_v) + row * D.d_v_stride + c, zero);
+        });
+    }
+}
+
+// the source pass's hub rows, laid out as in dot_join_kernel
+template <typename T>
+__global__ void dot_join_src_kernel(EngineArgs A, DotArgs D, int cols) {
+    __shared__ double red[1024];
+    const int t = threadIdx.x, runs = blockDim.x / cols, run = t / cols;
+    const int64_t W = (int64_t)D.K * D.F, col = (int64_t)blockIdx.y * cols + (t - run * cols);
+    const int64_t row = A.csr.perm[blockIdx.x];
+    const int s0 = A.csr.hub_off[blockIdx.x], s1 = A.csr.hub_off[blockIdx.x + 1];
+    const bool ok = col < 2 * W;
+    double x = 0.0;
+    if (ok) {
+        constexpr int U = 4;
+        for (int s = s0 + run; s < s1; s += U * runs) {
+            float y[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                y[u] = D.part[(int64_t)(s + u * runs < s1 ? s + u * runs : s) * D.part_stride + col];
+#pragma unroll
+            for (int u = 0; u < U; ++u)
+                if (s + u * runs < s1) x += (double)y[u];
+        }
+    }
+    red[t] = x;
+    __syncthreads();
+    if (run != 0 || !ok) return;
+    for (int k = 1; k < runs; ++k) x += red[t + k * cols];
+    if (col < W) {
+        if (D.d_k)
+            IO<T, 1>::store1(reinterpret_cast<T*>(D.d_k) + row * D.d_k_stride + col, (float)((double)D.scale * x));
+    } else if (D.d_v) {
+        IO<T, 1>::store1(reinterpret_cast<T*>(D.d_v) + row * D.d_v_stride + (col - W), (float)x);
+    }
+}
+
+// ---------------------------------------------------------------------------
+
+template <int C, bool OV>
+using SpDot = Spec<T_NBR, OK_FULL, T_NBR, OK_FULL, C, false, true, OV>;
+
+template <typename T, int V>
+constexpr bool dot_fast = V == (sizeof(T) == 4 ? 4 : 8);
+
+// columns and threads of a workgroup that joins segments
+struct Join {
+    int cols, threads;
+    dim3 grid(const EngineArgs& a, int64_t width) const {
+        return dim3((unsigned)a.sch.n_hub, (unsigned)((width + cols - 1) / cols));
+    }
+};
+Join join_of(const EngineArgs& a) {
+    const bool many = a.sch.n_seg > 64ll * a.sch.n_hub;
+    return many ? Join{16, 1024} : Join{64, 256};
+}
+
+template <typename T, int V, class S>
+void dot_pass(const EngineArgs& a, const DotArgs& d, int pass, hipStream_t s) {
+    const dim3 grid(blocks_for_waves(a.sch.w_total), (unsigned)d.slices), block(WAVE * WPB);
+    const Join j = join_of(a);
+    const int64_t HF = (int64_t)d.H * d.F, KF = (int64_t)d.K * d.F;
+    if (pass == 0) {
+        hipLaunchKernelGGL((dot_forward_kernel<T, V, S>), grid, block, 0, s, a, d);
+        if (a.sch.n_hub > 0)
+            hipLaunchKernelGGL((dot_join_kernel<T>), j.grid(a, HF), dim3(j.threads), 0, s, a, d, j.cols);
+    } else if (pass == 1) {
+        hipLaunchKernelGGL((dot_backward_dst_kernel<T, V, S>), grid, block, 0, s, a, d);
+        if (a.sch.n_hub > 0)
+            hipLaunchKernelGGL((dot_join_dst_kernel<T>), j.grid(a, HF), dim3(j.threads), 0, s, a, d, j.cols);
+    } else if (pass == 2) {
+        hipLaunchKernelGGL((dot_backward_src_kernel<T, V, S>), grid, block, 0, s, a, d);
+        if (a.sch.n_hub > 0)
+            hipLaunchKernelGGL((dot_join_src_kernel<T>), j.grid(a, 2 * KF), dim3(j.threads), 0, s, a, d, j.cols);
+    } else {
+        const dim3 egrid(blocks_for_waves(a.sch.w_small_end), (unsigned)d.slices);
+        hipLaunchKernelGGL((dot_backward_edge_kernel<T, V, S>), egrid, block, 0, s, a, d);
+    }
+}
+
+template <typename T, int V>
+void dot_t(const EngineArgs& a, const DotArgs& d, int pass, int gc, hipStream_t s) {
+    if constexpr (dot_fast<T, V>) {
+        if (gc > 0 && d.F % V == 0) {
+            GNNK_GC_DISPATCH(gc, dot_pass<T, V, SpDot<C, false>>(a, d, pass, s))
+            return;
+        }
+        if (gc > 0) {
+            GNNK_GC_DISPATCH(gc, dot_pass<T, V, SpDot<C, true>>(a, d, pass, s))
+            return;
+        }
+    }
+    dot_pass<T, V, SpDot<0, true>>(a, d, pass, s);
+}
+
+}  // namespace
+
+hipError_t launch_dot(const EngineArgs& a, const DotArgs& d, int pass, int dtype, int vec, int gc, hipStream_t s) {
+    if (a.sch.w_total <= 0 || (pass == 3 && a.sch.w_small_end <= 0)) return hipSuccess;
+    if (dtype == 0) {
+        GNNK_VEC_DISPATCH_F32(vec, dot_t<float, V>(a, d, pass, gc, s))
+    } else {
+        GNNK_VEC_DISPATCH_BF16(vec, dot_t<bf16_t, V>(a, d, pass, gc, s))
+    }
+    return hipGetLastError();
+}
+
+}  // namespace gnnk

@@ -178,7 +178,8 @@ enum SpecId : int32_t {
     SP_VU = 7,       // a: own row; b: neighbour row            (edge gradient dZ[v] . X[u])
 };
 
-// ----- host-side launchers (spmm.hip, sddmm.hip, edge.hip, gat.hip, rotary.hip, softmax.hip, misc.hip) -----
+// ----- host-side launchers (spmm.hip, sddmm.hip, edge.hip, gat.hip, dot.hip, rotary.hip, softmax.hip,
+// misc.hip) -----
 // dtype: 0 fp32, 1 bf16; opk: 0 copy-a, 1 mul-ab, 2 generic; gc: lane groups
 // of a fast spec
 bool fast_vec(int dtype, int vec);
@@ -238,6 +239,43 @@ struct GatBwdArgs {
 };
 hipError_t launch_gat_backward(const EngineArgs& ain, const EngineArgs& aout, const GatBwdArgs& b, int dtype, int vec,
                                int gc, hipStream_t s);
+// dot-product attention, dot.hip: A walks the in-CSR (a = k, b = v at the
+// neighbour; the forward, pass 1 and pass 3) or the reverse graph's CSR (a =
+// q, b = dout at the neighbour, x2 = rec; pass 2)
+struct DotArgs {
+    const void* q;           // (N_dst, H, F) T
+    int64_t q_stride;
+    const void* k;           // (N_src, K, F) T
+    int64_t k_stride;
+    const void* v;
+    int64_t v_stride;
+    const void* bias;        // (E, H or 1) T, nullable
+    int64_t bias_stride;
+    void* out;               // forward: (N_dst, H, F) T
+    int64_t out_stride;
+    float* stats;            // (N_dst, H, 2) fp32: maximum score in base 2 and 1 / sum (forward: nullable)
+    int64_t stats_stride;
+    const void* o;           // backward: the forward's out
+    int64_t o_stride;
+    const void* dz;          // backward: gradient of out
+    int64_t dz_stride;
+    void *d_q, *d_k, *d_v, *d_bias;  // gradients, nullable
+    int64_t d_q_stride, d_k_stride, d_v_stride, d_bias_stride;
+    float4* rec;             // backward: (N_dst, H) {max, 1 / sum, S, 0}
+    float* part;             // partial results of hub segments
+    int64_t part_stride;
+    float* edge_acc;         // pass 3, a bias that the heads share in several passes: sums by edge id
+    float scale, scale2;     // of the scores; times log2(e)
+    int32_t H, K, R, F;      // query heads, key heads, query heads per key head, columns
+    int32_t FV, log2HL;      // vectors of a head, log2 of the lanes they take
+    int32_t heads_slice, slices, slice0;  // key heads of a slice, slices of a launch, its first one
+    int32_t bias_per_head;
+    int32_t r0, r1;          // pass 3: query heads of each key head
+    int32_t edge_first, edge_last;  // pass 3 of a shared bias: the first, the last of its passes
+    int32_t pad;
+};
+// pass: 0 forward, 1 backward by destination, 2 by source, 3 by edge
+hipError_t launch_dot(const EngineArgs& a, const DotArgs& d, int pass, int dtype, int vec, int gc, hipStream_t s);
 // rotary positions and norms of heads, rotary.hip: up to two tensors (queries
 // and keys) of one head width in one launch
 struct RotarySide {

@@ -117,6 +117,8 @@ SYMBOLS = {
     "gat_aggregate_backward": [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_float,
                                ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p,
                                ctypes.c_void_p],
+    "dot_aggregate": [ctypes.c_void_p] * 5 + [ctypes.c_float] + [ctypes.c_void_p] * 3,
+    "dot_aggregate_backward": [ctypes.c_void_p] * 5 + [ctypes.c_float] + [ctypes.c_void_p] * 8,
     "node_rotary": [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_int32, ctypes.c_void_p, ctypes.c_void_p],
     "node_norm_rotary": [ctypes.c_void_p] * 8 + [ctypes.c_float, ctypes.c_void_p],
     "node_norm_rotary_backward": [ctypes.c_void_p] * 12 + [ctypes.c_float, ctypes.c_void_p, ctypes.c_size_t,
@@ -676,3 +678,39 @@ def node_norm_rotary_backward(q, wq, grad_q, k=None, wk=None, grad_k=None, rot: 
     dwq = dwq.view(wq.shape) if dwq is not None else None
     dwk = dwk.view(wk.shape) if dwk is not None else None
     return (dq, dwq, dk, dwk) if k is not None else (dq, dwq)
+
+
+def dot_aggregate(g: Graph, q, k, v, bias=None, scale: float = None, out=None, stats=None, want_stats: bool = False,
+                  stream=None):
+    """Dot-product attention over the in-edges: out[v, h] = sum of softmax_v(scale q[v, h].k[u, j] + bias[e, h]) *
+    v[u, j], j being the key head that query head h shares.  q (num_dst, H, F), k and v (num_src, K, F), bias
+    (num_edges, H or 1, 1), -inf masking an edge; scale: default 1 / sqrt(F).  Returns out, with want_stats (or stats
+    given) followed by the per-row statistics (num_dst, H, 2) fp32 that dot_aggregate_backward takes."""
+    q, k, v = _as3(q), _as3(k), _as3(v)
+    bias = _as3(bias) if bias is not None else None
+    _here(q, k, v, bias, out, stats)
+    if scale is None:
+        scale = q.shape[2] ** -0.5
+    if out is None:
+        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+    if want_stats and stats is None:
+        stats = torch.empty((g.num_dst, q.shape[1], 2), dtype=torch.float32, device=q.device)
+    _run(g, stream, load().dot_aggregate, g.handle, _desc(q), _desc(k), _desc(v), _desc(bias), scale, _desc(out),
+         _desc(stats))
+    return (out, stats) if stats is not None else out
+
+
+def dot_aggregate_backward(g: Graph, q, k, v, out, stats, grad_out, bias=None, scale: float = None,
+                           want_q: bool = True, want_k: bool = True, want_v: bool = True, want_bias: bool = True,
+                           stream=None):
+    """(dq, dk, dv, dbias) of dot_aggregate from its output and statistics (None where not wanted, or without bias)."""
+    q, k, v, out, grad_out = _as3(q), _as3(k), _as3(v), _as3(out), _as3(grad_out)
+    bias = _as3(bias) if bias is not None else None
+    _here(q, k, v, bias, out, stats, grad_out)
+    if scale is None:
+        scale = q.shape[2] ** -0.5
+    like = lambda t, want: torch.empty(t.shape, dtype=t.dtype, device=t.device) if want and t is not None else None
+    dq, dk, dv, db = like(q, want_q), like(k, want_k), like(v, want_v), like(bias, want_bias)
+    _run(g, stream, load().dot_aggregate_backward, g.handle, _desc(q), _desc(k), _desc(v), _desc(bias), scale,
+         _desc(out), _desc(stats), _desc(grad_out), _desc(dq), _desc(dk), _desc(dv), _desc(db))
+    return dq, dk, dv, db

@@ -15,6 +15,8 @@ the aggregation layers of the paper's experiments built from them:
   RelGraphConv  R-GCN aggregation: per-relation transformed source rows
                 gathered by (relation, source) on a bipartite encoding and
                 summed with 1/in-degree-per-relation weights
+  DotAttentionConv  multi-head attention by dot products of queries and keys,
+                normed per head and turned by the nodes' positions
 
 Dense projections (the node-wise update) are ordinary torch layers.  Graph
 handles come from gnnk.Graph; the caller keeps them alive while tensors that
@@ -177,6 +179,27 @@ class _NormRotary(torch.autograd.Function):
         return view(dq, q), dwq, view(dk, k), dwk, None, None, None, None
 
 
+class _DotAggregate(torch.autograd.Function):
+    """dot_aggregate keeping its output and per-row statistics; the backward
+    recomputes the attention from them, no tensor of E x H scores is formed."""
+
+    @staticmethod
+    def forward(ctx, g, q, k, v, bias, scale):
+        out, stats = gnnk.dot_aggregate(g, q, k, v, bias=bias, scale=scale, want_stats=True)
+        ctx.g, ctx.scale = g, scale
+        ctx.save_for_backward(q, k, v, bias, out, stats)
+        return out
+
+    @staticmethod
+    def backward(ctx, dout):
+        q, k, v, bias, out, stats = ctx.saved_tensors
+        nf = ctx.needs_input_grad
+        grads = gnnk.dot_aggregate_backward(ctx.g, q, k, v, out, stats, _c(dout), bias=bias, scale=ctx.scale,
+                                            want_q=nf[1], want_k=nf[2], want_v=nf[3], want_bias=nf[4])
+        view = lambda t, like: t.view(like.shape) if t is not None else None
+        return (None, *(view(t, x) for t, x in zip(grads, (q, k, v, bias))), None)
+
+
 # ---------------------------------------------------------------------------
 # functional API (same names and argument order as the C ABI)
 
@@ -215,6 +238,11 @@ def norm_rotary(q, wq, k, wk, rot=None, pos_q=None, pos_k=None, eps: float = 1e-
     """Differentiable norms of the heads of queries and keys, with weights (F,), (H, F) or None, and their rotation by
     positions (rot None: none)."""
     return _NormRotary.apply(_c(q), _c(wq), _c(k), _c(wk), rot, pos_q, pos_k, float(eps))
+
+
+def dot_aggregate(g, q, k, v, bias=None, scale: float = None):
+    """Differentiable dot-product attention over the in-edges (dot_aggregate)."""
+    return _DotAggregate.apply(g, _c(q), _c(k), _c(v), _c(bias), scale)
 
 
 def degrees(g):
@@ -312,6 +340,51 @@ class RelGraphConv(torch.nn.Module):
         xr = torch.matmul(x.unsqueeze(0), self.weight).reshape(self.R * x.shape[0], 1, -1)  # (R, N, out)
         out = gspmm(g_rel, "mul", "sum", xr, norm).view(g_rel.num_dst, -1)
         return out + self.loop(x[: g_rel.num_dst]) if self.loop is not None else out
+
+
+class DotAttentionConv(torch.nn.Module):
+    """Multi-head dot-product attention over the in-edges: queries of the
+    destinations, keys and values of the sources, kv_heads of them shared by
+    num_heads query heads.  Queries and keys are normed per head (qk_norm) and
+    turned by the nodes' positions (axis_pairs: pairs of a head's columns per
+    axis) in one pass; an edge bias is added to the scores, -inf masking its
+    edge.  Where sources and destinations differ, the destinations come first
+    among the sources (as in SAGEConv)."""
+
+    def __init__(self, in_feats: int, out_feats: int, num_heads: int, kv_heads: int = None, qk_norm: bool = True,
+                 axis_pairs=None, base: float = 10000.0, interleaved: bool = False, eps: float = 1e-6):
+        super().__init__()
+        self.H, self.K, self.F = num_heads, kv_heads or num_heads, out_feats
+        if self.H % self.K:
+            raise ValueError("kv_heads must divide num_heads")
+        if axis_pairs is not None and 2 * sum(axis_pairs) > out_feats:
+            raise ValueError("more pairs than a head's columns hold")
+        self.fc_q = torch.nn.Linear(in_feats, out_feats * self.H, bias=False)
+        self.fc_k = torch.nn.Linear(in_feats, out_feats * self.K, bias=False)
+        self.fc_v = torch.nn.Linear(in_feats, out_feats * self.K, bias=False)
+        self.norm_q = torch.nn.Parameter(torch.ones(out_feats)) if qk_norm else None
+        self.norm_k = torch.nn.Parameter(torch.ones(out_feats)) if qk_norm else None
+        self.axis_pairs, self.base, self.interleaved, self.eps = axis_pairs, base, interleaved, eps
+        self._rotary = {}  # device -> gnnk.Rotary (fp32 frequencies whatever the layer's type)
+
+    def rotary(self, device):
+        if self.axis_pairs is None:
+            return None
+        if device not in self._rotary:
+            self._rotary[device] = gnnk.Rotary.geometric(self.axis_pairs, self.base, device, self.interleaved)
+        return self._rotary[device]
+
+    def forward(self, g, x, pos=None, bias=None):
+        q = self.fc_q(x[: g.num_dst]).view(-1, self.H, self.F)
+        k = self.fc_k(x).view(-1, self.K, self.F)
+        v = self.fc_v(x).view(-1, self.K, self.F)
+        rot = self.rotary(x.device)
+        pos_q = pos[: g.num_dst] if pos is not None else None
+        if self.norm_q is not None:
+            q, k = norm_rotary(q, self.norm_q, k, self.norm_k, rot, pos_q, pos, self.eps)
+        elif rot is not None:
+            q, k = rotary(rot, q, pos_q), rotary(rot, k, pos)
+        return dot_aggregate(g, q, k, v, bias)
 
 
 def rel_norm(etype, dst, num_rels: int, num_dst: int):
