@@ -628,7 +628,7 @@ gnnk_status graph_scratch_bytes(gnnk_graph_t g, int64_t max_cols, int32_t flags,
     const size_t dot = al((size_t)g->n_dst * C * 16 + 16) + al(std::max(si * 4 * C, so * 2 * C) * 4 + 8);
     need = std::max(need, dot);
     if (flags & GNNK_SCRATCH_WIDE_SUMS)  // running sums per edge between passes
-        need = std::max({need, al(E * 8), dot + al(E * 4)});
+        need = std::max({need, al(E * 8), dot + al(E * 4 + 8)});
     if (options().schedule >= 2) {
         // edge-parallel walks: two partial rows per sub-chunk of at least 64
         // positions, or one per row with atomics
@@ -1608,34 +1608,51 @@ struct DotCall {
 };
 
 // a lane's vectors: the widest of a type, or for narrower heads the largest
-// power of two; a head's last vector starts where it ends with the head
+// power of two; a head's last vector ends with the head
 gnnk_status dot_geo(const gnnk_tensor* q, const gnnk_tensor* k, DotCall& c) {
     const int F = q->feat;
     c.dt = dtype_code(q);
-    Geo& geo = c.geo;
-    geo.vec = c.dt == 1 ? 8 : 4;
-    while (geo.vec > F) geo.vec >>= 1;
+    c.geo.vec = c.dt == 1 ? 8 : 4;
+    while (c.geo.vec > F) c.geo.vec >>= 1;
     DotArgs& D = c.D;
     D.H = q->heads;
     D.K = k->heads;
     D.R = D.H / D.K;
     D.F = F;
-    D.FV = (F + geo.vec - 1) / geo.vec;
+    D.FV = (F + c.geo.vec - 1) / c.geo.vec;
     if (D.FV > 64 || (int64_t)D.H * F > 65536)
-        return fail(GNNK_EUNSUPPORTED, "heads of at most %d columns, rows of at most 65536", 64 * geo.vec);
-    const int lanes = pow2ceil(D.FV);
-    while ((1 << D.log2HL) < lanes) ++D.log2HL;
+        return fail(GNNK_EUNSUPPORTED, "heads of at most %d columns, rows of at most 65536", 64 * c.geo.vec);
+    while ((1 << D.log2HL) < D.FV) ++D.log2HL;
+    return GNNK_OK;
+}
+
+// the lanes of a pass: RC query heads of a key head in a lane's registers, RL
+// (a power of two) in lanes beside each other
+void dot_lanes(DotCall& c, int RC, int RL) {
+    DotArgs& D = c.D;
+    Geo& geo = c.geo;
+    D.RC = RC;
+    D.log2RL = 0;
+    while ((1 << D.log2RL) < RL) ++D.log2RL;
+    const int lanes = RL << D.log2HL;
     D.heads_slice = std::min(D.K, 64 / lanes);
     D.slices = (D.K + D.heads_slice - 1) / D.heads_slice;
-    geo.F = F;
+    D.slice0 = 0;
+    geo.F = D.F;
     geo.H = D.K;
-    geo.D = (int64_t)D.K * F;
-    geo.L = pow2ceil(D.heads_slice * lanes);
-    while ((1 << geo.log2L) < geo.L) ++geo.log2L;
-    geo.G = 64 / geo.L;
+    geo.D = (int64_t)D.K * D.F;
     geo.FV = D.FV;
     geo.NV = D.heads_slice * lanes;
-    return GNNK_OK;
+    geo.L = pow2ceil(geo.NV);
+    geo.log2L = 0;
+    while ((1 << geo.log2L) < geo.L) ++geo.log2L;
+    geo.G = 64 / geo.L;
+}
+
+// the largest of 1..most that divides R
+int dot_share(int R, int most) {
+    while (R % most) --most;
+    return most;
 }
 
 gnnk_status dot_check(gnnk_graph_t g, const gnnk_tensor* q, const gnnk_tensor* k, const gnnk_tensor* v,
@@ -1709,7 +1726,9 @@ gnnk_status dot_aggregate(gnnk_graph_t g, const gnnk_tensor* q, const gnnk_tenso
     D.out = out->data;
     D.out_stride = out->row_stride;
     EngineArgs A{};
+    dot_lanes(c, dot_share(D.R, 4), 1);
     const int gc = dot_walk(g, g->in_nbr, c, k, v, bias != nullptr, A);
+    if (!gc) D.RC = 1;
     D.part_stride = (int64_t)D.H * D.F + 2 * D.H;
     if (A.sch.n_seg > 0) {
         Scratch sc = scratch_of(g, stream);
@@ -1751,40 +1770,53 @@ static gnnk_status dot_backward(gnnk_graph_t g, const gnnk_tensor* q, const gnnk
     grad(grad_v, D.d_v, D.d_v_stride);
     grad(grad_bias, D.d_bias, D.d_bias_stride);
     const int64_t W = (int64_t)D.H * D.F, KW = (int64_t)D.K * D.F;
-    EngineArgs ain{}, aout{};
-    const int gin = dot_walk(g, g->in_nbr, c, k, v, bias != nullptr, ain);
-    int gout = dot_walk(g, g->out_fine_nbr, c, q, grad_out, bias != nullptr, aout);
+    const bool ids = bias != nullptr;
+    // by destination
+    EngineArgs ain{}, aout{}, aedge{};
+    DotCall in = c, src = c, edge = c;
+    dot_lanes(in, dot_share(D.R, 2), 1);
+    const int gin = dot_walk(g, g->in_nbr, in, k, v, ids, ain);
+    if (!gin) in.D.RC = 1;
+    // by source: the query heads of a key head in lanes beside each other, as
+    // many as a power of two that divides them and one wavefront hold
+    int RL = 1;
+    while (D.R % (2 * RL) == 0 && (2 * RL) << D.log2HL <= 64) RL *= 2;
+    dot_lanes(src, 1, RL);
+    int gout = dot_walk(g, g->out_fine_nbr, src, q, grad_out, ids, aout);
     if ((int64_t)D.H * 16 >= (1 << 24) || (uint64_t)g->n_dst * D.H * 16 > 0xFFFFFFFFull) gout = 0;
-    // a bias that the heads share: one pass over the edges per slice and query head of it
-    const int passes = grad_bias && !D.bias_per_head ? D.slices * D.R : 1;
+    // the gradient of the bias: in that pass, unless the heads that share it
+    // take several, in which it is summed over the slices and query heads
+    const bool by_edge = grad_bias && !D.bias_per_head && (src.D.slices > 1 || RL < D.R);
+    src.D.src_bias = grad_bias && !by_edge;
+    dot_lanes(edge, 1, 1);
+    const int gedge = dot_walk(g, g->in_nbr, edge, k, v, true, aedge);
+    const int passes = by_edge ? edge.D.slices * D.R : 0;
+
     Scratch sc = scratch_of(g, stream);
-    D.rec = static_cast<float4*>(sc.take((size_t)g->n_dst * D.H * 16 + 16));
+    float4* rec = static_cast<float4*>(sc.take((size_t)g->n_dst * D.H * 16 + 16));
     const size_t pa = (size_t)ain.sch.n_seg * (2 * W + 2 * D.H), pb = (size_t)aout.sch.n_seg * 2 * KW;
-    if (D.rec) D.part = static_cast<float*>(sc.take(std::max(pa, pb) * 4 + 8));
-    if (D.part && passes > 1) D.edge_acc = static_cast<float*>(sc.take((size_t)g->n_edges * 4));
-    if (!D.rec || !D.part || (passes > 1 && !D.edge_acc)) return scratch_fail(sc);
-    aout.x2 = D.rec;
+    float* part = rec ? static_cast<float*>(sc.take(std::max(pa, pb) * 4 + 8)) : nullptr;
+    float* acc = part && passes > 1 ? static_cast<float*>(sc.take((size_t)g->n_edges * 4 + 8)) : nullptr;
+    if (!rec || !part || (passes > 1 && !acc)) return scratch_fail(sc);
+    in.D.rec = src.D.rec = edge.D.rec = rec;
+    in.D.part = src.D.part = part;
+    in.D.part_stride = 2 * W + 2 * D.H;
+    src.D.part_stride = 2 * KW;
+    aout.x2 = rec;
     aout.x2_stride = D.H;
-    D.part_stride = 2 * W + 2 * D.H;
-    st = GNNK_LAUNCH(launch_dot(ain, D, 1, c.dt, c.geo.vec, gin, stream), "dot-product attention backward launch");
-    if (st == GNNK_OK && (grad_k || grad_v)) {
-        D.part_stride = 2 * KW;
-        st = GNNK_LAUNCH(launch_dot(aout, D, 2, c.dt, c.geo.vec, gout, stream),
+    st = GNNK_LAUNCH(launch_dot(ain, in.D, 1, c.dt, c.geo.vec, gin, stream), "dot-product attention backward launch");
+    if (st == GNNK_OK && (grad_k || grad_v || src.D.src_bias))
+        st = GNNK_LAUNCH(launch_dot(aout, src.D, 2, c.dt, c.geo.vec, gout, stream),
                          "dot-product attention backward launch (sources)");
-    }
-    if (st != GNNK_OK || !grad_bias) return st;
-    const int slices = D.slices;
-    D.r1 = D.R;
+    const int slices = edge.D.slices;
+    edge.D.edge_acc = acc;
+    edge.D.slices = 1;
     for (int i = 0; i < passes && st == GNNK_OK; ++i) {
-        if (!D.bias_per_head) {
-            D.slices = 1;
-            D.slice0 = i % slices;
-            D.r0 = i / slices;
-            D.r1 = D.r0 + 1;
-            D.edge_first = i == 0;
-            D.edge_last = i == passes - 1;
-        }
-        st = GNNK_LAUNCH(launch_dot(ain, D, 3, c.dt, c.geo.vec, gin, stream),
+        edge.D.slice0 = i % slices;
+        edge.D.r0 = i / slices;
+        edge.D.edge_first = i == 0;
+        edge.D.edge_last = i == passes - 1;
+        st = GNNK_LAUNCH(launch_dot(aedge, edge.D, 3, c.dt, c.geo.vec, gedge, stream),
                          "dot-product attention backward launch (edges)");
     }
     return st;

@@ -8,8 +8,10 @@
 // and one of values; a lane holds VEC columns of a key head, the vectors of a
 // head in a power of two of neighbouring lanes, so that a head's dot product
 // is one shuffle-free reduction and every lane of the head gets it.  Heads
-// beyond one wavefront's lanes are slices of the grid.  Query heads that share
-// a key head are taken one after another by the same lanes.
+// beyond one wavefront's lanes are slices of the grid.  Of the R query heads
+// that share a key head, a lane takes RC at once in registers (each key and
+// value row is then gathered and widened once for them), RL neighbouring runs
+// of lanes take as many beside each other, and what is left takes turns.
 //
 // Scores are kept in base 2: the query is scaled by scale * log2(e) once per
 // row.  Dot products and the sums over the edges of one wavefront's share of a
@@ -53,9 +55,10 @@ __device__ __forceinline__ void run_totals(float* v, int red) {
         for (int u = 0; u < N; ++u) v[u] += __shfl_xor(v[u], 32, WAVE);
 }
 
-// a lane's place in the row of key heads (a slice of them)
+// a lane's place in the row of heads (a slice of them)
 struct Place {
     int j;     // key head
+    int rl;    // which run of the key head's lanes
     int c;     // first column within the head
     int skip;  // columns that the vector before holds too
     bool act;  // the lane holds a vector
@@ -63,11 +66,13 @@ struct Place {
 };
 template <int VEC>
 __device__ __forceinline__ Place place_of(const DotArgs& D, int lig) {
-    const int hl = lig >> D.log2HL, f = lig & ((1 << D.log2HL) - 1);
+    const int x = lig >> D.log2HL, f = lig & ((1 << D.log2HL) - 1);
+    const int hl = x >> D.log2RL;
     const int j = (D.slice0 + (int)blockIdx.y) * D.heads_slice + hl;
     Place p;
     p.act = hl < D.heads_slice && j < D.K && f < D.FV;
     p.j = p.act ? j : 0;
+    p.rl = x & ((1 << D.log2RL) - 1);
     const int at = f * VEC, last = D.F - VEC;
     p.c = p.act ? (at < last ? at : last) : 0;
     p.skip = p.act && at > last ? at - last : 0;
@@ -122,21 +127,26 @@ __device__ __forceinline__ void scores(const DotArgs& D, const float* bs, const 
 // ---------------------------------------------------------------------------
 // forward
 
-template <typename T, int VEC, bool OV>
+template <typename T, int VEC, int RC, bool OV>
 struct Forward {
     const DotArgs& D;
     const Place& p;
-    int hq;
-    float q[VEC];
-    float m = -INFINITY, l = 0.0f, acc[VEC];
+    int hq;  // the first of the lane's RC query heads
+    float q[RC][VEC];
+    float m[RC], l[RC], acc[RC][VEC];
 
     __device__ __forceinline__ Forward(const DotArgs& D_, const Place& p_, int hq_, int64_t row)
         : D(D_), p(p_), hq(hq_) {
-        IO<T, VEC>::load(reinterpret_cast<const T*>(D.q) + row * D.q_stride + (int64_t)hq * D.F + p.c, q);
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) {
-            q[i] *= D.scale2;
-            acc[i] = 0.0f;
+        for (int r = 0; r < RC; ++r) {
+            IO<T, VEC>::load(reinterpret_cast<const T*>(D.q) + row * D.q_stride + (int64_t)(hq + r) * D.F + p.c, q[r]);
+            m[r] = -INFINITY;
+            l[r] = 0.0f;
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) {
+                q[r][i] *= D.scale2;
+                acc[r][i] = 0.0f;
+            }
         }
     }
     static constexpr bool kBatch = true, kSlots = true;
@@ -146,52 +156,62 @@ struct Forward {
     }
     template <bool ALL>
     __device__ __forceinline__ void take(const Raw<VEC>* rw, const int32_t* ed, const bool* ok) {
-        float bs[UNR], s[UNR];
-        bool gone[UNR];
+        float bs[RC][UNR], s[RC * UNR];
         if (D.bias) {
 #pragma unroll
-            for (int u = 0; u < UNR; ++u) bs[u] = load_bias<T>(D, ed[u], hq);
+            for (int r = 0; r < RC; ++r)
+#pragma unroll
+                for (int u = 0; u < UNR; ++u) bs[r][u] = load_bias<T>(D, ed[u], hq + r);
         }
 #pragma unroll
-        for (int u = 0; u < UNR; ++u) s[u] = share<VEC, OV>(q, rw[u].a, p);
-        run_totals<UNR>(s, 1 << D.log2HL);
-        scores<T, UNR, ALL>(D, bs, ok, s, gone);
-        float mn = m;
+        for (int r = 0; r < RC; ++r)
 #pragma unroll
-        for (int u = 0; u < UNR; ++u) {
-            s[u] = gone[u] ? -INFINITY : s[u];
-            mn = fmaxf(mn, s[u]);
-        }
-        const float at = mn == -INFINITY ? 0.0f : mn;
-        if (__ballot(mn > m) != 0ull) {
-            const float f = __builtin_amdgcn_exp2f(m - at);
-            l *= f;
+            for (int u = 0; u < UNR; ++u) s[r * UNR + u] = share<VEC, OV>(q[r], rw[u].a, p);
+        run_totals<RC * UNR>(s, 1 << D.log2HL);
 #pragma unroll
-            for (int i = 0; i < VEC; ++i) acc[i] *= f;
-        }
+        for (int r = 0; r < RC; ++r) {
+            bool gone[UNR];
+            float* sr = s + r * UNR;
+            scores<T, UNR, ALL>(D, bs[r], ok, sr, gone);
+            float mn = m[r];
 #pragma unroll
-        for (int u = 0; u < UNR; ++u) {
-            const float w = __builtin_amdgcn_exp2f(s[u] - at);
-            // (a slot that is gone adds nothing, whatever value it holds)
-            if (!gone[u]) {
-                l += w;
-#pragma unroll
-                for (int i = 0; i < VEC; ++i) acc[i] = fmaf(w, rw[u].b[i], acc[i]);
+            for (int u = 0; u < UNR; ++u) {
+                sr[u] = gone[u] ? -INFINITY : sr[u];
+                mn = fmaxf(mn, sr[u]);
             }
+            const float at = mn == -INFINITY ? 0.0f : mn;
+            if (__ballot(mn > m[r]) != 0ull) {
+                const float f = __builtin_amdgcn_exp2f(m[r] - at);
+                l[r] *= f;
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) acc[r][i] *= f;
+            }
+#pragma unroll
+            for (int u = 0; u < UNR; ++u) {
+                const float w = __builtin_amdgcn_exp2f(sr[u] - at);
+                // (a slot that is gone adds nothing, whatever value it holds)
+                if (!gone[u]) {
+                    l[r] += w;
+#pragma unroll
+                    for (int i = 0; i < VEC; ++i) acc[r][i] = fmaf(w, rw[u].b[i], acc[r][i]);
+                }
+            }
+            m[r] = mn;
         }
-        m = mn;
     }
     // the states of the wavefront's lane groups, pairwise
     __device__ __forceinline__ void join_groups(int L) {
-        for (int x = L; x < WAVE; x <<= 1) {
-            const float om = __shfl_xor(m, x, WAVE), ol = __shfl_xor(l, x, WAVE);
-            const float mn = fmaxf(m, om), at = mn == -INFINITY ? 0.0f : mn;
-            const float f = __builtin_amdgcn_exp2f(m - at), g = __builtin_amdgcn_exp2f(om - at);
-            l = l * f + ol * g;
+        for (int x = L; x < WAVE; x <<= 1)
 #pragma unroll
-            for (int i = 0; i < VEC; ++i) acc[i] = acc[i] * f + __shfl_xor(acc[i], x, WAVE) * g;
-            m = mn;
-        }
+            for (int r = 0; r < RC; ++r) {
+                const float om = __shfl_xor(m[r], x, WAVE), ol = __shfl_xor(l[r], x, WAVE);
+                const float mn = fmaxf(m[r], om), at = mn == -INFINITY ? 0.0f : mn;
+                const float f = __builtin_amdgcn_exp2f(m[r] - at), g = __builtin_amdgcn_exp2f(om - at);
+                l[r] = l[r] * f + ol * g;
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) acc[r][i] = acc[r][i] * f + __shfl_xor(acc[r][i], x, WAVE) * g;
+                m[r] = mn;
+            }
     }
 };
 
@@ -234,14 +254,14 @@ __device__ __forceinline__ void empty_rows(const EngineArgs& A, int w, int G, in
         if (k0 + x < A.sch.n_rows) fn((int64_t)A.csr.perm[k0 + x]);
 }
 
-template <typename T, int VEC, class S>
+template <typename T, int VEC, int RC, class S>
 __global__ __launch_bounds__(256) void dot_forward_kernel(EngineArgs A, DotArgs D) {
     const int w = wave_id();
     if (w >= A.sch.w_total) return;
     const Lanes ln = lanes_of<S::GC>(A.geo);
     const int G = S::GC > 0 ? S::GC : A.geo.G, L = WAVE / G;
     const Place p = place_of<VEC>(D, ln.lig);
-    const int kcol = p.j * D.F + p.c;
+    const int kcol = p.j * D.F + p.c, step = RC << D.log2RL, h0 = p.j * D.R + p.rl * RC;
     const Pre<VEC> pre{};
     auto store = [&](int64_t row, int hq, const float* v, float f) {
         float o[VEC];
@@ -249,43 +269,53 @@ __global__ __launch_bounds__(256) void dot_forward_kernel(EngineArgs A, DotArgs 
         for (int i = 0; i < VEC; ++i) o[i] = v[i] * f;
         IO<T, VEC>::store(reinterpret_cast<T*>(D.out) + row * D.out_stride + (int64_t)hq * D.F + p.c, o);
     };
+    using State = Forward<T, VEC, RC, S::OV>;
+    auto finish = [&](const State& st, int64_t row) {
+#pragma unroll
+        for (int x = 0; x < RC; ++x) {
+            store(row, st.hq + x, st.acc[x], st.l[x] == 0.0f ? 0.0f : 1.0f / st.l[x]);
+            if (p.first) write_stats(D, row, st.hq + x, st.m[x], st.l[x]);
+        }
+    };
     if (w < A.sch.w_big_end) {
         const Work k = wave_work(A, w);
-        for (int r = 0; r < D.R; ++r) {
-            Forward<T, VEC, S::OV> st(D, p, p.j * D.R + r, k.r);
+        for (int r = 0; r < D.R; r += step) {
+            State st(D, p, h0 + r, k.r);
             walk_row<T, VEC, 1, EXT_NONE, S>(A, (int32_t)k.r, k.b, k.e, ln.g, G, kcol, 0, pre, st);
             st.join_groups(L);
             if (ln.g != 0 || !p.act) continue;
             if (k.slot >= 0) {
                 float* P = D.part + (int64_t)k.slot * D.part_stride;
-                for (int i = 0; i < VEC; ++i) P[(int64_t)st.hq * D.F + p.c + i] = st.acc[i];
-                if (p.first) {
-                    float* ml = P + (int64_t)D.H * D.F + 2 * st.hq;
-                    ml[0] = st.m;
-                    ml[1] = st.l;
+#pragma unroll
+                for (int x = 0; x < RC; ++x) {
+                    if (p.first) {
+                        float* ml = P + (int64_t)D.H * D.F + 2 * (st.hq + x);
+                        ml[0] = st.m[x];
+                        ml[1] = st.l[x];
+                    }
+#pragma unroll
+                    for (int i = 0; i < VEC; ++i) P[(int64_t)(st.hq + x) * D.F + p.c + i] = st.acc[x][i];
                 }
             } else {
-                store(k.r, st.hq, st.acc, st.l == 0.0f ? 0.0f : 1.0f / st.l);
-                if (p.first) write_stats(D, k.r, st.hq, st.m, st.l);
+                finish(st, k.r);
             }
         }
     } else if (w < A.sch.w_small_end) {
         const Work k = lane_work(A, w, G, ln.g);
         const int64_t self = k.r >= 0 ? k.r : 0;
-        for (int r = 0; r < D.R; ++r) {
-            Forward<T, VEC, S::OV> st(D, p, p.j * D.R + r, self);
+        for (int r = 0; r < D.R; r += step) {
+            State st(D, p, h0 + r, self);
             walk_lane<T, VEC, 1, EXT_NONE, S>(A, (int32_t)self, k.b, k.e, kcol, 0, pre, st);
-            if (k.r < 0 || !p.act) continue;
-            store(k.r, st.hq, st.acc, st.l == 0.0f ? 0.0f : 1.0f / st.l);
-            if (p.first) write_stats(D, k.r, st.hq, st.m, st.l);
+            if (k.r >= 0 && p.act) finish(st, k.r);
         }
     } else {
         empty_rows(A, w, G, ln.g, [&](int64_t row) {
             const float zero[VEC] = {};
-            for (int r = 0; r < D.R && p.act; ++r) {
-                store(row, p.j * D.R + r, zero, 0.0f);
-                if (p.first) write_stats(D, row, p.j * D.R + r, 0.0f, 0.0f);
-            }
+            for (int r = 0; r < D.R && p.act; r += step)
+                for (int x = 0; x < RC; ++x) {
+                    store(row, h0 + r + x, zero, 0.0f);
+                    if (p.first) write_stats(D, row, h0 + r + x, 0.0f, 0.0f);
+                }
         });
     }
 }
@@ -355,30 +385,34 @@ __global__ void dot_join_kernel(EngineArgs A, DotArgs D, int cols) {
 // destination and head for the source pass, which walks the reverse graph's
 // CSR and gathers q, dout and the record.
 
-template <typename T, int VEC, bool OV>
+template <typename T, int VEC, int RC, bool OV>
 struct ToDst {
     const DotArgs& D;
     const Place& p;
-    int hq;
-    float q[VEC], dz[VEC], m, il, S0;
-    float e1[VEC], e2[VEC], delta = 0.0f;
+    int hq;  // the first of the lane's RC query heads
+    float q[RC][VEC], dz[RC][VEC], m[RC], il[RC], S0[RC];
+    float e1[RC][VEC], e2[RC][VEC], delta[RC];
 
     __device__ __forceinline__ ToDst(const DotArgs& D_, const Place& p_, int hq_, int64_t row)
         : D(D_), p(p_), hq(hq_) {
-        const int64_t c = (int64_t)hq * D.F + p.c;
-        float o[VEC];
-        IO<T, VEC>::load(reinterpret_cast<const T*>(D.q) + row * D.q_stride + c, q);
-        IO<T, VEC>::load(reinterpret_cast<const T*>(D.dz) + row * D.dz_stride + c, dz);
-        IO<T, VEC>::load(reinterpret_cast<const T*>(D.o) + row * D.o_stride + c, o);
-        m = D.stats[row * D.stats_stride + 2 * hq];
-        il = D.stats[row * D.stats_stride + 2 * hq + 1];
-        S0 = share<VEC, OV>(dz, o, p);
-        run_totals<1>(&S0, 1 << D.log2HL);
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) {
-            q[i] *= D.scale2;
-            e1[i] = e2[i] = 0.0f;
+        for (int r = 0; r < RC; ++r) {
+            const int64_t c = (int64_t)(hq + r) * D.F + p.c;
+            float o[VEC];
+            IO<T, VEC>::load(reinterpret_cast<const T*>(D.q) + row * D.q_stride + c, q[r]);
+            IO<T, VEC>::load(reinterpret_cast<const T*>(D.dz) + row * D.dz_stride + c, dz[r]);
+            IO<T, VEC>::load(reinterpret_cast<const T*>(D.o) + row * D.o_stride + c, o);
+            m[r] = D.stats[row * D.stats_stride + 2 * (hq + r)];
+            il[r] = D.stats[row * D.stats_stride + 2 * (hq + r) + 1];
+            S0[r] = share<VEC, OV>(dz[r], o, p);
+            delta[r] = 0.0f;
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) {
+                q[r][i] *= D.scale2;
+                e1[r][i] = e2[r][i] = 0.0f;
+            }
         }
+        run_totals<RC>(S0, 1 << D.log2HL);
     }
     static constexpr bool kBatch = true, kSlots = true;
     __device__ __forceinline__ void batch(const Raw<VEC>* rw, const int32_t* ed) { take<true>(rw, ed, nullptr); }
@@ -387,56 +421,69 @@ struct ToDst {
     }
     template <bool ALL>
     __device__ __forceinline__ void take(const Raw<VEC>* rw, const int32_t* ed, const bool* ok) {
-        float bs[UNR], s[2 * UNR];
-        bool gone[UNR];
+        float bs[RC][UNR], s[2 * RC * UNR];
         if (D.bias) {
 #pragma unroll
-            for (int u = 0; u < UNR; ++u) bs[u] = load_bias<T>(D, ed[u], hq);
+            for (int r = 0; r < RC; ++r)
+#pragma unroll
+                for (int u = 0; u < UNR; ++u) bs[r][u] = load_bias<T>(D, ed[u], hq + r);
         }
 #pragma unroll
-        for (int u = 0; u < UNR; ++u) {
-            s[u] = share<VEC, OV>(q, rw[u].a, p);
-            s[UNR + u] = share<VEC, OV>(dz, rw[u].b, p);
-        }
-        run_totals<2 * UNR>(s, 1 << D.log2HL);
-        scores<T, UNR, ALL>(D, bs, ok, s, gone);
+        for (int r = 0; r < RC; ++r)
 #pragma unroll
-        for (int u = 0; u < UNR; ++u) {
-            const float a = __builtin_amdgcn_exp2f(s[u] - m) * il, w = a * (s[UNR + u] - S0);
-            if (!gone[u]) {
-                delta += w;
+            for (int u = 0; u < UNR; ++u) {
+                s[2 * r * UNR + u] = share<VEC, OV>(q[r], rw[u].a, p);
+                s[(2 * r + 1) * UNR + u] = share<VEC, OV>(dz[r], rw[u].b, p);
+            }
+        run_totals<2 * RC * UNR>(s, 1 << D.log2HL);
 #pragma unroll
-                for (int i = 0; i < VEC; ++i) {
-                    e1[i] = fmaf(w, rw[u].a[i], e1[i]);
-                    e2[i] = fmaf(a, rw[u].a[i], e2[i]);
+        for (int r = 0; r < RC; ++r) {
+            bool gone[UNR];
+            float *sr = s + 2 * r * UNR, *tr = sr + UNR;
+            scores<T, UNR, ALL>(D, bs[r], ok, sr, gone);
+#pragma unroll
+            for (int u = 0; u < UNR; ++u) {
+                const float a = __builtin_amdgcn_exp2f(sr[u] - m[r]) * il[r], w = a * (tr[u] - S0[r]);
+                if (!gone[u]) {
+                    delta[r] += w;
+#pragma unroll
+                    for (int i = 0; i < VEC; ++i) {
+                        e1[r][i] = fmaf(w, rw[u].a[i], e1[r][i]);
+                        e2[r][i] = fmaf(a, rw[u].a[i], e2[r][i]);
+                    }
                 }
             }
         }
     }
     __device__ __forceinline__ void join_groups(int L) {
-        for (int x = L; x < WAVE; x <<= 1) {
-            delta += __shfl_xor(delta, x, WAVE);
+        for (int x = L; x < WAVE; x <<= 1)
 #pragma unroll
-            for (int i = 0; i < VEC; ++i) {
-                e1[i] += __shfl_xor(e1[i], x, WAVE);
-                e2[i] += __shfl_xor(e2[i], x, WAVE);
+            for (int r = 0; r < RC; ++r) {
+                delta[r] += __shfl_xor(delta[r], x, WAVE);
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) {
+                    e1[r][i] += __shfl_xor(e1[r][i], x, WAVE);
+                    e2[r][i] += __shfl_xor(e2[r][i], x, WAVE);
+                }
             }
-        }
     }
     __device__ __forceinline__ void write(int64_t row) const {
-        if (D.d_q) {
-            float v[VEC];
 #pragma unroll
-            for (int i = 0; i < VEC; ++i) v[i] = D.scale * (e1[i] - delta * e2[i]);
-            IO<T, VEC>::store(reinterpret_cast<T*>(D.d_q) + row * D.d_q_stride + (int64_t)hq * D.F + p.c, v);
+        for (int r = 0; r < RC; ++r) {
+            if (D.d_q) {
+                float v[VEC];
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) v[i] = D.scale * (e1[r][i] - delta[r] * e2[r][i]);
+                IO<T, VEC>::store(reinterpret_cast<T*>(D.d_q) + row * D.d_q_stride + (int64_t)(hq + r) * D.F + p.c, v);
+            }
+            if (p.first) D.rec[row * D.H + hq + r] = make_float4(m[r], il[r], S0[r] + delta[r], 0.0f);
         }
-        if (p.first) D.rec[row * D.H + hq] = make_float4(m, il, S0 + delta, 0.0f);
     }
 };
 
-// gradients of the bias, edge by edge, once the records are complete; of a
-// bias that the heads share, the sum over this pass's heads, added to those of
-// the passes before (their sums by edge id in D.edge_acc)
+// gradients of a bias that the heads share where they take several passes:
+// the sum over this pass's heads, added to those of the passes before (their
+// sums by edge id in D.edge_acc)
 template <typename T, int VEC, bool OV>
 struct ToEdge {
     const DotArgs& D;
@@ -477,14 +524,6 @@ struct ToEdge {
             ds[u] = __builtin_amdgcn_exp2f(s[u] - rec.x) * rec.y * (s[UNR + u] - rec.z);
             ds[u] = gone[u] ? 0.0f : ds[u];
         }
-        if (D.bias_per_head) {
-#pragma unroll
-            for (int u = 0; u < UNR; ++u)
-                if (p.first && (ALL || ok[u]))
-                    IO<T, 1>::store1(reinterpret_cast<T*>(D.d_bias) +
-                                         (uint64_t)(uint32_t)ed[u] * (uint32_t)D.d_bias_stride + hq, ds[u]);
-            return;
-        }
 #pragma unroll
         for (int u = 0; u < UNR; ++u) ds[u] = p.first ? ds[u] : 0.0f;
         run_totals<UNR>(ds, L);
@@ -502,32 +541,38 @@ struct ToEdge {
     }
 };
 
-template <typename T, int VEC, class S>
+template <typename T, int VEC, int RC, class S>
 __global__ __launch_bounds__(256) void dot_backward_dst_kernel(EngineArgs A, DotArgs D) {
     const int w = wave_id();
     if (w >= A.sch.w_total) return;
     const Lanes ln = lanes_of<S::GC>(A.geo);
     const int G = S::GC > 0 ? S::GC : A.geo.G, L = WAVE / G;
     const Place p = place_of<VEC>(D, ln.lig);
-    const int kcol = p.j * D.F + p.c;
+    const int kcol = p.j * D.F + p.c, step = RC << D.log2RL, h0 = p.j * D.R + p.rl * RC;
     const Pre<VEC> pre{};
+    using State = ToDst<T, VEC, RC, S::OV>;
     if (w < A.sch.w_big_end) {
         const Work k = wave_work(A, w);
-        for (int r = 0; r < D.R; ++r) {
-            ToDst<T, VEC, S::OV> st(D, p, p.j * D.R + r, k.r);
+        for (int r = 0; r < D.R; r += step) {
+            State st(D, p, h0 + r, k.r);
             walk_row<T, VEC, 1, EXT_NONE, S>(A, (int32_t)k.r, k.b, k.e, ln.g, G, kcol, 0, pre, st);
             st.join_groups(L);
             if (ln.g != 0 || !p.act) continue;
             if (k.slot >= 0) {
                 float* P = D.part + (int64_t)k.slot * D.part_stride;
-                const int64_t W = (int64_t)D.H * D.F, c = (int64_t)st.hq * D.F + p.c;
-                for (int i = 0; i < VEC; ++i) {
-                    P[c + i] = st.e1[i];
-                    P[W + c + i] = st.e2[i];
-                }
-                if (p.first) {
-                    P[2 * W + 2 * st.hq] = st.delta;
-                    P[2 * W + 2 * st.hq + 1] = st.S0;
+                const int64_t W = (int64_t)D.H * D.F;
+#pragma unroll
+                for (int x = 0; x < RC; ++x) {
+                    const int64_t c = (int64_t)(st.hq + x) * D.F + p.c;
+#pragma unroll
+                    for (int i = 0; i < VEC; ++i) {
+                        P[c + i] = st.e1[x][i];
+                        P[W + c + i] = st.e2[x][i];
+                    }
+                    if (p.first) {
+                        P[2 * W + 2 * (st.hq + x)] = st.delta[x];
+                        P[2 * W + 2 * (st.hq + x) + 1] = st.S0[x];
+                    }
                 }
             } else {
                 st.write(k.r);
@@ -536,17 +581,18 @@ __global__ __launch_bounds__(256) void dot_backward_dst_kernel(EngineArgs A, Dot
     } else if (w < A.sch.w_small_end) {
         const Work k = lane_work(A, w, G, ln.g);
         const int64_t self = k.r >= 0 ? k.r : 0;
-        for (int r = 0; r < D.R; ++r) {
-            ToDst<T, VEC, S::OV> st(D, p, p.j * D.R + r, self);
+        for (int r = 0; r < D.R; r += step) {
+            State st(D, p, h0 + r, self);
             walk_lane<T, VEC, 1, EXT_NONE, S>(A, (int32_t)self, k.b, k.e, kcol, 0, pre, st);
             if (k.r >= 0 && p.act) st.write(k.r);
         }
     } else if (D.d_q) {
         empty_rows(A, w, G, ln.g, [&](int64_t row) {
             const float zero[VEC] = {};
-            for (int r = 0; r < D.R && p.act; ++r)
-                IO<T, VEC>::store(reinterpret_cast<T*>(D.d_q) + row * D.d_q_stride +
-                                      (int64_t)(p.j * D.R + r) * D.F + p.c, zero);
+            for (int r = 0; r < D.R && p.act; r += step)
+                for (int x = 0; x < RC; ++x)
+                    IO<T, VEC>::store(reinterpret_cast<T*>(D.d_q) + row * D.d_q_stride +
+                                          (int64_t)(h0 + r + x) * D.F + p.c, zero);
         });
     }
 }
@@ -603,7 +649,7 @@ __global__ void dot_join_dst_kernel(EngineArgs A, DotArgs D, int cols) {
     }
 }
 
-// query heads r0 .. r1 - 1 of each key head
+// query head r0 of each key head of a slice
 template <typename T, int VEC, class S>
 __global__ __launch_bounds__(256) void dot_backward_edge_kernel(EngineArgs A, DotArgs D) {
     const int w = wave_id();
@@ -611,34 +657,33 @@ __global__ __launch_bounds__(256) void dot_backward_edge_kernel(EngineArgs A, Do
     const Lanes ln = lanes_of<S::GC>(A.geo);
     const int G = S::GC > 0 ? S::GC : A.geo.G, L = WAVE / G;
     const Place p = place_of<VEC>(D, ln.lig);
-    const int kcol = p.j * D.F + p.c, r0 = D.r0, r1 = D.r1;
+    const int kcol = p.j * D.F + p.c, hq = p.j * D.R + D.r0;
     const Pre<VEC> pre{};
     if (w < A.sch.w_big_end) {
         const Work k = wave_work(A, w);
-        for (int r = r0; r < r1; ++r) {
-            ToEdge<T, VEC, S::OV> st(D, p, p.j * D.R + r, k.r, L);
-            walk_row<T, VEC, 1, EXT_NONE, S>(A, (int32_t)k.r, k.b, k.e, ln.g, G, kcol, 0, pre, st);
-        }
+        ToEdge<T, VEC, S::OV> st(D, p, hq, k.r, L);
+        walk_row<T, VEC, 1, EXT_NONE, S>(A, (int32_t)k.r, k.b, k.e, ln.g, G, kcol, 0, pre, st);
     } else {
         const Work k = lane_work(A, w, G, ln.g);
         const int64_t self = k.r >= 0 ? k.r : A.csr.rowt[0].x;
-        for (int r = r0; r < r1; ++r) {
-            ToEdge<T, VEC, S::OV> st(D, p, p.j * D.R + r, self, L);
-            walk_lane<T, VEC, 1, EXT_NONE, S>(A, (int32_t)self, k.b, k.e, kcol, 0, pre, st);
-        }
+        ToEdge<T, VEC, S::OV> st(D, p, hq, self, L);
+        walk_lane<T, VEC, 1, EXT_NONE, S>(A, (int32_t)self, k.b, k.e, kcol, 0, pre, st);
     }
 }
 
-// the source pass: dk and dv of a row over its out-edges
+// the source pass: dk and dv of a row over its out-edges, and the gradients of
+// the bias where this pass sees what they take (a value per head, or all heads
+// of a shared one side by side)
 template <typename T, int VEC, bool OV>
 struct ToSrc {
     const DotArgs& D;
     const Place& p;
-    int hq = 0;
+    int hq = 0, L;
     float k[VEC], v[VEC];
     float dk[VEC], dv[VEC];
 
-    __device__ __forceinline__ ToSrc(const DotArgs& D_, const Place& p_, int64_t row) : D(D_), p(p_) {
+    __device__ __forceinline__ ToSrc(const DotArgs& D_, const Place& p_, int64_t row, int L_)
+        : D(D_), p(p_), L(L_) {
         const int64_t c = (int64_t)p.j * D.F + p.c;
         IO<T, VEC>::load(reinterpret_cast<const T*>(D.k) + row * D.k_stride + c, k);
         IO<T, VEC>::load(reinterpret_cast<const T*>(D.v) + row * D.v_stride + c, v);
@@ -679,16 +724,36 @@ struct ToSrc {
                     dv[i] = fmaf(a, rw[u].b[i], dv[i]);
                 }
             }
+            s[u] = gone[u] ? 0.0f : w;
+        }
+        if (!D.src_bias) return;
+        if (D.bias_per_head) {
+#pragma unroll
+            for (int u = 0; u < UNR; ++u)
+                if (p.first && (ALL || ok[u])) store_dbias(ed[u], hq, s[u]);
+        } else {
+#pragma unroll
+            for (int u = 0; u < UNR; ++u) s[u] = p.first ? s[u] : 0.0f;
+            run_totals<UNR>(s, L);
+#pragma unroll
+            for (int u = 0; u < UNR; ++u)
+                if ((__lane_id() & (L - 1)) == 0 && (ALL || ok[u])) store_dbias(ed[u], 0, s[u]);
         }
     }
-    __device__ __forceinline__ void join_groups(int L) {
-        for (int x = L; x < WAVE; x <<= 1)
+    __device__ __forceinline__ void store_dbias(int32_t ed, int h, float x) {
+        IO<T, 1>::store1(reinterpret_cast<T*>(D.d_bias) + (uint64_t)(uint32_t)ed * (uint32_t)D.d_bias_stride + h, x);
+    }
+    // sums over the lanes that differ in the bits from .. to / 2 of their number
+    __device__ __forceinline__ void join(int from, int to) {
+        for (int x = from; x < to; x <<= 1)
 #pragma unroll
             for (int i = 0; i < VEC; ++i) {
                 dk[i] += __shfl_xor(dk[i], x, WAVE);
                 dv[i] += __shfl_xor(dv[i], x, WAVE);
             }
     }
+    // over the query heads of a key head, side by side
+    __device__ __forceinline__ void join_heads() { join(1 << D.log2HL, 1 << (D.log2HL + D.log2RL)); }
     __device__ __forceinline__ void write(int64_t row) {
         const int64_t c = (int64_t)p.j * D.F + p.c;
 #pragma unroll
@@ -708,13 +773,14 @@ __global__ __launch_bounds__(256) void dot_backward_src_kernel(EngineArgs A, Dot
     const Pre<VEC> pre{};
     if (w < A.sch.w_big_end) {
         const Work k = wave_work(A, w);
-        ToSrc<T, VEC, S::OV> st(D, p, k.r);
-        for (int r = 0; r < D.R; ++r) {
+        ToSrc<T, VEC, S::OV> st(D, p, k.r, L);
+        for (int r = p.rl; r < D.R; r += 1 << D.log2RL) {
             st.hq = p.j * D.R + r;
             walk_row<T, VEC, 1, EXT_REC, S>(A, (int32_t)k.r, k.b, k.e, ln.g, G, st.hq * D.F + p.c, st.hq, pre, st);
         }
-        st.join_groups(L);
-        if (ln.g != 0 || !p.act) return;
+        st.join(L, WAVE);
+        st.join_heads();
+        if (ln.g != 0 || !p.act || p.rl != 0) return;
         if (k.slot >= 0) {
             float* P = D.part + (int64_t)k.slot * D.part_stride;
             const int64_t W = (int64_t)D.K * D.F, c = (int64_t)p.j * D.F + p.c;
@@ -728,17 +794,18 @@ __global__ __launch_bounds__(256) void dot_backward_src_kernel(EngineArgs A, Dot
     } else if (w < A.sch.w_small_end) {
         const Work k = lane_work(A, w, G, ln.g);
         const int64_t self = k.r >= 0 ? k.r : 0;
-        ToSrc<T, VEC, S::OV> st(D, p, self);
-        for (int r = 0; r < D.R; ++r) {
+        ToSrc<T, VEC, S::OV> st(D, p, self, L);
+        for (int r = p.rl; r < D.R; r += 1 << D.log2RL) {
             st.hq = p.j * D.R + r;
             walk_lane<T, VEC, 1, EXT_REC, S>(A, (int32_t)self, k.b, k.e, st.hq * D.F + p.c, st.hq, pre, st);
         }
-        if (k.r >= 0 && p.act) st.write(k.r);
+        st.join_heads();
+        if (k.r >= 0 && p.act && p.rl == 0) st.write(k.r);
     } else {
         empty_rows(A, w, G, ln.g, [&](int64_t row) {
             const float zero[VEC] = {};
             const int64_t c = (int64_t)p.j * D.F + p.c;
-            if (!p.act) return;
+            if (!p.act || p.rl != 0) return;
             if (D.d_k) IO<T, VEC>::store(reinterpret_cast<T*>(D.d_k) + row * D.d_k_stride + c, zero);
             if (D.d_v) IO<T, VEC>::store(reinterpret_cast<T*>(D.d_v) + row * D.d_v_stride + c, zero);
         });
@@ -799,17 +866,37 @@ Join join_of(const EngineArgs& a) {
     return many ? Join{16, 1024} : Join{64, 256};
 }
 
+// query heads of a key head that a lane takes at once: 1 (forward and
+// destination pass) on the runtime layouts, which hold no more
+#define GNNK_RC_DISPATCH(RC_, S_, ...)                                    \
+    if constexpr (S_::FAST) {                                             \
+        switch (RC_) {                                                    \
+            case 4: { constexpr int RC = 4; __VA_ARGS__; } break;         \
+            case 3: { constexpr int RC = 3; __VA_ARGS__; } break;         \
+            case 2: { constexpr int RC = 2; __VA_ARGS__; } break;         \
+            default: { constexpr int RC = 1; __VA_ARGS__; } break;        \
+        }                                                                 \
+    } else {                                                              \
+        constexpr int RC = 1;                                             \
+        __VA_ARGS__;                                                      \
+    }
+
 template <typename T, int V, class S>
 void dot_pass(const EngineArgs& a, const DotArgs& d, int pass, hipStream_t s) {
     const dim3 grid(blocks_for_waves(a.sch.w_total), (unsigned)d.slices), block(WAVE * WPB);
     const Join j = join_of(a);
     const int64_t HF = (int64_t)d.H * d.F, KF = (int64_t)d.K * d.F;
     if (pass == 0) {
-        hipLaunchKernelGGL((dot_forward_kernel<T, V, S>), grid, block, 0, s, a, d);
+        GNNK_RC_DISPATCH(d.RC, S, hipLaunchKernelGGL((dot_forward_kernel<T, V, RC, S>), grid, block, 0, s, a, d))
         if (a.sch.n_hub > 0)
             hipLaunchKernelGGL((dot_join_kernel<T>), j.grid(a, HF), dim3(j.threads), 0, s, a, d, j.cols);
     } else if (pass == 1) {
-        hipLaunchKernelGGL((dot_backward_dst_kernel<T, V, S>), grid, block, 0, s, a, d);
+        if (d.RC == 2 && S::FAST) {
+            if constexpr (S::FAST)
+                hipLaunchKernelGGL((dot_backward_dst_kernel<T, V, 2, S>), grid, block, 0, s, a, d);
+        } else {
+            hipLaunchKernelGGL((dot_backward_dst_kernel<T, V, 1, S>), grid, block, 0, s, a, d);
+        }
         if (a.sch.n_hub > 0)
             hipLaunchKernelGGL((dot_join_dst_kernel<T>), j.grid(a, HF), dim3(j.threads), 0, s, a, d, j.cols);
     } else if (pass == 2) {

@@ -268,11 +268,12 @@ struct DotArgs {
     float scale, scale2;     // of the scores; times log2(e)
     int32_t H, K, R, F;      // query heads, key heads, query heads per key head, columns
     int32_t FV, log2HL;      // vectors of a head, log2 of the lanes they take
+    int32_t RC, log2RL;      // query heads of a key head in a lane's registers, log2 of those in lanes beside each other
     int32_t heads_slice, slices, slice0;  // key heads of a slice, slices of a launch, its first one
     int32_t bias_per_head;
-    int32_t r0, r1;          // pass 3: query heads of each key head
-    int32_t edge_first, edge_last;  // pass 3 of a shared bias: the first, the last of its passes
-    int32_t pad;
+    int32_t src_bias;        // pass 2 writes the gradient of the bias
+    int32_t r0;              // pass 3: the query head of each key head
+    int32_t edge_first, edge_last;  // pass 3: the first, the last of its passes
 };
 // pass: 0 forward, 1 backward by destination, 2 by source, 3 by edge
 hipError_t launch_dot(const EngineArgs& a, const DotArgs& d, int pass, int dtype, int vec, int gc, hipStream_t s);
