@@ -14,7 +14,7 @@
 // of lanes take as many beside each other, and what is left takes turns.
 //
 // Scores are kept in base 2: the query is scaled by scale * log2(e) once per
-// row.  Dot products and the sums over the edges of one wavefront's share of a
+// row (bf16: the product).  Dot products and the sums over the edges of one wavefront's share of a
 // row are fp32; the partial results of a long row's segments are joined in
 // fp64 in segment order.
 #include "walk.h"
@@ -22,6 +22,63 @@
 namespace gnnk {
 
 namespace {
+
+// bf16 rows stay in their packed words until a column is needed: dot products
+// of two bf16 rows take a pair of columns an instruction (v_dot2_f32_bf16: the
+// exact products and the sum so far, off by at most 2.4 units of the last
+// place of their sizes' sum; bf16 numbers below 2^-126 count as 0), which
+// spares the widening and half the multiplications
+struct bf16_pair_t {
+    uint16_t x;
+};
+
+}  // namespace
+
+// vectors of words: VEC values of fp32, VEC / 2 pairs of bf16
+template <int VEC>
+struct IO<bf16_pair_t, VEC> {
+    static __device__ __forceinline__ void load(const bf16_pair_t* p, float* w) {
+        if constexpr (VEC == 8) {
+            const u4_h x = *reinterpret_cast<const u4_h*>(p);
+            w[0] = __uint_as_float(x.x); w[1] = __uint_as_float(x.y);
+            w[2] = __uint_as_float(x.z); w[3] = __uint_as_float(x.w);
+        } else if constexpr (VEC == 4) {
+            const u2_h x = *reinterpret_cast<const u2_h*>(p);
+            w[0] = __uint_as_float(x.x); w[1] = __uint_as_float(x.y);
+        } else if constexpr (VEC == 2) {
+            w[0] = __uint_as_float(*reinterpret_cast<const u1_h*>(p));
+        } else {
+            w[0] = __uint_as_float((uint32_t)p->x);
+        }
+    }
+    static __device__ __forceinline__ void load_nt(const bf16_pair_t* p, float* w) { load(p, w); }
+    static __device__ __forceinline__ float load1(const bf16_pair_t* p) { return bf_lo(p->x); }
+    static __device__ __forceinline__ float load1_nt(const bf16_pair_t* p) { return load1(p); }
+};
+
+namespace {
+
+typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+__device__ __forceinline__ bf16x2 pair(float w) { return __builtin_bit_cast(bf16x2, w); }
+
+// rows of T in words
+template <typename T, int VEC>
+struct Words {
+    using type = float;
+    static constexpr int N = VEC;
+    static constexpr bool PAIRS = false;
+    static __device__ __forceinline__ float at(const float* w, int i) { return w[i]; }
+};
+template <int VEC>
+struct Words<bf16_t, VEC> {
+    using type = bf16_pair_t;
+    static constexpr int N = (VEC + 1) / 2;
+    static constexpr bool PAIRS = true;
+    static __device__ __forceinline__ float at(const float* w, int i) {
+        const uint32_t x = __float_as_uint(w[i / 2]);
+        return (i & 1) ? bf_hi(x) : bf_lo(x);
+    }
+};
 
 constexpr float LOG2E = 1.44269504088896341f;
 
@@ -80,16 +137,47 @@ __device__ __forceinline__ Place place_of(const DotArgs& D, int lig) {
     return p;
 }
 
-// a lane's share of a dot product, without the columns it shares
-template <int VEC, bool OV>
+// a lane's share of a dot product of two rows in words, without the columns
+// it shares
+template <typename T, int VEC, bool OV>
 __device__ __forceinline__ float share(const float* x, const float* y, const Place& p) {
+    using W = Words<T, VEC>;
     float s = 0.0f;
 #pragma unroll
-    for (int i = 0; i < VEC; ++i) {
-        if constexpr (OV) s = i < p.skip ? s : fmaf(x[i], y[i], s);
-        else s = fmaf(x[i], y[i], s);
+    for (int i = 0; i < W::N; ++i) {
+        if constexpr (W::PAIRS) {
+            float yi = y[i], xi = x[i];
+            if constexpr (OV) {
+                // (both, so that an infinite value of a shared column meets no 0)
+                const uint32_t m = (2 * i < p.skip ? 0u : 0xFFFFu) | (2 * i + 1 < p.skip ? 0u : 0xFFFF0000u);
+                yi = __uint_as_float(__float_as_uint(yi) & m);
+                xi = __uint_as_float(__float_as_uint(xi) & m);
+            }
+            s = __builtin_amdgcn_fdot2_f32_bf16(pair(xi), pair(yi), s, false);
+        } else if constexpr (OV) {
+            s = i < p.skip ? s : fmaf(x[i], y[i], s);
+        } else {
+            s = fmaf(x[i], y[i], s);
+        }
     }
     return p.act ? s : 0.0f;
+}
+
+// a row's own operand of the scores: fp32 scaled by scale * log2(e) once, bf16
+// as it is (its totals are scaled instead)
+template <typename T, int VEC>
+__device__ __forceinline__ void own_row(const DotArgs& D, const void* base, int64_t at, float* w) {
+    using W = Words<T, VEC>;
+    IO<typename W::type, VEC>::load(reinterpret_cast<const typename W::type*>(base) + at, w);
+    if constexpr (!W::PAIRS) {
+#pragma unroll
+        for (int i = 0; i < W::N; ++i) w[i] *= D.scale2;
+    }
+}
+template <typename T, int VEC>
+__device__ __forceinline__ void row_words(const void* base, int64_t at, float* w) {
+    using W = Words<T, VEC>;
+    IO<typename W::type, VEC>::load(reinterpret_cast<const typename W::type*>(base) + at, w);
 }
 
 // the bias of an edge in base 2; false: the edge is masked (-inf)
@@ -113,7 +201,10 @@ __device__ __forceinline__ float load_bias(const DotArgs& D, int32_t ed, int hq)
 template <typename T, int N, bool ALL>
 __device__ __forceinline__ void scores(const DotArgs& D, const float* bs, const bool* ok, float* s, bool* gone) {
 #pragma unroll
-    for (int u = 0; u < N; ++u) gone[u] = ALL ? false : !ok[u];
+    for (int u = 0; u < N; ++u) {
+        gone[u] = ALL ? false : !ok[u];
+        if constexpr (Words<T, 2>::PAIRS) s[u] *= D.scale2;
+    }
     if (D.bias) {
 #pragma unroll
         for (int u = 0; u < N; ++u) {
@@ -132,21 +223,19 @@ struct Forward {
     const DotArgs& D;
     const Place& p;
     int hq;  // the first of the lane's RC query heads
-    float q[RC][VEC];
+    using W = Words<T, VEC>;
+    float q[RC][W::N];
     float m[RC], l[RC], acc[RC][VEC];
 
     __device__ __forceinline__ Forward(const DotArgs& D_, const Place& p_, int hq_, int64_t row)
         : D(D_), p(p_), hq(hq_) {
 #pragma unroll
         for (int r = 0; r < RC; ++r) {
-            IO<T, VEC>::load(reinterpret_cast<const T*>(D.q) + row * D.q_stride + (int64_t)(hq + r) * D.F + p.c, q[r]);
+            own_row<T, VEC>(D, D.q, row * D.q_stride + (int64_t)(hq + r) * D.F + p.c, q[r]);
             m[r] = -INFINITY;
             l[r] = 0.0f;
 #pragma unroll
-            for (int i = 0; i < VEC; ++i) {
-                q[r][i] *= D.scale2;
-                acc[r][i] = 0.0f;
-            }
+            for (int i = 0; i < VEC; ++i) acc[r][i] = 0.0f;
         }
     }
     static constexpr bool kBatch = true, kSlots = true;
@@ -166,7 +255,7 @@ struct Forward {
 #pragma unroll
         for (int r = 0; r < RC; ++r)
 #pragma unroll
-            for (int u = 0; u < UNR; ++u) s[r * UNR + u] = share<VEC, OV>(q[r], rw[u].a, p);
+            for (int u = 0; u < UNR; ++u) s[r * UNR + u] = share<T, VEC, OV>(q[r], rw[u].a, p);
         run_totals<RC * UNR>(s, 1 << D.log2HL);
 #pragma unroll
         for (int r = 0; r < RC; ++r) {
@@ -193,7 +282,7 @@ struct Forward {
                 if (!gone[u]) {
                     l[r] += w;
 #pragma unroll
-                    for (int i = 0; i < VEC; ++i) acc[r][i] = fmaf(w, rw[u].b[i], acc[r][i]);
+                    for (int i = 0; i < VEC; ++i) acc[r][i] = fmaf(w, W::at(rw[u].b, i), acc[r][i]);
                 }
             }
             m[r] = mn;
@@ -281,7 +370,7 @@ __global__ __launch_bounds__(256) void dot_forward_kernel(EngineArgs A, DotArgs 
         const Work k = wave_work(A, w);
         for (int r = 0; r < D.R; r += step) {
             State st(D, p, h0 + r, k.r);
-            walk_row<T, VEC, 1, EXT_NONE, S>(A, (int32_t)k.r, k.b, k.e, ln.g, G, kcol, 0, pre, st);
+            walk_row<typename Words<T, VEC>::type, VEC, 1, EXT_NONE, S>(A, (int32_t)k.r, k.b, k.e, ln.g, G, kcol, 0, pre, st);
             st.join_groups(L);
             if (ln.g != 0 || !p.act) continue;
             if (k.slot >= 0) {
@@ -305,7 +394,7 @@ __global__ __launch_bounds__(256) void dot_forward_kernel(EngineArgs A, DotArgs 
         const int64_t self = k.r >= 0 ? k.r : 0;
         for (int r = 0; r < D.R; r += step) {
             State st(D, p, h0 + r, self);
-            walk_lane<T, VEC, 1, EXT_NONE, S>(A, (int32_t)self, k.b, k.e, kcol, 0, pre, st);
+            walk_lane<typename Words<T, VEC>::type, VEC, 1, EXT_NONE, S>(A, (int32_t)self, k.b, k.e, kcol, 0, pre, st);
             if (k.r >= 0 && p.act) finish(st, k.r);
         }
     } else {
@@ -390,7 +479,8 @@ struct ToDst {
     const DotArgs& D;
     const Place& p;
     int hq;  // the first of the lane's RC query heads
-    float q[RC][VEC], dz[RC][VEC], m[RC], il[RC], S0[RC];
+    using W = Words<T, VEC>;
+    float q[RC][W::N], dz[RC][W::N], m[RC], il[RC], S0[RC];
     float e1[RC][VEC], e2[RC][VEC], delta[RC];
 
     __device__ __forceinline__ ToDst(const DotArgs& D_, const Place& p_, int hq_, int64_t row)
@@ -398,19 +488,16 @@ struct ToDst {
 #pragma unroll
         for (int r = 0; r < RC; ++r) {
             const int64_t c = (int64_t)(hq + r) * D.F + p.c;
-            float o[VEC];
-            IO<T, VEC>::load(reinterpret_cast<const T*>(D.q) + row * D.q_stride + c, q[r]);
-            IO<T, VEC>::load(reinterpret_cast<const T*>(D.dz) + row * D.dz_stride + c, dz[r]);
-            IO<T, VEC>::load(reinterpret_cast<const T*>(D.o) + row * D.o_stride + c, o);
+            float o[W::N];
+            own_row<T, VEC>(D, D.q, row * D.q_stride + c, q[r]);
+            row_words<T, VEC>(D.dz, row * D.dz_stride + c, dz[r]);
+            row_words<T, VEC>(D.o, row * D.o_stride + c, o);
             m[r] = D.stats[row * D.stats_stride + 2 * (hq + r)];
             il[r] = D.stats[row * D.stats_stride + 2 * (hq + r) + 1];
-            S0[r] = share<VEC, OV>(dz[r], o, p);
+            S0[r] = share<T, VEC, OV>(dz[r], o, p);
             delta[r] = 0.0f;
 #pragma unroll
-            for (int i = 0; i < VEC; ++i) {
-                q[r][i] *= D.scale2;
-                e1[r][i] = e2[r][i] = 0.0f;
-            }
+            for (int i = 0; i < VEC; ++i) e1[r][i] = e2[r][i] = 0.0f;
         }
         run_totals<RC>(S0, 1 << D.log2HL);
     }
@@ -432,8 +519,8 @@ struct ToDst {
         for (int r = 0; r < RC; ++r)
 #pragma unroll
             for (int u = 0; u < UNR; ++u) {
-                s[2 * r * UNR + u] = share<VEC, OV>(q[r], rw[u].a, p);
-                s[(2 * r + 1) * UNR + u] = share<VEC, OV>(dz[r], rw[u].b, p);
+                s[2 * r * UNR + u] = share<T, VEC, OV>(q[r], rw[u].a, p);
+                s[(2 * r + 1) * UNR + u] = share<T, VEC, OV>(dz[r], rw[u].b, p);
             }
         run_totals<2 * RC * UNR>(s, 1 << D.log2HL);
 #pragma unroll
@@ -448,8 +535,9 @@ struct ToDst {
                     delta[r] += w;
 #pragma unroll
                     for (int i = 0; i < VEC; ++i) {
-                        e1[r][i] = fmaf(w, rw[u].a[i], e1[r][i]);
-                        e2[r][i] = fmaf(a, rw[u].a[i], e2[r][i]);
+                        const float x = W::at(rw[u].a, i);
+                        e1[r][i] = fmaf(w, x, e1[r][i]);
+                        e2[r][i] = fmaf(a, x, e2[r][i]);
                     }
                 }
             }
@@ -489,17 +577,16 @@ struct ToEdge {
     const DotArgs& D;
     const Place& p;
     int hq, L;
-    float q[VEC], dz[VEC];
+    using W = Words<T, VEC>;
+    float q[W::N], dz[W::N];
     float4 rec;
 
     __device__ __forceinline__ ToEdge(const DotArgs& D_, const Place& p_, int hq_, int64_t row, int L_)
         : D(D_), p(p_), hq(hq_), L(L_) {
         const int64_t c = (int64_t)hq * D.F + p.c;
-        IO<T, VEC>::load(reinterpret_cast<const T*>(D.q) + row * D.q_stride + c, q);
-        IO<T, VEC>::load(reinterpret_cast<const T*>(D.dz) + row * D.dz_stride + c, dz);
+        own_row<T, VEC>(D, D.q, row * D.q_stride + c, q);
+        row_words<T, VEC>(D.dz, row * D.dz_stride + c, dz);
         rec = D.rec[row * D.H + hq];
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) q[i] *= D.scale2;
     }
     static constexpr bool kBatch = true, kSlots = true;
     __device__ __forceinline__ void batch(const Raw<VEC>* rw, const int32_t* ed) { take<true>(rw, ed, nullptr); }
@@ -514,8 +601,8 @@ struct ToEdge {
         for (int u = 0; u < UNR; ++u) bs[u] = load_bias<T>(D, ed[u], hq);
 #pragma unroll
         for (int u = 0; u < UNR; ++u) {
-            s[u] = share<VEC, OV>(q, rw[u].a, p);
-            s[UNR + u] = share<VEC, OV>(dz, rw[u].b, p);
+            s[u] = share<T, VEC, OV>(q, rw[u].a, p);
+            s[UNR + u] = share<T, VEC, OV>(dz, rw[u].b, p);
         }
         run_totals<2 * UNR>(s, 1 << D.log2HL);
         scores<T, UNR, ALL>(D, bs, ok, s, gone);
@@ -555,7 +642,7 @@ __global__ __launch_bounds__(256) void dot_backward_dst_kernel(EngineArgs A, Dot
         const Work k = wave_work(A, w);
         for (int r = 0; r < D.R; r += step) {
             State st(D, p, h0 + r, k.r);
-            walk_row<T, VEC, 1, EXT_NONE, S>(A, (int32_t)k.r, k.b, k.e, ln.g, G, kcol, 0, pre, st);
+            walk_row<typename Words<T, VEC>::type, VEC, 1, EXT_NONE, S>(A, (int32_t)k.r, k.b, k.e, ln.g, G, kcol, 0, pre, st);
             st.join_groups(L);
             if (ln.g != 0 || !p.act) continue;
             if (k.slot >= 0) {
@@ -583,7 +670,7 @@ __global__ __launch_bounds__(256) void dot_backward_dst_kernel(EngineArgs A, Dot
         const int64_t self = k.r >= 0 ? k.r : 0;
         for (int r = 0; r < D.R; r += step) {
             State st(D, p, h0 + r, self);
-            walk_lane<T, VEC, 1, EXT_NONE, S>(A, (int32_t)self, k.b, k.e, kcol, 0, pre, st);
+            walk_lane<typename Words<T, VEC>::type, VEC, 1, EXT_NONE, S>(A, (int32_t)self, k.b, k.e, kcol, 0, pre, st);
             if (k.r >= 0 && p.act) st.write(k.r);
         }
     } else if (D.d_q) {
@@ -662,12 +749,12 @@ __global__ __launch_bounds__(256) void dot_backward_edge_kernel(EngineArgs A, Do
     if (w < A.sch.w_big_end) {
         const Work k = wave_work(A, w);
         ToEdge<T, VEC, S::OV> st(D, p, hq, k.r, L);
-        walk_row<T, VEC, 1, EXT_NONE, S>(A, (int32_t)k.r, k.b, k.e, ln.g, G, kcol, 0, pre, st);
+        walk_row<typename Words<T, VEC>::type, VEC, 1, EXT_NONE, S>(A, (int32_t)k.r, k.b, k.e, ln.g, G, kcol, 0, pre, st);
     } else {
         const Work k = lane_work(A, w, G, ln.g);
         const int64_t self = k.r >= 0 ? k.r : A.csr.rowt[0].x;
         ToEdge<T, VEC, S::OV> st(D, p, hq, self, L);
-        walk_lane<T, VEC, 1, EXT_NONE, S>(A, (int32_t)self, k.b, k.e, kcol, 0, pre, st);
+        walk_lane<typename Words<T, VEC>::type, VEC, 1, EXT_NONE, S>(A, (int32_t)self, k.b, k.e, kcol, 0, pre, st);
     }
 }
 
@@ -679,19 +766,17 @@ struct ToSrc {
     const DotArgs& D;
     const Place& p;
     int hq = 0, L;
-    float k[VEC], v[VEC];
+    using W = Words<T, VEC>;
+    float k[W::N], v[W::N];
     float dk[VEC], dv[VEC];
 
     __device__ __forceinline__ ToSrc(const DotArgs& D_, const Place& p_, int64_t row, int L_)
         : D(D_), p(p_), L(L_) {
         const int64_t c = (int64_t)p.j * D.F + p.c;
-        IO<T, VEC>::load(reinterpret_cast<const T*>(D.k) + row * D.k_stride + c, k);
-        IO<T, VEC>::load(reinterpret_cast<const T*>(D.v) + row * D.v_stride + c, v);
+        own_row<T, VEC>(D, D.k, row * D.k_stride + c, k);
+        row_words<T, VEC>(D.v, row * D.v_stride + c, v);
 #pragma unroll
-        for (int i = 0; i < VEC; ++i) {
-            k[i] *= D.scale2;
-            dk[i] = dv[i] = 0.0f;
-        }
+        for (int i = 0; i < VEC; ++i) dk[i] = dv[i] = 0.0f;
     }
     static constexpr bool kBatch = true, kSlots = true;
     __device__ __forceinline__ void batch(const Raw<VEC>* rw, const int32_t* ed) { take<true>(rw, ed, nullptr); }
@@ -708,8 +793,8 @@ struct ToSrc {
         }
 #pragma unroll
         for (int u = 0; u < UNR; ++u) {
-            s[u] = share<VEC, OV>(k, rw[u].a, p);
-            s[UNR + u] = share<VEC, OV>(v, rw[u].b, p);
+            s[u] = share<T, VEC, OV>(k, rw[u].a, p);
+            s[UNR + u] = share<T, VEC, OV>(v, rw[u].b, p);
         }
         run_totals<2 * UNR>(s, 1 << D.log2HL);
         scores<T, UNR, ALL>(D, bs, ok, s, gone);
@@ -720,8 +805,8 @@ struct ToSrc {
             if (!gone[u]) {
 #pragma unroll
                 for (int i = 0; i < VEC; ++i) {
-                    dk[i] = fmaf(w, rw[u].a[i], dk[i]);
-                    dv[i] = fmaf(a, rw[u].b[i], dv[i]);
+                    dk[i] = fmaf(w, W::at(rw[u].a, i), dk[i]);
+                    dv[i] = fmaf(a, W::at(rw[u].b, i), dv[i]);
                 }
             }
             s[u] = gone[u] ? 0.0f : w;
@@ -776,7 +861,7 @@ __global__ __launch_bounds__(256) void dot_backward_src_kernel(EngineArgs A, Dot
         ToSrc<T, VEC, S::OV> st(D, p, k.r, L);
         for (int r = p.rl; r < D.R; r += 1 << D.log2RL) {
             st.hq = p.j * D.R + r;
-            walk_row<T, VEC, 1, EXT_REC, S>(A, (int32_t)k.r, k.b, k.e, ln.g, G, st.hq * D.F + p.c, st.hq, pre, st);
+            walk_row<typename Words<T, VEC>::type, VEC, 1, EXT_REC, S>(A, (int32_t)k.r, k.b, k.e, ln.g, G, st.hq * D.F + p.c, st.hq, pre, st);
         }
         st.join(L, WAVE);
         st.join_heads();
@@ -797,7 +882,7 @@ __global__ __launch_bounds__(256) void dot_backward_src_kernel(EngineArgs A, Dot
         ToSrc<T, VEC, S::OV> st(D, p, self, L);
         for (int r = p.rl; r < D.R; r += 1 << D.log2RL) {
             st.hq = p.j * D.R + r;
-            walk_lane<T, VEC, 1, EXT_REC, S>(A, (int32_t)self, k.b, k.e, st.hq * D.F + p.c, st.hq, pre, st);
+            walk_lane<typename Words<T, VEC>::type, VEC, 1, EXT_REC, S>(A, (int32_t)self, k.b, k.e, st.hq * D.F + p.c, st.hq, pre, st);
         }
         st.join_heads();
         if (k.r >= 0 && p.act && p.rl == 0) st.write(k.r);
