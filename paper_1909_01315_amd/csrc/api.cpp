@@ -1649,9 +1649,11 @@ void dot_lanes(DotCall& c, int RC, int RL) {
     geo.G = 64 / geo.L;
 }
 
-// the largest of 1..most that divides R
-int dot_share(int R, int most) {
-    while (R % most) --most;
+// the largest power of two up to `most` that divides the query heads of a key
+// head (narrow heads, of less than the widest vectors: 1)
+int dot_share(const DotCall& c, int most) {
+    if (c.geo.vec != (c.dt == 1 ? 8 : 4)) return 1;
+    while (c.D.R % most) most >>= 1;
     return most;
 }
 
@@ -1693,9 +1695,9 @@ void dot_operands(const gnnk_tensor* q, const gnnk_tensor* k, const gnnk_tensor*
     }
 }
 
-// a walk over d that gathers rows of a and b; returns the lane groups of its
-// compile-time layout, 0 for the runtime one (64-bit addresses)
-int dot_walk(const gnnk_graph* g, const Dir& d, const DotCall& c, const gnnk_tensor* a, const gnnk_tensor* b, bool ids,
+// a walk over d that gathers rows of a and b; true: their tables take 32-bit
+// byte offsets
+bool dot_walk(const gnnk_graph* g, const Dir& d, const DotCall& c, const gnnk_tensor* a, const gnnk_tensor* b, bool ids,
              EngineArgs& A) {
     A.a = operand(a, K_FULL, T_NBR);
     A.b = operand(b, K_FULL, T_NBR);
@@ -1703,9 +1705,7 @@ int dot_walk(const gnnk_graph* g, const Dir& d, const DotCall& c, const gnnk_ten
     set_geo(A, c.geo);
     A.sch = schedule(d, c.geo, true);
     const int es = c.dt == 1 ? 2 : 4;
-    return !options().no_fast && fast_geo(c.geo, c.dt) && fits32(A.a, a->rows, es) && fits32(A.b, b->rows, es)
-               ? c.geo.G
-               : 0;
+    return !options().no_fast && fits32(A.a, a->rows, es) && fits32(A.b, b->rows, es);
 }
 
 }  // namespace
@@ -1726,16 +1726,16 @@ gnnk_status dot_aggregate(gnnk_graph_t g, const gnnk_tensor* q, const gnnk_tenso
     D.out = out->data;
     D.out_stride = out->row_stride;
     EngineArgs A{};
-    dot_lanes(c, dot_share(D.R, 4), 1);
-    const int gc = dot_walk(g, g->in_nbr, c, k, v, bias != nullptr, A);
-    if (!gc) D.RC = 1;
+    dot_lanes(c, dot_share(c, 4), 1);
+    const bool fast = dot_walk(g, g->in_nbr, c, k, v, bias != nullptr, A);
+    if (!fast) D.RC = 1;
     D.part_stride = (int64_t)D.H * D.F + 2 * D.H;
     if (A.sch.n_seg > 0) {
         Scratch sc = scratch_of(g, stream);
         D.part = static_cast<float*>(sc.take((size_t)A.sch.n_seg * D.part_stride * 4));
         if (!D.part) return scratch_fail(sc);
     }
-    return GNNK_LAUNCH(launch_dot(A, D, 0, c.dt, c.geo.vec, gc, stream), "dot-product attention launch");
+    return GNNK_LAUNCH(launch_dot(A, D, 0, c.dt, c.geo.vec, fast, stream), "dot-product attention launch");
 }
 
 static gnnk_status dot_backward(gnnk_graph_t g, const gnnk_tensor* q, const gnnk_tensor* k, const gnnk_tensor* v,
@@ -1774,22 +1774,22 @@ static gnnk_status dot_backward(gnnk_graph_t g, const gnnk_tensor* q, const gnnk
     // by destination
     EngineArgs ain{}, aout{}, aedge{};
     DotCall in = c, src = c, edge = c;
-    dot_lanes(in, dot_share(D.R, 2), 1);
-    const int gin = dot_walk(g, g->in_nbr, in, k, v, ids, ain);
+    dot_lanes(in, dot_share(c, 2), 1);
+    const bool gin = dot_walk(g, g->in_nbr, in, k, v, ids, ain);
     if (!gin) in.D.RC = 1;
     // by source: the query heads of a key head in lanes beside each other, as
     // many as a power of two that divides them and one wavefront hold
     int RL = 1;
     while (D.R % (2 * RL) == 0 && (2 * RL) << D.log2HL <= 64) RL *= 2;
     dot_lanes(src, 1, RL);
-    int gout = dot_walk(g, g->out_fine_nbr, src, q, grad_out, ids, aout);
-    if ((int64_t)D.H * 16 >= (1 << 24) || (uint64_t)g->n_dst * D.H * 16 > 0xFFFFFFFFull) gout = 0;
+    bool gout = dot_walk(g, g->out_fine_nbr, src, q, grad_out, ids, aout);
+    if ((int64_t)D.H * 16 >= (1 << 24) || (uint64_t)g->n_dst * D.H * 16 > 0xFFFFFFFFull) gout = false;
     // the gradient of the bias: in that pass, unless the heads that share it
     // take several, in which it is summed over the slices and query heads
     const bool by_edge = grad_bias && !D.bias_per_head && (src.D.slices > 1 || RL < D.R);
     src.D.src_bias = grad_bias && !by_edge;
     dot_lanes(edge, 1, 1);
-    const int gedge = dot_walk(g, g->in_nbr, edge, k, v, true, aedge);
+    const bool gedge = dot_walk(g, g->in_nbr, edge, k, v, true, aedge);
     const int passes = by_edge ? edge.D.slices * D.R : 0;
 
     Scratch sc = scratch_of(g, stream);
@@ -1802,8 +1802,6 @@ static gnnk_status dot_backward(gnnk_graph_t g, const gnnk_tensor* q, const gnnk
     in.D.part = src.D.part = part;
     in.D.part_stride = 2 * W + 2 * D.H;
     src.D.part_stride = 2 * KW;
-    aout.x2 = rec;
-    aout.x2_stride = D.H;
     st = GNNK_LAUNCH(launch_dot(ain, in.D, 1, c.dt, c.geo.vec, gin, stream), "dot-product attention backward launch");
     if (st == GNNK_OK && (grad_k || grad_v || src.D.src_bias))
         st = GNNK_LAUNCH(launch_dot(aout, src.D, 2, c.dt, c.geo.vec, gout, stream),

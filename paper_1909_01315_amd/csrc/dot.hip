@@ -17,7 +17,7 @@
 // row (bf16: the product).  Dot products and the sums over the edges of one wavefront's share of a
 // row are fp32; the partial results of a long row's segments are joined in
 // fp64 in segment order.
-#include "walk.h"
+#include "device.h"
 
 namespace gnnk {
 
@@ -51,9 +51,6 @@ struct IO<bf16_pair_t, VEC> {
             w[0] = __uint_as_float((uint32_t)p->x);
         }
     }
-    static __device__ __forceinline__ void load_nt(const bf16_pair_t* p, float* w) { load(p, w); }
-    static __device__ __forceinline__ float load1(const bf16_pair_t* p) { return bf_lo(p->x); }
-    static __device__ __forceinline__ float load1_nt(const bf16_pair_t* p) { return load1(p); }
 };
 
 namespace {
@@ -84,7 +81,7 @@ constexpr float LOG2E = 1.44269504088896341f;
 
 template <int CTRL>
 __device__ __forceinline__ float dpp_f(float x) {
-    return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), CTRL, 0xF, 0xF, false));
+    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, 0xF, 0xF, true));
 }
 constexpr int DPP_HALF_MIRROR = 0x141, DPP_MIRROR = 0x140;
 
@@ -190,26 +187,131 @@ __device__ __forceinline__ bool bias2(float b, float& out) {
     return b != -INFINITY;
 }
 
-template <typename T>
-__device__ __forceinline__ float load_bias(const DotArgs& D, int32_t ed, int hq) {
-    return IO<T, 1>::load1(reinterpret_cast<const T*>(D.bias) + (uint64_t)(uint32_t)ed * (uint32_t)D.bias_stride +
-                           (D.bias_per_head ? hq : 0));
+// ---------------------------------------------------------------------------
+// the walk over a row's edges
+
+constexpr int U = 4;  // edges in flight per lane group
+
+// what U edges bring to a lane: words of the two gathered rows, the record of
+// the source pass, the bias of RC query heads
+template <int N, int RC>
+struct Batch {
+    float a[U][N], b[U][N];
+    float4 rec[U];
+    float bias[U][RC];
+    int32_t ed[U];
+    bool ok[U];
+};
+
+struct Ids {
+    int32_t nb[U], ed[U];
+};
+
+// ids of the positions p .. p + U - 1, all below e, or (PART) those past e
+// taken from p (side by side for a lane group: one load a batch, no selects)
+template <bool PART, bool EDGES>
+__device__ __forceinline__ void load_ids(const CsrDev& C, int32_t p, int32_t e, Ids& id) {
+    static_assert(U == 4, "one load of four ids");
+    if constexpr (PART) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const int32_t x = p + u < e ? p + u : p;
+            id.nb[u] = C.idx[x];
+            if constexpr (EDGES) id.ed[u] = C.eid ? C.eid[x] : x;
+        }
+    } else {
+        load_i32<U>(C.idx + p, id.nb);
+        if constexpr (EDGES) {
+            if (C.eid) load_i32<U>(C.eid + p, id.ed);
+            else
+#pragma unroll
+                for (int u = 0; u < U; ++u) id.ed[u] = p + u;
+        }
+    }
 }
 
-// scores of N slots of one query head (totals of the shares, plus the bias);
-// gone[u]: the slot lies outside the row or is masked
-template <typename T, int N, bool ALL>
-__device__ __forceinline__ void scores(const DotArgs& D, const float* bs, const bool* ok, float* s, bool* gone) {
-#pragma unroll
-    for (int u = 0; u < N; ++u) {
-        gone[u] = ALL ? false : !ok[u];
-        if constexpr (Words<T, 2>::PAIRS) s[u] *= D.scale2;
+// a row of a node table; FAST: byte offsets of 32 bits (the host checks)
+template <typename T, int VEC, bool FAST>
+__device__ __forceinline__ void gather(const OperandDev& o, int32_t nb, int col, float* w) {
+    using W = typename Words<T, VEC>::type;
+    if constexpr (FAST) {
+        const uint32_t off = __umul24((uint32_t)nb, (uint32_t)o.stride * (uint32_t)sizeof(T)) +
+                             (uint32_t)col * (uint32_t)sizeof(T);
+        IO<W, VEC>::load(reinterpret_cast<const W*>(reinterpret_cast<const char*>(o.data) + off), w);
+    } else {
+        IO<W, VEC>::load(reinterpret_cast<const W*>(o.data) + (uint64_t)(uint32_t)nb * (uint32_t)o.stride + col, w);
     }
-    if (D.bias) {
+}
+
+// The loads of a batch at p: columns col of the tables a and b, with REC the
+// record of (neighbour, head hq), with BIAS the values of heads hq .. hq + RC - 1.
+template <typename T, int VEC, int RC, bool FAST, bool BIAS, bool REC, bool PART>
+__device__ __forceinline__ void issue(const EngineArgs& A, const DotArgs& D, const Ids& id, int32_t p, int32_t e,
+                                      int col, int hq, Batch<Words<T, VEC>::N, RC>& x) {
 #pragma unroll
-        for (int u = 0; u < N; ++u) {
+    for (int u = 0; u < U; ++u) {
+        gather<T, VEC, FAST>(A.a, id.nb[u], col, x.a[u]);
+        gather<T, VEC, FAST>(A.b, id.nb[u], col, x.b[u]);
+        if constexpr (REC && FAST)
+            x.rec[u] = *reinterpret_cast<const float4*>(
+                reinterpret_cast<const char*>(D.rec) +
+                (__umul24((uint32_t)id.nb[u], (uint32_t)D.H * 16u) + (uint32_t)hq * 16u));
+        else if constexpr (REC) x.rec[u] = D.rec[(uint64_t)(uint32_t)id.nb[u] * (uint32_t)D.H + (uint32_t)hq];
+        x.ok[u] = !PART || p + u < e;
+    }
+    if constexpr (BIAS) {
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            x.ed[u] = id.ed[u];
+            const T* b = reinterpret_cast<const T*>(D.bias) +
+                         (uint64_t)(uint32_t)id.ed[u] * (uint32_t)D.bias_stride;
+            if (D.bias_per_head) {
+                IO<T, RC>::load(b + hq, x.bias[u]);
+            } else {
+                x.bias[u][0] = IO<T, 1>::load1(b);
+#pragma unroll
+                for (int r = 1; r < RC; ++r) x.bias[u][r] = x.bias[u][0];
+            }
+        }
+    }
+}
+
+// A lane group takes U edges at b + start, b + start + stride, ... of a row
+// [b, e): the groups of a wavefront side by side (start U g, stride U G), or a
+// group its own row (0, U).  The ids of the next batch load behind the
+// gathers of this one.
+template <typename T, int VEC, int RC, bool FAST, bool BIAS, bool REC, class F>
+__device__ __forceinline__ void walk(const EngineArgs& A, const DotArgs& D, int32_t b, int32_t e, int32_t start,
+                                     int32_t stride, int col, int hq, F& sink) {
+    int32_t p = b + start;
+    Ids id;
+    if (p + U <= e) load_ids<false, BIAS>(A.csr, p, e, id);
+    else if (p < e) load_ids<true, BIAS>(A.csr, p, e, id);
+    Batch<Words<T, VEC>::N, RC> x;
+    while (p + U <= e) {
+        issue<T, VEC, RC, FAST, BIAS, REC, false>(A, D, id, p, e, col, hq, x);
+        p += stride;
+        if (p + U <= e) load_ids<false, BIAS>(A.csr, p, e, id);
+        else if (p < e) load_ids<true, BIAS>(A.csr, p, e, id);
+        sink.template take<true>(x);
+    }
+    if (p < e) {
+        issue<T, VEC, RC, FAST, BIAS, REC, true>(A, D, id, p, e, col, hq, x);
+        sink.template take<false>(x);
+    }
+}
+
+// scores of a batch for one query head from their totals; gone[u]: the slot
+// lies outside the row or is masked
+template <typename T, int RC, bool BIAS, bool ALL, class B>
+__device__ __forceinline__ void scores(const DotArgs& D, const B& x, int r, float* s, bool* gone) {
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+        gone[u] = ALL ? false : !x.ok[u];
+        if constexpr (Words<T, 2>::PAIRS) s[u] *= D.scale2;
+        if constexpr (BIAS) {
             float b2;
-            gone[u] |= !bias2(bs[u], b2);
+            gone[u] |= !bias2(x.bias[u][r], b2);
             s[u] += b2;
         }
     }
@@ -218,7 +320,7 @@ __device__ __forceinline__ void scores(const DotArgs& D, const float* bs, const 
 // ---------------------------------------------------------------------------
 // forward
 
-template <typename T, int VEC, int RC, bool OV>
+template <typename T, int VEC, int RC, bool OV, bool BIAS>
 struct Forward {
     const DotArgs& D;
     const Place& p;
@@ -238,33 +340,22 @@ struct Forward {
             for (int i = 0; i < VEC; ++i) acc[r][i] = 0.0f;
         }
     }
-    static constexpr bool kBatch = true, kSlots = true;
-    __device__ __forceinline__ void batch(const Raw<VEC>* rw, const int32_t* ed) { take<true>(rw, ed, nullptr); }
-    __device__ __forceinline__ void slots(const Raw<VEC>* rw, const int32_t* ed, const bool* ok) {
-        take<false>(rw, ed, ok);
-    }
-    template <bool ALL>
-    __device__ __forceinline__ void take(const Raw<VEC>* rw, const int32_t* ed, const bool* ok) {
-        float bs[RC][UNR], s[RC * UNR];
-        if (D.bias) {
-#pragma unroll
-            for (int r = 0; r < RC; ++r)
-#pragma unroll
-                for (int u = 0; u < UNR; ++u) bs[r][u] = load_bias<T>(D, ed[u], hq + r);
-        }
+    template <bool ALL, class B>
+    __device__ __forceinline__ void take(const B& x) {
+        float s[RC * U];
 #pragma unroll
         for (int r = 0; r < RC; ++r)
 #pragma unroll
-            for (int u = 0; u < UNR; ++u) s[r * UNR + u] = share<T, VEC, OV>(q[r], rw[u].a, p);
-        run_totals<RC * UNR>(s, 1 << D.log2HL);
+            for (int u = 0; u < U; ++u) s[r * U + u] = share<T, VEC, OV>(q[r], x.a[u], p);
+        run_totals<RC * U>(s, 1 << D.log2HL);
 #pragma unroll
         for (int r = 0; r < RC; ++r) {
-            bool gone[UNR];
-            float* sr = s + r * UNR;
-            scores<T, UNR, ALL>(D, bs[r], ok, sr, gone);
+            bool gone[U];
+            float* sr = s + r * U;
+            scores<T, RC, BIAS, ALL>(D, x, r, sr, gone);
             float mn = m[r];
 #pragma unroll
-            for (int u = 0; u < UNR; ++u) {
+            for (int u = 0; u < U; ++u) {
                 sr[u] = gone[u] ? -INFINITY : sr[u];
                 mn = fmaxf(mn, sr[u]);
             }
@@ -276,13 +367,13 @@ struct Forward {
                 for (int i = 0; i < VEC; ++i) acc[r][i] *= f;
             }
 #pragma unroll
-            for (int u = 0; u < UNR; ++u) {
+            for (int u = 0; u < U; ++u) {
                 const float w = __builtin_amdgcn_exp2f(sr[u] - at);
                 // (a slot that is gone adds nothing, whatever value it holds)
                 if (!gone[u]) {
                     l[r] += w;
 #pragma unroll
-                    for (int i = 0; i < VEC; ++i) acc[r][i] = fmaf(w, W::at(rw[u].b, i), acc[r][i]);
+                    for (int i = 0; i < VEC; ++i) acc[r][i] = fmaf(w, W::at(x.b[u], i), acc[r][i]);
                 }
             }
             m[r] = mn;
@@ -343,22 +434,21 @@ __device__ __forceinline__ void empty_rows(const EngineArgs& A, int w, int G, in
         if (k0 + x < A.sch.n_rows) fn((int64_t)A.csr.perm[k0 + x]);
 }
 
-template <typename T, int VEC, int RC, class S>
+template <typename T, int VEC, int RC, bool OV, bool BIAS, bool FAST>
 __global__ __launch_bounds__(256) void dot_forward_kernel(EngineArgs A, DotArgs D) {
     const int w = wave_id();
     if (w >= A.sch.w_total) return;
-    const Lanes ln = lanes_of<S::GC>(A.geo);
-    const int G = S::GC > 0 ? S::GC : A.geo.G, L = WAVE / G;
+    const Lanes ln = lanes_of(A.geo);
+    const int G = A.geo.G, L = A.geo.L;
     const Place p = place_of<VEC>(D, ln.lig);
     const int kcol = p.j * D.F + p.c, step = RC << D.log2RL, h0 = p.j * D.R + p.rl * RC;
-    const Pre<VEC> pre{};
     auto store = [&](int64_t row, int hq, const float* v, float f) {
         float o[VEC];
 #pragma unroll
         for (int i = 0; i < VEC; ++i) o[i] = v[i] * f;
         IO<T, VEC>::store(reinterpret_cast<T*>(D.out) + row * D.out_stride + (int64_t)hq * D.F + p.c, o);
     };
-    using State = Forward<T, VEC, RC, S::OV>;
+    using State = Forward<T, VEC, RC, OV, BIAS>;
     auto finish = [&](const State& st, int64_t row) {
 #pragma unroll
         for (int x = 0; x < RC; ++x) {
@@ -366,13 +456,16 @@ __global__ __launch_bounds__(256) void dot_forward_kernel(EngineArgs A, DotArgs 
             if (p.first) write_stats(D, row, st.hq + x, st.m[x], st.l[x]);
         }
     };
-    if (w < A.sch.w_big_end) {
-        const Work k = wave_work(A, w);
+    if (w < A.sch.w_small_end) {
+        const bool wave = w < A.sch.w_big_end;
+        const Work k = wave ? wave_work(A, w) : lane_work(A, w, G, ln.g);
+        const int64_t self = k.r >= 0 ? k.r : 0;
         for (int r = 0; r < D.R; r += step) {
-            State st(D, p, h0 + r, k.r);
-            walk_row<typename Words<T, VEC>::type, VEC, 1, EXT_NONE, S>(A, (int32_t)k.r, k.b, k.e, ln.g, G, kcol, 0, pre, st);
-            st.join_groups(L);
-            if (ln.g != 0 || !p.act) continue;
+            State st(D, p, h0 + r, self);
+            walk<T, VEC, RC, FAST, BIAS, false>(A, D, (int32_t)k.b, (int32_t)k.e, wave ? U * ln.g : 0,
+                                                wave ? U * G : U, kcol, st.hq, st);
+            if (wave) st.join_groups(L);
+            if ((wave && ln.g != 0) || k.r < 0 || !p.act) continue;
             if (k.slot >= 0) {
                 float* P = D.part + (int64_t)k.slot * D.part_stride;
 #pragma unroll
@@ -388,14 +481,6 @@ __global__ __launch_bounds__(256) void dot_forward_kernel(EngineArgs A, DotArgs 
             } else {
                 finish(st, k.r);
             }
-        }
-    } else if (w < A.sch.w_small_end) {
-        const Work k = lane_work(A, w, G, ln.g);
-        const int64_t self = k.r >= 0 ? k.r : 0;
-        for (int r = 0; r < D.R; r += step) {
-            State st(D, p, h0 + r, self);
-            walk_lane<typename Words<T, VEC>::type, VEC, 1, EXT_NONE, S>(A, (int32_t)self, k.b, k.e, kcol, 0, pre, st);
-            if (k.r >= 0 && p.act) finish(st, k.r);
         }
     } else {
         empty_rows(A, w, G, ln.g, [&](int64_t row) {
@@ -433,7 +518,6 @@ __global__ void dot_join_kernel(EngineArgs A, DotArgs D, int cols) {
         m = mn;
     };
     if (ok) {
-        constexpr int U = 4;
         for (int s = s0 + run; s < s1; s += U * runs) {
             float pm[U], pl[U], pa[U];
 #pragma unroll
@@ -474,7 +558,7 @@ __global__ void dot_join_kernel(EngineArgs A, DotArgs D, int cols) {
 // destination and head for the source pass, which walks the reverse graph's
 // CSR and gathers q, dout and the record.
 
-template <typename T, int VEC, int RC, bool OV>
+template <typename T, int VEC, int RC, bool OV, bool BIAS>
 struct ToDst {
     const DotArgs& D;
     const Place& p;
@@ -501,43 +585,32 @@ struct ToDst {
         }
         run_totals<RC>(S0, 1 << D.log2HL);
     }
-    static constexpr bool kBatch = true, kSlots = true;
-    __device__ __forceinline__ void batch(const Raw<VEC>* rw, const int32_t* ed) { take<true>(rw, ed, nullptr); }
-    __device__ __forceinline__ void slots(const Raw<VEC>* rw, const int32_t* ed, const bool* ok) {
-        take<false>(rw, ed, ok);
-    }
-    template <bool ALL>
-    __device__ __forceinline__ void take(const Raw<VEC>* rw, const int32_t* ed, const bool* ok) {
-        float bs[RC][UNR], s[2 * RC * UNR];
-        if (D.bias) {
-#pragma unroll
-            for (int r = 0; r < RC; ++r)
-#pragma unroll
-                for (int u = 0; u < UNR; ++u) bs[r][u] = load_bias<T>(D, ed[u], hq + r);
-        }
+    template <bool ALL, class B>
+    __device__ __forceinline__ void take(const B& x) {
+        float s[2 * RC * U];
 #pragma unroll
         for (int r = 0; r < RC; ++r)
 #pragma unroll
-            for (int u = 0; u < UNR; ++u) {
-                s[2 * r * UNR + u] = share<T, VEC, OV>(q[r], rw[u].a, p);
-                s[(2 * r + 1) * UNR + u] = share<T, VEC, OV>(dz[r], rw[u].b, p);
+            for (int u = 0; u < U; ++u) {
+                s[2 * r * U + u] = share<T, VEC, OV>(q[r], x.a[u], p);
+                s[(2 * r + 1) * U + u] = share<T, VEC, OV>(dz[r], x.b[u], p);
             }
-        run_totals<2 * RC * UNR>(s, 1 << D.log2HL);
+        run_totals<2 * RC * U>(s, 1 << D.log2HL);
 #pragma unroll
         for (int r = 0; r < RC; ++r) {
-            bool gone[UNR];
-            float *sr = s + 2 * r * UNR, *tr = sr + UNR;
-            scores<T, UNR, ALL>(D, bs[r], ok, sr, gone);
+            bool gone[U];
+            float *sr = s + 2 * r * U, *tr = sr + U;
+            scores<T, RC, BIAS, ALL>(D, x, r, sr, gone);
 #pragma unroll
-            for (int u = 0; u < UNR; ++u) {
+            for (int u = 0; u < U; ++u) {
                 const float a = __builtin_amdgcn_exp2f(sr[u] - m[r]) * il[r], w = a * (tr[u] - S0[r]);
                 if (!gone[u]) {
                     delta[r] += w;
 #pragma unroll
                     for (int i = 0; i < VEC; ++i) {
-                        const float x = W::at(rw[u].a, i);
-                        e1[r][i] = fmaf(w, x, e1[r][i]);
-                        e2[r][i] = fmaf(a, x, e2[r][i]);
+                        const float y = W::at(x.a[u], i);
+                        e1[r][i] = fmaf(w, y, e1[r][i]);
+                        e2[r][i] = fmaf(a, y, e2[r][i]);
                     }
                 }
             }
@@ -572,7 +645,7 @@ struct ToDst {
 // gradients of a bias that the heads share where they take several passes:
 // the sum over this pass's heads, added to those of the passes before (their
 // sums by edge id in D.edge_acc)
-template <typename T, int VEC, bool OV>
+template <typename T, int VEC, bool OV, bool BIAS>
 struct ToEdge {
     const DotArgs& D;
     const Place& p;
@@ -588,63 +661,58 @@ struct ToEdge {
         row_words<T, VEC>(D.dz, row * D.dz_stride + c, dz);
         rec = D.rec[row * D.H + hq];
     }
-    static constexpr bool kBatch = true, kSlots = true;
-    __device__ __forceinline__ void batch(const Raw<VEC>* rw, const int32_t* ed) { take<true>(rw, ed, nullptr); }
-    __device__ __forceinline__ void slots(const Raw<VEC>* rw, const int32_t* ed, const bool* ok) {
-        take<false>(rw, ed, ok);
-    }
-    template <bool ALL>
-    __device__ __forceinline__ void take(const Raw<VEC>* rw, const int32_t* ed, const bool* ok) {
-        float bs[UNR], s[2 * UNR], ds[UNR];
-        bool gone[UNR];
+    template <bool ALL, class B>
+    __device__ __forceinline__ void take(const B& x) {
+        float s[2 * U], ds[U];
+        bool gone[U];
 #pragma unroll
-        for (int u = 0; u < UNR; ++u) bs[u] = load_bias<T>(D, ed[u], hq);
-#pragma unroll
-        for (int u = 0; u < UNR; ++u) {
-            s[u] = share<T, VEC, OV>(q, rw[u].a, p);
-            s[UNR + u] = share<T, VEC, OV>(dz, rw[u].b, p);
+        for (int u = 0; u < U; ++u) {
+            s[u] = share<T, VEC, OV>(q, x.a[u], p);
+            s[U + u] = share<T, VEC, OV>(dz, x.b[u], p);
         }
-        run_totals<2 * UNR>(s, 1 << D.log2HL);
-        scores<T, UNR, ALL>(D, bs, ok, s, gone);
+        run_totals<2 * U>(s, 1 << D.log2HL);
+        scores<T, 1, BIAS, ALL>(D, x, 0, s, gone);
 #pragma unroll
-        for (int u = 0; u < UNR; ++u) {
-            ds[u] = __builtin_amdgcn_exp2f(s[u] - rec.x) * rec.y * (s[UNR + u] - rec.z);
+        for (int u = 0; u < U; ++u) {
+            ds[u] = __builtin_amdgcn_exp2f(s[u] - rec.x) * rec.y * (s[U + u] - rec.z);
             ds[u] = gone[u] ? 0.0f : ds[u];
         }
 #pragma unroll
-        for (int u = 0; u < UNR; ++u) ds[u] = p.first ? ds[u] : 0.0f;
-        run_totals<UNR>(ds, L);
+        for (int u = 0; u < U; ++u) ds[u] = p.first ? ds[u] : 0.0f;
+        run_totals<U>(ds, L);
         if (__lane_id() & (L - 1)) return;
 #pragma unroll
-        for (int u = 0; u < UNR; ++u) {
-            if (!ALL && !ok[u]) continue;
-            float x = ds[u];
-            if (!D.edge_first) x += D.edge_acc[(uint32_t)ed[u]];
+        for (int u = 0; u < U; ++u) {
+            if (!ALL && !x.ok[u]) continue;
+            float y = ds[u];
+            if (!D.edge_first) y += D.edge_acc[(uint32_t)x.ed[u]];
             if (D.edge_last)
                 IO<T, 1>::store1(reinterpret_cast<T*>(D.d_bias) +
-                                     (uint64_t)(uint32_t)ed[u] * (uint32_t)D.d_bias_stride, x);
-            else D.edge_acc[(uint32_t)ed[u]] = x;
+                                     (uint64_t)(uint32_t)x.ed[u] * (uint32_t)D.d_bias_stride, y);
+            else D.edge_acc[(uint32_t)x.ed[u]] = y;
         }
     }
 };
 
-template <typename T, int VEC, int RC, class S>
+template <typename T, int VEC, int RC, bool OV, bool BIAS, bool FAST>
 __global__ __launch_bounds__(256) void dot_backward_dst_kernel(EngineArgs A, DotArgs D) {
     const int w = wave_id();
     if (w >= A.sch.w_total) return;
-    const Lanes ln = lanes_of<S::GC>(A.geo);
-    const int G = S::GC > 0 ? S::GC : A.geo.G, L = WAVE / G;
+    const Lanes ln = lanes_of(A.geo);
+    const int G = A.geo.G, L = A.geo.L;
     const Place p = place_of<VEC>(D, ln.lig);
     const int kcol = p.j * D.F + p.c, step = RC << D.log2RL, h0 = p.j * D.R + p.rl * RC;
-    const Pre<VEC> pre{};
-    using State = ToDst<T, VEC, RC, S::OV>;
-    if (w < A.sch.w_big_end) {
-        const Work k = wave_work(A, w);
+    using State = ToDst<T, VEC, RC, OV, BIAS>;
+    if (w < A.sch.w_small_end) {
+        const bool wave = w < A.sch.w_big_end;
+        const Work k = wave ? wave_work(A, w) : lane_work(A, w, G, ln.g);
+        const int64_t self = k.r >= 0 ? k.r : 0;
         for (int r = 0; r < D.R; r += step) {
-            State st(D, p, h0 + r, k.r);
-            walk_row<typename Words<T, VEC>::type, VEC, 1, EXT_NONE, S>(A, (int32_t)k.r, k.b, k.e, ln.g, G, kcol, 0, pre, st);
-            st.join_groups(L);
-            if (ln.g != 0 || !p.act) continue;
+            State st(D, p, h0 + r, self);
+            walk<T, VEC, RC, FAST, BIAS, false>(A, D, (int32_t)k.b, (int32_t)k.e, wave ? U * ln.g : 0,
+                                                wave ? U * G : U, kcol, st.hq, st);
+            if (wave) st.join_groups(L);
+            if ((wave && ln.g != 0) || k.r < 0 || !p.act) continue;
             if (k.slot >= 0) {
                 float* P = D.part + (int64_t)k.slot * D.part_stride;
                 const int64_t W = (int64_t)D.H * D.F;
@@ -664,14 +732,6 @@ __global__ __launch_bounds__(256) void dot_backward_dst_kernel(EngineArgs A, Dot
             } else {
                 st.write(k.r);
             }
-        }
-    } else if (w < A.sch.w_small_end) {
-        const Work k = lane_work(A, w, G, ln.g);
-        const int64_t self = k.r >= 0 ? k.r : 0;
-        for (int r = 0; r < D.R; r += step) {
-            State st(D, p, h0 + r, self);
-            walk_lane<typename Words<T, VEC>::type, VEC, 1, EXT_NONE, S>(A, (int32_t)self, k.b, k.e, kcol, 0, pre, st);
-            if (k.r >= 0 && p.act) st.write(k.r);
         }
     } else if (D.d_q) {
         empty_rows(A, w, G, ln.g, [&](int64_t row) {
@@ -696,7 +756,6 @@ __global__ void dot_join_dst_kernel(EngineArgs A, DotArgs D, int cols) {
     const int hq = ok ? (int)(col / D.F) : 0;
     double x1 = 0.0, x2 = 0.0, dl = 0.0;
     if (ok) {
-        constexpr int U = 4;
         for (int s = s0 + run; s < s1; s += U * runs) {
             float p1[U], p2[U], pd[U];
 #pragma unroll
@@ -737,31 +796,25 @@ __global__ void dot_join_dst_kernel(EngineArgs A, DotArgs D, int cols) {
 }
 
 // query head r0 of each key head of a slice
-template <typename T, int VEC, class S>
+template <typename T, int VEC, bool OV, bool FAST>
 __global__ __launch_bounds__(256) void dot_backward_edge_kernel(EngineArgs A, DotArgs D) {
     const int w = wave_id();
     if (w >= A.sch.w_small_end) return;
-    const Lanes ln = lanes_of<S::GC>(A.geo);
-    const int G = S::GC > 0 ? S::GC : A.geo.G, L = WAVE / G;
+    const Lanes ln = lanes_of(A.geo);
+    const int G = A.geo.G, L = A.geo.L;
     const Place p = place_of<VEC>(D, ln.lig);
-    const int kcol = p.j * D.F + p.c, hq = p.j * D.R + D.r0;
-    const Pre<VEC> pre{};
-    if (w < A.sch.w_big_end) {
-        const Work k = wave_work(A, w);
-        ToEdge<T, VEC, S::OV> st(D, p, hq, k.r, L);
-        walk_row<typename Words<T, VEC>::type, VEC, 1, EXT_NONE, S>(A, (int32_t)k.r, k.b, k.e, ln.g, G, kcol, 0, pre, st);
-    } else {
-        const Work k = lane_work(A, w, G, ln.g);
-        const int64_t self = k.r >= 0 ? k.r : A.csr.rowt[0].x;
-        ToEdge<T, VEC, S::OV> st(D, p, hq, self, L);
-        walk_lane<typename Words<T, VEC>::type, VEC, 1, EXT_NONE, S>(A, (int32_t)self, k.b, k.e, kcol, 0, pre, st);
-    }
+    const bool wave = w < A.sch.w_big_end;
+    const Work k = wave ? wave_work(A, w) : lane_work(A, w, G, ln.g);
+    const int64_t self = k.r >= 0 ? k.r : A.csr.rowt[0].x;
+    ToEdge<T, VEC, OV, true> st(D, p, p.j * D.R + D.r0, self, L);
+    walk<T, VEC, 1, FAST, true, false>(A, D, (int32_t)k.b, (int32_t)k.e, wave ? U * ln.g : 0, wave ? U * G : U,
+                                       p.j * D.F + p.c, st.hq, st);
 }
 
 // the source pass: dk and dv of a row over its out-edges, and the gradients of
 // the bias where this pass sees what they take (a value per head, or all heads
 // of a shared one side by side)
-template <typename T, int VEC, bool OV>
+template <typename T, int VEC, bool OV, bool BIAS>
 struct ToSrc {
     const DotArgs& D;
     const Place& p;
@@ -778,51 +831,42 @@ struct ToSrc {
 #pragma unroll
         for (int i = 0; i < VEC; ++i) dk[i] = dv[i] = 0.0f;
     }
-    static constexpr bool kBatch = true, kSlots = true;
-    __device__ __forceinline__ void batch(const Raw<VEC>* rw, const int32_t* ed) { take<true>(rw, ed, nullptr); }
-    __device__ __forceinline__ void slots(const Raw<VEC>* rw, const int32_t* ed, const bool* ok) {
-        take<false>(rw, ed, ok);
-    }
-    template <bool ALL>
-    __device__ __forceinline__ void take(const Raw<VEC>* rw, const int32_t* ed, const bool* ok) {
-        float bs[UNR], s[2 * UNR];
-        bool gone[UNR];
-        if (D.bias) {
+    template <bool ALL, class B>
+    __device__ __forceinline__ void take(const B& x) {
+        float s[2 * U];
+        bool gone[U];
 #pragma unroll
-            for (int u = 0; u < UNR; ++u) bs[u] = load_bias<T>(D, ed[u], hq);
+        for (int u = 0; u < U; ++u) {
+            s[u] = share<T, VEC, OV>(k, x.a[u], p);
+            s[U + u] = share<T, VEC, OV>(v, x.b[u], p);
         }
+        run_totals<2 * U>(s, 1 << D.log2HL);
+        scores<T, 1, BIAS, ALL>(D, x, 0, s, gone);
 #pragma unroll
-        for (int u = 0; u < UNR; ++u) {
-            s[u] = share<T, VEC, OV>(k, rw[u].a, p);
-            s[UNR + u] = share<T, VEC, OV>(v, rw[u].b, p);
-        }
-        run_totals<2 * UNR>(s, 1 << D.log2HL);
-        scores<T, UNR, ALL>(D, bs, ok, s, gone);
-#pragma unroll
-        for (int u = 0; u < UNR; ++u) {
-            const float a = __builtin_amdgcn_exp2f(s[u] - rw[u].rec.x) * rw[u].rec.y;
-            const float w = a * (s[UNR + u] - rw[u].rec.z);
+        for (int u = 0; u < U; ++u) {
+            const float a = __builtin_amdgcn_exp2f(s[u] - x.rec[u].x) * x.rec[u].y;
+            const float w = a * (s[U + u] - x.rec[u].z);
             if (!gone[u]) {
 #pragma unroll
                 for (int i = 0; i < VEC; ++i) {
-                    dk[i] = fmaf(w, W::at(rw[u].a, i), dk[i]);
-                    dv[i] = fmaf(a, W::at(rw[u].b, i), dv[i]);
+                    dk[i] = fmaf(w, W::at(x.a[u], i), dk[i]);
+                    dv[i] = fmaf(a, W::at(x.b[u], i), dv[i]);
                 }
             }
             s[u] = gone[u] ? 0.0f : w;
         }
-        if (!D.src_bias) return;
+        if (!BIAS || !D.src_bias) return;
         if (D.bias_per_head) {
 #pragma unroll
-            for (int u = 0; u < UNR; ++u)
-                if (p.first && (ALL || ok[u])) store_dbias(ed[u], hq, s[u]);
+            for (int u = 0; u < U; ++u)
+                if (p.first && (ALL || x.ok[u])) store_dbias(x.ed[u], hq, s[u]);
         } else {
 #pragma unroll
-            for (int u = 0; u < UNR; ++u) s[u] = p.first ? s[u] : 0.0f;
-            run_totals<UNR>(s, L);
+            for (int u = 0; u < U; ++u) s[u] = p.first ? s[u] : 0.0f;
+            run_totals<U>(s, L);
 #pragma unroll
-            for (int u = 0; u < UNR; ++u)
-                if ((__lane_id() & (L - 1)) == 0 && (ALL || ok[u])) store_dbias(ed[u], 0, s[u]);
+            for (int u = 0; u < U; ++u)
+                if ((__lane_id() & (L - 1)) == 0 && (ALL || x.ok[u])) store_dbias(x.ed[u], 0, s[u]);
         }
     }
     __device__ __forceinline__ void store_dbias(int32_t ed, int h, float x) {
@@ -848,27 +892,30 @@ struct ToSrc {
     }
 };
 
-template <typename T, int VEC, class S>
+template <typename T, int VEC, bool OV, bool BIAS, bool FAST>
 __global__ __launch_bounds__(256) void dot_backward_src_kernel(EngineArgs A, DotArgs D) {
     const int w = wave_id();
     if (w >= A.sch.w_total) return;
-    const Lanes ln = lanes_of<S::GC>(A.geo);
-    const int G = S::GC > 0 ? S::GC : A.geo.G, L = WAVE / G;
+    const Lanes ln = lanes_of(A.geo);
+    const int G = A.geo.G, L = A.geo.L;
     const Place p = place_of<VEC>(D, ln.lig);
-    const Pre<VEC> pre{};
-    if (w < A.sch.w_big_end) {
-        const Work k = wave_work(A, w);
-        ToSrc<T, VEC, S::OV> st(D, p, k.r, L);
+    if (w < A.sch.w_small_end) {
+        const bool wave = w < A.sch.w_big_end;
+        const Work k = wave ? wave_work(A, w) : lane_work(A, w, G, ln.g);
+        const int64_t self = k.r >= 0 ? k.r : 0;
+        ToSrc<T, VEC, OV, BIAS> st(D, p, self, L);
         for (int r = p.rl; r < D.R; r += 1 << D.log2RL) {
             st.hq = p.j * D.R + r;
-            walk_row<typename Words<T, VEC>::type, VEC, 1, EXT_REC, S>(A, (int32_t)k.r, k.b, k.e, ln.g, G, st.hq * D.F + p.c, st.hq, pre, st);
+            walk<T, VEC, 1, FAST, BIAS, true>(A, D, (int32_t)k.b, (int32_t)k.e, wave ? U * ln.g : 0,
+                                              wave ? U * G : U, st.hq * D.F + p.c, st.hq, st);
         }
-        st.join(L, WAVE);
+        if (wave) st.join(L, WAVE);
         st.join_heads();
-        if (ln.g != 0 || !p.act || p.rl != 0) return;
+        if ((wave && ln.g != 0) || k.r < 0 || !p.act || p.rl != 0) return;
         if (k.slot >= 0) {
             float* P = D.part + (int64_t)k.slot * D.part_stride;
             const int64_t W = (int64_t)D.K * D.F, c = (int64_t)p.j * D.F + p.c;
+#pragma unroll
             for (int i = 0; i < VEC; ++i) {
                 P[c + i] = st.dk[i];
                 P[W + c + i] = st.dv[i];
@@ -876,16 +923,6 @@ __global__ __launch_bounds__(256) void dot_backward_src_kernel(EngineArgs A, Dot
         } else {
             st.write(k.r);
         }
-    } else if (w < A.sch.w_small_end) {
-        const Work k = lane_work(A, w, G, ln.g);
-        const int64_t self = k.r >= 0 ? k.r : 0;
-        ToSrc<T, VEC, S::OV> st(D, p, self, L);
-        for (int r = p.rl; r < D.R; r += 1 << D.log2RL) {
-            st.hq = p.j * D.R + r;
-            walk_lane<typename Words<T, VEC>::type, VEC, 1, EXT_REC, S>(A, (int32_t)self, k.b, k.e, st.hq * D.F + p.c, st.hq, pre, st);
-        }
-        st.join_heads();
-        if (k.r >= 0 && p.act && p.rl == 0) st.write(k.r);
     } else {
         empty_rows(A, w, G, ln.g, [&](int64_t row) {
             const float zero[VEC] = {};
@@ -908,7 +945,6 @@ __global__ void dot_join_src_kernel(EngineArgs A, DotArgs D, int cols) {
     const bool ok = col < 2 * W;
     double x = 0.0;
     if (ok) {
-        constexpr int U = 4;
         for (int s = s0 + run; s < s1; s += U * runs) {
             float y[U];
 #pragma unroll
@@ -933,12 +969,6 @@ __global__ void dot_join_src_kernel(EngineArgs A, DotArgs D, int cols) {
 
 // ---------------------------------------------------------------------------
 
-template <int C, bool OV>
-using SpDot = Spec<T_NBR, OK_FULL, T_NBR, OK_FULL, C, false, true, OV>;
-
-template <typename T, int V>
-constexpr bool dot_fast = V == (sizeof(T) == 4 ? 4 : 8);
-
 // columns and threads of a workgroup that joins segments
 struct Join {
     int cols, threads;
@@ -951,72 +981,63 @@ Join join_of(const EngineArgs& a) {
     return many ? Join{16, 1024} : Join{64, 256};
 }
 
-// query heads of a key head that a lane takes at once: 1 (forward and
-// destination pass) on the runtime layouts, which hold no more
-#define GNNK_RC_DISPATCH(RC_, S_, ...)                                    \
-    if constexpr (S_::FAST) {                                             \
-        switch (RC_) {                                                    \
-            case 4: { constexpr int RC = 4; __VA_ARGS__; } break;         \
-            case 3: { constexpr int RC = 3; __VA_ARGS__; } break;         \
-            case 2: { constexpr int RC = 2; __VA_ARGS__; } break;         \
-            default: { constexpr int RC = 1; __VA_ARGS__; } break;        \
-        }                                                                 \
-    } else {                                                              \
-        constexpr int RC = 1;                                             \
-        __VA_ARGS__;                                                      \
-    }
-
-template <typename T, int V, class S>
-void dot_pass(const EngineArgs& a, const DotArgs& d, int pass, hipStream_t s) {
+template <typename T, int V, int RC, bool OV, bool BIAS, bool FAST>
+void dot_launch(const EngineArgs& a, const DotArgs& d, int pass, hipStream_t s) {
     const dim3 grid(blocks_for_waves(a.sch.w_total), (unsigned)d.slices), block(WAVE * WPB);
     const Join j = join_of(a);
     const int64_t HF = (int64_t)d.H * d.F, KF = (int64_t)d.K * d.F;
+    const dim3 threads(j.threads);
     if (pass == 0) {
-        GNNK_RC_DISPATCH(d.RC, S, hipLaunchKernelGGL((dot_forward_kernel<T, V, RC, S>), grid, block, 0, s, a, d))
-        if (a.sch.n_hub > 0)
-            hipLaunchKernelGGL((dot_join_kernel<T>), j.grid(a, HF), dim3(j.threads), 0, s, a, d, j.cols);
+        hipLaunchKernelGGL((dot_forward_kernel<T, V, RC, OV, BIAS, FAST>), grid, block, 0, s, a, d);
+        if (a.sch.n_hub > 0) hipLaunchKernelGGL((dot_join_kernel<T>), j.grid(a, HF), threads, 0, s, a, d, j.cols);
     } else if (pass == 1) {
-        if (d.RC == 2 && S::FAST) {
-            if constexpr (S::FAST)
-                hipLaunchKernelGGL((dot_backward_dst_kernel<T, V, 2, S>), grid, block, 0, s, a, d);
-        } else {
-            hipLaunchKernelGGL((dot_backward_dst_kernel<T, V, 1, S>), grid, block, 0, s, a, d);
-        }
-        if (a.sch.n_hub > 0)
-            hipLaunchKernelGGL((dot_join_dst_kernel<T>), j.grid(a, HF), dim3(j.threads), 0, s, a, d, j.cols);
+        constexpr int RD = RC < 2 ? RC : 2;
+        hipLaunchKernelGGL((dot_backward_dst_kernel<T, V, RD, OV, BIAS, FAST>), grid, block, 0, s, a, d);
+        if (a.sch.n_hub > 0) hipLaunchKernelGGL((dot_join_dst_kernel<T>), j.grid(a, HF), threads, 0, s, a, d, j.cols);
     } else if (pass == 2) {
-        hipLaunchKernelGGL((dot_backward_src_kernel<T, V, S>), grid, block, 0, s, a, d);
+        hipLaunchKernelGGL((dot_backward_src_kernel<T, V, OV, BIAS, FAST>), grid, block, 0, s, a, d);
         if (a.sch.n_hub > 0)
-            hipLaunchKernelGGL((dot_join_src_kernel<T>), j.grid(a, 2 * KF), dim3(j.threads), 0, s, a, d, j.cols);
+            hipLaunchKernelGGL((dot_join_src_kernel<T>), j.grid(a, 2 * KF), threads, 0, s, a, d, j.cols);
     } else {
         const dim3 egrid(blocks_for_waves(a.sch.w_small_end), (unsigned)d.slices);
-        hipLaunchKernelGGL((dot_backward_edge_kernel<T, V, S>), egrid, block, 0, s, a, d);
+        hipLaunchKernelGGL((dot_backward_edge_kernel<T, V, OV, FAST>), egrid, block, 0, s, a, d);
     }
 }
 
+template <typename T, int V, int RC, bool OV, bool FAST>
+void dot_bias(const EngineArgs& a, const DotArgs& d, int pass, hipStream_t s) {
+    if (d.bias) dot_launch<T, V, RC, OV, true, FAST>(a, d, pass, s);
+    else dot_launch<T, V, RC, OV, false, FAST>(a, d, pass, s);
+}
+
+// the widest vectors have kernels without shared columns and for several query
+// heads in registers; narrower heads and tables past 32-bit offsets one each
 template <typename T, int V>
-void dot_t(const EngineArgs& a, const DotArgs& d, int pass, int gc, hipStream_t s) {
-    if constexpr (dot_fast<T, V>) {
-        if (gc > 0 && d.F % V == 0) {
-            GNNK_GC_DISPATCH(gc, dot_pass<T, V, SpDot<C, false>>(a, d, pass, s))
-            return;
-        }
-        if (gc > 0) {
-            GNNK_GC_DISPATCH(gc, dot_pass<T, V, SpDot<C, true>>(a, d, pass, s))
-            return;
-        }
+void dot_t(const EngineArgs& a, const DotArgs& d, int pass, bool fast, hipStream_t s) {
+    constexpr bool WIDE = V == (sizeof(T) == 4 ? 4 : 8);
+    if (!fast) {
+        dot_bias<T, V, 1, true, false>(a, d, pass, s);
+    } else if constexpr (!WIDE) {
+        dot_bias<T, V, 1, true, true>(a, d, pass, s);
+    } else if (d.F % V != 0) {
+        if (d.RC == 4) dot_bias<T, V, 4, true, true>(a, d, pass, s);
+        else if (d.RC == 2) dot_bias<T, V, 2, true, true>(a, d, pass, s);
+        else dot_bias<T, V, 1, true, true>(a, d, pass, s);
+    } else {
+        if (d.RC == 4) dot_bias<T, V, 4, false, true>(a, d, pass, s);
+        else if (d.RC == 2) dot_bias<T, V, 2, false, true>(a, d, pass, s);
+        else dot_bias<T, V, 1, false, true>(a, d, pass, s);
     }
-    dot_pass<T, V, SpDot<0, true>>(a, d, pass, s);
 }
 
 }  // namespace
 
-hipError_t launch_dot(const EngineArgs& a, const DotArgs& d, int pass, int dtype, int vec, int gc, hipStream_t s) {
+hipError_t launch_dot(const EngineArgs& a, const DotArgs& d, int pass, int dtype, int vec, bool fast, hipStream_t s) {
     if (a.sch.w_total <= 0 || (pass == 3 && a.sch.w_small_end <= 0)) return hipSuccess;
     if (dtype == 0) {
-        GNNK_VEC_DISPATCH_F32(vec, dot_t<float, V>(a, d, pass, gc, s))
+        GNNK_VEC_DISPATCH_F32(vec, dot_t<float, V>(a, d, pass, fast, s))
     } else {
-        GNNK_VEC_DISPATCH_BF16(vec, dot_t<bf16_t, V>(a, d, pass, gc, s))
+        GNNK_VEC_DISPATCH_BF16(vec, dot_t<bf16_t, V>(a, d, pass, fast, s))
     }
     return hipGetLastError();
 }

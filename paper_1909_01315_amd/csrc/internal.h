@@ -276,7 +276,8 @@ struct DotArgs {
     int32_t edge_first, edge_last;  // pass 3: the first, the last of its passes
 };
 // pass: 0 forward, 1 backward by destination, 2 by source, 3 by edge
-hipError_t launch_dot(const EngineArgs& a, const DotArgs& d, int pass, int dtype, int vec, int gc, hipStream_t s);
+// fast: the gathered tables take 32-bit byte offsets
+hipError_t launch_dot(const EngineArgs& a, const DotArgs& d, int pass, int dtype, int vec, bool fast, hipStream_t s);
 // rotary positions and norms of heads, rotary.hip: up to two tensors (queries
 // and keys) of one head width in one launch
 struct RotarySide {

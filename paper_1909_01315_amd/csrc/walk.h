@@ -150,13 +150,6 @@ struct TakesBatch : std::false_type {};
 template <class F>
 struct TakesBatch<F, std::void_t<decltype(F::kBatch)>> : std::integral_constant<bool, F::kBatch> {};
 
-// A consumer that takes a partial batch at once too says so with kSlots = true
-// and a method slots(r, ed, ok); slots with ok false hold another edge's values.
-template <class F, class = void>
-struct TakesSlots : std::false_type {};
-template <class F>
-struct TakesSlots<F, std::void_t<decltype(F::kSlots)>> : std::integral_constant<bool, F::kSlots> {};
-
 // Hand the edges of a full batch to consume (b of a CB spec arrives by
 // ds_bpermute from the coalesced load).
 template <int VEC, int OPK, class S, class F>
@@ -224,12 +217,8 @@ __device__ __forceinline__ void walk_strided(const EngineArgs& A, int32_t self, 
             nbc[u] = nb[u];
         }
         batch_ids(A.csr, b, e, p0 + step, stride, ok, nb, ed, ps);  // next batch, overlapping the gathers
-        if constexpr (TakesSlots<F>::value) {
-            consume.slots(r, edc, okc);
-        } else {
 #pragma unroll
-            for (int u = 0; u < UNR; ++u) consume(r[u], edc[u], nbc[u], okc[u]);
-        }
+        for (int u = 0; u < UNR; ++u) consume(r[u], edc[u], nbc[u], okc[u]);
     }
 }
 
