@@ -423,9 +423,9 @@ gnnk_status gat_aggregate_backward(gnnk_graph_t g, const gnnk_tensor* feat, cons
  * (nullable): (num_edges, H, 1), or (num_edges, 1, 1) for all heads.  A bias
  * of -inf masks its edge: it weighs nothing, whatever k and v hold there.  A
  * destination without in-edges, or with every score -inf, gets 0.  stats
- * (nullable, (num_dst, H, 2), always fp32) receives the maximum score times
- * log2(e) and the reciprocal of the sum of exp(s - max), (0, 0) where out is 0
- * for want of edges; dot_aggregate_backward takes it.  Scores and weighted
+ * (nullable, (num_dst, H, 2), always fp32) receives the maximum score and the
+ * reciprocal of the sum of exp(s - max), (0, 0) where out is 0 for want of
+ * edges; dot_aggregate_backward takes it.  Scores and weighted
  * sums over the edges of one wavefront's share of a row are fp32, the joins of
  * a long row's segments fp64.  F is at most 256 (fp32) or 512 (bf16) and H * F
  * at most 65,536 (GNNK_EUNSUPPORTED beyond).  Scratch: partials of hub rows'

@@ -1643,7 +1643,7 @@ void dot_lanes(DotCall& c, int RC, int RL) {
     geo.D = (int64_t)D.K * D.F;
     geo.FV = D.FV;
     geo.NV = D.heads_slice * lanes;
-    geo.L = pow2ceil(geo.NV);
+    geo.L = std::max(4, pow2ceil(geo.NV));  // (the walk hands ids around in quads)
     geo.log2L = 0;
     while ((1 << geo.log2L) < geo.L) ++geo.log2L;
     geo.G = 64 / geo.L;
@@ -1688,7 +1688,6 @@ void dot_operands(const gnnk_tensor* q, const gnnk_tensor* k, const gnnk_tensor*
         D.bias_per_head = bias->heads == q->heads;
     }
     D.scale = scale;
-    D.scale2 = (float)((double)scale * 1.4426950408889634);
     if (stats) {
         D.stats = static_cast<float*>(stats->data);
         D.stats_stride = stats->row_stride;
@@ -1774,7 +1773,7 @@ static gnnk_status dot_backward(gnnk_graph_t g, const gnnk_tensor* q, const gnnk
     // by destination
     EngineArgs ain{}, aout{}, aedge{};
     DotCall in = c, src = c, edge = c;
-    dot_lanes(in, dot_share(c, 2), 1);
+    dot_lanes(in, dot_share(c, 4), 1);
     const bool gin = dot_walk(g, g->in_nbr, in, k, v, ids, ain);
     if (!gin) in.D.RC = 1;
     // by source: the query heads of a key head in lanes beside each other, as

@@ -13,8 +13,7 @@
 // value row is then gathered and widened once for them), RL neighbouring runs
 // of lanes take as many beside each other, and what is left takes turns.
 //
-// Scores are kept in base 2: the query is scaled by scale * log2(e) once per
-// row (bf16: the product).  Dot products and the sums over the edges of one wavefront's share of a
+// Dot products and the sums over the edges of one wavefront's share of a
 // row are fp32; the partial results of a long row's segments are joined in
 // fp64 in segment order.
 #include "device.h"
@@ -76,8 +75,6 @@ struct Words<bf16_t, VEC> {
         return (i & 1) ? bf_hi(x) : bf_lo(x);
     }
 };
-
-constexpr float LOG2E = 1.44269504088896341f;
 
 template <int CTRL>
 __device__ __forceinline__ float dpp_f(float x) {
@@ -160,31 +157,21 @@ __device__ __forceinline__ float share(const float* x, const float* y, const Pla
     return p.act ? s : 0.0f;
 }
 
-// a row's own operand of the scores: fp32 scaled by scale * log2(e) once, bf16
-// as it is (its totals are scaled instead)
+// a row's own operand of the scores: fp32 scaled once, bf16 as it is (its
+// totals are scaled instead)
 template <typename T, int VEC>
 __device__ __forceinline__ void own_row(const DotArgs& D, const void* base, int64_t at, float* w) {
     using W = Words<T, VEC>;
     IO<typename W::type, VEC>::load(reinterpret_cast<const typename W::type*>(base) + at, w);
     if constexpr (!W::PAIRS) {
 #pragma unroll
-        for (int i = 0; i < W::N; ++i) w[i] *= D.scale2;
+        for (int i = 0; i < W::N; ++i) w[i] *= D.scale;
     }
 }
 template <typename T, int VEC>
 __device__ __forceinline__ void row_words(const void* base, int64_t at, float* w) {
     using W = Words<T, VEC>;
     IO<typename W::type, VEC>::load(reinterpret_cast<const typename W::type*>(base) + at, w);
-}
-
-// the bias of an edge in base 2; false: the edge is masked (-inf)
-__device__ __forceinline__ bool bias2(float b, float& out) {
-    float v = b * LOG2E;
-    // (a finite bias stays finite: with a row of the lowest value everywhere
-    // the edges weigh the same, they are not masked)
-    if (fabsf(v) == INFINITY && fabsf(b) != INFINITY) v = copysignf(3.402823466e38f, b);
-    out = v;
-    return b != -INFINITY;
 }
 
 // ---------------------------------------------------------------------------
@@ -207,25 +194,33 @@ struct Ids {
     int32_t nb[U], ed[U];
 };
 
-// ids of the positions p .. p + U - 1, all below e, or (PART) those past e
-// taken from p (side by side for a lane group: one load a batch, no selects)
-template <bool PART, bool EDGES>
+// the value of lane u of each quad
+template <int L>
+__device__ __forceinline__ int32_t quad_lane(int32_t x) {
+    return __builtin_amdgcn_update_dpp(0, x, L * 0x55, 0xF, 0xF, true);
+}
+__device__ __forceinline__ void spread_quad(int32_t x, int32_t* v) {
+    v[0] = quad_lane<0>(x);
+    v[1] = quad_lane<1>(x);
+    v[2] = quad_lane<2>(x);
+    v[3] = quad_lane<3>(x);
+}
+
+// Ids of the positions p .. p + U - 1 (those past e take p's): lane u of each
+// quad loads one and hands it to the quad.  A load of all four in every lane
+// took the loads' return path as long as a gather.
+template <bool EDGES>
 __device__ __forceinline__ void load_ids(const CsrDev& C, int32_t p, int32_t e, Ids& id) {
-    static_assert(U == 4, "one load of four ids");
-    if constexpr (PART) {
+    static_assert(U == 4, "an id a lane of a quad");
+    int32_t x = p + (__lane_id() & 3);
+    x = x < e ? x : p;
+    spread_quad(C.idx[x], id.nb);
+    if constexpr (EDGES) {
+        if (C.eid) {
+            spread_quad(C.eid[x], id.ed);
+        } else {
 #pragma unroll
-        for (int u = 0; u < U; ++u) {
-            const int32_t x = p + u < e ? p + u : p;
-            id.nb[u] = C.idx[x];
-            if constexpr (EDGES) id.ed[u] = C.eid ? C.eid[x] : x;
-        }
-    } else {
-        load_i32<U>(C.idx + p, id.nb);
-        if constexpr (EDGES) {
-            if (C.eid) load_i32<U>(C.eid + p, id.ed);
-            else
-#pragma unroll
-                for (int u = 0; u < U; ++u) id.ed[u] = p + u;
+            for (int u = 0; u < U; ++u) id.ed[u] = p + u < e ? p + u : p;
         }
     }
 }
@@ -243,11 +238,11 @@ __device__ __forceinline__ void gather(const OperandDev& o, int32_t nb, int col,
     }
 }
 
-// The loads of a batch at p: columns col of the tables a and b, with REC the
-// record of (neighbour, head hq), with BIAS the values of heads hq .. hq + RC - 1.
-template <typename T, int VEC, int RC, bool FAST, bool BIAS, bool REC, bool PART>
-__device__ __forceinline__ void issue(const EngineArgs& A, const DotArgs& D, const Ids& id, int32_t p, int32_t e,
-                                      int col, int hq, Batch<Words<T, VEC>::N, RC>& x) {
+// The loads of a batch: columns col of the tables a and b, with REC the record
+// of (neighbour, head hq), with BIAS the values of heads hq .. hq + RC - 1.
+template <typename T, int VEC, int RC, bool FAST, bool BIAS, bool REC>
+__device__ __forceinline__ void issue(const EngineArgs& A, const DotArgs& D, const Ids& id, int col, int hq,
+                                      Batch<Words<T, VEC>::N, RC>& x) {
 #pragma unroll
     for (int u = 0; u < U; ++u) {
         gather<T, VEC, FAST>(A.a, id.nb[u], col, x.a[u]);
@@ -257,7 +252,6 @@ __device__ __forceinline__ void issue(const EngineArgs& A, const DotArgs& D, con
                 reinterpret_cast<const char*>(D.rec) +
                 (__umul24((uint32_t)id.nb[u], (uint32_t)D.H * 16u) + (uint32_t)hq * 16u));
         else if constexpr (REC) x.rec[u] = D.rec[(uint64_t)(uint32_t)id.nb[u] * (uint32_t)D.H + (uint32_t)hq];
-        x.ok[u] = !PART || p + u < e;
     }
     if constexpr (BIAS) {
 #pragma unroll
@@ -278,27 +272,31 @@ __device__ __forceinline__ void issue(const EngineArgs& A, const DotArgs& D, con
 
 // A lane group takes U edges at b + start, b + start + stride, ... of a row
 // [b, e): the groups of a wavefront side by side (start U g, stride U G), or a
-// group its own row (0, U).  The ids of the next batch load behind the
-// gathers of this one.
+// group its own row (0, U).  The ids of a batch load behind the gathers of the
+// one before it.  (The next batch's gathers in flight while one is summed
+// took registers that wavefronts need: 8.4M edges, 8 query and 2 key heads of
+// 32 bf16, forward 499 -> 533 us, source pass 1,537 -> 1,810.)
 template <typename T, int VEC, int RC, bool FAST, bool BIAS, bool REC, class F>
 __device__ __forceinline__ void walk(const EngineArgs& A, const DotArgs& D, int32_t b, int32_t e, int32_t start,
                                      int32_t stride, int col, int hq, F& sink) {
     int32_t p = b + start;
+    if (p >= e) return;
     Ids id;
-    if (p + U <= e) load_ids<false, BIAS>(A.csr, p, e, id);
-    else if (p < e) load_ids<true, BIAS>(A.csr, p, e, id);
     Batch<Words<T, VEC>::N, RC> x;
-    while (p + U <= e) {
-        issue<T, VEC, RC, FAST, BIAS, REC, false>(A, D, id, p, e, col, hq, x);
-        p += stride;
-        if (p + U <= e) load_ids<false, BIAS>(A.csr, p, e, id);
-        else if (p < e) load_ids<true, BIAS>(A.csr, p, e, id);
+    load_ids<BIAS>(A.csr, p, e, id);
+    issue<T, VEC, RC, FAST, BIAS, REC>(A, D, id, col, hq, x);
+    int32_t pn = p + stride;
+    load_ids<BIAS>(A.csr, pn < e ? pn : p, e, id);
+    while (pn < e) {
         sink.template take<true>(x);
+        issue<T, VEC, RC, FAST, BIAS, REC>(A, D, id, col, hq, x);
+        p = pn;
+        pn += stride;
+        load_ids<BIAS>(A.csr, pn < e ? pn : p, e, id);
     }
-    if (p < e) {
-        issue<T, VEC, RC, FAST, BIAS, REC, true>(A, D, id, p, e, col, hq, x);
-        sink.template take<false>(x);
-    }
+#pragma unroll
+    for (int u = 0; u < U; ++u) x.ok[u] = p + u < e;
+    sink.template take<false>(x);
 }
 
 // scores of a batch for one query head from their totals; gone[u]: the slot
@@ -308,12 +306,9 @@ __device__ __forceinline__ void scores(const DotArgs& D, const B& x, int r, floa
 #pragma unroll
     for (int u = 0; u < U; ++u) {
         gone[u] = ALL ? false : !x.ok[u];
-        if constexpr (Words<T, 2>::PAIRS) s[u] *= D.scale2;
-        if constexpr (BIAS) {
-            float b2;
-            gone[u] |= !bias2(x.bias[u][r], b2);
-            s[u] += b2;
-        }
+        if constexpr (Words<T, 2>::PAIRS) s[u] = BIAS ? fmaf(s[u], D.scale, x.bias[u][r]) : s[u] * D.scale;
+        else if constexpr (BIAS) s[u] += x.bias[u][r];
+        if constexpr (BIAS) gone[u] |= x.bias[u][r] == -INFINITY;
     }
 }
 
@@ -361,14 +356,14 @@ struct Forward {
             }
             const float at = mn == -INFINITY ? 0.0f : mn;
             if (__ballot(mn > m[r]) != 0ull) {
-                const float f = __builtin_amdgcn_exp2f(m[r] - at);
+                const float f = exp_le0(m[r] - at);
                 l[r] *= f;
 #pragma unroll
                 for (int i = 0; i < VEC; ++i) acc[r][i] *= f;
             }
 #pragma unroll
             for (int u = 0; u < U; ++u) {
-                const float w = __builtin_amdgcn_exp2f(sr[u] - at);
+                const float w = exp_le0(sr[u] - at);
                 // (a slot that is gone adds nothing, whatever value it holds)
                 if (!gone[u]) {
                     l[r] += w;
@@ -386,7 +381,7 @@ struct Forward {
             for (int r = 0; r < RC; ++r) {
                 const float om = __shfl_xor(m[r], x, WAVE), ol = __shfl_xor(l[r], x, WAVE);
                 const float mn = fmaxf(m[r], om), at = mn == -INFINITY ? 0.0f : mn;
-                const float f = __builtin_amdgcn_exp2f(m[r] - at), g = __builtin_amdgcn_exp2f(om - at);
+                const float f = exp_le0(m[r] - at), g = exp_le0(om - at);
                 l[r] = l[r] * f + ol * g;
 #pragma unroll
                 for (int i = 0; i < VEC; ++i) acc[r][i] = acc[r][i] * f + __shfl_xor(acc[r][i], x, WAVE) * g;
@@ -395,7 +390,7 @@ struct Forward {
     }
 };
 
-// out and the statistics of a row's head: the maximum in base 2 and 1 / sum
+// the statistics of a row's head: the maximum and 1 / sum
 __device__ __forceinline__ void write_stats(const DotArgs& D, int64_t row, int hq, float m, float l) {
     if (!D.stats) return;
     float* st = D.stats + row * D.stats_stride + 2 * hq;
@@ -435,7 +430,7 @@ __device__ __forceinline__ void empty_rows(const EngineArgs& A, int w, int G, in
 }
 
 template <typename T, int VEC, int RC, bool OV, bool BIAS, bool FAST>
-__global__ __launch_bounds__(256) void dot_forward_kernel(EngineArgs A, DotArgs D) {
+__global__ __launch_bounds__(256, 3) void dot_forward_kernel(EngineArgs A, DotArgs D) {
     const int w = wave_id();
     if (w >= A.sch.w_total) return;
     const Lanes ln = lanes_of(A.geo);
@@ -512,7 +507,7 @@ __global__ void dot_join_kernel(EngineArgs A, DotArgs D, int cols) {
     double l = 0.0, a = 0.0;
     auto add = [&](float om, double ol, double oa) {
         const float mn = fmaxf(m, om), at = mn == -INFINITY ? 0.0f : mn;
-        const double f = (double)__builtin_amdgcn_exp2f(m - at), g = (double)__builtin_amdgcn_exp2f(om - at);
+        const double f = (double)exp_le0(m - at), g = (double)exp_le0(om - at);
         l = l * f + ol * g;
         a = a * f + oa * g;
         m = mn;
@@ -603,7 +598,7 @@ struct ToDst {
             scores<T, RC, BIAS, ALL>(D, x, r, sr, gone);
 #pragma unroll
             for (int u = 0; u < U; ++u) {
-                const float a = __builtin_amdgcn_exp2f(sr[u] - m[r]) * il[r], w = a * (tr[u] - S0[r]);
+                const float a = exp_le0(sr[u] - m[r]) * il[r], w = a * (tr[u] - S0[r]);
                 if (!gone[u]) {
                     delta[r] += w;
 #pragma unroll
@@ -674,7 +669,7 @@ struct ToEdge {
         scores<T, 1, BIAS, ALL>(D, x, 0, s, gone);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            ds[u] = __builtin_amdgcn_exp2f(s[u] - rec.x) * rec.y * (s[U + u] - rec.z);
+            ds[u] = exp_le0(s[u] - rec.x) * rec.y * (s[U + u] - rec.z);
             ds[u] = gone[u] ? 0.0f : ds[u];
         }
 #pragma unroll
@@ -695,7 +690,7 @@ struct ToEdge {
 };
 
 template <typename T, int VEC, int RC, bool OV, bool BIAS, bool FAST>
-__global__ __launch_bounds__(256) void dot_backward_dst_kernel(EngineArgs A, DotArgs D) {
+__global__ __launch_bounds__(256, RC == 4 ? 2 : 3) void dot_backward_dst_kernel(EngineArgs A, DotArgs D) {
     const int w = wave_id();
     if (w >= A.sch.w_total) return;
     const Lanes ln = lanes_of(A.geo);
@@ -844,7 +839,7 @@ struct ToSrc {
         scores<T, 1, BIAS, ALL>(D, x, 0, s, gone);
 #pragma unroll
         for (int u = 0; u < U; ++u) {
-            const float a = __builtin_amdgcn_exp2f(s[u] - x.rec[u].x) * x.rec[u].y;
+            const float a = exp_le0(s[u] - x.rec[u].x) * x.rec[u].y;
             const float w = a * (s[U + u] - x.rec[u].z);
             if (!gone[u]) {
 #pragma unroll
@@ -893,7 +888,7 @@ struct ToSrc {
 };
 
 template <typename T, int VEC, bool OV, bool BIAS, bool FAST>
-__global__ __launch_bounds__(256) void dot_backward_src_kernel(EngineArgs A, DotArgs D) {
+__global__ __launch_bounds__(256, 3) void dot_backward_src_kernel(EngineArgs A, DotArgs D) {
     const int w = wave_id();
     if (w >= A.sch.w_total) return;
     const Lanes ln = lanes_of(A.geo);
@@ -991,8 +986,7 @@ void dot_launch(const EngineArgs& a, const DotArgs& d, int pass, hipStream_t s) 
         hipLaunchKernelGGL((dot_forward_kernel<T, V, RC, OV, BIAS, FAST>), grid, block, 0, s, a, d);
         if (a.sch.n_hub > 0) hipLaunchKernelGGL((dot_join_kernel<T>), j.grid(a, HF), threads, 0, s, a, d, j.cols);
     } else if (pass == 1) {
-        constexpr int RD = RC < 2 ? RC : 2;
-        hipLaunchKernelGGL((dot_backward_dst_kernel<T, V, RD, OV, BIAS, FAST>), grid, block, 0, s, a, d);
+        hipLaunchKernelGGL((dot_backward_dst_kernel<T, V, RC, OV, BIAS, FAST>), grid, block, 0, s, a, d);
         if (a.sch.n_hub > 0) hipLaunchKernelGGL((dot_join_dst_kernel<T>), j.grid(a, HF), threads, 0, s, a, d, j.cols);
     } else if (pass == 2) {
         hipLaunchKernelGGL((dot_backward_src_kernel<T, V, OV, BIAS, FAST>), grid, block, 0, s, a, d);

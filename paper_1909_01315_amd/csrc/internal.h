@@ -253,7 +253,7 @@ struct DotArgs {
     int64_t bias_stride;
     void* out;               // forward: (N_dst, H, F) T
     int64_t out_stride;
-    float* stats;            // (N_dst, H, 2) fp32: maximum score in base 2 and 1 / sum (forward: nullable)
+    float* stats;            // (N_dst, H, 2) fp32: maximum score and 1 / sum (forward: nullable)
     int64_t stats_stride;
     const void* o;           // backward: the forward's out
     int64_t o_stride;
@@ -265,7 +265,8 @@ struct DotArgs {
     float* part;             // partial results of hub segments
     int64_t part_stride;
     float* edge_acc;         // pass 3, a bias that the heads share in several passes: sums by edge id
-    float scale, scale2;     // of the scores; times log2(e)
+    float scale;             // of the scores
+    int32_t pad;
     int32_t H, K, R, F;      // query heads, key heads, query heads per key head, columns
     int32_t FV, log2HL;      // vectors of a head, log2 of the lanes they take
     int32_t RC, log2RL;      // query heads of a key head in a lane's registers, log2 of those in lanes beside each other
