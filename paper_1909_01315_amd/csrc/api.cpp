@@ -1333,6 +1333,7 @@ namespace {
 
 constexpr int ROTARY_MAX_FEAT = 2048;
 constexpr size_t ROTARY_LDS = 32768;     // bytes of a block's cosines and sines, at most
+constexpr int ROTARY_BLOCKS = 2048;      // blocks that fill the chip: longer tiles from there on
 constexpr int ROTARY_BWD_BLOCKS = 1024;  // blocks that share a backward's rows, each leaving one partial row
 
 bool rotary_ok(const gnnk_rotary* r, int64_t rows, int F) {
@@ -1355,7 +1356,7 @@ bool same_pairs(const gnnk_rotary* a, const gnnk_rotary* b) {
 }
 
 // the geometry that both tensors of a call share; returns the pairs of a lane
-int rotary_geo(RotaryArgs& A, int F, const gnnk_rotary* rot, int dtype) {
+int rotary_geo(RotaryArgs& A, int F, const gnnk_rotary* rot, int dtype, bool bwd) {
     A.F = F;
     A.inv_F = 1.0f / (float)F;
     A.P = 0;
@@ -1364,12 +1365,19 @@ int rotary_geo(RotaryArgs& A, int F, const gnnk_rotary* rot, int dtype) {
         A.P += A.pairs[a];
     }
     A.interleaved = rot ? rot->interleaved != 0 : 1;
-    // the widest vectors that divide both the pairs and the columns after
-    // them, 16 bytes (two of them a lane)
-    const int rest = F - 2 * A.P;
-    int V = dtype == 1 ? 8 : 4;
-    while (V > 1 && (A.P % V != 0 || rest % (2 * V) != 0)) V >>= 1;
-    A.NV = A.P / V + (rest + 2 * V - 1) / (2 * V);
+    // vectors of 16 bytes (backward: four columns, which leave registers for
+    // four wavefronts), two of them a lane, or half as wide if those divide
+    // both the pairs and the columns after them; else the narrowest that take
+    // no more lanes than the widest, the last ones in part
+    const int rest = F - 2 * A.P, wide = dtype == 1 && !bwd ? 8 : 4;
+    auto count = [&](int v) { return (A.P + v - 1) / v + (rest + 2 * v - 1) / (2 * v); };
+    auto exact = [&](int v) { return A.P % v == 0 && rest % (2 * v) == 0; };
+    int V = exact(wide) || !exact(wide / 2) ? wide : wide / 2;
+    if (!exact(V))
+        while (V > 1 && pow2ceil(count(V / 2)) <= pow2ceil(count(V))) V >>= 1;
+    A.NA = (A.P + V - 1) / V;
+    A.NV = count(V);
+    A.part = !exact(V);
     A.L = std::min(64, pow2ceil(A.NV));
     A.nchunk = (A.NV + 63) / 64;
     A.log2L = 0;
@@ -1379,7 +1387,7 @@ int rotary_geo(RotaryArgs& A, int F, const gnnk_rotary* rot, int dtype) {
 
 // blocks of one tensor: a block's 256 / L lane groups take HB heads of RB rows
 // at once, and a tile of several such steps where the rows make more than
-// 2,048 blocks (the angles are computed once per tile; 16 steps at most)
+// ROTARY_BLOCKS blocks (16 steps at most)
 void rotary_blocks(const RotaryArgs& A, RotarySide& S, bool bwd) {
     const int groups = 256 / A.L;
     S.HB = std::min(S.H, groups);
@@ -1387,7 +1395,7 @@ void rotary_blocks(const RotaryArgs& A, RotarySide& S, bool bwd) {
     S.RB = groups / S.HB;
     const int most = A.P > 0 ? (int)(ROTARY_LDS / 8) / A.P : 1 << 20;  // rows whose angles fit
     S.RB = std::max(1, std::min(S.RB, most));
-    const int64_t steps = std::min<int64_t>(16, std::max<int64_t>(1, S.n * S.hblocks * A.nchunk / (2048 * S.RB)));
+    const int64_t steps = std::min<int64_t>(16, std::max<int64_t>(1, S.n * S.hblocks * A.nchunk / (ROTARY_BLOCKS * S.RB)));
     S.tile_rows = S.RB * (int)std::min<int64_t>(steps, std::max(1, most / S.RB));
     const int64_t tiles = (S.n + S.tile_rows - 1) / S.tile_rows;
     S.row_blocks = (int32_t)std::min<int64_t>(tiles, bwd ? ROTARY_BWD_BLOCKS : (1 << 20) / (S.hblocks * A.nchunk));
@@ -1401,7 +1409,7 @@ size_t rotary_lds(const RotaryArgs& A, int V, bool bwd) {
     size_t n = 0;
     for (const RotarySide& S : A.side)
         if (S.blocks) n = std::max(n, (size_t)S.tile_rows * A.P * 8);
-    return bwd ? std::max(n, (size_t)256 * 2 * V * 8) : n;
+    return bwd ? std::max(n, (size_t)(256 + A.L) * 2 * V * 8) : n;
 }
 
 void rotary_positions(RotarySide& S, const gnnk_rotary* r) {
@@ -1451,7 +1459,7 @@ gnnk_status norm_check(const NormSide& s, bool bwd, const char* name) {
 
 // the sides' arguments and blocks; bytes: of the partial weight gradients
 int norm_args(const NormSide* sides, int n, float eps, bool bwd, RotaryArgs& A, size_t& bytes) {
-    const int V = rotary_geo(A, sides[0].x->feat, sides[0].rot, dtype_code(sides[0].x));
+    const int V = rotary_geo(A, sides[0].x->feat, sides[0].rot, dtype_code(sides[0].x), bwd);
     A.sign = 1.0f;
     A.eps = eps;
     bytes = 0;
@@ -1516,7 +1524,7 @@ gnnk_status node_rotary(const gnnk_rotary* rot, const gnnk_tensor* x, int32_t in
         return fail(GNNK_EINVAL, "fewer than 2^31 rows, at most 1024 heads of at most %d columns", ROTARY_MAX_FEAT);
     if (x->rows == 0) return GNNK_OK;
     RotaryArgs A{};
-    const int V = rotary_geo(A, x->feat, rot, dtype_code(x));
+    const int V = rotary_geo(A, x->feat, rot, dtype_code(x), false);
     A.sign = inverse ? -1.0f : 1.0f;
     RotarySide& S = A.side[0];
     S.x = x->data;

@@ -16,95 +16,11 @@
 // Dot products and the sums over the edges of one wavefront's share of a
 // row are fp32; the partial results of a long row's segments are joined in
 // fp64 in segment order.
-#include "device.h"
+#include "words.h"
 
 namespace gnnk {
 
 namespace {
-
-// bf16 rows stay in their packed words until a column is needed: dot products
-// of two bf16 rows take a pair of columns an instruction (v_dot2_f32_bf16: the
-// exact products and the sum so far, off by at most 2.4 units of the last
-// place of their sizes' sum; bf16 numbers below 2^-126 count as 0), which
-// spares the widening and half the multiplications
-struct bf16_pair_t {
-    uint16_t x;
-};
-
-}  // namespace
-
-// vectors of words: VEC values of fp32, VEC / 2 pairs of bf16
-template <int VEC>
-struct IO<bf16_pair_t, VEC> {
-    static __device__ __forceinline__ void load(const bf16_pair_t* p, float* w) {
-        if constexpr (VEC == 8) {
-            const u4_h x = *reinterpret_cast<const u4_h*>(p);
-            w[0] = __uint_as_float(x.x); w[1] = __uint_as_float(x.y);
-            w[2] = __uint_as_float(x.z); w[3] = __uint_as_float(x.w);
-        } else if constexpr (VEC == 4) {
-            const u2_h x = *reinterpret_cast<const u2_h*>(p);
-            w[0] = __uint_as_float(x.x); w[1] = __uint_as_float(x.y);
-        } else if constexpr (VEC == 2) {
-            w[0] = __uint_as_float(*reinterpret_cast<const u1_h*>(p));
-        } else {
-            w[0] = __uint_as_float((uint32_t)p->x);
-        }
-    }
-};
-
-namespace {
-
-typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
-__device__ __forceinline__ bf16x2 pair(float w) { return __builtin_bit_cast(bf16x2, w); }
-
-// rows of T in words
-template <typename T, int VEC>
-struct Words {
-    using type = float;
-    static constexpr int N = VEC;
-    static constexpr bool PAIRS = false;
-    static __device__ __forceinline__ float at(const float* w, int i) { return w[i]; }
-};
-template <int VEC>
-struct Words<bf16_t, VEC> {
-    using type = bf16_pair_t;
-    static constexpr int N = (VEC + 1) / 2;
-    static constexpr bool PAIRS = true;
-    static __device__ __forceinline__ float at(const float* w, int i) {
-        const uint32_t x = __float_as_uint(w[i / 2]);
-        return (i & 1) ? bf_hi(x) : bf_lo(x);
-    }
-};
-
-template <int CTRL>
-__device__ __forceinline__ float dpp_f(float x) {
-    return __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(x), CTRL, 0xF, 0xF, true));
-}
-constexpr int DPP_HALF_MIRROR = 0x141, DPP_MIRROR = 0x140;
-
-// sums over the aligned run of `red` lanes (a power of two) that holds the
-// lane, of N values at once; every lane gets the totals
-template <int N>
-__device__ __forceinline__ void run_totals(float* v, int red) {
-    if (red >= 2)
-#pragma unroll
-        for (int u = 0; u < N; ++u) v[u] += dpp_f<DPP_QUAD_1032>(v[u]);
-    if (red >= 4)
-#pragma unroll
-        for (int u = 0; u < N; ++u) v[u] += dpp_f<DPP_QUAD_2301>(v[u]);
-    if (red >= 8)
-#pragma unroll
-        for (int u = 0; u < N; ++u) v[u] += dpp_f<DPP_HALF_MIRROR>(v[u]);
-    if (red >= 16)
-#pragma unroll
-        for (int u = 0; u < N; ++u) v[u] += dpp_f<DPP_MIRROR>(v[u]);
-    if (red >= 32)
-#pragma unroll
-        for (int u = 0; u < N; ++u) v[u] += __shfl_xor(v[u], 16, WAVE);
-    if (red >= 64)
-#pragma unroll
-        for (int u = 0; u < N; ++u) v[u] += __shfl_xor(v[u], 32, WAVE);
-}
 
 // a lane's place in the row of heads (a slice of them)
 struct Place {
@@ -491,7 +407,7 @@ __global__ __launch_bounds__(256, 3) void dot_forward_kernel(EngineArgs A, DotAr
 
 // Hub rows: the states of a row's segments joined.  A workgroup takes `cols`
 // columns of one row, its threads the columns of every (threads / cols)-th
-// segment; the runs are then joined in order.  A few columns and many runs
+// segment; the runs are then joined in pairs.  A few columns and many runs
 // where rows have many segments (one node of 100,000 edges has 1,563).
 template <typename T>
 __global__ void dot_join_kernel(EngineArgs A, DotArgs D, int cols) {
@@ -528,12 +444,15 @@ __global__ void dot_join_kernel(EngineArgs A, DotArgs D, int cols) {
                 if (s + u * runs < s1) add(pm[u], (double)pl[u], (double)pa[u]);
         }
     }
-    sm[t] = m;
-    sl[t] = l;
-    sa[t] = a;
-    __syncthreads();
+    for (int half = runs >> 1; half > 0; half >>= 1) {
+        sm[t] = m;
+        sl[t] = l;
+        sa[t] = a;
+        __syncthreads();
+        if (run < half) add(sm[t + half * cols], sl[t + half * cols], sa[t + half * cols]);
+        __syncthreads();
+    }
     if (run != 0 || !ok) return;
-    for (int k = 1; k < runs; ++k) add(sm[t + k * cols], sl[t + k * cols], sa[t + k * cols]);
     IO<T, 1>::store1(reinterpret_cast<T*>(D.out) + row * D.out_stride + col, l == 0.0 ? 0.0f : (float)(a / l));
     if (col % D.F == 0) write_stats(D, row, hq, m, (float)l);
 }
@@ -770,16 +689,19 @@ __global__ void dot_join_dst_kernel(EngineArgs A, DotArgs D, int cols) {
                 }
         }
     }
-    s1m[t] = x1;
-    s2m[t] = x2;
-    sdm[t] = dl;
-    __syncthreads();
-    if (run != 0 || !ok) return;
-    for (int k = 1; k < runs; ++k) {
-        x1 += s1m[t + k * cols];
-        x2 += s2m[t + k * cols];
-        dl += sdm[t + k * cols];
+    for (int half = runs >> 1; half > 0; half >>= 1) {
+        s1m[t] = x1;
+        s2m[t] = x2;
+        sdm[t] = dl;
+        __syncthreads();
+        if (run < half) {
+            x1 += s1m[t + half * cols];
+            x2 += s2m[t + half * cols];
+            dl += sdm[t + half * cols];
+        }
+        __syncthreads();
     }
+    if (run != 0 || !ok) return;
     if (D.d_q)
         IO<T, 1>::store1(reinterpret_cast<T*>(D.d_q) + row * D.d_q_stride + col,
                          (float)((double)D.scale * (x1 - dl * x2)));
@@ -950,10 +872,13 @@ __global__ void dot_join_src_kernel(EngineArgs A, DotArgs D, int cols) {
                 if (s + u * runs < s1) x += (double)y[u];
         }
     }
-    red[t] = x;
-    __syncthreads();
+    for (int half = runs >> 1; half > 0; half >>= 1) {
+        red[t] = x;
+        __syncthreads();
+        if (run < half) x += red[t + half * cols];
+        __syncthreads();
+    }
     if (run != 0 || !ok) return;
-    for (int k = 1; k < runs; ++k) x += red[t + k * cols];
     if (col < W) {
         if (D.d_k)
             IO<T, 1>::store1(reinterpret_cast<T*>(D.d_k) + row * D.d_k_stride + col, (float)((double)D.scale * x));
@@ -973,7 +898,7 @@ struct Join {
 };
 Join join_of(const EngineArgs& a) {
     const bool many = a.sch.n_seg > 64ll * a.sch.n_hub;
-    return many ? Join{16, 1024} : Join{64, 256};
+    return many ? Join{8, 1024} : Join{64, 256};
 }
 
 template <typename T, int V, int RC, bool OV, bool BIAS, bool FAST>

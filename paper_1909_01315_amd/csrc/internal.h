@@ -305,7 +305,8 @@ struct RotarySide {
 struct RotaryArgs {
     RotarySide side[2];
     int32_t F, P;            // columns and pairs of a head
-    int32_t NV, L, log2L, nchunk;  // lanes' vectors of a head, lanes of a group, passes over a head
+    int32_t NA, NV, L, log2L, nchunk;  // lanes' vectors of pairs, of a head, lanes of a group, passes over a head
+    int32_t part;            // the last vector of either kind holds fewer columns
     int32_t pairs[4];
     int32_t interleaved;
     float sign;              // of the angles (rotation alone)

@@ -13,13 +13,15 @@
 // head each, neighbouring groups neighbouring heads, so that a wavefront's
 // loads are contiguous.  A lane holds V pairs (2V columns): of the halves
 // layout V columns of either half, of the interleaved one 2V columns side by
-// side; columns past the last pair pass as they are, 2V a lane.
+// side; columns past the last pair pass as they are, 2V a lane.  Where V
+// divides neither, the last lane of either kind reads whole vectors all the
+// same, past its columns, and leaves the others alone.
 //
 // Angles are products in fp64, reduced to turns there (a position of 10^6 at
 // frequency 1 keeps its angle to 10^-10), and their sines and cosines fp32.
 // Sums over a head (at most 2,048 columns) are fp32, weight gradients, sums
 // over all rows, fp64.
-#include "device.h"
+#include "words.h"
 
 namespace gnnk {
 
@@ -27,27 +29,105 @@ namespace {
 
 constexpr double INV_2PI = 0.15915494309189533577;
 
-// sum over the aligned run of `red` lanes (a power of two) that holds the
-// lane; every lane gets the total.  All lanes must take part.
-template <int CTRL>
-__device__ __forceinline__ float dpp_f(float x) {
-    return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x), CTRL, 0xF, 0xF, false));
-}
-constexpr int DPP_HALF_MIRROR = 0x141, DPP_MIRROR = 0x140;
-__device__ __forceinline__ float run_total(float v, int red) {
-    if (red >= 2) v += dpp_f<DPP_QUAD_1032>(v);
-    if (red >= 4) v += dpp_f<DPP_QUAD_2301>(v);
-    if (red >= 8) v += dpp_f<DPP_HALF_MIRROR>(v);  // (the lanes of a quad hold one value)
-    if (red >= 16) v += dpp_f<DPP_MIRROR>(v);
-    if (red >= 32) v += __shfl_xor(v, 16, WAVE);
-    if (red >= 64) v += __shfl_xor(v, 32, WAVE);
-    return v;
-}
-
 enum : int { TURN = 0, NORM = 1, NORM_BWD = 2 };
 
-// IL: the pairs are columns (2i, 2i + 1), else (i, i + P)
-template <typename T, int V, bool IL, int MODE>
+// the 2V columns of a lane's vector: V from c0 on and V from c1 on, of which
+// the first n0 and n1 are its own
+template <int V>
+struct Lane {
+    int s0;       // first pair
+    int c0, c1;
+    int n0, n1;
+    bool turn;    // they are pairs, not columns after them
+};
+template <int V, bool IL, bool PART>
+__device__ __forceinline__ Lane<V> lane_of(const RotaryArgs& A, int vec) {
+    Lane<V> x;
+    x.turn = vec < A.NA;
+    x.s0 = x.turn ? vec * V : 0;
+    x.c0 = x.turn ? (IL ? 2 * x.s0 : x.s0) : 2 * A.P + 2 * V * (vec - A.NA);
+    x.c1 = x.turn && !IL ? A.P + x.s0 : x.c0 + V;
+    if constexpr (PART) {
+        const int m = x.turn ? 2 * (A.P - x.s0) : A.F - x.c0;  // columns from here on
+        if (x.turn && !IL) {
+            x.n0 = x.n1 = m < 2 * V ? m / 2 : V;
+        } else {
+            x.n0 = m < V ? m : V;
+            x.n1 = m - V < 0 ? 0 : (m - V < V ? m - V : V);
+        }
+    } else {
+        x.n0 = x.n1 = V;
+    }
+    return x;
+}
+
+// V values at p in words, the first n of them the caller's (PART); all of them
+// are read where they lie within `room` values
+template <typename T, int V, bool PART>
+__device__ __forceinline__ void fetch(const T* p, int n, int64_t room, float* w) {
+    using W = Words<T, V>;
+    if (!PART || room >= V) {
+        IO<typename W::type, V>::load(reinterpret_cast<const typename W::type*>(p), w);
+    } else {
+#pragma unroll
+        for (int i = 0; i < W::N; ++i) {
+            if constexpr (W::PAIRS) {
+                const uint32_t lo = 2 * i < n ? p[2 * i] : 0, hi = 2 * i + 1 < n ? p[2 * i + 1] : 0;
+                w[i] = __uint_as_float(lo | hi << 16);
+            } else {
+                w[i] = i < n ? p[i] : 0.0f;
+            }
+        }
+    }
+}
+template <typename T, int V, bool PART>
+__device__ __forceinline__ void widen(const float* w, int n, float* t) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        const float x = Words<T, V>::at(w, i);
+        t[i] = !PART || i < n ? x : 0.0f;
+    }
+}
+// V values stored; bf16 rounded two an instruction (to nearest even)
+template <typename T, int V>
+__device__ __forceinline__ void put(T* p, const float* t) {
+    if constexpr (sizeof(T) == 2 && V > 1) {
+        typedef __bf16 two __attribute__((ext_vector_type(2)));
+        uint32_t w[V / 2];
+#pragma unroll
+        for (int i = 0; i < V / 2; ++i) {
+            const two x = {(__bf16)t[2 * i], (__bf16)t[2 * i + 1]};
+            w[i] = __builtin_bit_cast(uint32_t, x);
+        }
+        if constexpr (V == 8) *reinterpret_cast<u4_h*>(p) = u4_h{w[0], w[1], w[2], w[3]};
+        else if constexpr (V == 4) *reinterpret_cast<u2_h*>(p) = u2_h{w[0], w[1]};
+        else *reinterpret_cast<u1_h*>(p) = w[0];
+    } else {
+        IO<T, V>::store(p, t);
+    }
+}
+template <typename T, int V>
+__device__ __forceinline__ void store_few(T* p, const float* t, int n) {
+    if constexpr (V == 1) {
+        if (n & 1) put<T, 1>(p, t);
+    } else {
+        if (n & V) {
+            put<T, V>(p, t);
+            store_few<T, V / 2>(p + V, t + V, n);
+        } else {
+            store_few<T, V / 2>(p, t, n);
+        }
+    }
+}
+template <typename T, int V, bool PART>
+__device__ __forceinline__ void store_part(T* p, const float* t, int n) {
+    if (!PART || n == V) put<T, V>(p, t);
+    else if constexpr (PART && V > 1) store_few<T, V / 2>(p, t, n);
+}
+
+// IL: the pairs are columns (2i, 2i + 1), else (i, i + P); PART: V divides
+// neither the pairs nor what follows them
+template <typename T, int V, bool IL, bool PART, int MODE>
 __global__ __launch_bounds__(256) void node_rotary_kernel(RotaryArgs A) {
     extern __shared__ float lds[];
     const bool second = blockIdx.x >= (unsigned)A.side[0].blocks;
@@ -62,60 +142,85 @@ __global__ __launch_bounds__(256) void node_rotary_kernel(RotaryArgs A) {
     const bool group_ok = rr < S.RB && h < S.H;
     const int vec = ch * A.L + lig;
     const bool act = group_ok && vec < A.NV;
-    const int s0 = act ? vec * V : 0;          // first pair of the lane
-    const bool turn = s0 < P;
-    const int c0 = IL || !turn ? 2 * s0 : s0;
-    const int c1 = IL || !turn ? 2 * s0 + V : P + s0;
-    const bool has1 = V > 1 || c1 < A.F;       // (an odd width's last column has no partner)
+    const Lane<V> me = lane_of<V, IL, PART>(A, act ? vec : 0);
     const int64_t head = (int64_t)(group_ok ? h : 0) * A.F;
     float* const cosv = lds;
     float* const sinv = lds + RT * P;
 
-    float w[2 * V];
-    if constexpr (MODE != TURN) {
-#pragma unroll
-        for (int i = 0; i < 2 * V; ++i) w[i] = 1.0f;
+    auto load_w = [&](const Lane<V>& x, float* t) {
         if (S.w) {
             const T* p = reinterpret_cast<const T*>(S.w) + (S.w_per_head ? head : 0);
-            IO<T, V>::load(p + c0, w);
-            if (has1) IO<T, V>::load(p + c1, w + V);
+            if constexpr (PART) {
+                // (one row, with nothing behind it that could be read past it)
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    t[i] = IO<T, 1>::load1(p + x.c0 + (i < x.n0 ? i : 0));
+                    t[V + i] = IO<T, 1>::load1(p + (i < x.n1 ? x.c1 + i : x.c0));
+                }
+            } else {
+                IO<T, V>::load(p + x.c0, t);
+                IO<T, V>::load(p + x.c1, t + V);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < 2 * V; ++i) t[i] = 1.0f;
         }
-    }
+    };
+    float w[2 * V];
+    if constexpr (MODE != TURN) load_w(me, w);
     double dw[MODE == NORM_BWD ? 2 * V : 1];
 #pragma unroll
     for (int i = 0; i < (MODE == NORM_BWD ? 2 * V : 1); ++i) dw[i] = 0.0;
 
-    // 2V columns of a row's head, zeros for a lane outside it
-    auto load = [&](const void* base, int64_t stride, int64_t n, bool ok, int at0, int at1, bool with1, float* t) {
+    // 2V columns of a row's head in words, zeros for a lane outside it; and
+    // the words as values
+    constexpr int N = Words<T, V>::N;
+    auto get = [&](const void* base, int64_t stride, int64_t n, bool ok, const Lane<V>& x, float* raw) {
 #pragma unroll
-        for (int i = 0; i < 2 * V; ++i) t[i] = 0.0f;
+        for (int i = 0; i < 2 * N; ++i) raw[i] = 0.0f;
         if (ok) {
-            const T* p = reinterpret_cast<const T*>(base) + n * stride + head;
-            IO<T, V>::load(p + at0, t);
-            if (with1) IO<T, V>::load(p + at1, t + V);
+            const int64_t at = n * stride + head, room = (S.n - 1) * stride + (int64_t)S.H * A.F - at;
+            const T* p = reinterpret_cast<const T*>(base) + at;
+            fetch<T, V, PART>(p + x.c0, x.n0, room - x.c0, raw);
+            fetch<T, V, PART>(p + x.c1, x.n1, room - x.c1, raw + N);
         }
     };
-    auto rotate = [&](float* t, int r, float sgn) {
-        if (!turn) return;
+    auto values = [&](const Lane<V>& x, const float* raw, float* t) {
+        widen<T, V, PART>(raw, x.n0, t);
+        widen<T, V, PART>(raw + N, x.n1, t + V);
+    };
+    auto load = [&](const void* base, int64_t stride, int64_t n, bool ok, const Lane<V>& x, float* t) {
+        float raw[2 * N];
+        get(base, stride, n, ok, x, raw);
+        values(x, raw, t);
+    };
+    auto rotate = [&](const Lane<V>& x, float* t, int r, float sgn) {
+        if (!x.turn) return;
         float c[V], s[V];
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            c[i] = cosv[r * P + s0 + i];
-            s[i] = sgn * sinv[r * P + s0 + i];
+            const bool in = !PART || x.s0 + i < P;
+            c[i] = in ? cosv[r * P + x.s0 + i] : 1.0f;
+            s[i] = in ? sgn * sinv[r * P + x.s0 + i] : 0.0f;
         }
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-            float& x = t[IL ? 2 * i : i];
-            float& y = t[IL ? 2 * i + 1 : V + i];
-            const float xr = x * c[i] - y * s[i], yr = x * s[i] + y * c[i];
-            x = xr;
-            y = yr;
+            float& a = t[IL ? 2 * i : i];
+            float& z = t[IL ? 2 * i + 1 : V + i];
+            const float ar = a * c[i] - z * s[i], zr = a * s[i] + z * c[i];
+            a = ar;
+            z = zr;
         }
     };
 
     const int64_t tiles = (S.n + RT - 1) / RT;
     for (int64_t tile = rb; tile < tiles; tile += S.row_blocks) {
         const int64_t n0 = tile * RT;
+        // the first step's rows load while the angles are computed
+        float xr[2 * N], gr[2 * N];
+        const bool first_ok = act && rr < RT && n0 + rr < S.n;
+        get(S.x, S.x_stride, n0 + rr, first_ok, me, xr);
+        if constexpr (MODE == NORM_BWD) get(S.g, S.g_stride, n0 + rr, first_ok, me, gr);
         if (P > 0) {
             __syncthreads();  // (the tile before may still be read)
             for (int i = tid; i < RT * P; i += 256) {
@@ -141,18 +246,22 @@ __global__ __launch_bounds__(256) void node_rotary_kernel(RotaryArgs A) {
             const int64_t n = n0 + r;
             const bool row_ok = group_ok && r < RT && n < S.n;
             const bool ok = act && row_ok;
+            if (r0 > 0) {
+                get(S.x, S.x_stride, n, ok, me, xr);
+                if constexpr (MODE == NORM_BWD) get(S.g, S.g_stride, n, ok, me, gr);
+            }
             float t[2 * V];
-            load(S.x, S.x_stride, n, ok, c0, c1, has1, t);
+            values(me, xr, t);
             if constexpr (MODE == TURN) {
-                if (ok) rotate(t, r, A.sign);
+                if (ok) rotate(me, t, r, A.sign);
             } else {
                 float g[2 * V];
                 float ss = 0.0f, dd = 0.0f;
 #pragma unroll
                 for (int i = 0; i < 2 * V; ++i) ss = fmaf(t[i], t[i], ss);
                 if constexpr (MODE == NORM_BWD) {
-                    load(S.g, S.g_stride, n, ok, c0, c1, has1, g);
-                    if (ok) rotate(g, r, -1.0f);
+                    values(me, gr, g);
+                    if (ok) rotate(me, g, r, -1.0f);
 #pragma unroll
                     for (int i = 0; i < 2 * V; ++i) dd = fmaf(g[i] * w[i], t[i], dd);
                 }
@@ -160,48 +269,28 @@ __global__ __launch_bounds__(256) void node_rotary_kernel(RotaryArgs A) {
                 for (int o = 1; o < A.nchunk; ++o) {
                     const int ov = ((ch + o) % A.nchunk) * A.L + lig;
                     const bool ook = row_ok && ov < A.NV;
-                    const int q0 = ook ? ov * V : 0;
-                    const bool ot = q0 < P;
-                    const int o0 = IL || !ot ? 2 * q0 : q0, o1 = IL || !ot ? 2 * q0 + V : P + q0;
-                    const bool oh = V > 1 || o1 < A.F;
+                    const Lane<V> other = lane_of<V, IL, PART>(A, ook ? ov : 0);
                     float y[2 * V];
-                    load(S.x, S.x_stride, n, ook, o0, o1, oh, y);
+                    load(S.x, S.x_stride, n, ook, other, y);
 #pragma unroll
                     for (int i = 0; i < 2 * V; ++i) ss = fmaf(y[i], y[i], ss);
                     if constexpr (MODE == NORM_BWD) {
-                        // sum of (R^-1 g) w x
                         float z[2 * V], u[2 * V];
-                        load(S.g, S.g_stride, n, ook, o0, o1, oh, z);
-                        if (S.w) {
-                            // (the weight has one row: a stride of 0)
-                            const int64_t back = S.w_per_head ? 0 : -head;
-                            load(reinterpret_cast<const T*>(S.w) + back, 0, 0, ook, o0, o1, oh, u);
-                        } else {
+                        load(S.g, S.g_stride, n, ook, other, z);
+                        load_w(other, u);
+                        if (ook) rotate(other, z, r, -1.0f);
 #pragma unroll
-                            for (int i = 0; i < 2 * V; ++i) u[i] = 1.0f;
-                        }
-#pragma unroll
-                        for (int i = 0; i < V; ++i) {
-                            const int ia = IL ? 2 * i : i, ib = IL ? 2 * i + 1 : V + i;
-                            float za = z[ia], zb = z[ib];
-                            if (ook && ot) {
-                                const float c = cosv[r * P + q0 + i], s = sinv[r * P + q0 + i];
-                                za = z[ia] * c + z[ib] * s;
-                                zb = z[ib] * c - z[ia] * s;
-                            }
-                            dd = fmaf(za * u[ia], y[ia], dd);
-                            dd = fmaf(zb * u[ib], y[ib], dd);
-                        }
+                        for (int i = 0; i < 2 * V; ++i) dd = fmaf(z[i] * u[i], y[i], dd);
                     }
                 }
-                ss = run_total(ss, A.L);
+                run_totals<1>(&ss, A.L);
                 const float rn = 1.0f / sqrtf(ss * A.inv_F + A.eps);
                 if constexpr (MODE == NORM) {
 #pragma unroll
                     for (int i = 0; i < 2 * V; ++i) t[i] = t[i] * rn * w[i];
-                    if (ok) rotate(t, r, 1.0f);
+                    if (ok) rotate(me, t, r, 1.0f);
                 } else {
-                    dd = run_total(dd, A.L);
+                    run_totals<1>(&dd, A.L);
                     const float k = rn * rn * dd * A.inv_F;
 #pragma unroll
                     for (int i = 0; i < 2 * V; ++i) {
@@ -213,8 +302,8 @@ __global__ __launch_bounds__(256) void node_rotary_kernel(RotaryArgs A) {
             }
             if (ok && S.out) {
                 T* p = reinterpret_cast<T*>(S.out) + n * S.out_stride + head;
-                IO<T, V>::store(p + c0, t);
-                if (has1) IO<T, V>::store(p + c1, t + V);
+                store_part<T, V, PART>(p + me.c0, t, me.n0);
+                store_part<T, V, PART>(p + me.c1, t + V, me.n1);
             }
         }
     }
@@ -223,9 +312,10 @@ __global__ __launch_bounds__(256) void node_rotary_kernel(RotaryArgs A) {
         // the block's sums: over its groups of one head, or of all heads, in
         // the order of the groups
         double* red = reinterpret_cast<double*>(lds);
+        const int ld = 256 + A.L;  // (threads that differ in i meet in other banks)
         __syncthreads();
 #pragma unroll
-        for (int i = 0; i < 2 * V; ++i) red[i * 256 + tid] = act ? dw[i] : 0.0;
+        for (int i = 0; i < 2 * V; ++i) red[i * ld + tid] = act ? dw[i] : 0.0;
         __syncthreads();
         const int per = A.L * 2 * V;  // sums of one head
         const int heads = S.w_per_head ? S.HB : 1;
@@ -234,17 +324,15 @@ __global__ __launch_bounds__(256) void node_rotary_kernel(RotaryArgs A) {
             const int i = x / A.L, l = x - i * A.L;
             const int v = ch * A.L + l;
             if (v >= A.NV || hb * S.HB + hq >= S.H) continue;
+            const Lane<V> at = lane_of<V, IL, PART>(A, v);
+            if ((i < V ? i : i - V) >= (i < V ? at.n0 : at.n1)) continue;
             double sum = 0.0;
             if (S.w_per_head) {
-                for (int k = 0; k < S.RB; ++k) sum += red[i * 256 + ((k * S.HB + hq) << A.log2L) + l];
+                for (int k = 0; k < S.RB; ++k) sum += red[i * ld + ((k * S.HB + hq) << A.log2L) + l];
             } else {
-                for (int k = 0; k < S.RB * S.HB; ++k) sum += red[i * 256 + (k << A.log2L) + l];
+                for (int k = 0; k < S.RB * S.HB; ++k) sum += red[i * ld + (k << A.log2L) + l];
             }
-            const int sl = v * V;
-            const bool tn = sl < P;
-            const int d0 = IL || !tn ? 2 * sl : sl, d1 = IL || !tn ? 2 * sl + V : P + sl;
-            const int col = i < V ? d0 + i : d1 + i - V;
-            if (col >= A.F) continue;
+            const int col = i < V ? at.c0 + i : at.c1 + i - V;
             const int64_t part = S.w_per_head ? rb : (int64_t)rb * S.hblocks + hb;
             S.dw_part[part * S.dw_cols + (S.w_per_head ? (int64_t)(hb * S.HB + hq) * A.F : 0) + col] = sum;
         }
@@ -264,7 +352,14 @@ __global__ __launch_bounds__(1024) void node_rotary_dw_kernel(RotaryArgs A) {
     double sum = 0.0;
     if (col < S.dw_cols) {
         const int64_t end = (run + 1) * per < S.dw_parts ? (run + 1) * per : S.dw_parts;
-        for (int64_t p = run * per; p < end; ++p) sum += S.dw_part[p * S.dw_cols + col];
+        constexpr int U = 8;  // loads in flight
+        for (int64_t p = run * per; p < end; p += U) {
+            double x[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) x[u] = S.dw_part[(p + u < end ? p + u : p) * S.dw_cols + col];
+#pragma unroll
+            for (int u = 0; u < U; ++u) sum += p + u < end ? x[u] : 0.0;
+        }
     }
     red[run][c] = sum;
     __syncthreads();
@@ -277,17 +372,21 @@ __global__ __launch_bounds__(1024) void node_rotary_dw_kernel(RotaryArgs A) {
 template <typename T, int V, int MODE>
 void launch_v(const RotaryArgs& a, size_t lds, hipStream_t s) {
     const dim3 grid((unsigned)(a.side[0].blocks + a.side[1].blocks)), block(256);
-    if (a.interleaved) hipLaunchKernelGGL((node_rotary_kernel<T, V, true, MODE>), grid, block, lds, s, a);
-    else hipLaunchKernelGGL((node_rotary_kernel<T, V, false, MODE>), grid, block, lds, s, a);
+    if (a.part) {
+        if (a.interleaved) hipLaunchKernelGGL((node_rotary_kernel<T, V, true, true, MODE>), grid, block, lds, s, a);
+        else hipLaunchKernelGGL((node_rotary_kernel<T, V, false, true, MODE>), grid, block, lds, s, a);
+    } else {
+        if (a.interleaved) hipLaunchKernelGGL((node_rotary_kernel<T, V, true, false, MODE>), grid, block, lds, s, a);
+        else hipLaunchKernelGGL((node_rotary_kernel<T, V, false, false, MODE>), grid, block, lds, s, a);
+    }
 }
 
 template <typename T, int MODE>
 void launch_mode(const RotaryArgs& a, int vec, size_t lds, hipStream_t s) {
-    if constexpr (sizeof(T) == 2) {
-        GNNK_VEC_DISPATCH_BF16(vec, launch_v<T, V, MODE>(a, lds, s))
-    } else {
-        GNNK_VEC_DISPATCH_F32(vec, launch_v<T, V, MODE>(a, lds, s))
-    }
+    if (sizeof(T) == 2 && vec == 8) launch_v<T, sizeof(T) == 2 ? 8 : 4, MODE>(a, lds, s);
+    else if (vec == 4) launch_v<T, 4, MODE>(a, lds, s);
+    else if (vec == 2) launch_v<T, 2, MODE>(a, lds, s);
+    else launch_v<T, 1, MODE>(a, lds, s);
 }
 
 template <typename T>
