@@ -554,6 +554,11 @@ def edge_leaky_relu_backward(x, dy, slope: float = 0.2, dx=None, stream=None):
 _ROTARY = struct.Struct("=QqqQIIIIIIII")
 
 
+def _like(t):
+    """an output of t's shape and type, contiguous (half the time of torch.empty with both spelled out)"""
+    return torch.empty_like(t, memory_format=torch.contiguous_format)
+
+
 def _here(*ts):
     """Refuse tensors of another device than the current one, whose stream the call would run on."""
     cur = _device() if _device is not None else torch.cuda.current_device()
@@ -622,7 +627,7 @@ def node_rotary(rot: Rotary, x, pos, inverse: bool = False, out=None, stream=Non
     x = _as3(x)
     _here(x, out)
     if out is None:
-        out = torch.empty(x.shape, dtype=x.dtype, device=x.device)
+        out = _like(x)
     _check(load().node_rotary(rot._desc(pos), _desc(x), int(inverse), _desc(out), _stream(stream)))
     return out
 
@@ -643,11 +648,13 @@ def node_norm_rotary(q, wq=None, k=None, wk=None, rot: Rotary = None, pos_q=None
     k = _as3(k) if k is not None else None
     _here(q, wq, k, wk, out_q, out_k)
     if out_q is None:
-        out_q = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        out_q = _like(q)
     if k is not None and out_k is None:
-        out_k = torch.empty(k.shape, dtype=k.dtype, device=k.device)
+        out_k = _like(k)
     rq = rot._desc(pos_q) if rot is not None else None
-    rk = rot._desc(pos_k) if rot is not None and k is not None else None
+    rk = None
+    if rot is not None and k is not None:
+        rk = rq if pos_k is pos_q else rot._desc(pos_k)
     _check(load().node_norm_rotary(_desc(q), _desc(wq), rq, _desc(out_q), _desc(k), _desc(wk), rk, _desc(out_k), eps,
                                    _stream(stream)))
     return (out_q, out_k) if k is not None else out_q
@@ -661,10 +668,12 @@ def node_norm_rotary_backward(q, wq, grad_q, k=None, wk=None, grad_k=None, rot: 
     q, wq3, wk3, grad_q = _as3(q), _weight3(wq), _weight3(wk), _as3(grad_q)
     k, grad_k = (_as3(k) if k is not None else None), (_as3(grad_k) if grad_k is not None else None)
     _here(q, wq3, k, wk3, grad_q, grad_k)
-    like = lambda t, want: torch.empty(t.shape, dtype=t.dtype, device=t.device) if want and t is not None else None
+    like = lambda t, want: _like(t) if want and t is not None else None
     dq, dwq, dk, dwk = like(q, want_q), like(wq3, want_wq), like(k, want_k), like(wk3, want_wk and k is not None)
     rq = rot._desc(pos_q) if rot is not None else None
-    rk = rot._desc(pos_k) if rot is not None and k is not None else None
+    rk = None
+    if rot is not None and k is not None:
+        rk = rq if pos_k is pos_q else rot._desc(pos_k)
     work, nbytes = None, 0
     if dwq is not None or dwk is not None:
         need = ctypes.c_size_t(0)
@@ -692,7 +701,7 @@ def dot_aggregate(g: Graph, q, k, v, bias=None, scale: float = None, out=None, s
     if scale is None:
         scale = q.shape[2] ** -0.5
     if out is None:
-        out = torch.empty(q.shape, dtype=q.dtype, device=q.device)
+        out = _like(q)
     if want_stats and stats is None:
         stats = torch.empty((g.num_dst, q.shape[1], 2), dtype=torch.float32, device=q.device)
     _run(g, stream, load().dot_aggregate, g.handle, _desc(q), _desc(k), _desc(v), _desc(bias), scale, _desc(out),
@@ -709,7 +718,7 @@ def dot_aggregate_backward(g: Graph, q, k, v, out, stats, grad_out, bias=None, s
     _here(q, k, v, bias, out, stats, grad_out)
     if scale is None:
         scale = q.shape[2] ** -0.5
-    like = lambda t, want: torch.empty(t.shape, dtype=t.dtype, device=t.device) if want and t is not None else None
+    like = lambda t, want: _like(t) if want and t is not None else None
     dq, dk, dv, db = like(q, want_q), like(k, want_k), like(v, want_v), like(bias, want_bias)
     _run(g, stream, load().dot_aggregate_backward, g.handle, _desc(q), _desc(k), _desc(v), _desc(bias), scale,
          _desc(out), _desc(stats), _desc(grad_out), _desc(dq), _desc(dk), _desc(dv), _desc(db))
