@@ -16,6 +16,8 @@
 // Dot products and the sums over the edges of one wavefront's share of a
 // row are fp32; the partial results of a long row's segments are joined in
 // fp64 in segment order.
+#include <type_traits>
+
 #include "words.h"
 
 namespace gnnk {
@@ -28,8 +30,9 @@ struct Place {
     int rl;    // which run of the key head's lanes
     int c;     // first column within the head
     int skip;  // columns that the vector before holds too
-    bool act;  // the lane holds a vector
-    bool first;  // and the head's first one
+    bool own;  // the lane belongs to a head
+    bool act;  // and holds a vector of it
+    bool first;  // the first one
 };
 template <int VEC>
 __device__ __forceinline__ Place place_of(const DotArgs& D, int lig) {
@@ -37,8 +40,9 @@ __device__ __forceinline__ Place place_of(const DotArgs& D, int lig) {
     const int hl = x >> D.log2RL;
     const int j = (D.slice0 + (int)blockIdx.y) * D.heads_slice + hl;
     Place p;
-    p.act = hl < D.heads_slice && j < D.K && f < D.FV;
-    p.j = p.act ? j : 0;
+    p.own = hl < D.heads_slice && j < D.K;
+    p.act = p.own && f < D.FV;
+    p.j = p.own ? j : 0;
     p.rl = x & ((1 << D.log2RL) - 1);
     const int at = f * VEC, last = D.F - VEC;
     p.c = p.act ? (at < last ? at : last) : 0;
@@ -110,11 +114,6 @@ struct Ids {
     int32_t nb[U], ed[U];
 };
 
-// the value of lane u of each quad
-template <int L>
-__device__ __forceinline__ int32_t quad_lane(int32_t x) {
-    return __builtin_amdgcn_update_dpp(0, x, L * 0x55, 0xF, 0xF, true);
-}
 __device__ __forceinline__ void spread_quad(int32_t x, int32_t* v) {
     v[0] = quad_lane<0>(x);
     v[1] = quad_lane<1>(x);
@@ -155,7 +154,8 @@ __device__ __forceinline__ void gather(const OperandDev& o, int32_t nb, int col,
 }
 
 // The loads of a batch: columns col of the tables a and b, with REC the record
-// of (neighbour, head hq), with BIAS the values of heads hq .. hq + RC - 1.
+// of (neighbour, head hq), with BIAS the values of heads hq .. hq + RC - 1, RC
+// being the heads whose scores the lane takes.
 template <typename T, int VEC, int RC, bool FAST, bool BIAS, bool REC>
 __device__ __forceinline__ void issue(const EngineArgs& A, const DotArgs& D, const Ids& id, int col, int hq,
                                       Batch<Words<T, VEC>::N, RC>& x) {
@@ -231,25 +231,46 @@ __device__ __forceinline__ void scores(const DotArgs& D, const B& x, int r, floa
 // ---------------------------------------------------------------------------
 // forward
 
-template <typename T, int VEC, int RC, bool OV, bool BIAS>
+// the weight of a slot that lies outside the row or is masked: a zero that no
+// exponential gives
+constexpr float GONE = -0.0f;
+__device__ __forceinline__ bool is_gone(float w) { return __float_as_uint(w) == 0x80000000u; }
+
+// Of four query heads in registers (SPLIT, heads of at least four lanes), the
+// totals are shared out: lane r of each quad keeps the scores, maximum and sum
+// of head r and hands its weights around, a quarter of the exponentials and
+// comparisons that every lane would make for itself.
+template <typename T, int VEC, int RC, bool SPLIT, bool OV, bool BIAS>
 struct Forward {
+    static constexpr int SC = SPLIT ? 1 : RC;  // heads whose scores a lane keeps
     const DotArgs& D;
     const Place& p;
     int hq;  // the first of the lane's RC query heads
     using W = Words<T, VEC>;
     float q[RC][W::N];
-    float m[RC], l[RC], acc[RC][VEC];
+    float m[SC], l[SC], acc[RC][VEC];
 
     __device__ __forceinline__ Forward(const DotArgs& D_, const Place& p_, int hq_, int64_t row)
         : D(D_), p(p_), hq(hq_) {
 #pragma unroll
         for (int r = 0; r < RC; ++r) {
             own_row<T, VEC>(D, D.q, row * D.q_stride + (int64_t)(hq + r) * D.F + p.c, q[r]);
-            m[r] = -INFINITY;
-            l[r] = 0.0f;
 #pragma unroll
             for (int i = 0; i < VEC; ++i) acc[r][i] = 0.0f;
         }
+#pragma unroll
+        for (int r = 0; r < SC; ++r) {
+            m[r] = -INFINITY;
+            l[r] = 0.0f;
+        }
+    }
+    // the first head whose scores the lane keeps
+    __device__ __forceinline__ int score_head() const { return SPLIT ? hq + (int)(__lane_id() & 3) : hq; }
+    // a value that the lane of head r keeps
+    template <int R>
+    static __device__ __forceinline__ float of(const float* v) {
+        if constexpr (SPLIT) return quad_lane<R>(v[0]);
+        else return v[R];
     }
     template <bool ALL, class B>
     __device__ __forceinline__ void take(const B& x) {
@@ -258,51 +279,99 @@ struct Forward {
         for (int r = 0; r < RC; ++r)
 #pragma unroll
             for (int u = 0; u < U; ++u) s[r * U + u] = share<T, VEC, OV>(q[r], x.a[u], p);
-        run_totals<RC * U>(s, 1 << D.log2HL);
+        if constexpr (SPLIT) quad_totals<U>(s, 1 << D.log2HL, s);
+        else run_totals<RC * U>(s, 1 << D.log2HL);
+        bool gone[SC][U];
+        float f[SC];
+        bool grew = false;
 #pragma unroll
-        for (int r = 0; r < RC; ++r) {
-            bool gone[U];
+        for (int r = 0; r < SC; ++r) {
             float* sr = s + r * U;
-            scores<T, RC, BIAS, ALL>(D, x, r, sr, gone);
+            scores<T, SC, BIAS, ALL>(D, x, r, sr, gone[r]);
             float mn = m[r];
 #pragma unroll
             for (int u = 0; u < U; ++u) {
-                sr[u] = gone[u] ? -INFINITY : sr[u];
+                sr[u] = gone[r][u] ? -INFINITY : sr[u];
                 mn = fmaxf(mn, sr[u]);
             }
             const float at = mn == -INFINITY ? 0.0f : mn;
-            if (__ballot(mn > m[r]) != 0ull) {
-                const float f = exp_le0(m[r] - at);
-                l[r] *= f;
-#pragma unroll
-                for (int i = 0; i < VEC; ++i) acc[r][i] *= f;
-            }
-#pragma unroll
-            for (int u = 0; u < U; ++u) {
-                const float w = exp_le0(sr[u] - at);
-                // (a slot that is gone adds nothing, whatever value it holds)
-                if (!gone[u]) {
-                    l[r] += w;
-#pragma unroll
-                    for (int i = 0; i < VEC; ++i) acc[r][i] = fmaf(w, W::at(x.b[u], i), acc[r][i]);
-                }
-            }
+            grew |= mn > m[r];
+            f[r] = exp_le0(m[r] - at);
             m[r] = mn;
+#pragma unroll
+            for (int u = 0; u < U; ++u) sr[u] = gone[r][u] ? GONE : exp_le0(sr[u] - at);  // the weights
+        }
+        if (__ballot(grew) != 0ull) {
+#pragma unroll
+            for (int r = 0; r < SC; ++r) l[r] *= f[r];
+            each([&](auto R) {
+                const float g = of<R()>(f);
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) acc[R()][i] *= g;
+            });
+        }
+#pragma unroll
+        for (int r = 0; r < SC; ++r)
+#pragma unroll
+            for (int u = 0; u < U; ++u) l[r] += s[r * U + u];
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            float v[VEC];
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) v[i] = W::at(x.b[u], i);
+            each([&](auto R) {
+                float w;
+                if constexpr (SPLIT) w = quad_lane<R()>(s[u]);
+                else w = s[R() * U + u];
+                // (a slot that is gone adds nothing, whatever value it holds)
+                if ((BIAS || !ALL) && is_gone(w)) return;
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) acc[R()][i] = fmaf(w, v[i], acc[R()][i]);
+            });
+        }
+    }
+    // fn(integral constant r) for each query head in registers
+    template <class F>
+    static __device__ __forceinline__ void each(F fn) {
+        heads<0>(fn);
+    }
+    template <int R, class F>
+    static __device__ __forceinline__ void heads(F& fn) {
+        if constexpr (R < RC) {
+            fn(std::integral_constant<int, R>{});
+            heads<R + 1>(fn);
         }
     }
     // the states of the wavefront's lane groups, pairwise
     __device__ __forceinline__ void join_groups(int L) {
-        for (int x = L; x < WAVE; x <<= 1)
+        for (int x = L; x < WAVE; x <<= 1) {
+            float f[SC], g[SC];
 #pragma unroll
-            for (int r = 0; r < RC; ++r) {
+            for (int r = 0; r < SC; ++r) {
                 const float om = __shfl_xor(m[r], x, WAVE), ol = __shfl_xor(l[r], x, WAVE);
                 const float mn = fmaxf(m[r], om), at = mn == -INFINITY ? 0.0f : mn;
-                const float f = exp_le0(m[r] - at), g = exp_le0(om - at);
-                l[r] = l[r] * f + ol * g;
-#pragma unroll
-                for (int i = 0; i < VEC; ++i) acc[r][i] = acc[r][i] * f + __shfl_xor(acc[r][i], x, WAVE) * g;
+                f[r] = exp_le0(m[r] - at);
+                g[r] = exp_le0(om - at);
+                l[r] = l[r] * f[r] + ol * g[r];
                 m[r] = mn;
             }
+            each([&](auto R) {
+                const float fr = of<R()>(f), gr = of<R()>(g);
+#pragma unroll
+                for (int i = 0; i < VEC; ++i)
+                    acc[R()][i] = acc[R()][i] * fr + __shfl_xor(acc[R()][i], x, WAVE) * gr;
+            });
+        }
+    }
+    // fn(head, maximum, sum) in one lane for each of the heads
+    template <class F>
+    __device__ __forceinline__ void each_score(F fn) const {
+        if constexpr (SPLIT) {
+            if ((__lane_id() & ((1 << D.log2HL) - 1)) < 4) fn(score_head(), m[0], l[0]);
+        } else if (p.first) {
+#pragma unroll
+            for (int r = 0; r < RC; ++r) fn(hq + r, m[r], l[r]);
+        }
     }
 };
 
@@ -345,7 +414,7 @@ __device__ __forceinline__ void empty_rows(const EngineArgs& A, int w, int G, in
         if (k0 + x < A.sch.n_rows) fn((int64_t)A.csr.perm[k0 + x]);
 }
 
-template <typename T, int VEC, int RC, bool OV, bool BIAS, bool FAST>
+template <typename T, int VEC, int RC, bool SPLIT, bool OV, bool BIAS, bool FAST>
 __global__ __launch_bounds__(256, 3) void dot_forward_kernel(EngineArgs A, DotArgs D) {
     const int w = wave_id();
     if (w >= A.sch.w_total) return;
@@ -353,44 +422,46 @@ __global__ __launch_bounds__(256, 3) void dot_forward_kernel(EngineArgs A, DotAr
     const int G = A.geo.G, L = A.geo.L;
     const Place p = place_of<VEC>(D, ln.lig);
     const int kcol = p.j * D.F + p.c, step = RC << D.log2RL, h0 = p.j * D.R + p.rl * RC;
-    auto store = [&](int64_t row, int hq, const float* v, float f) {
-        float o[VEC];
-#pragma unroll
-        for (int i = 0; i < VEC; ++i) o[i] = v[i] * f;
-        IO<T, VEC>::store(reinterpret_cast<T*>(D.out) + row * D.out_stride + (int64_t)hq * D.F + p.c, o);
-    };
-    using State = Forward<T, VEC, RC, OV, BIAS>;
-    auto finish = [&](const State& st, int64_t row) {
-#pragma unroll
-        for (int x = 0; x < RC; ++x) {
-            store(row, st.hq + x, st.acc[x], st.l[x] == 0.0f ? 0.0f : 1.0f / st.l[x]);
-            if (p.first) write_stats(D, row, st.hq + x, st.m[x], st.l[x]);
-        }
-    };
+    using State = Forward<T, VEC, RC, SPLIT, OV, BIAS>;
     if (w < A.sch.w_small_end) {
         const bool wave = w < A.sch.w_big_end;
         const Work k = wave ? wave_work(A, w) : lane_work(A, w, G, ln.g);
         const int64_t self = k.r >= 0 ? k.r : 0;
         for (int r = 0; r < D.R; r += step) {
             State st(D, p, h0 + r, self);
-            walk<T, VEC, RC, FAST, BIAS, false>(A, D, (int32_t)k.b, (int32_t)k.e, wave ? U * ln.g : 0,
-                                                wave ? U * G : U, kcol, st.hq, st);
+            walk<T, VEC, State::SC, FAST, BIAS, false>(A, D, (int32_t)k.b, (int32_t)k.e, wave ? U * ln.g : 0,
+                                                       wave ? U * G : U, kcol, st.score_head(), st);
             if (wave) st.join_groups(L);
-            if ((wave && ln.g != 0) || k.r < 0 || !p.act) continue;
+            float il[State::SC];
+#pragma unroll
+            for (int x = 0; x < State::SC; ++x) il[x] = st.l[x] == 0.0f ? 0.0f : 1.0f / st.l[x];
+            float ih[RC];  // (lanes read each other's: before any of them is done)
+            State::each([&](auto x) { ih[x()] = State::template of<x()>(il); });
+            if ((wave && ln.g != 0) || k.r < 0 || !(p.act || SPLIT)) continue;
+            const int64_t W = (int64_t)D.H * D.F;
+            const bool own = p.own;
             if (k.slot >= 0) {
                 float* P = D.part + (int64_t)k.slot * D.part_stride;
+                if (own)
+                    st.each_score([&](int hq, float m, float l) {
+                        P[W + 2 * hq] = m;
+                        P[W + 2 * hq + 1] = l;
+                    });
+                if (!p.act) continue;
 #pragma unroll
-                for (int x = 0; x < RC; ++x) {
-                    if (p.first) {
-                        float* ml = P + (int64_t)D.H * D.F + 2 * (st.hq + x);
-                        ml[0] = st.m[x];
-                        ml[1] = st.l[x];
-                    }
+                for (int x = 0; x < RC; ++x)
 #pragma unroll
                     for (int i = 0; i < VEC; ++i) P[(int64_t)(st.hq + x) * D.F + p.c + i] = st.acc[x][i];
-                }
             } else {
-                finish(st, k.r);
+                if (own) st.each_score([&](int hq, float m, float l) { write_stats(D, k.r, hq, m, l); });
+                if (!p.act) continue;
+#pragma unroll
+                for (int x = 0; x < RC; ++x) {
+#pragma unroll
+                    for (int i = 0; i < VEC; ++i) st.acc[x][i] *= ih[x];
+                    IO<T, VEC>::store(reinterpret_cast<T*>(D.out) + k.r * D.out_stride +
+                                          (int64_t)(st.hq + x) * D.F + p.c, st.acc[x]);
+                }
             }
         }
     } else {
@@ -398,7 +469,8 @@ __global__ __launch_bounds__(256, 3) void dot_forward_kernel(EngineArgs A, DotAr
             const float zero[VEC] = {};
             for (int r = 0; r < D.R && p.act; r += step)
                 for (int x = 0; x < RC; ++x) {
-                    store(row, h0 + r + x, zero, 0.0f);
+                    IO<T, VEC>::store(reinterpret_cast<T*>(D.out) + row * D.out_stride +
+                                          (int64_t)(h0 + r + x) * D.F + p.c, zero);
                     if (p.first) write_stats(D, row, h0 + r + x, 0.0f, 0.0f);
                 }
         });
@@ -472,17 +544,20 @@ __global__ void dot_join_kernel(EngineArgs A, DotArgs D, int cols) {
 // destination and head for the source pass, which walks the reverse graph's
 // CSR and gathers q, dout and the record.
 
-template <typename T, int VEC, int RC, bool OV, bool BIAS>
+template <typename T, int VEC, int RC, bool SPLIT, bool OV, bool BIAS>
 struct ToDst {
+    using Fwd = Forward<T, VEC, RC, SPLIT, OV, BIAS>;
+    static constexpr int SC = Fwd::SC;  // heads whose scores a lane keeps, as in the forward
     const DotArgs& D;
     const Place& p;
     int hq;  // the first of the lane's RC query heads
     using W = Words<T, VEC>;
-    float q[RC][W::N], dz[RC][W::N], m[RC], il[RC], S0[RC];
-    float e1[RC][VEC], e2[RC][VEC], delta[RC];
+    float q[RC][W::N], dz[RC][W::N], m[SC], il[SC], S0[SC], delta[SC];
+    float e1[RC][VEC], e2[RC][VEC];
 
     __device__ __forceinline__ ToDst(const DotArgs& D_, const Place& p_, int hq_, int64_t row)
         : D(D_), p(p_), hq(hq_) {
+        float zo[RC];
 #pragma unroll
         for (int r = 0; r < RC; ++r) {
             const int64_t c = (int64_t)(hq + r) * D.F + p.c;
@@ -490,68 +565,94 @@ struct ToDst {
             own_row<T, VEC>(D, D.q, row * D.q_stride + c, q[r]);
             row_words<T, VEC>(D.dz, row * D.dz_stride + c, dz[r]);
             row_words<T, VEC>(D.o, row * D.o_stride + c, o);
-            m[r] = D.stats[row * D.stats_stride + 2 * (hq + r)];
-            il[r] = D.stats[row * D.stats_stride + 2 * (hq + r) + 1];
-            S0[r] = share<T, VEC, OV>(dz[r], o, p);
-            delta[r] = 0.0f;
+            zo[r] = share<T, VEC, OV>(dz[r], o, p);
 #pragma unroll
             for (int i = 0; i < VEC; ++i) e1[r][i] = e2[r][i] = 0.0f;
         }
-        run_totals<RC>(S0, 1 << D.log2HL);
+        if constexpr (SPLIT) quad_totals<1>(zo, 1 << D.log2HL, S0);
+        else run_totals<RC>(zo, 1 << D.log2HL);
+#pragma unroll
+        for (int r = 0; r < SC; ++r) {
+            if constexpr (!SPLIT) S0[r] = zo[r];
+            m[r] = D.stats[row * D.stats_stride + 2 * (score_head() + r)];
+            il[r] = D.stats[row * D.stats_stride + 2 * (score_head() + r) + 1];
+            delta[r] = 0.0f;
+        }
     }
+    __device__ __forceinline__ int score_head() const { return SPLIT ? hq + (int)(__lane_id() & 3) : hq; }
     template <bool ALL, class B>
     __device__ __forceinline__ void take(const B& x) {
-        float s[2 * RC * U];
+        float s[RC * U], t[RC * U];
 #pragma unroll
         for (int r = 0; r < RC; ++r)
 #pragma unroll
             for (int u = 0; u < U; ++u) {
-                s[2 * r * U + u] = share<T, VEC, OV>(q[r], x.a[u], p);
-                s[(2 * r + 1) * U + u] = share<T, VEC, OV>(dz[r], x.b[u], p);
+                s[r * U + u] = share<T, VEC, OV>(q[r], x.a[u], p);
+                t[r * U + u] = share<T, VEC, OV>(dz[r], x.b[u], p);
             }
-        run_totals<2 * RC * U>(s, 1 << D.log2HL);
+        if constexpr (SPLIT) {
+            quad_totals<U>(s, 1 << D.log2HL, s);
+            quad_totals<U>(t, 1 << D.log2HL, t);
+        } else {
+            run_totals<RC * U>(s, 1 << D.log2HL);
+            run_totals<RC * U>(t, 1 << D.log2HL);
+        }
 #pragma unroll
-        for (int r = 0; r < RC; ++r) {
+        for (int r = 0; r < SC; ++r) {
             bool gone[U];
-            float *sr = s + 2 * r * U, *tr = sr + U;
-            scores<T, RC, BIAS, ALL>(D, x, r, sr, gone);
+            float *sr = s + r * U, *tr = t + r * U;
+            scores<T, SC, BIAS, ALL>(D, x, r, sr, gone);
 #pragma unroll
             for (int u = 0; u < U; ++u) {
-                const float a = exp_le0(sr[u] - m[r]) * il[r], w = a * (tr[u] - S0[r]);
-                if (!gone[u]) {
-                    delta[r] += w;
-#pragma unroll
-                    for (int i = 0; i < VEC; ++i) {
-                        const float y = W::at(x.a[u], i);
-                        e1[r][i] = fmaf(w, y, e1[r][i]);
-                        e2[r][i] = fmaf(a, y, e2[r][i]);
-                    }
-                }
+                sr[u] = gone[u] ? GONE : exp_le0(sr[u] - m[r]) * il[r];  // the weight
+                tr[u] = gone[u] ? 0.0f : sr[u] * (tr[u] - S0[r]);
+                delta[r] += tr[u];
             }
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            float v[VEC];
+#pragma unroll
+            for (int i = 0; i < VEC; ++i) v[i] = W::at(x.a[u], i);
+            Fwd::each([&](auto R) {
+                float a, w;
+                if constexpr (SPLIT) {
+                    a = quad_lane<R()>(s[u]);
+                    w = quad_lane<R()>(t[u]);
+                } else {
+                    a = s[R() * U + u];
+                    w = t[R() * U + u];
+                }
+                if ((BIAS || !ALL) && is_gone(a)) return;
+#pragma unroll
+                for (int i = 0; i < VEC; ++i) {
+                    e1[R()][i] = fmaf(w, v[i], e1[R()][i]);
+                    e2[R()][i] = fmaf(a, v[i], e2[R()][i]);
+                }
+            });
         }
     }
     __device__ __forceinline__ void join_groups(int L) {
-        for (int x = L; x < WAVE; x <<= 1)
+        for (int x = L; x < WAVE; x <<= 1) {
 #pragma unroll
-            for (int r = 0; r < RC; ++r) {
-                delta[r] += __shfl_xor(delta[r], x, WAVE);
+            for (int r = 0; r < SC; ++r) delta[r] += __shfl_xor(delta[r], x, WAVE);
+#pragma unroll
+            for (int r = 0; r < RC; ++r)
 #pragma unroll
                 for (int i = 0; i < VEC; ++i) {
                     e1[r][i] += __shfl_xor(e1[r][i], x, WAVE);
                     e2[r][i] += __shfl_xor(e2[r][i], x, WAVE);
                 }
-            }
+        }
     }
-    __device__ __forceinline__ void write(int64_t row) const {
+    // fn(head, index of its score) in one lane for each of the heads
+    template <class F>
+    __device__ __forceinline__ void each_score(F fn) const {
+        if constexpr (SPLIT) {
+            if ((__lane_id() & ((1 << D.log2HL) - 1)) < 4) fn(score_head(), 0);
+        } else if (p.first) {
 #pragma unroll
-        for (int r = 0; r < RC; ++r) {
-            if (D.d_q) {
-                float v[VEC];
-#pragma unroll
-                for (int i = 0; i < VEC; ++i) v[i] = D.scale * (e1[r][i] - delta[r] * e2[r][i]);
-                IO<T, VEC>::store(reinterpret_cast<T*>(D.d_q) + row * D.d_q_stride + (int64_t)(hq + r) * D.F + p.c, v);
-            }
-            if (p.first) D.rec[row * D.H + hq + r] = make_float4(m[r], il[r], S0[r] + delta[r], 0.0f);
+            for (int r = 0; r < RC; ++r) fn(hq + r, r);
         }
     }
 };
@@ -608,7 +709,7 @@ struct ToEdge {
     }
 };
 
-template <typename T, int VEC, int RC, bool OV, bool BIAS, bool FAST>
+template <typename T, int VEC, int RC, bool SPLIT, bool OV, bool BIAS, bool FAST>
 __global__ __launch_bounds__(256, RC == 4 ? 2 : 3) void dot_backward_dst_kernel(EngineArgs A, DotArgs D) {
     const int w = wave_id();
     if (w >= A.sch.w_total) return;
@@ -616,20 +717,28 @@ __global__ __launch_bounds__(256, RC == 4 ? 2 : 3) void dot_backward_dst_kernel(
     const int G = A.geo.G, L = A.geo.L;
     const Place p = place_of<VEC>(D, ln.lig);
     const int kcol = p.j * D.F + p.c, step = RC << D.log2RL, h0 = p.j * D.R + p.rl * RC;
-    using State = ToDst<T, VEC, RC, OV, BIAS>;
+    using State = ToDst<T, VEC, RC, SPLIT, OV, BIAS>;
     if (w < A.sch.w_small_end) {
         const bool wave = w < A.sch.w_big_end;
         const Work k = wave ? wave_work(A, w) : lane_work(A, w, G, ln.g);
         const int64_t self = k.r >= 0 ? k.r : 0;
         for (int r = 0; r < D.R; r += step) {
             State st(D, p, h0 + r, self);
-            walk<T, VEC, RC, FAST, BIAS, false>(A, D, (int32_t)k.b, (int32_t)k.e, wave ? U * ln.g : 0,
-                                                wave ? U * G : U, kcol, st.hq, st);
+            walk<T, VEC, State::SC, FAST, BIAS, false>(A, D, (int32_t)k.b, (int32_t)k.e, wave ? U * ln.g : 0,
+                                                       wave ? U * G : U, kcol, st.score_head(), st);
             if (wave) st.join_groups(L);
-            if ((wave && ln.g != 0) || k.r < 0 || !p.act) continue;
+            float dh[RC];  // (lanes read each other's: before any of them is done)
+            State::Fwd::each([&](auto x) { dh[x()] = State::Fwd::template of<x()>(st.delta); });
+            if ((wave && ln.g != 0) || k.r < 0 || !(p.act || SPLIT)) continue;
+            const int64_t W = (int64_t)D.H * D.F;
             if (k.slot >= 0) {
                 float* P = D.part + (int64_t)k.slot * D.part_stride;
-                const int64_t W = (int64_t)D.H * D.F;
+                if (p.own)
+                    st.each_score([&](int hq, int x) {
+                        P[2 * W + 2 * hq] = st.delta[x];
+                        P[2 * W + 2 * hq + 1] = st.S0[x];
+                    });
+                if (!p.act) continue;
 #pragma unroll
                 for (int x = 0; x < RC; ++x) {
                     const int64_t c = (int64_t)(st.hq + x) * D.F + p.c;
@@ -638,13 +747,21 @@ __global__ __launch_bounds__(256, RC == 4 ? 2 : 3) void dot_backward_dst_kernel(
                         P[c + i] = st.e1[x][i];
                         P[W + c + i] = st.e2[x][i];
                     }
-                    if (p.first) {
-                        P[2 * W + 2 * (st.hq + x)] = st.delta[x];
-                        P[2 * W + 2 * (st.hq + x) + 1] = st.S0[x];
-                    }
                 }
             } else {
-                st.write(k.r);
+                if (p.own)
+                    st.each_score([&](int hq, int x) {
+                        D.rec[k.r * D.H + hq] = make_float4(st.m[x], st.il[x], st.S0[x] + st.delta[x], 0.0f);
+                    });
+                if (!p.act || !D.d_q) continue;
+#pragma unroll
+                for (int x = 0; x < RC; ++x) {
+                    float v[VEC];
+#pragma unroll
+                    for (int i = 0; i < VEC; ++i) v[i] = D.scale * (st.e1[x][i] - dh[x] * st.e2[x][i]);
+                    IO<T, VEC>::store(reinterpret_cast<T*>(D.d_q) + k.r * D.d_q_stride +
+                                          (int64_t)(st.hq + x) * D.F + p.c, v);
+                }
             }
         }
     } else if (D.d_q) {
@@ -907,11 +1024,18 @@ void dot_launch(const EngineArgs& a, const DotArgs& d, int pass, hipStream_t s) 
     const Join j = join_of(a);
     const int64_t HF = (int64_t)d.H * d.F, KF = (int64_t)d.K * d.F;
     const dim3 threads(j.threads);
+    const bool split = RC == 4 && d.log2HL >= 2;
     if (pass == 0) {
-        hipLaunchKernelGGL((dot_forward_kernel<T, V, RC, OV, BIAS, FAST>), grid, block, 0, s, a, d);
+        if constexpr (RC == 4)
+            if (split) hipLaunchKernelGGL((dot_forward_kernel<T, V, RC, true, OV, BIAS, FAST>), grid, block, 0, s, a, d);
+        if (!split) hipLaunchKernelGGL((dot_forward_kernel<T, V, RC, false, OV, BIAS, FAST>), grid, block, 0, s, a, d);
         if (a.sch.n_hub > 0) hipLaunchKernelGGL((dot_join_kernel<T>), j.grid(a, HF), threads, 0, s, a, d, j.cols);
     } else if (pass == 1) {
-        hipLaunchKernelGGL((dot_backward_dst_kernel<T, V, RC, OV, BIAS, FAST>), grid, block, 0, s, a, d);
+        if constexpr (RC == 4)
+            if (split)
+                hipLaunchKernelGGL((dot_backward_dst_kernel<T, V, RC, true, OV, BIAS, FAST>), grid, block, 0, s, a, d);
+        if (!split)
+            hipLaunchKernelGGL((dot_backward_dst_kernel<T, V, RC, false, OV, BIAS, FAST>), grid, block, 0, s, a, d);
         if (a.sch.n_hub > 0) hipLaunchKernelGGL((dot_join_dst_kernel<T>), j.grid(a, HF), threads, 0, s, a, d, j.cols);
     } else if (pass == 2) {
         hipLaunchKernelGGL((dot_backward_src_kernel<T, V, OV, BIAS, FAST>), grid, block, 0, s, a, d);

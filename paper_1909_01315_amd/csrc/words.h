@@ -86,4 +86,43 @@ __device__ __forceinline__ void run_totals(float* v, int red) {
         for (int u = 0; u < N; ++u) v[u] += __shfl_xor(v[u], 32, WAVE);
 }
 
+// the value of lane X of each quad
+template <int X>
+__device__ __forceinline__ int32_t quad_lane(int32_t x) {
+    return __builtin_amdgcn_update_dpp(0, x, X * 0x55, 0xF, 0xF, true);
+}
+template <int X>
+__device__ __forceinline__ float quad_lane(float x) {
+    return dpp_f<X * 0x55>(x);
+}
+
+// Sums over the aligned run of `red` >= 4 lanes of four groups of N values
+// v[g N + n]: lane g of each quad gets the totals of group g (out[n]), a
+// quarter of what every lane would get.
+constexpr int DPP_QUAD_3210 = 0x1B;  // lane i reads lane 3 - i of its quad
+template <int N>
+__device__ __forceinline__ void quad_totals(const float* v, int red, float* out) {
+    const bool b0 = __lane_id() & 1, b1 = __lane_id() & 2;
+#pragma unroll
+    for (int n = 0; n < N; ++n) {
+        const float v0 = v[n], v1 = v[N + n], v2 = v[2 * N + n], v3 = v[3 * N + n];
+        const float lo = (b0 ? v1 : v0) + dpp_f<DPP_QUAD_1032>(b0 ? v0 : v1);  // groups 0 and 1 in lanes 0 and 1
+        const float hi = (b0 ? v3 : v2) + dpp_f<DPP_QUAD_1032>(b0 ? v2 : v3);
+        out[n] = (b1 ? hi : lo) + dpp_f<DPP_QUAD_2301>(b1 ? lo : hi);
+    }
+    // the lanes 4, 8, 16 and 32 apart (mirrors reverse a run: reversed twice)
+    if (red >= 8)
+#pragma unroll
+        for (int n = 0; n < N; ++n) out[n] += dpp_f<DPP_HALF_MIRROR>(dpp_f<DPP_QUAD_3210>(out[n]));
+    if (red >= 16)
+#pragma unroll
+        for (int n = 0; n < N; ++n) out[n] += dpp_f<DPP_MIRROR>(dpp_f<DPP_HALF_MIRROR>(out[n]));
+    if (red >= 32)
+#pragma unroll
+        for (int n = 0; n < N; ++n) out[n] += __shfl_xor(out[n], 16, WAVE);
+    if (red >= 64)
+#pragma unroll
+        for (int n = 0; n < N; ++n) out[n] += __shfl_xor(out[n], 32, WAVE);
+}
+
 }  // namespace gnnk
