@@ -192,8 +192,9 @@ CsrDev csr_of(const gnnk_graph* g, const Dir& d, bool ids = true) {
 }
 
 // hub_above >= 0: the hub rows are the rows longer than hub_above, taken
-// whole (a kernel that gives each one a workgroup, with no segments)
-SchedDev schedule(const Dir& d, const Geo& geo, bool fill_empty, int64_t hub_above = -1) {
+// whole (a kernel that gives each one a workgroup, with no segments);
+// small_auto: the automatic limit of rows that take one lane group each
+SchedDev schedule(const Dir& d, const Geo& geo, bool fill_empty, int64_t hub_above = -1, int64_t small_auto = 32) {
     SchedDev s{};
     const Options& o = options();
     const bool split = o.no_split == 0;
@@ -201,7 +202,7 @@ SchedDev schedule(const Dir& d, const Geo& geo, bool fill_empty, int64_t hub_abo
     const int64_t n_seg = hub_above >= 0 ? 0 : (split ? d.n_seg : 0);
     // rows of at most T edges take one lane group each; automatic: 32 (at
     // least the lane groups of a wavefront), none when a wavefront is one group
-    int64_t T = o.small_deg >= 0 ? o.small_deg : (geo.G > 1 ? std::max<int64_t>(geo.G, 32) : 0);
+    int64_t T = o.small_deg >= 0 ? o.small_deg : (geo.G > 1 ? std::max<int64_t>(geo.G, small_auto) : 0);
     int64_t n_big = std::max(d.count_above(T), n_hub);
     n_big = std::min(n_big, d.n_nz);
     const int fr = 4;
@@ -1711,6 +1712,11 @@ bool dot_walk(const gnnk_graph* g, const Dir& d, const DotCall& c, const gnnk_te
     A.csr = csr_of(g, d, ids);
     set_geo(A, c.geo);
     A.sch = schedule(d, c.geo, true);
+    // where all wavefronts run at once, the longest lane group's row is what
+    // takes time: a wavefront each for rows of more than 8 edges (20,000 rows,
+    // 109,170 edges, 8 heads of 8 fp32: 12.6 -> 11.5 us a pass; 262,144 rows
+    // of 32 edges, 8 and 2 heads of 32 bf16, forward 366 -> 755)
+    if (A.sch.w_small_end < 8192) A.sch = schedule(d, c.geo, true, -1, 8);
     const int es = c.dt == 1 ? 2 : 4;
     return !options().no_fast && fits32(A.a, a->rows, es) && fits32(A.b, b->rows, es);
 }
