@@ -426,8 +426,9 @@ gnnk_status gat_aggregate_backward(gnnk_graph_t g, const gnnk_tensor* feat, cons
  * (nullable, (num_dst, H, 2), always fp32) receives the maximum score and the
  * reciprocal of the sum of exp(s - max), (0, 0) where out is 0 for want of
  * edges; dot_aggregate_backward takes it.  Scores and weighted
- * sums over the edges of one wavefront's share of a row are fp32, the joins of
- * a long row's segments fp64.  F is at most 256 (fp32) or 512 (bf16) and H * F
+ * sums over the edges of one wavefront's share of a row are fp32 (bf16 values
+ * below 2^-126 count as 0 in the dot products), the joins of a long row's
+ * segments fp64.  F is at most 256 (fp32) or 512 (bf16) and H * F
  * at most 65,536 (GNNK_EUNSUPPORTED beyond).  Scratch: partials of hub rows'
  * segments.  Errors: GNNK_EINVAL on shapes or dtypes. */
 gnnk_status dot_aggregate(gnnk_graph_t g, const gnnk_tensor* q, const gnnk_tensor* k, const gnnk_tensor* v,
@@ -548,7 +549,9 @@ gnnk_status node_norm_rotary_work_bytes(const gnnk_tensor* q, const gnnk_tensor*
  *                 graph's CSR, 3 for both, 0 for none
  *   "small_deg"   rows of at most this many edges take one lane group each
  *                 and share a wavefront (-1 = auto: 32, or the lane groups
- *                 per wavefront if more; none when a wavefront is one group)
+ *                 per wavefront if more; none when a wavefront is one group;
+ *                 dot_aggregate: 8 in place of 32 on graphs whose wavefronts
+ *                 all run at once)
  *   "schedule"    0 auto (the row engine), 1 the row engine (node-parallel over the degree-
  *                 sorted rows), 2 the edge-parallel walk over the COO form
  *                 (equal edges per lane group; split rows combined in a fixed

@@ -561,10 +561,13 @@ def _like(t):
 
 def _here(*ts):
     """Refuse tensors of another device than the current one, whose stream the call would run on."""
-    cur = _device() if _device is not None else torch.cuda.current_device()
+    cur = -1
     for t in ts:
-        if t is not None and t.is_cuda and t.get_device() != cur:
-            raise ValueError(f"a tensor is on cuda:{t.get_device()}, the current device is cuda:{cur}")
+        if t is not None and t.is_cuda:
+            if cur < 0:
+                cur = _device() if _device is not None else torch.cuda.current_device()
+            if t.get_device() != cur:
+                raise ValueError(f"a tensor is on cuda:{t.get_device()}, the current device is cuda:{cur}")
 
 
 class Rotary:
@@ -580,7 +583,9 @@ class Rotary:
             raise ValueError("tensors must be on the GPU")
         if freq.dtype is not torch.float32 or freq.shape != (sum(self.pairs),):
             raise ValueError(f"freq must be float32 of shape ({sum(self.pairs)},)")
-        self.freq = freq.detach().contiguous()
+        if freq.requires_grad:
+            raise ValueError("no gradient is formed for frequencies: detach them")
+        self.freq = freq.contiguous()
         self.interleaved = bool(interleaved)
         self._tail = (len(self.pairs), *self.pairs, *(0,) * (4 - len(self.pairs)), int(self.interleaved), 0)
 
@@ -607,8 +612,6 @@ class Rotary:
         rows, axes = pos.shape
         if axes != len(self.pairs):
             raise ValueError(f"positions have {axes} axes, the rotation {len(self.pairs)}")
-        if pos.requires_grad and torch.is_grad_enabled():
-            raise ValueError("no gradient is formed for positions: detach them")
         stride = axes
         if rows:
             if axes > 1 and pos.stride(1) != 1:

@@ -229,14 +229,22 @@ def gat_aggregate(g, feat, el, er, slope: float = 0.2):
     return _FusedGAT.apply(g, _c(feat), _c(el), _c(er), float(slope))
 
 
+def _fixed(*positions):
+    """Positions get no gradient: refuse those that ask for one."""
+    if any(p is not None and p.requires_grad for p in positions):
+        raise ValueError("no gradient is formed for positions: detach them")
+
+
 def rotary(rot, x, pos):
     """Differentiable rotation of x (rows, H, F) by the positions pos (rows, axes)."""
+    _fixed(pos)
     return _Rotary.apply(rot, _c(x), pos)
 
 
 def norm_rotary(q, wq, k, wk, rot=None, pos_q=None, pos_k=None, eps: float = 1e-6):
     """Differentiable norms of the heads of queries and keys, with weights (F,), (H, F) or None, and their rotation by
     positions (rot None: none)."""
+    _fixed(pos_q, pos_k)
     return _NormRotary.apply(_c(q), _c(wq), _c(k), _c(wk), rot, pos_q, pos_k, float(eps))
 
 
