@@ -677,18 +677,23 @@ def node_norm_rotary_backward(q, wq, grad_q, k=None, wk=None, grad_k=None, rot: 
     rk = None
     if rot is not None and k is not None:
         rk = rq if pos_k is pos_q else rot._desc(pos_k)
+    xq, xk, gwq, gwk = _desc(q), _desc(k), _desc(dwq), _desc(dwk)
     work, nbytes = None, 0
-    if dwq is not None or dwk is not None:
+    if gwq is not None or gwk is not None:
         need = ctypes.c_size_t(0)
-        _check(load().node_norm_rotary_work_bytes(_desc(q), _desc(dwq), _desc(k), _desc(dwk), ctypes.byref(need)))
+        _check(load().node_norm_rotary_work_bytes(xq, gwq, xk, gwk, ctypes.byref(need)))
         nbytes = need.value
-        with torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext():
+        if stream is None:
             work = torch.empty(nbytes, dtype=torch.uint8, device=q.device)
-    _check(load().node_norm_rotary_backward(_desc(q), _desc(wq3), rq, _desc(grad_q), _desc(dq), _desc(dwq), _desc(k),
-                                            _desc(wk3), rk, _desc(grad_k), _desc(dk), _desc(dwk), eps, _ptr(work),
-                                            nbytes, _stream(stream)))
-    dwq = dwq.view(wq.shape) if dwq is not None else None
-    dwk = dwk.view(wk.shape) if dwk is not None else None
+        else:
+            with torch.cuda.stream(stream):
+                work = torch.empty(nbytes, dtype=torch.uint8, device=q.device)
+    _check(load().node_norm_rotary_backward(xq, _desc(wq3), rq, _desc(grad_q), _desc(dq), gwq, xk, _desc(wk3), rk,
+                                            _desc(grad_k), _desc(dk), gwk, eps, _ptr(work), nbytes, _stream(stream)))
+    if dwq is not None and wq.dim() != 3:
+        dwq = dwq.view(wq.shape)
+    if dwk is not None and wk.dim() != 3:
+        dwk = dwk.view(wk.shape)
     return (dq, dwq, dk, dwk) if k is not None else (dq, dwq)
 
 
