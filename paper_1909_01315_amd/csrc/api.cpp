@@ -1658,12 +1658,17 @@ void dot_lanes(DotCall& c, int RC, int RL) {
     geo.G = 64 / geo.L;
 }
 
-// the largest power of two up to `most` that divides the query heads of a key
-// head (narrow heads, of less than the widest vectors: 1)
-int dot_share(const DotCall& c, int most) {
-    if (c.geo.vec != (c.dt == 1 ? 8 : 4)) return 1;
-    while (c.D.R % most) most >>= 1;
-    return most;
+// The query heads of a key head in the passes that gather keys and values: up
+// to four in a lane's registers (narrow heads, of less than the widest
+// vectors, and tables past 32-bit offsets: one), the rest in lanes beside each
+// other as far as a wavefront holds them.  In turns instead, each of which
+// gathers the rows anew, 4.2M edges of 131,072 rows, forward, heads of 64: 16
+// query and 2 key heads bf16 483 -> 643 us, fp32 717 -> 1,315.
+void dot_share(DotCall& c, bool fast) {
+    const int R = c.D.R;
+    const bool wide = c.geo.vec == (c.dt == 1 ? 8 : 4);
+    const int RC = !wide || !fast || R == 1 ? 1 : (R == 2 ? 2 : 4);
+    dot_lanes(c, RC, std::min(pow2ceil((R + RC - 1) / RC), 64 >> c.D.log2HL));
 }
 
 gnnk_status dot_check(gnnk_graph_t g, const gnnk_tensor* q, const gnnk_tensor* k, const gnnk_tensor* v,
@@ -1703,9 +1708,15 @@ void dot_operands(const gnnk_tensor* q, const gnnk_tensor* k, const gnnk_tensor*
     }
 }
 
-// a walk over d that gathers rows of a and b; true: their tables take 32-bit
-// byte offsets
-bool dot_walk(const gnnk_graph* g, const Dir& d, const DotCall& c, const gnnk_tensor* a, const gnnk_tensor* b, bool ids,
+// the tables a and b take 32-bit byte offsets
+bool dot_fast(const DotCall& c, const gnnk_tensor* a, const gnnk_tensor* b) {
+    const int es = c.dt == 1 ? 2 : 4;
+    return !options().no_fast && fits32(operand(a, K_FULL, T_NBR), a->rows, es) &&
+           fits32(operand(b, K_FULL, T_NBR), b->rows, es);
+}
+
+// a walk over d that gathers rows of a and b
+void dot_walk(const gnnk_graph* g, const Dir& d, const DotCall& c, const gnnk_tensor* a, const gnnk_tensor* b, bool ids,
              EngineArgs& A) {
     A.a = operand(a, K_FULL, T_NBR);
     A.b = operand(b, K_FULL, T_NBR);
@@ -1717,8 +1728,6 @@ bool dot_walk(const gnnk_graph* g, const Dir& d, const DotCall& c, const gnnk_te
     // 109,170 edges, 8 heads of 8 fp32: 12.6 -> 11.5 us a pass; 262,144 rows
     // of 32 edges, 8 and 2 heads of 32 bf16, forward 366 -> 755)
     if (A.sch.w_small_end < 8192) A.sch = schedule(d, c.geo, true, -1, 8);
-    const int es = c.dt == 1 ? 2 : 4;
-    return !options().no_fast && fits32(A.a, a->rows, es) && fits32(A.b, b->rows, es);
 }
 
 }  // namespace
@@ -1739,9 +1748,9 @@ gnnk_status dot_aggregate(gnnk_graph_t g, const gnnk_tensor* q, const gnnk_tenso
     D.out = out->data;
     D.out_stride = out->row_stride;
     EngineArgs A{};
-    dot_lanes(c, dot_share(c, 4), 1);
-    const bool fast = dot_walk(g, g->in_nbr, c, k, v, bias != nullptr, A);
-    if (!fast) D.RC = 1;
+    const bool fast = dot_fast(c, k, v);
+    dot_share(c, fast);
+    dot_walk(g, g->in_nbr, c, k, v, bias != nullptr, A);
     D.part_stride = (int64_t)D.H * D.F + 2 * D.H;
     if (A.sch.n_seg > 0) {
         Scratch sc = scratch_of(g, stream);
@@ -1787,22 +1796,23 @@ static gnnk_status dot_backward(gnnk_graph_t g, const gnnk_tensor* q, const gnnk
     // by destination
     EngineArgs ain{}, aout{}, aedge{};
     DotCall in = c, src = c, edge = c;
-    dot_lanes(in, dot_share(c, 4), 1);
-    const bool gin = dot_walk(g, g->in_nbr, in, k, v, ids, ain);
-    if (!gin) in.D.RC = 1;
+    const bool gin = dot_fast(c, k, v);
+    dot_share(in, gin);
+    dot_walk(g, g->in_nbr, in, k, v, ids, ain);
     // by source: the query heads of a key head in lanes beside each other, as
     // many as a power of two that divides them and one wavefront hold
     int RL = 1;
     while (D.R % (2 * RL) == 0 && (2 * RL) << D.log2HL <= 64) RL *= 2;
     dot_lanes(src, 1, RL);
-    bool gout = dot_walk(g, g->out_fine_nbr, src, q, grad_out, ids, aout);
-    if ((int64_t)D.H * 16 >= (1 << 24) || (uint64_t)g->n_dst * D.H * 16 > 0xFFFFFFFFull) gout = false;
+    dot_walk(g, g->out_fine_nbr, src, q, grad_out, ids, aout);
+    const bool gout = dot_fast(c, q, grad_out) && (int64_t)D.H * 16 < (1 << 24) &&
+                      (uint64_t)g->n_dst * D.H * 16 <= 0xFFFFFFFFull;
     // the gradient of the bias: in that pass, unless the heads that share it
     // take several, in which it is summed over the slices and query heads
     const bool by_edge = grad_bias && !D.bias_per_head && (src.D.slices > 1 || RL < D.R);
     src.D.src_bias = grad_bias && !by_edge;
     dot_lanes(edge, 1, 1);
-    const bool gedge = dot_walk(g, g->in_nbr, edge, k, v, true, aedge);
+    dot_walk(g, g->in_nbr, edge, k, v, true, aedge);
     const int passes = by_edge ? edge.D.slices * D.R : 0;
 
     Scratch sc = scratch_of(g, stream);
@@ -1827,7 +1837,7 @@ static gnnk_status dot_backward(gnnk_graph_t g, const gnnk_tensor* q, const gnnk
         edge.D.r0 = i / slices;
         edge.D.edge_first = i == 0;
         edge.D.edge_last = i == passes - 1;
-        st = GNNK_LAUNCH(launch_dot(aedge, edge.D, 3, c.dt, c.geo.vec, gedge, stream),
+        st = GNNK_LAUNCH(launch_dot(aedge, edge.D, 3, c.dt, c.geo.vec, gin, stream),
                          "dot-product attention backward launch (edges)");
     }
     return st;

@@ -11,7 +11,9 @@
 // beyond one wavefront's lanes are slices of the grid.  Of the R query heads
 // that share a key head, a lane takes RC at once in registers (each key and
 // value row is then gathered and widened once for them), RL neighbouring runs
-// of lanes take as many beside each other, and what is left takes turns.
+// of lanes take as many beside each other, and what is left takes turns; where
+// R is no multiple, the last ones do the last head's work again and write
+// nothing.
 //
 // Dot products and the sums over the edges of one wavefront's share of a
 // row are fp32; the partial results of a long row's segments are joined in
@@ -176,7 +178,15 @@ __device__ __forceinline__ void issue(const EngineArgs& A, const DotArgs& D, con
             const T* b = reinterpret_cast<const T*>(D.bias) +
                          (uint64_t)(uint32_t)id.ed[u] * (uint32_t)D.bias_stride;
             if (D.bias_per_head) {
-                IO<T, RC>::load(b + hq, x.bias[u]);
+                if (RC <= 2 || D.R % (RC << D.log2RL) == 0) {  // (2: of key heads that two share)
+                    IO<T, RC>::load(b + hq, x.bias[u]);
+                } else {
+#pragma unroll
+                    for (int r = 0; r < RC; ++r) {
+                        const int h = hq + r < D.H ? hq + r : D.H - 1;  // (past the key head's: not used)
+                        x.bias[u][r] = IO<T, 1>::load1(b + h);
+                    }
+                }
             } else {
                 x.bias[u][0] = IO<T, 1>::load1(b);
 #pragma unroll
@@ -231,6 +241,16 @@ __device__ __forceinline__ void scores(const DotArgs& D, const B& x, int r, floa
 // ---------------------------------------------------------------------------
 // forward
 
+// the RC query heads that a lane takes in one turn
+template <int RC>
+struct Heads {
+    int first, last;  // and the last one of its key head
+    __device__ __forceinline__ Heads(const DotArgs& D, const Place& p, int turn)
+        : first(p.j * D.R + turn + p.rl * RC), last(p.j * D.R + D.R - 1) {}
+    __device__ __forceinline__ bool has(int r) const { return first + r <= last; }
+    __device__ __forceinline__ int at(int r) const { return has(r) ? first + r : last; }
+};
+
 // the weight of a slot that lies outside the row or is masked: a zero that no
 // exponential gives
 constexpr float GONE = -0.0f;
@@ -245,16 +265,16 @@ struct Forward {
     static constexpr int SC = SPLIT ? 1 : RC;  // heads whose scores a lane keeps
     const DotArgs& D;
     const Place& p;
-    int hq;  // the first of the lane's RC query heads
+    Heads<RC> hq;  // the lane's query heads
     using W = Words<T, VEC>;
     float q[RC][W::N];
     float m[SC], l[SC], acc[RC][VEC];
 
-    __device__ __forceinline__ Forward(const DotArgs& D_, const Place& p_, int hq_, int64_t row)
-        : D(D_), p(p_), hq(hq_) {
+    __device__ __forceinline__ Forward(const DotArgs& D_, const Place& p_, int turn, int64_t row)
+        : D(D_), p(p_), hq(D_, p_, turn) {
 #pragma unroll
         for (int r = 0; r < RC; ++r) {
-            own_row<T, VEC>(D, D.q, row * D.q_stride + (int64_t)(hq + r) * D.F + p.c, q[r]);
+            own_row<T, VEC>(D, D.q, row * D.q_stride + (int64_t)hq.at(r) * D.F + p.c, q[r]);
 #pragma unroll
             for (int i = 0; i < VEC; ++i) acc[r][i] = 0.0f;
         }
@@ -265,7 +285,7 @@ struct Forward {
         }
     }
     // the first head whose scores the lane keeps
-    __device__ __forceinline__ int score_head() const { return SPLIT ? hq + (int)(__lane_id() & 3) : hq; }
+    __device__ __forceinline__ int score_head() const { return SPLIT ? hq.at(__lane_id() & 3) : hq.at(0); }
     // a value that the lane of head r keeps
     template <int R>
     static __device__ __forceinline__ float of(const float* v) {
@@ -367,10 +387,12 @@ struct Forward {
     template <class F>
     __device__ __forceinline__ void each_score(F fn) const {
         if constexpr (SPLIT) {
-            if ((__lane_id() & ((1 << D.log2HL) - 1)) < 4) fn(score_head(), m[0], l[0]);
+            const int x = __lane_id() & ((1 << D.log2HL) - 1);
+            if (x < 4 && hq.has(x)) fn(score_head(), m[0], l[0]);
         } else if (p.first) {
 #pragma unroll
-            for (int r = 0; r < RC; ++r) fn(hq + r, m[r], l[r]);
+            for (int r = 0; r < RC; ++r)
+                if (hq.has(r)) fn(hq.at(r), m[r], l[r]);
         }
     }
 };
@@ -421,14 +443,14 @@ __global__ __launch_bounds__(256, 3) void dot_forward_kernel(EngineArgs A, DotAr
     const Lanes ln = lanes_of(A.geo);
     const int G = A.geo.G, L = A.geo.L;
     const Place p = place_of<VEC>(D, ln.lig);
-    const int kcol = p.j * D.F + p.c, step = RC << D.log2RL, h0 = p.j * D.R + p.rl * RC;
+    const int kcol = p.j * D.F + p.c, step = RC << D.log2RL;
     using State = Forward<T, VEC, RC, SPLIT, OV, BIAS>;
     if (w < A.sch.w_small_end) {
         const bool wave = w < A.sch.w_big_end;
         const Work k = wave ? wave_work(A, w) : lane_work(A, w, G, ln.g);
         const int64_t self = k.r >= 0 ? k.r : 0;
         for (int r = 0; r < D.R; r += step) {
-            State st(D, p, h0 + r, self);
+            State st(D, p, r, self);
             walk<T, VEC, State::SC, FAST, BIAS, false>(A, D, (int32_t)k.b, (int32_t)k.e, wave ? U * ln.g : 0,
                                                        wave ? U * G : U, kcol, st.score_head(), st);
             if (wave) st.join_groups(L);
@@ -450,8 +472,9 @@ __global__ __launch_bounds__(256, 3) void dot_forward_kernel(EngineArgs A, DotAr
                 if (!p.act) continue;
 #pragma unroll
                 for (int x = 0; x < RC; ++x)
+                    if (st.hq.has(x))
 #pragma unroll
-                    for (int i = 0; i < VEC; ++i) P[(int64_t)(st.hq + x) * D.F + p.c + i] = st.acc[x][i];
+                        for (int i = 0; i < VEC; ++i) P[(int64_t)st.hq.at(x) * D.F + p.c + i] = st.acc[x][i];
             } else {
                 if (own) st.each_score([&](int hq, float m, float l) { write_stats(D, k.r, hq, m, l); });
                 if (!p.act) continue;
@@ -459,20 +482,20 @@ __global__ __launch_bounds__(256, 3) void dot_forward_kernel(EngineArgs A, DotAr
                 for (int x = 0; x < RC; ++x) {
 #pragma unroll
                     for (int i = 0; i < VEC; ++i) st.acc[x][i] *= ih[x];
-                    IO<T, VEC>::store(reinterpret_cast<T*>(D.out) + k.r * D.out_stride +
-                                          (int64_t)(st.hq + x) * D.F + p.c, st.acc[x]);
+                    if (st.hq.has(x))
+                        IO<T, VEC>::store(reinterpret_cast<T*>(D.out) + k.r * D.out_stride +
+                                              (int64_t)st.hq.at(x) * D.F + p.c, st.acc[x]);
                 }
             }
         }
     } else {
         empty_rows(A, w, G, ln.g, [&](int64_t row) {
             const float zero[VEC] = {};
-            for (int r = 0; r < D.R && p.act; r += step)
-                for (int x = 0; x < RC; ++x) {
-                    IO<T, VEC>::store(reinterpret_cast<T*>(D.out) + row * D.out_stride +
-                                          (int64_t)(h0 + r + x) * D.F + p.c, zero);
-                    if (p.first) write_stats(D, row, h0 + r + x, 0.0f, 0.0f);
-                }
+            for (int r = p.rl; r < D.R && p.act; r += 1 << D.log2RL) {
+                const int hq = p.j * D.R + r;
+                IO<T, VEC>::store(reinterpret_cast<T*>(D.out) + row * D.out_stride + (int64_t)hq * D.F + p.c, zero);
+                if (p.first) write_stats(D, row, hq, 0.0f, 0.0f);
+            }
         });
     }
 }
@@ -550,17 +573,17 @@ struct ToDst {
     static constexpr int SC = Fwd::SC;  // heads whose scores a lane keeps, as in the forward
     const DotArgs& D;
     const Place& p;
-    int hq;  // the first of the lane's RC query heads
+    Heads<RC> hq;  // the lane's query heads
     using W = Words<T, VEC>;
     float q[RC][W::N], dz[RC][W::N], m[SC], il[SC], S0[SC], delta[SC];
     float e1[RC][VEC], e2[RC][VEC];
 
-    __device__ __forceinline__ ToDst(const DotArgs& D_, const Place& p_, int hq_, int64_t row)
-        : D(D_), p(p_), hq(hq_) {
+    __device__ __forceinline__ ToDst(const DotArgs& D_, const Place& p_, int turn, int64_t row)
+        : D(D_), p(p_), hq(D_, p_, turn) {
         float zo[RC];
 #pragma unroll
         for (int r = 0; r < RC; ++r) {
-            const int64_t c = (int64_t)(hq + r) * D.F + p.c;
+            const int64_t c = (int64_t)hq.at(r) * D.F + p.c;
             float o[W::N];
             own_row<T, VEC>(D, D.q, row * D.q_stride + c, q[r]);
             row_words<T, VEC>(D.dz, row * D.dz_stride + c, dz[r]);
@@ -574,12 +597,13 @@ struct ToDst {
 #pragma unroll
         for (int r = 0; r < SC; ++r) {
             if constexpr (!SPLIT) S0[r] = zo[r];
-            m[r] = D.stats[row * D.stats_stride + 2 * (score_head() + r)];
-            il[r] = D.stats[row * D.stats_stride + 2 * (score_head() + r) + 1];
+            const int h = SPLIT ? score_head() : hq.at(r);
+            m[r] = D.stats[row * D.stats_stride + 2 * h];
+            il[r] = D.stats[row * D.stats_stride + 2 * h + 1];
             delta[r] = 0.0f;
         }
     }
-    __device__ __forceinline__ int score_head() const { return SPLIT ? hq + (int)(__lane_id() & 3) : hq; }
+    __device__ __forceinline__ int score_head() const { return SPLIT ? hq.at(__lane_id() & 3) : hq.at(0); }
     template <bool ALL, class B>
     __device__ __forceinline__ void take(const B& x) {
         float s[RC * U], t[RC * U];
@@ -649,10 +673,12 @@ struct ToDst {
     template <class F>
     __device__ __forceinline__ void each_score(F fn) const {
         if constexpr (SPLIT) {
-            if ((__lane_id() & ((1 << D.log2HL) - 1)) < 4) fn(score_head(), 0);
+            const int x = __lane_id() & ((1 << D.log2HL) - 1);
+            if (x < 4 && hq.has(x)) fn(score_head(), 0);
         } else if (p.first) {
 #pragma unroll
-            for (int r = 0; r < RC; ++r) fn(hq + r, r);
+            for (int r = 0; r < RC; ++r)
+                if (hq.has(r)) fn(hq.at(r), r);
         }
     }
 };
@@ -716,14 +742,14 @@ __global__ __launch_bounds__(256, RC == 4 ? 2 : 3) void dot_backward_dst_kernel(
     const Lanes ln = lanes_of(A.geo);
     const int G = A.geo.G, L = A.geo.L;
     const Place p = place_of<VEC>(D, ln.lig);
-    const int kcol = p.j * D.F + p.c, step = RC << D.log2RL, h0 = p.j * D.R + p.rl * RC;
+    const int kcol = p.j * D.F + p.c, step = RC << D.log2RL;
     using State = ToDst<T, VEC, RC, SPLIT, OV, BIAS>;
     if (w < A.sch.w_small_end) {
         const bool wave = w < A.sch.w_big_end;
         const Work k = wave ? wave_work(A, w) : lane_work(A, w, G, ln.g);
         const int64_t self = k.r >= 0 ? k.r : 0;
         for (int r = 0; r < D.R; r += step) {
-            State st(D, p, h0 + r, self);
+            State st(D, p, r, self);
             walk<T, VEC, State::SC, FAST, BIAS, false>(A, D, (int32_t)k.b, (int32_t)k.e, wave ? U * ln.g : 0,
                                                        wave ? U * G : U, kcol, st.score_head(), st);
             if (wave) st.join_groups(L);
@@ -741,7 +767,8 @@ __global__ __launch_bounds__(256, RC == 4 ? 2 : 3) void dot_backward_dst_kernel(
                 if (!p.act) continue;
 #pragma unroll
                 for (int x = 0; x < RC; ++x) {
-                    const int64_t c = (int64_t)(st.hq + x) * D.F + p.c;
+                    if (!st.hq.has(x)) break;
+                    const int64_t c = (int64_t)st.hq.at(x) * D.F + p.c;
 #pragma unroll
                     for (int i = 0; i < VEC; ++i) {
                         P[c + i] = st.e1[x][i];
@@ -759,18 +786,18 @@ __global__ __launch_bounds__(256, RC == 4 ? 2 : 3) void dot_backward_dst_kernel(
                     float v[VEC];
 #pragma unroll
                     for (int i = 0; i < VEC; ++i) v[i] = D.scale * (st.e1[x][i] - dh[x] * st.e2[x][i]);
-                    IO<T, VEC>::store(reinterpret_cast<T*>(D.d_q) + k.r * D.d_q_stride +
-                                          (int64_t)(st.hq + x) * D.F + p.c, v);
+                    if (st.hq.has(x))
+                        IO<T, VEC>::store(reinterpret_cast<T*>(D.d_q) + k.r * D.d_q_stride +
+                                              (int64_t)st.hq.at(x) * D.F + p.c, v);
                 }
             }
         }
     } else if (D.d_q) {
         empty_rows(A, w, G, ln.g, [&](int64_t row) {
             const float zero[VEC] = {};
-            for (int r = 0; r < D.R && p.act; r += step)
-                for (int x = 0; x < RC; ++x)
-                    IO<T, VEC>::store(reinterpret_cast<T*>(D.d_q) + row * D.d_q_stride +
-                                          (int64_t)(h0 + r + x) * D.F + p.c, zero);
+            for (int r = p.rl; r < D.R && p.act; r += 1 << D.log2RL)
+                IO<T, VEC>::store(reinterpret_cast<T*>(D.d_q) + row * D.d_q_stride +
+                                      (int64_t)(p.j * D.R + r) * D.F + p.c, zero);
         });
     }
 }

@@ -128,6 +128,18 @@ def test_small_rows(H, K, F, dtype, kind):
     check(uniform(), H, K, F, dtype, kind)
 
 
+# query heads of a key head that are no multiple of what a lane takes, more
+# than a wavefront holds, in narrow and wide heads
+@pytest.mark.parametrize("kind", [None, "heads", "shared", "mask"])
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("H,K,F", [(3, 1, 64), (6, 2, 32), (12, 1, 8), (5, 1, 40), (7, 1, 16), (24, 2, 64), (10, 2, 3),
+                                   (16, 1, 256), (11, 1, 100), (64, 1, 8), (32, 4, 128)])
+def test_query_heads_of_a_key_head(H, K, F, dtype, kind):
+    check(uniform(e=700), H, K, F, dtype, kind)
+    gnnk.set_option("seg_edges", 64)
+    check(hubs(), H, K, F, dtype, kind)
+
+
 @pytest.mark.parametrize("no_fast", [0, 1])
 @pytest.mark.parametrize("seg", [0, 64])
 @pytest.mark.parametrize("H,K,F,dtype,kind", [
