@@ -483,8 +483,9 @@ typedef struct {
 } gnnk_rotary;
 
 /* out = x with its pairs turned by their angles (inverse != 0: by the
- * opposite angles, which is also the gradient).  x and out: (rows, H, F), F at
- * most 2,048.  Errors: GNNK_EINVAL on shapes, pairs or dtypes. */
+ * opposite angles, which is also the gradient).  x and out: (rows, H, F), fewer
+ * than 2^31 rows of at most 1,024 heads of at most 2,048 columns.  Errors:
+ * GNNK_EINVAL on shapes, pairs or dtypes. */
 gnnk_status node_rotary(const gnnk_rotary* rot, const gnnk_tensor* x, int32_t inverse, gnnk_tensor* out,
                         hipStream_t stream);
 
@@ -495,7 +496,7 @@ gnnk_status node_rotary(const gnnk_rotary* rot, const gnnk_tensor* x, int32_t in
  * (nullable: all ones) one row of (H, F) or (1, F), out_q like q; k may have
  * other rows and heads but the same F.  rot_q / rot_k (nullable, both or
  * neither: no rotation) have q's and k's rows and the same pairs and layout.
- * The sum of a head's squares is fp32.  F is at most 2,048, eps >= 0.
+ * The sum of a head's squares is fp32.  Sizes as in node_rotary, eps >= 0.
  * Errors: GNNK_EINVAL. */
 gnnk_status node_norm_rotary(const gnnk_tensor* q, const gnnk_tensor* wq, const gnnk_rotary* rot_q,
                              gnnk_tensor* out_q, const gnnk_tensor* k, const gnnk_tensor* wk,

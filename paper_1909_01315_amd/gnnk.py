@@ -248,6 +248,7 @@ class Graph:
         self._h = handle
         self._keep = keep  # tensors the handle points into
         self._lent = {}    # stream handle -> scratch buffer lent for that stream
+        self._replaced = []  # smaller ones lent before
         self.num_src, self.num_dst, self.num_edges = num_src, num_dst, num_edges
 
     @property
@@ -263,15 +264,19 @@ class Graph:
 
     def lend_scratch(self, nbytes: int, stream=None):
         """Lend the handle a scratch buffer of at least nbytes for the calls on
-        `stream` (default: the current stream), allocated on that stream; the
-        buffer it replaces goes back to torch's allocator, which reuses it only
-        for work ordered after the calls already queued on that stream."""
+        `stream` (default: the current stream), allocated on that stream.  A
+        buffer that it replaces stays with the handle: a captured graph holds
+        its address (each is at least twice as large as the one before, so all
+        of them together take less than twice the last one).  Graphs captured
+        on one stream share its buffer: their replays must not overlap."""
         s = stream if stream is not None else torch.cuda.current_stream()
         old = self._lent.get(s.cuda_stream)
-        size = max(int(nbytes), int(old.numel() * 5 // 4) if old is not None else 0, 256)
+        size = max(int(nbytes), 2 * old.numel() if old is not None else 0, 256)
         with torch.cuda.stream(s):
             buf = torch.empty(size, dtype=torch.uint8, device=self.device)
         _check(load().graph_attach_scratch(self.handle, s.cuda_stream, buf.data_ptr(), size))
+        if old is not None:
+            self._replaced.append(old)
         self._lent[s.cuda_stream] = buf
 
     @classmethod
@@ -365,7 +370,7 @@ class Graph:
             _check(load().graph_destroy(self._h))
             self._h = None
             self._keep = None
-            self._lent = None
+            self._lent = self._replaced = None
 
     def __del__(self):
         try:

@@ -27,6 +27,7 @@ from __future__ import annotations
 import math
 
 import torch
+from torch.autograd.function import once_differentiable
 
 from . import gnnk
 
@@ -152,6 +153,7 @@ class _Rotary(torch.autograd.Function):
         return gnnk.node_rotary(rot, x, pos).view(x.shape)
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dy):
         (pos,) = ctx.saved_tensors
         return None, gnnk.node_rotary(ctx.rot, _c(dy), pos, inverse=True).view(dy.shape), None
@@ -165,16 +167,19 @@ class _NormRotary(torch.autograd.Function):
     def forward(ctx, q, wq, k, wk, rot, pos_q, pos_k, eps):
         ctx.rot, ctx.eps = rot, eps
         ctx.save_for_backward(q, wq, k, wk, pos_q, pos_k)
+        if k is None:
+            return gnnk.node_norm_rotary(q, wq, rot=rot, pos_q=pos_q, eps=eps).view(q.shape)
         oq, ok = gnnk.node_norm_rotary(q, wq, k, wk, rot=rot, pos_q=pos_q, pos_k=pos_k, eps=eps)
         return oq.view(q.shape), ok.view(k.shape)
 
     @staticmethod
-    def backward(ctx, gq, gk):
+    @once_differentiable
+    def backward(ctx, gq, gk=None):
         q, wq, k, wk, pos_q, pos_k = ctx.saved_tensors
         nf = ctx.needs_input_grad
-        dq, dwq, dk, dwk = gnnk.node_norm_rotary_backward(q, wq, _c(gq), k, wk, _c(gk), rot=ctx.rot, pos_q=pos_q,
-                                                          pos_k=pos_k, eps=ctx.eps, want_q=nf[0], want_wq=nf[1],
-                                                          want_k=nf[2], want_wk=nf[3])
+        grads = gnnk.node_norm_rotary_backward(q, wq, _c(gq), k, wk, _c(gk), rot=ctx.rot, pos_q=pos_q, pos_k=pos_k,
+                                               eps=ctx.eps, want_q=nf[0], want_wq=nf[1], want_k=nf[2], want_wk=nf[3])
+        dq, dwq, dk, dwk = grads if k is not None else (*grads, None, None)
         view = lambda t, like: t.view(like.shape) if t is not None else None
         return view(dq, q), dwq, view(dk, k), dwk, None, None, None, None
 
@@ -191,6 +196,7 @@ class _DotAggregate(torch.autograd.Function):
         return out
 
     @staticmethod
+    @once_differentiable
     def backward(ctx, dout):
         q, k, v, bias, out, stats = ctx.saved_tensors
         nf = ctx.needs_input_grad
@@ -241,9 +247,9 @@ def rotary(rot, x, pos):
     return _Rotary.apply(rot, _c(x), pos)
 
 
-def norm_rotary(q, wq, k, wk, rot=None, pos_q=None, pos_k=None, eps: float = 1e-6):
+def norm_rotary(q, wq=None, k=None, wk=None, rot=None, pos_q=None, pos_k=None, eps: float = 1e-6):
     """Differentiable norms of the heads of queries and keys, with weights (F,), (H, F) or None, and their rotation by
-    positions (rot None: none)."""
+    positions (rot None: none).  Returns both, or the queries alone without keys."""
     _fixed(pos_q, pos_k)
     return _NormRotary.apply(_c(q), _c(wq), _c(k), _c(wk), rot, pos_q, pos_k, float(eps))
 

@@ -175,6 +175,27 @@ def test_graphs_from_no_edges_to_one_long_row(name, H, K, F, dtype, kind):
     check(GRAPHS[name](), H, K, F, dtype, kind)
 
 
+@pytest.mark.parametrize("H,K,F,dtype,kind", [
+    (1, 1, 256, F32, "heads"), (2, 1, 512, BF16, "shared"), (256, 256, 256, F32, "shared"), (128, 32, 512, BF16, "mask"),
+    (1024, 8, 64, BF16, None), (300, 300, 1, F32, "shared")])
+def test_widest_heads_and_rows(H, K, F, dtype, kind):
+    check(uniform(30, 20, 60), H, K, F, dtype, kind)
+
+
+@pytest.mark.parametrize("n_src,n_dst", [(0, 4), (5, 0), (0, 0)])
+@pytest.mark.parametrize("shared", [False, True])
+def test_graphs_without_a_side(n_src, n_dst, shared):
+    none = torch.empty(0, dtype=torch.long)
+    gr = Graph(none, none, n_src, n_dst)
+    q, kv = torch.randn((n_dst, 4, 8), device="cuda"), torch.randn((n_src, 2, 8), device="cuda")
+    b = torch.empty((0, 1 if shared else 4, 1), device="cuda")
+    out, stats = gnnk.dot_aggregate(gr.g, q, kv, kv, bias=b, want_stats=True)
+    assert out.shape == q.shape and bool((out == 0).all()) and bool((stats == 0).all())
+    grads = gnnk.dot_aggregate_backward(gr.g, q, kv, kv, out, stats, q, bias=b)
+    for t, x in zip(grads, (q, kv, kv, b)):
+        assert t.shape == x.shape and bool((t == 0).all())
+
+
 @pytest.mark.parametrize("pad", [1, 2, 8])
 @pytest.mark.parametrize("H,K,F,dtype", [(8, 8, 16, F32), (6, 3, 47, BF16), (4, 4, 8, BF16), (2, 2, 3, F32)])
 def test_strided_rows_of_any_alignment(H, K, F, dtype, pad):
@@ -391,6 +412,47 @@ def test_replays_and_two_streams_equal_eager():
         torch.cuda.synchronize()
         assert all(torch.equal(x, y) for x, y in zip(outs, eager))
         _ = (q * 2).sum().item()
+
+
+def test_a_larger_call_leaves_a_captured_one_its_scratch():
+    """Scratch grows for an eager call on the stream of a captured one: a
+    replay afterwards writes into no tensor that lives since."""
+    gnnk.set_option("seg_edges", 64)
+    gr = hubs()
+    g = gen(61)
+    mk = lambda h, f: tuple(torch.randn((gr.n_dst, h, f), generator=g).cuda() for _ in range(3))
+    small, large = mk(2, 16), mk(16, 64)
+    s = torch.cuda.Stream()
+    s.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(s):
+        want = gnnk.dot_aggregate(gr.g, *small)
+    torch.cuda.synchronize()
+    before = gr.g._lent[s.cuda_stream]
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=s):
+        got = gnnk.dot_aggregate(gr.g, *small)
+    with torch.cuda.stream(s):
+        gnnk.dot_aggregate(gr.g, *large)
+        after = gr.g._lent[s.cuda_stream]
+        size = before.numel()
+        assert after.numel() >= 2 * size
+        del before
+        since = [torch.full((size,), 7, dtype=torch.uint8, device="cuda") for _ in range(4)]
+    torch.cuda.synchronize()
+    for _ in range(3):
+        got.fill_(float("nan"))
+        graph.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(got, want)
+        assert all(bool((t == 7).all()) for t in since)
+
+
+def test_second_derivatives_are_refused():
+    gr = uniform()
+    q, k = (torch.randn(n, 2, 8, device="cuda", requires_grad=True) for n in (gr.n_dst, gr.n_src))
+    (d,) = torch.autograd.grad((nn.dot_aggregate(gr.g, q, k, k) ** 2).sum(), q, create_graph=True)
+    with pytest.raises(RuntimeError):
+        (d ** 2).sum().backward()
 
 
 @pytest.mark.parametrize("shared", [False, True])

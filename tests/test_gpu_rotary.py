@@ -106,6 +106,19 @@ def test_rotary_writes_only_its_columns_and_passes_what_is_not_turned():
     assert torch.equal(gnnk.node_rotary(rot, x.cuda(), wide[:, 1:3]).nan_to_num(3.5), out.nan_to_num(3.5))
 
 
+def test_positions_at_the_ends_of_int32_and_many_heads():
+    """An angle near 2^31 is off by 2.5 half steps of fp64 (the product, the
+    constant's own, the product with it): 2.5 2^-53 2^31 = 10 u."""
+    pairs, H, F, n = (4, 4), 1024, 16, 6
+    g = gen(7)
+    x = normal(g, n, H, F)
+    ends = torch.tensor([-2 ** 31, 2 ** 31 - 1, 2 ** 31 - 2, 0, -1, 2 ** 30 + 1])
+    pos, freq = torch.stack([ends, ends.flip(0)], 1).int(), frequencies(pairs)
+    theta = angles(pos, freq, pairs)
+    got = gnnk.node_rotary(gnnk.Rotary(freq.cuda(), pairs), x.cuda(), pos.cuda())
+    close(got, turn(x.double(), theta, False), (TURN_U + 10) * U32 * pair_size(x.double(), 8, False), "rotary")
+
+
 def test_rotary_of_no_rows():
     rot = gnnk.Rotary.geometric((2, 2))
     x = torch.empty((0, 2, 8), device="cuda")
@@ -145,7 +158,8 @@ def norm_reference(x, w, theta, il, eps, g=None):
 
 @pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("per_head", [False, True])
-@pytest.mark.parametrize("n,H,F,pairs,il", SHAPES + [(50, 4, 40, None, False), (200, 1, 5, None, False)])
+@pytest.mark.parametrize("n,H,F,pairs,il", SHAPES + [(50, 4, 40, None, False), (200, 1, 5, None, False),
+                                                        (40, 2, 1, None, False)])
 def test_norm_rotary_and_gradients(n, H, F, pairs, il, per_head, dtype):
     g = gen(n * 3 + F)
     eps = 1e-5
@@ -245,6 +259,35 @@ def test_differentiable_forms_match_differences():
         got = float((grad * d).sum())
         # fp32 gradients, at most 300 u of each term; differences exact to h^2
         assert abs(got - want) <= 300 * U32 * float((grad.abs() * d.abs()).sum()) + 1e-6 * (1 + abs(want)), i
+
+
+def test_differentiable_norms_of_queries_alone():
+    """Without keys the layer gives and derives the queries' part of the pair, also of two rows."""
+    g = gen(23)
+    rot = gnnk.Rotary.geometric((2, 2))
+    for n in (2, 30):
+        x, c, w = normal(g, n, 3, 8).cuda(), normal(g, n, 3, 8).cuda(), (1 + 0.2 * normal(g, 8)).cuda()
+        pos = positions(g, n, 2, "f32").cuda()
+        grads = []
+        for k in (None, x):
+            q, wq = x.clone().requires_grad_(True), w.clone().requires_grad_(True)
+            out = nn.norm_rotary(q, wq, k, None, rot=rot, pos_q=pos, pos_k=pos)
+            out = out if k is None else out[0]
+            (out * c).sum().backward()
+            grads.append((out.detach(), q.grad, wq.grad))
+        assert grads[0][0].shape == x.shape
+        for a, b in zip(*grads):
+            assert torch.equal(a, b)
+
+
+def test_second_derivatives_are_refused():
+    x = torch.randn(5, 2, 8, device="cuda", requires_grad=True)
+    pos = torch.arange(5, device="cuda", dtype=torch.int32)
+    rot = gnnk.Rotary.geometric((4,))
+    for f in (lambda: nn.rotary(rot, x, pos), lambda: nn.norm_rotary(x, rot=rot, pos_q=pos)):
+        (d,) = torch.autograd.grad((f() ** 2).sum(), x, create_graph=True)
+        with pytest.raises(RuntimeError):
+            (d ** 2).sum().backward()
 
 
 def test_replays_on_another_stream_equal_eager():
