@@ -312,6 +312,31 @@ def test_writes_only_its_columns():
     assert torch.equal(out, gnnk.dot_aggregate(gr.g, q, k, v))
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("H,K,F,shared", [(8, 2, 16, False), (6, 3, 47, True), (3, 3, 5, False)])
+def test_strided_bias_statistics_and_gradients(H, K, F, shared, dtype):
+    """Every tensor of a call in wider rows: the same values, and nothing else written."""
+    gnnk.set_option("seg_edges", 64)
+    gr = hubs()
+    g = gen(41)
+    mk = lambda n, h, f=F: torch.randn((n, h, f), generator=g).to(dtype)
+    q, k, v, z, b = mk(gr.n_dst, H), mk(gr.n_src, K), mk(gr.n_src, K), mk(gr.n_dst, H), mk(gr.e, 1 if shared else H, 1)
+    up = [t.cuda() for t in (q, k, v, z, b)]
+    out, stats = gnnk.dot_aggregate(gr.g, *up[:3], bias=up[4], want_stats=True)
+    want = gnnk.dot_aggregate_backward(gr.g, *up[:3], out, stats, up[3], bias=up[4])
+    wide = [spread(t, 5) for t in (q, k, v, z, b)]
+    bufs = [torch.full((t.shape[0], t.shape[1] * t.shape[2] + 3), 7.0, dtype=t.dtype, device="cuda")
+            for t in (out, stats, *want)]
+    view = [w[:, 1: w.shape[1] - 2].unflatten(1, t.shape[1:]) for w, t in zip(bufs, (out, stats, *want))]
+    gnnk.dot_aggregate(gr.g, *wide[:3], bias=wide[4], out=view[0], stats=view[1])
+    d = gnnk._desc
+    gnnk._run(gr.g, None, gnnk.load().dot_aggregate_backward, gr.g.handle, *(d(t) for t in wide[:3]), d(wide[4]),
+              F ** -0.5, d(view[0]), d(view[1]), d(wide[3]), *(d(t) for t in view[2:]))
+    for w, x, t in zip(bufs, view, (out, stats, *want)):
+        assert torch.equal(x, t)
+        assert bool((w[:, 0] == 7).all()) and bool((w[:, -2:] == 7).all())
+
+
 def test_refusals():
     gr = uniform()
     ones = lambda n, h, f, t=F32: torch.ones((n, h, f), dtype=t, device="cuda")
