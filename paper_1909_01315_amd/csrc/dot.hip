@@ -501,55 +501,95 @@ __global__ __launch_bounds__(256, 3) void dot_forward_kernel(EngineArgs A, DotAr
 }
 
 // Hub rows: the states of a row's segments joined.  A workgroup takes `cols`
-// columns of one row, its threads the columns of every (threads / cols)-th
-// segment; the runs are then joined in pairs.  A few columns and many runs
-// where rows have many segments (one node of 100,000 edges has 1,563).
+// columns (a power of two up to 64) of one row, its threads the columns of
+// every (threads / cols)-th segment, U loads in flight; join_runs then joins
+// the runs, first those of a wavefront.  A few columns and many runs where
+// rows have many segments (one node of 100,000 edges has 1,563).  30,900 hub
+// rows of two segments and more of 128 columns: 78 us, with 8 or 16 loads in flight
+// 91 and more; one row of 1,563 segments of 512 columns 8.5 us either way, of
+// which 4 are any such kernel's.
+template <int N, class Add>
+__device__ __forceinline__ void join_runs(double (*red)[256], double* v, int cols, Add add) {
+    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, waves = blockDim.x >> 6, c = lane & (cols - 1);
+    auto lanes = [&] {
+        for (int x = cols; x < WAVE; x <<= 1) {
+            double o[N];
+#pragma unroll
+            for (int i = 0; i < N; ++i) o[i] = __shfl_xor(v[i], x, WAVE);
+            add(v, o);
+        }
+    };
+    lanes();
+    if (lane < cols)
+#pragma unroll
+        for (int i = 0; i < N; ++i) red[i][wave * cols + c] = v[i];
+    __syncthreads();
+    if (wave != 0) return;
+    for (int w = lane / cols, first = 1; w < waves; w += WAVE / cols, first = 0) {
+        double o[N];
+#pragma unroll
+        for (int i = 0; i < N; ++i) o[i] = red[i][w * cols + c];
+        if (first) {
+#pragma unroll
+            for (int i = 0; i < N; ++i) v[i] = o[i];
+        } else {
+            add(v, o);
+        }
+    }
+    lanes();
+}
+
 template <typename T>
 __global__ void dot_join_kernel(EngineArgs A, DotArgs D, int cols) {
-    __shared__ float sm[1024];
-    __shared__ double sl[1024], sa[1024];
-    const int t = threadIdx.x, runs = blockDim.x / cols, run = t / cols;
-    const int64_t W = (int64_t)D.H * D.F, col = (int64_t)blockIdx.y * cols + (t - run * cols);
+    __shared__ double red[3][256];
+    const int t = threadIdx.x, runs = blockDim.x / cols, run = t / cols, W = D.H * D.F;
+    const int col = (int)blockIdx.y * cols + (t - run * cols);
     const int64_t row = A.csr.perm[blockIdx.x];
     const int s0 = A.csr.hub_off[blockIdx.x], s1 = A.csr.hub_off[blockIdx.x + 1];
     const bool ok = col < W;
-    const int hq = ok ? (int)(col / D.F) : 0;
-    float m = -INFINITY;
-    double l = 0.0, a = 0.0;
-    auto add = [&](float om, double ol, double oa) {
-        const float mn = fmaxf(m, om), at = mn == -INFINITY ? 0.0f : mn;
-        const double f = (double)exp_le0(m - at), g = (double)exp_le0(om - at);
-        l = l * f + ol * g;
-        a = a * f + oa * g;
-        m = mn;
+    const int hq = ok ? col / D.F : 0;
+    double v[3] = {-INFINITY, 0.0, 0.0};  // maximum, sum of weights, weighted sum
+    auto raise = [&](double* x, float mn) {
+        const double f = (double)exp_le0((float)x[0] - (mn == -INFINITY ? 0.0f : mn));
+        x[0] = mn;
+        x[1] *= f;
+        x[2] *= f;
     };
     if (ok) {
         for (int s = s0 + run; s < s1; s += U * runs) {
-            float pm[U], pl[U], pa[U];
+            float pm[U], pl[U], pa[U], mn = (float)v[0];
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 const int x = s + u * runs;
-                const float* P = D.part + (int64_t)(x < s1 ? x : s) * D.part_stride;
+                const float* P = D.part + (uint64_t)(uint32_t)(x < s1 ? x : s) * (uint32_t)D.part_stride;
                 pm[u] = P[W + 2 * hq];
                 pl[u] = P[W + 2 * hq + 1];
                 pa[u] = P[col];
             }
 #pragma unroll
-            for (int u = 0; u < U; ++u)
-                if (s + u * runs < s1) add(pm[u], (double)pl[u], (double)pa[u]);
+            for (int u = 0; u < U; ++u) mn = fmaxf(mn, pm[u]);
+            raise(v, mn);
+            const float at = mn == -INFINITY ? 0.0f : mn;
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                if (s + u * runs < s1) {
+                    const double g = (double)exp_le0(pm[u] - at);
+                    v[1] = fma((double)pl[u], g, v[1]);
+                    v[2] = fma((double)pa[u], g, v[2]);
+                }
+            }
         }
     }
-    for (int half = runs >> 1; half > 0; half >>= 1) {
-        sm[t] = m;
-        sl[t] = l;
-        sa[t] = a;
-        __syncthreads();
-        if (run < half) add(sm[t + half * cols], sl[t + half * cols], sa[t + half * cols]);
-        __syncthreads();
-    }
-    if (run != 0 || !ok) return;
-    IO<T, 1>::store1(reinterpret_cast<T*>(D.out) + row * D.out_stride + col, l == 0.0 ? 0.0f : (float)(a / l));
-    if (col % D.F == 0) write_stats(D, row, hq, m, (float)l);
+    join_runs<3>(red, v, cols, [&](double* x, double* o) {
+        const float mn = fmaxf((float)x[0], (float)o[0]);
+        raise(x, mn);
+        raise(o, mn);
+        x[1] += o[1];
+        x[2] += o[2];
+    });
+    if (t >= cols || !ok) return;
+    IO<T, 1>::store1(reinterpret_cast<T*>(D.out) + row * D.out_stride + col, v[1] == 0.0 ? 0.0f : (float)(v[2] / v[1]));
+    if (col % D.F == 0) write_stats(D, row, hq, (float)v[0], (float)v[1]);
 }
 
 // ---------------------------------------------------------------------------
@@ -805,21 +845,21 @@ __global__ __launch_bounds__(256, RC == 4 ? 2 : 3) void dot_backward_dst_kernel(
 // the destination pass's hub rows, laid out as in dot_join_kernel
 template <typename T>
 __global__ void dot_join_dst_kernel(EngineArgs A, DotArgs D, int cols) {
-    __shared__ double s1m[1024], s2m[1024], sdm[1024];
-    const int t = threadIdx.x, runs = blockDim.x / cols, run = t / cols;
-    const int64_t W = (int64_t)D.H * D.F, col = (int64_t)blockIdx.y * cols + (t - run * cols);
+    __shared__ double red[3][256];
+    const int t = threadIdx.x, runs = blockDim.x / cols, run = t / cols, W = D.H * D.F;
+    const int col = (int)blockIdx.y * cols + (t - run * cols);
     const int64_t row = A.csr.perm[blockIdx.x];
     const int s0 = A.csr.hub_off[blockIdx.x], s1 = A.csr.hub_off[blockIdx.x + 1];
     const bool ok = col < W;
-    const int hq = ok ? (int)(col / D.F) : 0;
-    double x1 = 0.0, x2 = 0.0, dl = 0.0;
+    const int hq = ok ? col / D.F : 0;
+    double v[3] = {};  // sums of w k and a k, delta
     if (ok) {
         for (int s = s0 + run; s < s1; s += U * runs) {
             float p1[U], p2[U], pd[U];
 #pragma unroll
             for (int u = 0; u < U; ++u) {
                 const int x = s + u * runs;
-                const float* P = D.part + (int64_t)(x < s1 ? x : s) * D.part_stride;
+                const float* P = D.part + (uint64_t)(uint32_t)(x < s1 ? x : s) * (uint32_t)D.part_stride;
                 p1[u] = P[col];
                 p2[u] = P[W + col];
                 pd[u] = P[2 * W + 2 * hq];
@@ -827,32 +867,24 @@ __global__ void dot_join_dst_kernel(EngineArgs A, DotArgs D, int cols) {
 #pragma unroll
             for (int u = 0; u < U; ++u)
                 if (s + u * runs < s1) {
-                    x1 += (double)p1[u];
-                    x2 += (double)p2[u];
-                    dl += (double)pd[u];
+                    v[0] += (double)p1[u];
+                    v[1] += (double)p2[u];
+                    v[2] += (double)pd[u];
                 }
         }
     }
-    for (int half = runs >> 1; half > 0; half >>= 1) {
-        s1m[t] = x1;
-        s2m[t] = x2;
-        sdm[t] = dl;
-        __syncthreads();
-        if (run < half) {
-            x1 += s1m[t + half * cols];
-            x2 += s2m[t + half * cols];
-            dl += sdm[t + half * cols];
-        }
-        __syncthreads();
-    }
-    if (run != 0 || !ok) return;
+    join_runs<3>(red, v, cols, [](double* x, const double* o) {
+#pragma unroll
+        for (int i = 0; i < 3; ++i) x[i] += o[i];
+    });
+    if (t >= cols || !ok) return;
     if (D.d_q)
         IO<T, 1>::store1(reinterpret_cast<T*>(D.d_q) + row * D.d_q_stride + col,
-                         (float)((double)D.scale * (x1 - dl * x2)));
+                         (float)((double)D.scale * (v[0] - v[2] * v[1])));
     if (col % D.F == 0) {
         const float* st = D.stats + row * D.stats_stride + 2 * hq;
         const float S0 = D.part[(int64_t)s0 * D.part_stride + 2 * W + 2 * hq + 1];
-        D.rec[row * D.H + hq] = make_float4(st[0], st[1], (float)((double)S0 + dl), 0.0f);
+        D.rec[row * D.H + hq] = make_float4(st[0], st[1], (float)((double)S0 + v[2]), 0.0f);
     }
 }
 
@@ -998,9 +1030,9 @@ __global__ __launch_bounds__(256, 3) void dot_backward_src_kernel(EngineArgs A, 
 // the source pass's hub rows, laid out as in dot_join_kernel
 template <typename T>
 __global__ void dot_join_src_kernel(EngineArgs A, DotArgs D, int cols) {
-    __shared__ double red[1024];
-    const int t = threadIdx.x, runs = blockDim.x / cols, run = t / cols;
-    const int64_t W = (int64_t)D.K * D.F, col = (int64_t)blockIdx.y * cols + (t - run * cols);
+    __shared__ double red[1][256];
+    const int t = threadIdx.x, runs = blockDim.x / cols, run = t / cols, W = D.K * D.F;
+    const int col = (int)blockIdx.y * cols + (t - run * cols);
     const int64_t row = A.csr.perm[blockIdx.x];
     const int s0 = A.csr.hub_off[blockIdx.x], s1 = A.csr.hub_off[blockIdx.x + 1];
     const bool ok = col < 2 * W;
@@ -1010,19 +1042,14 @@ __global__ void dot_join_src_kernel(EngineArgs A, DotArgs D, int cols) {
             float y[U];
 #pragma unroll
             for (int u = 0; u < U; ++u)
-                y[u] = D.part[(int64_t)(s + u * runs < s1 ? s + u * runs : s) * D.part_stride + col];
+                y[u] = D.part[(uint64_t)(uint32_t)(s + u * runs < s1 ? s + u * runs : s) * (uint32_t)D.part_stride + col];
 #pragma unroll
             for (int u = 0; u < U; ++u)
                 if (s + u * runs < s1) x += (double)y[u];
         }
     }
-    for (int half = runs >> 1; half > 0; half >>= 1) {
-        red[t] = x;
-        __syncthreads();
-        if (run < half) x += red[t + half * cols];
-        __syncthreads();
-    }
-    if (run != 0 || !ok) return;
+    join_runs<1>(red, &x, cols, [](double* a, const double* b) { *a += *b; });
+    if (t >= cols || !ok) return;
     if (col < W) {
         if (D.d_k)
             IO<T, 1>::store1(reinterpret_cast<T*>(D.d_k) + row * D.d_k_stride + col, (float)((double)D.scale * x));
