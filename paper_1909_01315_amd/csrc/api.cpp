@@ -1334,8 +1334,8 @@ namespace {
 
 constexpr int ROTARY_MAX_FEAT = 2048;
 constexpr size_t ROTARY_LDS = 32768;     // bytes of a block's cosines and sines, at most
-constexpr int ROTARY_BLOCKS = 2048;      // blocks that fill the chip: longer tiles from there on
-constexpr int ROTARY_BWD_BLOCKS = 1024;  // blocks that share a backward's rows, each leaving one partial row
+constexpr int ROTARY_BLOCKS = 4096;      // blocks that fill the chip: tiles of two steps from there on
+constexpr int ROTARY_BWD_BLOCKS = 512;   // blocks that share a backward's rows, each leaving one partial row
 
 bool rotary_ok(const gnnk_rotary* r, int64_t rows, int F) {
     if (r->rows != rows || r->axes < 1 || r->axes > 4 || (r->pos_type != GNNK_POS_F32 && r->pos_type != GNNK_POS_I32))
@@ -1387,8 +1387,13 @@ int rotary_geo(RotaryArgs& A, int F, const gnnk_rotary* rot, int dtype, bool bwd
 }
 
 // blocks of one tensor: a block's 256 / L lane groups take HB heads of RB rows
-// at once, and a tile of several such steps where the rows make more than
-// ROTARY_BLOCKS blocks (16 steps at most)
+// at once, and a tile of two such steps where the rows make more than
+// ROTARY_BLOCKS blocks.  Longer tiles share nothing more and leave fewer loads
+// in flight around the angles: 262,144 rows of 16 heads of 128 bf16 turned in
+// tiles of 2 / 4 / 16 steps 365 / 375 / 431 us, in tiles of one 400; 50,176
+// rows of 8 heads of 32 fp32, both directions, 50 us in tiles of two, 54 of
+// one or four.  The backward of 20,011 rows of 6 and 3 heads of 47 bf16 by
+// 256 / 512 / 1,024 / 2,048 blocks: 58 / 37 / 41 / 52 us.
 void rotary_blocks(const RotaryArgs& A, RotarySide& S, bool bwd) {
     const int groups = 256 / A.L;
     S.HB = std::min(S.H, groups);
@@ -1396,7 +1401,7 @@ void rotary_blocks(const RotaryArgs& A, RotarySide& S, bool bwd) {
     S.RB = groups / S.HB;
     const int most = A.P > 0 ? (int)(ROTARY_LDS / 8) / A.P : 1 << 20;  // rows whose angles fit
     S.RB = std::max(1, std::min(S.RB, most));
-    const int64_t steps = std::min<int64_t>(16, std::max<int64_t>(1, S.n * S.hblocks * A.nchunk / (ROTARY_BLOCKS * S.RB)));
+    const int64_t steps = S.n * S.hblocks * A.nchunk > (int64_t)ROTARY_BLOCKS * S.RB ? 2 : 1;
     S.tile_rows = S.RB * (int)std::min<int64_t>(steps, std::max(1, most / S.RB));
     const int64_t tiles = (S.n + S.tile_rows - 1) / S.tile_rows;
     S.row_blocks = (int32_t)std::min<int64_t>(tiles, bwd ? ROTARY_BWD_BLOCKS : (1 << 20) / (S.hblocks * A.nchunk));

@@ -17,12 +17,13 @@
 // divides neither, the last lane of either kind reads whole vectors all the
 // same, past its columns, and leaves the others alone.
 //
-// It is bound by the copy rate (about 5 TB/s from 256 MiB on): 262,144 rows of
-// 16 heads of 128 bf16 turned in 432 us (5.0 TB/s; stores that bypass the
-// caches 575), 8 and 8 heads of 32 fp32 normed and turned in 218 (4.9), their
-// backward in 335 and 9 for the blocks' weight gradients (4.7).  Odd widths
-// are bound by instructions and a small call's latency: 20,011 rows of 6 and 3
-// heads of 47 bf16 23 us, backward 35 and 6.  One row: 4 us.
+// It is bound by the memory's streaming rate: 262,144 rows of 16 heads of 128
+// bf16 turned in 365 us (5.9 TB/s read and written; a plain copy reaches 5.1;
+// stores that bypass the caches take a third more), 8 and 8 heads of 32 fp32
+// normed and turned in 184 (5.8), their backward in 309 and 5 for the blocks'
+// weight gradients (5.1).  Odd widths are bound by instructions and a small
+// call's latency: 20,011 rows of 6 and 3 heads of 47 bf16 23 us, backward 33
+// and 4.  One row: 4 us.
 //
 // Angles are products in fp64, reduced to turns there (a position of 10^6 at
 // frequency 1 keeps its angle to 10^-10), and their sines and cosines fp32.
