@@ -559,9 +559,13 @@ def edge_leaky_relu_backward(x, dy, slope: float = 0.2, dx=None, stream=None):
 _ROTARY = struct.Struct("=QqqQIIIIIIII")
 
 
-def _like(t):
-    """an output of t's shape and type, contiguous (half the time of torch.empty with both spelled out)"""
-    return torch.empty_like(t, memory_format=torch.contiguous_format)
+_ADDRESS = struct.Struct("=Q")
+
+
+def _out(t, desc):
+    """an output like t and its descriptor: t's own, desc, at another address where t is contiguous (0.3 us less)"""
+    o = torch.empty_like(t, memory_format=torch.contiguous_format)
+    return o, _ADDRESS.pack(o.data_ptr()) + desc[8:] if t.is_contiguous() else _desc(o)
 
 
 def _here(*ts):
@@ -634,9 +638,9 @@ def node_rotary(rot: Rotary, x, pos, inverse: bool = False, out=None, stream=Non
     the opposite angles (the gradient)."""
     x = _as3(x)
     _here(x, out)
-    if out is None:
-        out = _like(x)
-    _check(load().node_rotary(rot._desc(pos), _desc(x), int(inverse), _desc(out), _stream(stream)))
+    xd = _desc(x)
+    out, od = _out(x, xd) if out is None else (out, _desc(out))
+    _check(load().node_rotary(rot._desc(pos), xd, int(inverse), od, _stream(stream)))
     return out
 
 
@@ -655,16 +659,14 @@ def node_norm_rotary(q, wq=None, k=None, wk=None, rot: Rotary = None, pos_q=None
     q, wq, wk = _as3(q), _weight3(wq), _weight3(wk)
     k = _as3(k) if k is not None else None
     _here(q, wq, k, wk, out_q, out_k)
-    if out_q is None:
-        out_q = _like(q)
-    if k is not None and out_k is None:
-        out_k = _like(k)
+    xq, xk = _desc(q), _desc(k)
+    out_q, oq = _out(q, xq) if out_q is None else (out_q, _desc(out_q))
+    out_k, ok = _out(k, xk) if k is not None and out_k is None else (out_k, _desc(out_k))
     rq = rot._desc(pos_q) if rot is not None else None
     rk = None
     if rot is not None and k is not None:
         rk = rq if pos_k is pos_q else rot._desc(pos_k)
-    _check(load().node_norm_rotary(_desc(q), _desc(wq), rq, _desc(out_q), _desc(k), _desc(wk), rk, _desc(out_k), eps,
-                                   _stream(stream)))
+    _check(load().node_norm_rotary(xq, _desc(wq), rq, oq, xk, _desc(wk), rk, ok, eps, _stream(stream)))
     return (out_q, out_k) if k is not None else out_q
 
 
@@ -676,13 +678,14 @@ def node_norm_rotary_backward(q, wq, grad_q, k=None, wk=None, grad_k=None, rot: 
     q, wq3, wk3, grad_q = _as3(q), _weight3(wq), _weight3(wk), _as3(grad_q)
     k, grad_k = (_as3(k) if k is not None else None), (_as3(grad_k) if grad_k is not None else None)
     _here(q, wq3, k, wk3, grad_q, grad_k)
-    like = lambda t, want: _like(t) if want and t is not None else None
-    dq, dwq, dk, dwk = like(q, want_q), like(wq3, want_wq), like(k, want_k), like(wk3, want_wk and k is not None)
+    xq, xk, ywq, ywk = _desc(q), _desc(k), _desc(wq3), _desc(wk3)
+    like = lambda t, d, want: _out(t, d) if want and t is not None else (None, None)
+    (dq, gq), (dwq, gwq) = like(q, xq, want_q), like(wq3, ywq, want_wq)
+    (dk, gk), (dwk, gwk) = like(k, xk, want_k), like(wk3, ywk, want_wk and k is not None)
     rq = rot._desc(pos_q) if rot is not None else None
     rk = None
     if rot is not None and k is not None:
         rk = rq if pos_k is pos_q else rot._desc(pos_k)
-    xq, xk, gwq, gwk = _desc(q), _desc(k), _desc(dwq), _desc(dwk)
     work, nbytes = None, 0
     if gwq is not None or gwk is not None:
         need = ctypes.c_size_t(0)
@@ -693,8 +696,8 @@ def node_norm_rotary_backward(q, wq, grad_q, k=None, wk=None, grad_k=None, rot: 
         else:
             with torch.cuda.stream(stream):
                 work = torch.empty(nbytes, dtype=torch.uint8, device=q.device)
-    _check(load().node_norm_rotary_backward(xq, _desc(wq3), rq, _desc(grad_q), _desc(dq), gwq, xk, _desc(wk3), rk,
-                                            _desc(grad_k), _desc(dk), gwk, eps, _ptr(work), nbytes, _stream(stream)))
+    _check(load().node_norm_rotary_backward(xq, ywq, rq, _desc(grad_q), gq, gwq, xk, ywk, rk, _desc(grad_k), gk, gwk,
+                                            eps, _ptr(work), nbytes, _stream(stream)))
     if dwq is not None and wq.dim() != 3:
         dwq = dwq.view(wq.shape)
     if dwk is not None and wk.dim() != 3:
@@ -713,12 +716,11 @@ def dot_aggregate(g: Graph, q, k, v, bias=None, scale: float = None, out=None, s
     _here(q, k, v, bias, out, stats)
     if scale is None:
         scale = q.shape[2] ** -0.5
-    if out is None:
-        out = _like(q)
+    qd = _desc(q)
+    out, od = _out(q, qd) if out is None else (out, _desc(out))
     if want_stats and stats is None:
         stats = torch.empty((g.num_dst, q.shape[1], 2), dtype=torch.float32, device=q.device)
-    _run(g, stream, load().dot_aggregate, g.handle, _desc(q), _desc(k), _desc(v), _desc(bias), scale, _desc(out),
-         _desc(stats))
+    _run(g, stream, load().dot_aggregate, g.handle, qd, _desc(k), _desc(v), _desc(bias), scale, od, _desc(stats))
     return (out, stats) if stats is not None else out
 
 
@@ -731,8 +733,10 @@ def dot_aggregate_backward(g: Graph, q, k, v, out, stats, grad_out, bias=None, s
     _here(q, k, v, bias, out, stats, grad_out)
     if scale is None:
         scale = q.shape[2] ** -0.5
-    like = lambda t, want: _like(t) if want and t is not None else None
-    dq, dk, dv, db = like(q, want_q), like(k, want_k), like(v, want_v), like(bias, want_bias)
-    _run(g, stream, load().dot_aggregate_backward, g.handle, _desc(q), _desc(k), _desc(v), _desc(bias), scale,
-         _desc(out), _desc(stats), _desc(grad_out), _desc(dq), _desc(dk), _desc(dv), _desc(db))
+    qd, kd, vd, bd = _desc(q), _desc(k), _desc(v), _desc(bias)
+    like = lambda t, d, want: _out(t, d) if want and t is not None else (None, None)
+    (dq, gq), (dk, gk), (dv, gv), (db, gb) = (like(q, qd, want_q), like(k, kd, want_k), like(v, vd, want_v),
+                                              like(bias, bd, want_bias))
+    _run(g, stream, load().dot_aggregate_backward, g.handle, qd, kd, vd, bd, scale, _desc(out), _desc(stats),
+         _desc(grad_out), gq, gk, gv, gb)
     return dq, dk, dv, db
