@@ -270,9 +270,15 @@ gnnk_status graph_scratch_bytes(gnnk_graph_t g, int64_t max_cols, int32_t flags,
  * buf == NULL or bytes == 0 takes the stream's buffer back.  Host-side only:
  * no GPU work.  The caller keeps the buffer alive, unchanged by other work,
  * until the calls queued on `stream` with it have finished (releasing it to
- * an allocator ordered on that stream is enough).  At most 16 streams per
- * handle (GNNK_EINVAL beyond). */
+ * an allocator ordered on that stream is enough), and, where calls with it
+ * were captured into a HIP graph, as long as that graph is launched.  At most
+ * 16 streams per handle (GNNK_EINVAL beyond). */
 gnnk_status graph_attach_scratch(gnnk_graph_t g, hipStream_t stream, void* buf, size_t bytes);
+
+/* *captured = 1 if a call that was captured into a HIP graph took the buffer
+ * attached for `stream` (since it was attached; attached again with another
+ * size it is the same buffer), so that the graph holds its address; else 0. */
+gnnk_status graph_scratch_captured(gnnk_graph_t g, hipStream_t stream, int32_t* captured);
 
 /* Bytes of scratch the last call on this thread that returned GNNK_ENOMEM for
  * lack of scratch asked for (0 after any other outcome): the whole call's

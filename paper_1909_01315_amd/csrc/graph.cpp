@@ -93,6 +93,17 @@ void* Scratch::take(size_t n) {
     return base + at;
 }
 
+// whether s is being captured into a graph (the null stream never is)
+static bool capturing(hipStream_t s) {
+    hipStreamCaptureStatus st = hipStreamCaptureStatusNone;
+    if (!s) return false;
+    if (hipStreamIsCapturing(s, &st) != hipSuccess) {
+        (void)hipGetLastError();  // (not the launch's error)
+        return true;
+    }
+    return st != hipStreamCaptureStatusNone;
+}
+
 Scratch scratch_of(gnnk_graph* g, hipStream_t s) {
     Scratch sc;
     if (g_plan) {
@@ -106,6 +117,7 @@ Scratch scratch_of(gnnk_graph* g, hipStream_t s) {
         if (g->lent[k].stream == s) {
             sc.base = g->lent[k].buf;
             sc.bytes = g->lent[k].bytes;
+            if (capturing(s)) g->lent[k].captured = true;
         }
     return sc;
 }
@@ -908,9 +920,20 @@ gnnk_status graph_attach_scratch(gnnk_graph_t g, hipStream_t stream, void* buf, 
     if (k == g->n_lent) {
         if (g->n_lent == gnnk_graph::MAX_STREAMS)
             return fail(GNNK_EINVAL, "a handle takes scratch for at most %d streams", gnnk_graph::MAX_STREAMS);
-        ++g->n_lent;
+        g->lent[g->n_lent++] = {stream, nullptr, 0, false};
     }
-    g->lent[k] = {stream, reinterpret_cast<char*>(buf), bytes};
+    char* b = reinterpret_cast<char*>(buf);
+    g->lent[k] = {stream, b, bytes, g->lent[k].buf == b && g->lent[k].captured};
+    return GNNK_OK;
+}
+
+gnnk_status graph_scratch_captured(gnnk_graph_t g, hipStream_t stream, int32_t* captured) {
+    clear_error();
+    if (!g || !captured) return fail(GNNK_EINVAL, "NULL argument");
+    *captured = 0;
+    std::lock_guard<std::mutex> lk(g->lent_mu);
+    for (int k = 0; k < g->n_lent; ++k)
+        if (g->lent[k].stream == stream) *captured = g->lent[k].captured;
     return GNNK_OK;
 }
 

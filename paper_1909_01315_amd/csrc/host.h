@@ -69,6 +69,7 @@ struct gnnk_graph {
         hipStream_t stream;
         char* buf;
         size_t bytes;
+        bool captured;  // a captured call has taken it
     };
     Lent lent[MAX_STREAMS];
     int n_lent = 0;

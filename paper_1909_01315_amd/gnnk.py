@@ -126,6 +126,7 @@ SYMBOLS = {
     "node_norm_rotary_work_bytes": [ctypes.c_void_p] * 5,
     "graph_scratch_bytes": [ctypes.c_void_p, ctypes.c_int64, ctypes.c_int32, ctypes.c_void_p],
     "graph_attach_scratch": [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_size_t],
+    "graph_scratch_captured": [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p],
     "gnnk_scratch_needed": [ctypes.c_void_p],
     "gnnk_set_option": [ctypes.c_char_p, ctypes.c_int64],
     "gnnk_last_error": [],
@@ -248,7 +249,7 @@ class Graph:
         self._h = handle
         self._keep = keep  # tensors the handle points into
         self._lent = {}    # stream handle -> scratch buffer lent for that stream
-        self._replaced = []  # smaller ones lent before
+        self._replaced = []  # smaller ones lent before, which captured graphs hold
         self.num_src, self.num_dst, self.num_edges = num_src, num_dst, num_edges
 
     @property
@@ -264,18 +265,25 @@ class Graph:
 
     def lend_scratch(self, nbytes: int, stream=None):
         """Lend the handle a scratch buffer of at least nbytes for the calls on
-        `stream` (default: the current stream), allocated on that stream.  A
-        buffer that it replaces stays with the handle: a captured graph holds
-        its address (each is at least twice as large as the one before, so all
-        of them together take less than twice the last one).  Graphs captured
-        on one stream share its buffer: their replays must not overlap."""
+        `stream` (default: the current stream), allocated on that stream,
+        unless the one it has is large enough.  The buffer it replaces goes
+        back to torch's allocator, which reuses it only for work ordered after
+        the calls already queued on that stream; one that a captured call has
+        taken stays with the handle, since the graph holds its address.
+        Graphs captured on one stream share its buffer: their replays must not
+        overlap."""
         s = stream if stream is not None else torch.cuda.current_stream()
         old = self._lent.get(s.cuda_stream)
-        size = max(int(nbytes), 2 * old.numel() if old is not None else 0, 256)
+        if old is not None and old.numel() >= nbytes:
+            _check(load().graph_attach_scratch(self.handle, s.cuda_stream, old.data_ptr(), old.numel()))
+            return
+        captured = ctypes.c_int32(0)
+        _check(load().graph_scratch_captured(self.handle, s.cuda_stream, ctypes.byref(captured)))
+        size = max(int(nbytes), old.numel() * 5 // 4 if old is not None else 0, 256)
         with torch.cuda.stream(s):
             buf = torch.empty(size, dtype=torch.uint8, device=self.device)
         _check(load().graph_attach_scratch(self.handle, s.cuda_stream, buf.data_ptr(), size))
-        if old is not None:
+        if captured.value and old is not None:
             self._replaced.append(old)
         self._lent[s.cuda_stream] = buf
 
