@@ -28,7 +28,8 @@
  *    stream (graph_attach_scratch).  A sequence of compute calls can
  *    therefore be captured into a HIP graph as it is.
  *  - Outputs are fully overwritten, never accumulated into.  Inputs may alias
- *    each other; outputs must not alias inputs or each other.
+ *    each other; outputs must not alias inputs or each other (but for
+ *    node_rotary and node_norm_rotary in place).
  *  - Edge tensors are indexed by edge id.  Node tensors by node id.
  *  - Index ranges are not checked on the compute path; use graph_validate.
  *  - All floating-point tensors of one call share one dtype.  Sums and dot
@@ -490,8 +491,9 @@ typedef struct {
 
 /* out = x with its pairs turned by their angles (inverse != 0: by the
  * opposite angles, which is also the gradient).  x and out: (rows, H, F), fewer
- * than 2^31 rows of at most 1,024 heads of at most 2,048 columns.  Errors:
- * GNNK_EINVAL on shapes, pairs or dtypes. */
+ * than 2^31 rows of at most 1,024 heads of at most 2,048 columns; out may be x
+ * itself (the same rows at the same address).  Errors: GNNK_EINVAL on shapes,
+ * pairs or dtypes, or if out overlaps an operand otherwise. */
 gnnk_status node_rotary(const gnnk_rotary* rot, const gnnk_tensor* x, int32_t inverse, gnnk_tensor* out,
                         hipStream_t stream);
 
@@ -503,7 +505,9 @@ gnnk_status node_rotary(const gnnk_rotary* rot, const gnnk_tensor* x, int32_t in
  * other rows and heads but the same F.  rot_q / rot_k (nullable, both or
  * neither: no rotation) have q's and k's rows and the same pairs and layout.
  * The sum of a head's squares is fp32.  Sizes as in node_rotary, eps >= 0.
- * Errors: GNNK_EINVAL. */
+ * out_q may be q itself and out_k k in heads that one wavefront holds (always
+ * up to 256 columns in fp32, 512 in bf16).  Errors: GNNK_EINVAL, also if an
+ * output overlaps an operand or the other one otherwise. */
 gnnk_status node_norm_rotary(const gnnk_tensor* q, const gnnk_tensor* wq, const gnnk_rotary* rot_q,
                              gnnk_tensor* out_q, const gnnk_tensor* k, const gnnk_tensor* wk,
                              const gnnk_rotary* rot_k, gnnk_tensor* out_k, float eps, hipStream_t stream);
@@ -517,7 +521,10 @@ gnnk_status node_norm_rotary(const gnnk_tensor* q, const gnnk_tensor* wq, const 
  * (with k) grad_out_k are required.  work: device memory of at least
  * node_norm_rotary_work_bytes bytes, 256-byte aligned, for calls that ask for
  * a weight gradient (else it may be NULL); it need not be initialised and is
- * the caller's again once the work queued on `stream` is done. */
+ * the caller's again once the work queued on `stream` is done.  grad_q may be
+ * q or grad_out_q itself, and grad_k k or grad_out_k, in heads of up to 256
+ * columns; no output may overlap an operand or another output otherwise
+ * (GNNK_EINVAL). */
 gnnk_status node_norm_rotary_backward(const gnnk_tensor* q, const gnnk_tensor* wq, const gnnk_rotary* rot_q,
                                       const gnnk_tensor* grad_out_q, gnnk_tensor* grad_q, gnnk_tensor* grad_wq,
                                       const gnnk_tensor* k, const gnnk_tensor* wk, const gnnk_rotary* rot_k,

@@ -1439,6 +1439,40 @@ bool rotary_size_ok(const gnnk_tensor* x) {
     return x->rows < ((int64_t)1 << 31) && x->heads <= 1024 && x->feat <= ROTARY_MAX_FEAT;
 }
 
+// the bytes of a tensor, or of positions and frequencies
+struct Span {
+    uintptr_t at = 0;
+    int64_t rows = 0, stride = 0, width = 0;
+};
+Span span(const gnnk_tensor* t) {
+    if (!t) return Span{};
+    const int64_t es = t->dtype == GNNK_BF16 ? 2 : 4, width = (int64_t)t->heads * t->feat;
+    return Span{(uintptr_t)t->data, t->rows, t->row_stride * es, width * es};
+}
+Span pos_span(const gnnk_rotary* r) {
+    return r ? Span{(uintptr_t)r->pos, r->rows, r->pos_stride * 4, r->axes * 4ll} : Span{};
+}
+Span freq_span(const gnnk_rotary* r) {
+    if (!r) return Span{};
+    int64_t P = 0;
+    for (int a = 0; a < r->axes; ++a) P += r->pairs[a];
+    return Span{(uintptr_t)r->freq, 1, P * 4, P * 4};
+}
+bool same_span(const Span& a, const Span& b) {
+    return a.at == b.at && a.rows == b.rows && a.width == b.width && (a.rows <= 1 || a.stride == b.stride);
+}
+// whether two may share a byte: no if their extents are apart, or if rows of
+// one stride take columns apart from each other
+bool overlap(const Span& a, const Span& b) {
+    if (!a.rows || !b.rows) return false;
+    auto end = [](const Span& s) { return s.at + (uintptr_t)((s.rows - 1) * s.stride + s.width); };
+    if (end(a) <= b.at || end(b) <= a.at) return false;
+    if (a.rows > 1 && b.rows > 1 && a.stride != b.stride) return true;
+    const int64_t stride = a.rows > 1 ? a.stride : b.stride;
+    const int64_t apart = ((int64_t)(b.at - a.at) % stride + stride) % stride;  // columns from a's row to b's
+    return apart < a.width || apart + b.width > stride;
+}
+
 struct NormSide {
     const gnnk_tensor *x, *w;
     const gnnk_rotary* rot;
@@ -1460,6 +1494,34 @@ gnnk_status norm_check(const NormSide& s, bool bwd, const char* name) {
     if (!rotary_size_ok(s.x))
         return fail(GNNK_EINVAL, "%s: fewer than 2^31 rows, at most 1024 heads of at most %d columns", name,
                     ROTARY_MAX_FEAT);
+    return GNNK_OK;
+}
+
+// No output may overlap what the call reads or another output; an output that
+// is its own side's x (backward: or the gradient of its output) in place is
+// written after the heads' own lanes have read it, unless a head takes several
+// blocks, which read each other's columns.
+gnnk_status norm_overlap_check(const NormSide* sides, int n, bool one_pass) {
+    Span outs[4];
+    int made = 0;
+    for (int i = 0; i < n; ++i) {
+        const NormSide& s = sides[i];
+        const Span out = span(s.out), dw = span(s.dw);
+        for (int j = 0; j < n; ++j) {
+            const NormSide& o = sides[j];
+            for (const Span& in : {span(o.x), span(o.g)}) {
+                if (overlap(dw, in) || (overlap(out, in) && !(i == j && one_pass && same_span(out, in))))
+                    return fail(GNNK_EINVAL, "an output overlaps an operand (in place: only in heads of one pass)");
+            }
+            for (const Span& in : {span(o.w), pos_span(o.rot), freq_span(o.rot)})
+                if (overlap(dw, in) || overlap(out, in)) return fail(GNNK_EINVAL, "an output overlaps an operand");
+        }
+        for (const Span& x : {out, dw}) {
+            for (int y = 0; y < made; ++y)
+                if (overlap(x, outs[y])) return fail(GNNK_EINVAL, "two outputs overlap");
+            outs[made++] = x;
+        }
+    }
     return GNNK_OK;
 }
 
@@ -1528,6 +1590,10 @@ gnnk_status node_rotary(const gnnk_rotary* rot, const gnnk_tensor* x, int32_t in
         return fail(GNNK_EINVAL, "positions: x's rows, 1 to 4 axes, and at least one pair within the head");
     if (!rotary_size_ok(x))
         return fail(GNNK_EINVAL, "fewer than 2^31 rows, at most 1024 heads of at most %d columns", ROTARY_MAX_FEAT);
+    // (in place: a lane reads its columns of a row before it writes them)
+    const Span o = span(out);
+    if ((overlap(o, span(x)) && !same_span(o, span(x))) || overlap(o, pos_span(rot)) || overlap(o, freq_span(rot)))
+        return fail(GNNK_EINVAL, "out overlaps an operand");
     if (x->rows == 0) return GNNK_OK;
     RotaryArgs A{};
     const int V = rotary_geo(A, x->feat, rot, dtype_code(x), false);
@@ -1556,6 +1622,8 @@ gnnk_status node_norm_rotary(const gnnk_tensor* q, const gnnk_tensor* wq, const 
     RotaryArgs A{};
     size_t bytes;
     const int V = norm_args(sides, n, eps, false, A, bytes);
+    st = norm_overlap_check(sides, n, A.nchunk == 1);
+    if (st != GNNK_OK) return st;
     return launch_status(launch_node_rotary(A, dtype_code(q), V, 1, rotary_lds(A, V, false), stream),
                          "norm and rotary launch");
 }
@@ -1576,6 +1644,8 @@ gnnk_status node_norm_rotary_backward(const gnnk_tensor* q, const gnnk_tensor* w
     if (bytes > 0 && (!work || work_bytes < bytes))
         return fail(GNNK_ENOMEM, "the weight gradients need %zu bytes of work, %zu given", bytes, work ? work_bytes : 0);
     if (bytes > 0 && ((uintptr_t)work & 255)) return fail(GNNK_EINVAL, "work must be 256-byte aligned");
+    st = norm_overlap_check(sides, n, A.nchunk == 1);
+    if (st != GNNK_OK) return st;
     char* p = static_cast<char*>(work);
     for (int i = 0; i < n; ++i) {
         RotarySide& S = A.side[i];

@@ -8,7 +8,8 @@ loaded, every call raises.
 
 Tensors are torch tensors on the GPU, float32 or bfloat16, shaped (rows, heads,
 feat) -- a 2-D (rows, d) tensor is read as (rows, 1, d) -- with the last two
-dimensions contiguous (the row stride may be larger).
+dimensions contiguous (the row stride may be larger).  Outputs that are passed
+in must not overlap what a call reads or each other, unless it says so.
 """
 from __future__ import annotations
 
@@ -643,7 +644,7 @@ class Rotary:
 
 def node_rotary(rot: Rotary, x, pos, inverse: bool = False, out=None, stream=None):
     """x (rows, H, F) with its pairs of columns turned by the angles of pos (rows, axes), float32 or int32; inverse: by
-    the opposite angles (the gradient)."""
+    the opposite angles (the gradient).  out may be x itself."""
     x = _as3(x)
     _here(x, out)
     xd = _desc(x)
@@ -663,7 +664,7 @@ def node_norm_rotary(q, wq=None, k=None, wk=None, rot: Rotary = None, pos_q=None
                      out_q=None, out_k=None, stream=None):
     """Each head of q (rows, H, F) divided by its root mean square, times wq ((F,), (H, F) or None), then turned by
     rot (None: not turned) at pos_q; the same of k, with wk and pos_k, in the same launch.  Returns out_q, or
-    (out_q, out_k) with k."""
+    (out_q, out_k) with k.  out_q may be q itself and out_k k in heads of up to 256 columns (bf16: 512)."""
     q, wq, wk = _as3(q), _weight3(wq), _weight3(wk)
     k = _as3(k) if k is not None else None
     _here(q, wq, k, wk, out_q, out_k)
