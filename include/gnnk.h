@@ -564,8 +564,8 @@ gnnk_status node_norm_rotary_work_bytes(const gnnk_tensor* q, const gnnk_tensor*
  *   "small_deg"   rows of at most this many edges take one lane group each
  *                 and share a wavefront (-1 = auto: 32, or the lane groups
  *                 per wavefront if more; none when a wavefront is one group;
- *                 dot_aggregate: 8 in place of 32 on graphs whose wavefronts
- *                 all run at once)
+ *                 dot_aggregate: 8 in place of 32 where the wavefronts that
+ *                 this makes all run at once)
  *   "schedule"    0 auto (the row engine), 1 the row engine (node-parallel over the degree-
  *                 sorted rows), 2 the edge-parallel walk over the COO form
  *                 (equal edges per lane group; split rows combined in a fixed

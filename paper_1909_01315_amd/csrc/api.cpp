@@ -1798,11 +1798,27 @@ void dot_walk(const gnnk_graph* g, const Dir& d, const DotCall& c, const gnnk_te
     A.csr = csr_of(g, d, ids);
     set_geo(A, c.geo);
     A.sch = schedule(d, c.geo, true);
-    // where all wavefronts run at once, the longest lane group's row is what
-    // takes time: a wavefront each for rows of more than 8 edges (20,000 rows,
-    // 109,170 edges, 8 heads of 8 fp32: 12.6 -> 11.5 us a pass; 262,144 rows
-    // of 32 edges, 8 and 2 heads of 32 bf16, forward 366 -> 755)
-    if (A.sch.w_small_end < 8192) A.sch = schedule(d, c.geo, true, -1, 8);
+    // Where all wavefronts run at once, the longest lane group's row is what
+    // takes time, so rows of more than 8 edges take a wavefront each, as long
+    // as the kernels hold all the wavefronts that makes: four a SIMD, two where
+    // a lane takes four query heads (up to twice as many where they are little
+    // more than the lane groups').  Beyond that a wavefront for a row wastes
+    // most of its slots.  Lane groups -> wavefronts, us, forward and backward:
+    //   8 and 2 heads of 32 bf16, rows of 16 edges: 1,000 rows 7.4 -> 7.3 and
+    //     21 -> 18; 4,000 7.7 -> 12.9 and 25 -> 33; 32,000 24 -> 67, 112 -> 198
+    //   the same, rows of 32: 2,000 rows 10.7 -> 8.8 and 28 -> 23; 4,000 11.8
+    //     -> 13.3 and 35 -> 38; 16,000 19 -> 38 and 96 -> 131
+    //   8 heads of 8 fp32, rows of 16: 4,000 rows 5.7 -> 5.5 and 17.1 -> 14.7;
+    //     8,000 7.7 -> 8.9 and 21 -> 27; rows of 32: 4,000 7.6 -> 6.8 and 23 ->
+    //     18, 8,000 10.5 -> 11.6 and 31 -> 32
+    //   the same, lengths by a power law, 4 a row on average, the wavefronts a
+    //     fifth more: 20,000 rows 15.2 -> 14.0 and 29.7 -> 28.5
+    // Over 448 graphs of 1,000 to 130,000 rows the choice takes 0.4% more than
+    // the better form of each, 17% at worst.
+    const SchedDev by_waves = schedule(d, c.geo, true, -1, 8);
+    const int64_t held = 1024 * (c.D.RC == 4 ? 2 : 4);
+    const int64_t waves = (int64_t)by_waves.w_small_end * c.D.slices, groups = (int64_t)A.sch.w_small_end * c.D.slices;
+    if (waves <= held || (waves <= 2 * held && 2 * waves <= 3 * groups)) A.sch = by_waves;
 }
 
 }  // namespace
