@@ -7,7 +7,8 @@
 // sum of the softmax, so no score is written.  An edge gathers one row of keys
 // and one of values; a lane holds VEC columns of a key head, the vectors of a
 // head in a power of two of neighbouring lanes, so that a head's dot product
-// is one shuffle-free reduction and every lane of the head gets it.  Heads
+// is one reduction over them (cross-lane moves up to 16 lanes, shuffles beyond)
+// and every lane of the head gets it.  Heads
 // beyond one wavefront's lanes are slices of the grid.  Of the R query heads
 // that share a key head, a lane takes RC at once in registers (each key and
 // value row is then gathered and widened once for them), RL neighbouring runs

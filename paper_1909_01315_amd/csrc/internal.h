@@ -241,7 +241,7 @@ hipError_t launch_gat_backward(const EngineArgs& ain, const EngineArgs& aout, co
                                int gc, hipStream_t s);
 // dot-product attention, dot.hip: A walks the in-CSR (a = k, b = v at the
 // neighbour; the forward, pass 1 and pass 3) or the reverse graph's CSR (a =
-// q, b = dout at the neighbour, x2 = rec; pass 2)
+// q, b = dout at the neighbour, with the neighbour's rec; pass 2)
 struct DotArgs {
     const void* q;           // (N_dst, H, F) T
     int64_t q_stride;

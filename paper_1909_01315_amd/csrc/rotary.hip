@@ -393,8 +393,10 @@ void launch_v(const RotaryArgs& a, size_t lds, hipStream_t s) {
 
 template <typename T, int MODE>
 void launch_mode(const RotaryArgs& a, int vec, size_t lds, hipStream_t s) {
-    if (sizeof(T) == 2 && vec == 8) launch_v<T, sizeof(T) == 2 ? 8 : 4, MODE>(a, lds, s);
-    else if (vec == 4) launch_v<T, 4, MODE>(a, lds, s);
+    // (eight columns: bf16 forward only, see rotary_geo)
+    if constexpr (sizeof(T) == 2 && MODE != NORM_BWD)
+        if (vec == 8) return launch_v<T, 8, MODE>(a, lds, s);
+    if (vec == 4) launch_v<T, 4, MODE>(a, lds, s);
     else if (vec == 2) launch_v<T, 2, MODE>(a, lds, s);
     else launch_v<T, 1, MODE>(a, lds, s);
 }
