@@ -585,7 +585,7 @@ def _here(*ts):
             if cur < 0:
                 cur = _device() if _device is not None else torch.cuda.current_device()
             if t.get_device() != cur:
-                raise ValueError(f"a tensor is on cuda:{t.get_device()}, the current device is cuda:{cur}")
+                raise ValueError(f"a tensor or graph is on cuda:{t.get_device()}, the current device is cuda:{cur}")
 
 
 class Rotary:
@@ -722,7 +722,7 @@ def dot_aggregate(g: Graph, q, k, v, bias=None, scale: float = None, out=None, s
     given) followed by the per-row statistics (num_dst, H, 2) fp32 that dot_aggregate_backward takes."""
     q, k, v = _as3(q), _as3(k), _as3(v)
     bias = _as3(bias) if bias is not None else None
-    _here(q, k, v, bias, out, stats)
+    _here(g._keep[0] if g._keep else None, q, k, v, bias, out, stats)
     if scale is None:
         scale = q.shape[2] ** -0.5
     qd = _desc(q)
@@ -739,7 +739,7 @@ def dot_aggregate_backward(g: Graph, q, k, v, out, stats, grad_out, bias=None, s
     """(dq, dk, dv, dbias) of dot_aggregate from its output and statistics (None where not wanted, or without bias)."""
     q, k, v, out, grad_out = _as3(q), _as3(k), _as3(v), _as3(out), _as3(grad_out)
     bias = _as3(bias) if bias is not None else None
-    _here(q, k, v, bias, out, stats, grad_out)
+    _here(g._keep[0] if g._keep else None, q, k, v, bias, out, stats, grad_out)
     if scale is None:
         scale = q.shape[2] ** -0.5
     qd, kd, vd, bd = _desc(q), _desc(k), _desc(v), _desc(bias)
