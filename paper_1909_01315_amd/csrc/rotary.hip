@@ -26,7 +26,9 @@
 // and 4.  One row: 4 us.
 //
 // Angles are products in fp64, reduced to turns there (a position of 10^6 at
-// frequency 1 keeps its angle to 10^-10), and their sines and cosines fp32.
+// frequency 1 keeps its angle to 10^-10), and their sines and cosines fp32, of
+// the angle in half turns rounded to fp32 (which moves them by at most 2^-23,
+// beside 2^-22 of their own).
 // Sums over a head (at most 2,048 columns) are fp32, weight gradients, sums
 // over all rows, fp64.
 #include "words.h"
