@@ -1802,8 +1802,9 @@ void dot_walk(const gnnk_graph* g, const Dir& d, const DotCall& c, const gnnk_te
     // takes time, so rows of more than 8 edges take a wavefront each, as long
     // as the kernels hold about all the wavefronts that makes: four a SIMD (3 to
     // 6 by their registers), two where a lane takes four query heads (2 or 3);
-    // up to twice as many where they are little more than the lane groups'.  Beyond that a wavefront for a row wastes
-    // most of its slots.  Lane groups -> wavefronts, us, forward and backward:
+    // up to twice as many where they are little more than the lane groups'.
+    // Beyond that a wavefront for a row wastes most of its slots.  Lane groups
+    // -> wavefronts, us, forward and backward:
     //   8 and 2 heads of 32 bf16, rows of 16 edges: 1,000 rows 7.4 -> 7.3 and
     //     21 -> 18; 4,000 7.7 -> 12.9 and 25 -> 33; 32,000 24 -> 67, 112 -> 198
     //   the same, rows of 32: 2,000 rows 10.7 -> 8.8 and 28 -> 23; 4,000 11.8
