@@ -64,23 +64,23 @@ CSRC = os.path.join(ROOT, "paper_1909_01315_amd", "csrc")
 # reads for the 1 GiB device copy after the timed region), for the library
 # sources with this digest; any other source state reports null.
 MEASURED_TRAFFIC = {
-    "sources_sha256": "45dc15552736725c175b0fab184b8e52bbd58950de16b751b3e572fffc2b5706",
+    "sources_sha256": "13aebe6307a8208a07f627f972853a36be16639760078ddcbd63c57c0cd3ecbd",
     "ops": {
-        "gsddmm u_add_v": (976315376, 3770055840),
-        "leaky_relu": (3667153504, 3667356416),
-        "edge_softmax": (6701751818, 3711605056),
-        "gspmm u_mul_e/sum": (15846645113, 578012288),
-        "gspmm_backward u_mul_e/sum (dX, d_attention)": (42347957405, 4398110560),
-        "edge_softmax_backward": (10937636776, 3733925472),
-        "leaky_relu_backward": (7334271169, 3667264768),
-        "gsddmm_backward u_add_v": (19964778826, 31045600),
-        "gspmm copy_u/mean": (10630776636, 578009984),
-        "gspmm_backward copy_u/mean": (11707067524, 577951616),
-        "gspmm copy_u/max": (11246035698, 1045944960),
-        "gspmm_backward copy_u/max": (5065488963, 2435779520),
-        "gsddmm u_dot_v": (11754003443, 3821276256),
-        "c4 gspmm copy_u/sum": (21625133926, 1144773976),
-        "c4 gsddmm u_dot_v": (22155036341, 385613829),
+        "gsddmm u_add_v": (975745916, 3769856352),
+        "leaky_relu": (3667153504, 3667353984),
+        "edge_softmax": (6700631715, 3711480640),
+        "gspmm u_mul_e/sum": (15849416380, 578011648),
+        "gspmm_backward u_mul_e/sum (dX, d_attention)": (42346684474, 4398830784),
+        "edge_softmax_backward": (10908940068, 3731257920),
+        "leaky_relu_backward": (7334271169, 3667262720),
+        "gsddmm_backward u_add_v": (19964335572, 31042176),
+        "gspmm copy_u/mean": (10630399044, 578011648),
+        "gspmm_backward copy_u/mean": (11706341652, 577951616),
+        "gspmm copy_u/max": (11249718048, 1045946880),
+        "gspmm_backward copy_u/max": (5066926883, 2435897952),
+        "gsddmm u_dot_v": (11756526011, 3821638912),
+        "c4 gspmm copy_u/sum": (21627681474, 1144822405),
+        "c4 gsddmm u_dot_v": (22156665308, 385195698),
     },
 }
 
