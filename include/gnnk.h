@@ -493,7 +493,9 @@ typedef struct {
  * opposite angles, which is also the gradient).  x and out: (rows, H, F), fewer
  * than 2^31 rows of at most 1,024 heads of at most 2,048 columns; out may be x
  * itself (the same rows at the same address).  Errors: GNNK_EINVAL on shapes,
- * pairs or dtypes, or if out overlaps an operand otherwise. */
+ * pairs or dtypes, or if out overlaps an operand otherwise (columns side by
+ * side in rows of one stride do not overlap; rows of different strides do if
+ * their extents cross). */
 gnnk_status node_rotary(const gnnk_rotary* rot, const gnnk_tensor* x, int32_t inverse, gnnk_tensor* out,
                         hipStream_t stream);
 
