@@ -29,7 +29,7 @@
  *    therefore be captured into a HIP graph as it is.
  *  - Outputs are fully overwritten, never accumulated into.  Inputs may alias
  *    each other; outputs must not alias inputs or each other (but for
- *    node_rotary and node_norm_rotary in place).
+ *    node_rotary, node_norm_rotary and node_add_norm in place).
  *  - Edge tensors are indexed by edge id.  Node tensors by node id.
  *  - Index ranges are not checked on the compute path; use graph_validate.
  *  - All floating-point tensors of one call share one dtype.  Sums and dot
@@ -537,6 +537,94 @@ gnnk_status node_norm_rotary_backward(const gnnk_tensor* q, const gnnk_tensor* w
  * tensors (wq, k and wk nullable; only shapes are read). */
 gnnk_status node_norm_rotary_work_bytes(const gnnk_tensor* q, const gnnk_tensor* wq, const gnnk_tensor* k,
                                         const gnnk_tensor* wk, size_t* bytes);
+
+/* ------------------------------------------------------------------------ */
+/* The residual stream between layers, and products in 8 bits.  A row is a
+ * node's; where a tensor is (rows, heads, feat) all its heads are the row. */
+
+/* Rows of 8-bit whole numbers, each with a scale: row n stands for the values
+ * scale[n] * data[n, c].  data at any address, row_stride in bytes (>= cols, <
+ * 2^31, 16-byte multiples are read fastest); 1 to 65,536 columns, fewer than
+ * 2^31 rows. */
+typedef struct {
+    int8_t* data;
+    float* scale; /* rows values */
+    int64_t rows;
+    int64_t row_stride;
+    int32_t cols;
+    int32_t reserved;
+} gnnk_rows8;
+
+/* A weight of (outs, cols) in 8 bits with a scale for each of its rows, laid
+ * out by weight8_pack. */
+typedef struct {
+    const void* packed; /* weight8_bytes bytes, 256-byte aligned */
+    const float* scale; /* outs values */
+    int32_t outs;
+    int32_t cols;
+} gnnk_weight8;
+
+/* sum = x + residual and its norm, in one pass:
+ *   sum = x + residual,  out = w * sum / sqrt(mean(sum^2) + eps)
+ * The norm is that of the whole row, all heads, and of the sum before it is
+ * rounded.  x, residual (nullable: none, then sum must be NULL), sum (nullable)
+ * and out are of one shape and dtype, at most 16,384 columns, fewer than 2^31
+ * rows; w (nullable: all ones) is one row.  The sum of a row's squares is fp32;
+ * eps >= 0.  sum or out may be x or residual itself (the same rows at the same
+ * address); no output may overlap an operand or the other output otherwise.
+ * Errors: GNNK_EINVAL on shapes, dtypes and overlaps. */
+gnnk_status node_add_norm(const gnnk_tensor* x, const gnnk_tensor* residual, const gnnk_tensor* w, float eps,
+                          gnnk_tensor* sum, gnnk_tensor* out, hipStream_t stream);
+
+/* The same with the norm in 8 bits: with y = w * sum / sqrt(mean(sum^2) + eps),
+ * in fp32, row by row
+ *   scale = max |y| / 127,  q = y / scale rounded to the nearest (ties to even)
+ * A row of zeros has scale 0, no other one a scale below 2^-126; a row with a
+ * NaN or an infinity has scale NaN and values 0, so that products with it are
+ * NaN.  out->data past its columns is left as it was. */
+gnnk_status node_add_norm_i8(const gnnk_tensor* x, const gnnk_tensor* residual, const gnnk_tensor* w, float eps,
+                             gnnk_tensor* sum, gnnk_rows8* out, hipStream_t stream);
+
+/* The rows of x in 8 bits by the same rule, without a norm. */
+gnnk_status node_quantize(const gnnk_tensor* x, gnnk_rows8* out, hipStream_t stream);
+
+/* Gradients of node_add_norm.  With r = 1 / sqrt(mean(sum^2) + eps),
+ *   grad_x = grad_sum + r (grad_out w - sum r^2 mean(grad_out w sum))
+ *   grad_w = sum over rows of grad_out sum r
+ * sum as node_add_norm wrote it (without residual: x); grad_x is the gradient
+ * of x and that of the residual.  grad_sum (nullable: 0) is the gradient of
+ * the sum from what else read it.  grad_w's sums: fp32 over at most 32 rows,
+ * fp64 over those in a fixed order, rounded once.  grad_x and grad_w are
+ * nullable, grad_w needs w.  work: device memory of at least
+ * node_add_norm_work_bytes bytes, 256-byte aligned, for calls that ask for
+ * grad_w (else it may be NULL); it need not be initialised and is the caller's
+ * again once the work queued on `stream` is done.  grad_x may be sum, grad_out
+ * or grad_sum itself; no output may overlap an operand otherwise. */
+gnnk_status node_add_norm_backward(const gnnk_tensor* sum, const gnnk_tensor* w, const gnnk_tensor* grad_out,
+                                   const gnnk_tensor* grad_sum, float eps, gnnk_tensor* grad_x, gnnk_tensor* grad_w,
+                                   void* work, size_t work_bytes, hipStream_t stream);
+
+/* Bytes of work that such a call needs for the gradient of the weight (only
+ * the shape of sum is read). */
+gnnk_status node_add_norm_work_bytes(const gnnk_tensor* sum, size_t* bytes);
+
+/* Bytes of a weight of (outs, cols), 1 to 2^24 outputs and 1 to 65,536
+ * columns, in the layout that node_linear_i8 reads. */
+gnnk_status weight8_bytes(int32_t outs, int32_t cols, size_t* bytes);
+
+/* Lays out the values of w (its scale may be NULL: it is not read) in packed,
+ * weight8_bytes bytes, 256-byte aligned.  Once for a weight: the layout is read
+ * by any number of products. */
+gnnk_status weight8_pack(const gnnk_rows8* w, void* packed, size_t bytes, hipStream_t stream);
+
+/* Rows in 8 bits times a weight in 8 bits (a linear layer):
+ *   out[n, o] = x.scale[n] * w.scale[o] * sum over c of x[n, c] * w[o, c] + bias[o]
+ * The sums are exact (int32), the rest is fp32, rounded once to out's dtype.
+ * out: x.rows rows of w.outs columns, fp32 or bf16, in any heads; bias
+ * (nullable): one row of out's columns and dtype.  No gradient is formed.
+ * Errors: GNNK_EINVAL on shapes or dtypes, or if out overlaps an operand. */
+gnnk_status node_linear_i8(const gnnk_rows8* x, const gnnk_weight8* w, const gnnk_tensor* bias, gnnk_tensor* out,
+                           hipStream_t stream);
 
 /* ------------------------------------------------------------------------ */
 /* Tuning knobs, for schedule comparisons (forcing node- or edge-balanced

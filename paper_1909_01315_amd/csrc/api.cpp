@@ -1680,6 +1680,303 @@ gnnk_status node_norm_rotary_work_bytes(const gnnk_tensor* q, const gnnk_tensor*
 }  // extern "C"
 
 // ---------------------------------------------------------------------------
+// the residual stream's sums and norms, rows and products in 8 bits
+
+namespace gnnk {
+namespace {
+
+constexpr int NORM_MAX_COLS = 16384;
+constexpr int ROWS8_MAX_COLS = 65536;
+constexpr int WEIGHT8_MAX_OUTS = 1 << 24;
+constexpr int NORM_BLOCKS = 2048;      // blocks that share a call's rows
+constexpr int NORM_TILE_STEPS = 32;    // rows that a group of lanes adds up in fp32, at most
+constexpr int NORM_TILES = 2048;       // tiles that fill the chip
+
+int64_t cols_of(const gnnk_tensor* t) { return (int64_t)t->heads * t->feat; }
+
+bool rows_ok(const gnnk_tensor* t) {
+    return tensor_ok(t) && t->rows < ((int64_t)1 << 31) && cols_of(t) <= NORM_MAX_COLS;
+}
+bool row_weight_ok(const gnnk_tensor* w, const gnnk_tensor* x) {
+    return tensor_ok(w) && w->rows == 1 && cols_of(w) == cols_of(x);
+}
+bool rows8_ok(const gnnk_rows8* q) {
+    return q && q->rows >= 0 && q->rows < ((int64_t)1 << 31) && q->cols >= 1 && q->cols <= ROWS8_MAX_COLS &&
+           q->row_stride >= q->cols && q->row_stride < ((int64_t)1 << 31) && (q->data || q->rows == 0);
+}
+Span span(const gnnk_rows8* q) { return q ? Span{(uintptr_t)q->data, q->rows, q->row_stride, q->cols} : Span{}; }
+Span flat(const void* p, int64_t bytes) { return Span{(uintptr_t)p, bytes > 0 ? 1 : 0, bytes, bytes}; }
+
+// lanes and vectors of a row; returns the vectors a lane.  A wavefront holds
+// rows of up to 2,048 columns, four vectors of bf16 or eight of fp32 a lane;
+// wider ones take several.
+int add_norm_geo(AddNormArgs& A, const gnnk_tensor* x) {
+    A.C = (int32_t)cols_of(x);
+    A.inv_C = 1.0f / (float)A.C;
+    A.n = x->rows;
+    const int V = x->dtype == GNNK_BF16 ? 8 : 4, most = x->dtype == GNNK_BF16 ? 4 : 8;
+    const int NV = (A.C + V - 1) / V;
+    A.L = std::min(64, pow2ceil(NV));
+    A.waves = pow2ceil((NV + 64 * most - 1) / (64 * most));
+    A.threads = std::max(256, A.waves * 64);
+    const int lanes = A.waves > 1 ? A.waves * 64 : A.L;
+    return pow2ceil((NV + lanes - 1) / lanes);
+}
+int rows_of_block(const AddNormArgs& A) { return A.threads / (A.waves > 1 ? A.waves * 64 : A.L); }
+
+void add_norm_blocks(AddNormArgs& A) {
+    const int per = rows_of_block(A);
+    A.blocks = (int32_t)std::min<int64_t>((A.n + per - 1) / per, NORM_BLOCKS);
+}
+
+// the tiles of a backward: enough to fill the chip, and no longer than sums in
+// fp32 may be
+void add_norm_tiles(AddNormArgs& A) {
+    const int64_t groups = (A.n + rows_of_block(A) - 1) / rows_of_block(A);
+    A.steps = (int32_t)std::min<int64_t>(NORM_TILE_STEPS, std::max<int64_t>(1, groups / NORM_TILES));
+    A.parts = (groups + A.steps - 1) / A.steps;
+    A.blocks = (int32_t)std::min<int64_t>(A.parts, 1 << 20);
+}
+
+// 64 outputs and 128 columns at a time
+size_t weight8_size(int32_t outs, int32_t cols) {
+    return (size_t)((outs + 63) / 64) * ((cols + 127) / 128) * 8192;
+}
+
+size_t add_norm_work(const AddNormArgs& A) { return std::max<size_t>(256, (size_t)A.parts * A.C * 4); }
+
+// out overlaps none of the operands `in`, except the ones of its own rows that
+// it may replace
+bool clear_of(const Span& out, std::initializer_list<Span> in, std::initializer_list<Span> in_place) {
+    for (const Span& s : in)
+        if (overlap(out, s)) return false;
+    for (const Span& s : in_place)
+        if (overlap(out, s) && !same_span(out, s)) return false;
+    return true;
+}
+
+gnnk_status add_norm_check(const gnnk_tensor* x, const gnnk_tensor* r, const gnnk_tensor* w, float eps,
+                           const gnnk_tensor* sum) {
+    if (!rows_ok(x)) return fail(GNNK_EINVAL, "x: fewer than 2^31 rows of at most %d columns", NORM_MAX_COLS);
+    if (r && (!tensor_ok(r) || !same_shape(r, x))) return fail(GNNK_EINVAL, "the residual must have x's shape");
+    if (w && !row_weight_ok(w, x)) return fail(GNNK_EINVAL, "the weight must be one row of x's columns");
+    if (sum && (!r || !tensor_ok(sum) || !same_shape(sum, x)))
+        return fail(GNNK_EINVAL, "the sum needs a residual and must have x's shape");
+    if (!(eps >= 0.0f)) return fail(GNNK_EINVAL, "eps must not be negative");
+    return GNNK_OK;
+}
+
+void add_norm_operands(AddNormArgs& A, const gnnk_tensor* x, const gnnk_tensor* r, const gnnk_tensor* w, float eps,
+                       gnnk_tensor* sum) {
+    A.x = x->data;
+    A.x_stride = x->row_stride;
+    if (r) {
+        A.r = r->data;
+        A.r_stride = r->row_stride;
+    }
+    if (w) A.w = w->data;
+    if (sum) {
+        A.sum = sum->data;
+        A.sum_stride = sum->row_stride;
+    }
+    A.eps = eps;
+}
+
+gnnk_status rows8_check(const gnnk_rows8* out, const gnnk_tensor* x) {
+    if (!rows8_ok(out) || (!out->scale && out->rows > 0))
+        return fail(GNNK_EINVAL, "rows in 8 bits: data, scales, 1 to %d columns and a row stride of at least those",
+                    ROWS8_MAX_COLS);
+    if (out->rows != x->rows || out->cols != cols_of(x)) return fail(GNNK_EINVAL, "the 8-bit rows must have x's shape");
+    return GNNK_OK;
+}
+
+}  // namespace
+}  // namespace gnnk
+
+extern "C" {
+
+gnnk_status node_add_norm(const gnnk_tensor* x, const gnnk_tensor* residual, const gnnk_tensor* w, float eps,
+                          gnnk_tensor* sum, gnnk_tensor* out, hipStream_t stream) {
+    clear_error();
+    const gnnk_status st = add_norm_check(x, residual, w, eps, sum);
+    if (st != GNNK_OK) return st;
+    if (!tensor_ok(out) || !same_shape(out, x)) return fail(GNNK_EINVAL, "out must have x's shape");
+    if (!same_dtype({x, residual, w, sum, out})) return fail(GNNK_EINVAL, "all tensors must share one dtype");
+    const Span o = span(out), h = span(sum);
+    if (!clear_of(o, {span(w), h}, {span(x), span(residual)}) || !clear_of(h, {span(w)}, {span(x), span(residual)}))
+        return fail(GNNK_EINVAL, "an output overlaps an operand or the other one");
+    if (x->rows == 0) return GNNK_OK;
+    AddNormArgs A{};
+    const int npt = add_norm_geo(A, x);
+    add_norm_operands(A, x, residual, w, eps, sum);
+    A.out = out->data;
+    A.out_stride = out->row_stride;
+    add_norm_blocks(A);
+    return launch_status(launch_node_add_norm(A, dtype_code(x), npt, ADD_NORM, stream), "norm launch");
+}
+
+gnnk_status node_add_norm_i8(const gnnk_tensor* x, const gnnk_tensor* residual, const gnnk_tensor* w, float eps,
+                             gnnk_tensor* sum, gnnk_rows8* out, hipStream_t stream) {
+    clear_error();
+    gnnk_status st = add_norm_check(x, residual, w, eps, sum);
+    if (st != GNNK_OK) return st;
+    st = rows8_check(out, x);
+    if (st != GNNK_OK) return st;
+    if (!same_dtype({x, residual, w, sum})) return fail(GNNK_EINVAL, "all tensors must share one dtype");
+    const Span q = span(out), s = flat(out->scale, out->rows * 4), h = span(sum);
+    if (!clear_of(q, {span(x), span(residual), span(w), s, h}, {}) ||
+        !clear_of(s, {span(x), span(residual), span(w), h}, {}) || !clear_of(h, {span(w)}, {span(x), span(residual)}))
+        return fail(GNNK_EINVAL, "an output overlaps an operand or another one");
+    if (x->rows == 0) return GNNK_OK;
+    AddNormArgs A{};
+    const int npt = add_norm_geo(A, x);
+    add_norm_operands(A, x, residual, w, eps, sum);
+    A.q = out->data;
+    A.q_stride = out->row_stride;
+    A.scale = out->scale;
+    add_norm_blocks(A);
+    return launch_status(launch_node_add_norm(A, dtype_code(x), npt, ADD_NORM8, stream), "norm launch");
+}
+
+gnnk_status node_quantize(const gnnk_tensor* x, gnnk_rows8* out, hipStream_t stream) {
+    clear_error();
+    if (!rows_ok(x)) return fail(GNNK_EINVAL, "x: fewer than 2^31 rows of at most %d columns", NORM_MAX_COLS);
+    const gnnk_status st = rows8_check(out, x);
+    if (st != GNNK_OK) return st;
+    const Span q = span(out), s = flat(out->scale, out->rows * 4);
+    if (!clear_of(q, {span(x), s}, {}) || !clear_of(s, {span(x)}, {}))
+        return fail(GNNK_EINVAL, "an output overlaps an operand or another one");
+    if (x->rows == 0) return GNNK_OK;
+    AddNormArgs A{};
+    const int npt = add_norm_geo(A, x);
+    add_norm_operands(A, x, nullptr, nullptr, 0.0f, nullptr);
+    A.q = out->data;
+    A.q_stride = out->row_stride;
+    A.scale = out->scale;
+    add_norm_blocks(A);
+    return launch_status(launch_node_add_norm(A, dtype_code(x), npt, QUANT8, stream), "quantize launch");
+}
+
+gnnk_status node_add_norm_backward(const gnnk_tensor* sum, const gnnk_tensor* w, const gnnk_tensor* grad_out,
+                                   const gnnk_tensor* grad_sum, float eps, gnnk_tensor* grad_x, gnnk_tensor* grad_w,
+                                   void* work, size_t work_bytes, hipStream_t stream) {
+    clear_error();
+    if (!rows_ok(sum)) return fail(GNNK_EINVAL, "sum: fewer than 2^31 rows of at most %d columns", NORM_MAX_COLS);
+    if (!tensor_ok(grad_out) || !same_shape(grad_out, sum))
+        return fail(GNNK_EINVAL, "the gradient of the norm must have the sum's shape");
+    if (grad_sum && (!tensor_ok(grad_sum) || !same_shape(grad_sum, sum)))
+        return fail(GNNK_EINVAL, "the gradient of the sum must have its shape");
+    if (w && !row_weight_ok(w, sum)) return fail(GNNK_EINVAL, "the weight must be one row of the sum's columns");
+    if (grad_x && (!tensor_ok(grad_x) || !same_shape(grad_x, sum)))
+        return fail(GNNK_EINVAL, "the gradient of x must have the sum's shape");
+    if (grad_w && (!w || !row_weight_ok(grad_w, sum)))
+        return fail(GNNK_EINVAL, "the weight's gradient needs a weight and must have its columns");
+    if (!(eps >= 0.0f)) return fail(GNNK_EINVAL, "eps must not be negative");
+    if (!same_dtype({sum, w, grad_out, grad_sum, grad_x, grad_w}))
+        return fail(GNNK_EINVAL, "all tensors must share one dtype");
+    AddNormArgs A{};
+    const int npt = add_norm_geo(A, sum);
+    add_norm_tiles(A);
+    const size_t need = grad_w ? add_norm_work(A) : 0;
+    if (need && (!work || work_bytes < need))
+        return fail(GNNK_ENOMEM, "the weight's gradient needs %zu bytes of work, %zu given", need, work ? work_bytes : 0);
+    if (need && ((uintptr_t)work & 255)) return fail(GNNK_EINVAL, "work must be 256-byte aligned");
+    const Span dx = span(grad_x), dw = span(grad_w), scratch = flat(work, (int64_t)need);
+    const Span ins[4] = {span(sum), span(grad_out), span(grad_sum), span(w)};
+    if (!clear_of(dx, {ins[3], dw, scratch}, {ins[0], ins[1], ins[2]}) ||
+        !clear_of(dw, {ins[0], ins[1], ins[2], ins[3], scratch}, {}) ||
+        !clear_of(scratch, {ins[0], ins[1], ins[2], ins[3]}, {}))
+        return fail(GNNK_EINVAL, "an output or the work overlaps an operand or an output");
+    if (!grad_x && !grad_w) return GNNK_OK;
+    add_norm_operands(A, sum, grad_out, w, eps, nullptr);
+    if (grad_sum) {
+        A.gs = grad_sum->data;
+        A.gs_stride = grad_sum->row_stride;
+    }
+    if (grad_x) {
+        A.out = grad_x->data;
+        A.out_stride = grad_x->row_stride;
+    }
+    if (grad_w) {
+        A.dw = grad_w->data;
+        A.part = static_cast<float*>(work);
+    }
+    return launch_status(launch_node_add_norm(A, dtype_code(sum), npt, ADD_NORM_BWD, stream), "norm backward launch");
+}
+
+gnnk_status node_add_norm_work_bytes(const gnnk_tensor* sum, size_t* bytes) {
+    clear_error();
+    if (!sum || !bytes) return fail(GNNK_EINVAL, "NULL argument");
+    *bytes = 0;
+    if (sum->heads < 1 || sum->feat < 1 || sum->rows < 0 || sum->rows >= ((int64_t)1 << 31) ||
+        cols_of(sum) > NORM_MAX_COLS || (sum->dtype != GNNK_F32 && sum->dtype != GNNK_BF16))
+        return fail(GNNK_EINVAL, "fewer than 2^31 rows of at most %d columns", NORM_MAX_COLS);
+    AddNormArgs A{};
+    add_norm_geo(A, sum);
+    add_norm_tiles(A);
+    *bytes = add_norm_work(A);
+    return GNNK_OK;
+}
+
+gnnk_status weight8_bytes(int32_t outs, int32_t cols, size_t* bytes) {
+    clear_error();
+    if (!bytes) return fail(GNNK_EINVAL, "NULL argument");
+    *bytes = 0;
+    if (outs < 1 || outs > WEIGHT8_MAX_OUTS || cols < 1 || cols > ROWS8_MAX_COLS)
+        return fail(GNNK_EINVAL, "a weight of 1 to %d outputs and 1 to %d columns", WEIGHT8_MAX_OUTS, ROWS8_MAX_COLS);
+    *bytes = weight8_size(outs, cols);
+    return GNNK_OK;
+}
+
+gnnk_status weight8_pack(const gnnk_rows8* w, void* packed, size_t bytes, hipStream_t stream) {
+    clear_error();
+    if (!rows8_ok(w) || w->rows < 1 || w->rows > WEIGHT8_MAX_OUTS)
+        return fail(GNNK_EINVAL, "a weight of 1 to %d outputs and 1 to %d columns", WEIGHT8_MAX_OUTS, ROWS8_MAX_COLS);
+    const size_t need = weight8_size((int32_t)w->rows, w->cols);
+    if (!packed || bytes < need) return fail(GNNK_ENOMEM, "the layout takes %zu bytes, %zu given", need, packed ? bytes : 0);
+    if ((uintptr_t)packed & 255) return fail(GNNK_EINVAL, "packed must be 256-byte aligned");
+    if (overlap(flat(packed, (int64_t)need), span(w))) return fail(GNNK_EINVAL, "the layout overlaps the weight");
+    return launch_status(launch_weight8_pack(w->data, w->row_stride, (int32_t)w->rows, w->cols,
+                                             static_cast<int8_t*>(packed), stream),
+                         "weight layout launch");
+}
+
+gnnk_status node_linear_i8(const gnnk_rows8* x, const gnnk_weight8* w, const gnnk_tensor* bias, gnnk_tensor* out,
+                           hipStream_t stream) {
+    clear_error();
+    if (!rows8_ok(x) || (!x->scale && x->rows > 0))
+        return fail(GNNK_EINVAL, "rows in 8 bits: data, scales, 1 to %d columns and a row stride of at least those",
+                    ROWS8_MAX_COLS);
+    if (!w || !w->packed || !w->scale || ((uintptr_t)w->packed & 255) || w->outs < 1 || w->outs > WEIGHT8_MAX_OUTS)
+        return fail(GNNK_EINVAL, "malformed weight");
+    if (w->cols != x->cols) return fail(GNNK_EINVAL, "rows of %d columns, a weight of %d", x->cols, w->cols);
+    if (!tensor_ok(out) || out->rows != x->rows || cols_of(out) != w->outs)
+        return fail(GNNK_EINVAL, "out must have the rows' count and the weight's outputs");
+    if (bias && (!tensor_ok(bias) || bias->rows != 1 || cols_of(bias) != w->outs || bias->dtype != out->dtype))
+        return fail(GNNK_EINVAL, "the bias must be one row of out's columns and dtype");
+    const int64_t packed = (int64_t)weight8_size(w->outs, w->cols);
+    if (!clear_of(span(out), {span(x), flat(x->scale, x->rows * 4), flat(w->packed, packed),
+                              flat(w->scale, w->outs * 4ll), span(bias)}, {}))
+        return fail(GNNK_EINVAL, "out overlaps an operand");
+    if (x->rows == 0) return GNNK_OK;
+    Linear8Args A{};
+    A.x = x->data;
+    A.xs = x->scale;
+    A.w = static_cast<const int8_t*>(w->packed);
+    A.ws = w->scale;
+    A.bias = bias ? bias->data : nullptr;
+    A.out = out->data;
+    A.x_stride = x->row_stride;
+    A.out_stride = out->row_stride;
+    A.M = x->rows;
+    A.N = w->outs;
+    A.K = x->cols;
+    return launch_status(launch_linear8(A, dtype_code(out), (int)options().linear8_tile, stream), "8-bit product launch");
+}
+
+}  // extern "C"
+
+// ---------------------------------------------------------------------------
 // dot-product attention over the edges
 
 namespace gnnk {

@@ -314,6 +314,43 @@ struct RotaryArgs {
 };
 // mode: 0 rotation alone, 1 norm and rotation, 2 the backward of that
 hipError_t launch_node_rotary(const RotaryArgs& a, int dtype, int vec, int mode, size_t lds, hipStream_t s);
+// the residual stream's sum and norm, and rows in 8 bits, norm.hip
+enum AddNormMode : int32_t { ADD_NORM = 0, ADD_NORM8 = 1, QUANT8 = 2, ADD_NORM_BWD = 3 };
+struct AddNormArgs {
+    const void* x;           // (n, C) T; backward: the sum h
+    const void* r;           // the residual, nullable; backward: the gradient of the norm
+    const void* gs;          // backward: the gradient of the sum, nullable
+    const void* w;           // C values, nullable
+    void* sum;               // forward: x + r (nullable without r)
+    void* out;               // the norm; backward the gradient of the sum's operands, nullable
+    int8_t* q;               // in its place, in 8 bits
+    float* scale;            // of each row of q
+    void* dw;                // backward: gradient of w
+    float* part;             // parts x C sums of tiles, nullptr: dw not wanted
+    int64_t parts;
+    int64_t x_stride, r_stride, gs_stride, sum_stride, out_stride, q_stride, n;
+    int32_t C, L, waves;     // columns; lanes of a row, or wavefronts where it takes several
+    int32_t threads, blocks; // of a block, of the launch
+    int32_t steps;           // backward: a tile is that many times the rows that a block takes at once
+    float eps, inv_C;
+};
+// npt: vectors of 16 bytes a lane
+hipError_t launch_node_add_norm(const AddNormArgs& a, int dtype, int npt, int mode, hipStream_t s);
+// products with weights in 8 bits, linear8.hip
+struct Linear8Args {
+    const int8_t* x;         // (M, K), row stride in bytes
+    const float* xs;         // a scale for each row
+    const int8_t* w;         // the weight as laid out by launch_weight8_pack
+    const float* ws;         // a scale for each of the N columns of the output
+    const void* bias;        // N values of the output's type, nullable
+    void* out;               // (M, N)
+    int64_t x_stride, out_stride, M;
+    int32_t N, K;
+};
+// tile: 0 by the sizes, otherwise the kernel of that number
+constexpr int LINEAR8_TILES = 7;
+hipError_t launch_linear8(const Linear8Args& a, int dtype, int tile, hipStream_t s);
+hipError_t launch_weight8_pack(const int8_t* w, int64_t stride, int32_t N, int32_t K, int8_t* packed, hipStream_t s);
 hipError_t launch_fill_rows(const void* ptr, int ptr64, int64_t n_rows, int64_t n_edges, int32_t* row,
                             hipStream_t s);
 hipError_t launch_sddmm(const EngineArgs& a, int dtype, int vec, int opk, int spec, int gc, hipStream_t s);

@@ -1,0 +1,388 @@
+// The residual stream between attention layers: node_add_norm adds a layer's
+// output to the stream and divides each row by its root mean square, its
+// backward, and rows in 8 bits (after the norm, or as they are).
+//
+//   h = x + r,  rn = 1 / sqrt(mean(h^2) + eps),  y = h rn w
+//   s = max |y| / 127,  q = round(y / s)
+//   dx = gh + rn (gy w - h rn^2 mean(gy w h)),  dw = sum over rows of gy h rn
+//
+// A pure stream: every row is read once and written once.  A row lies in the
+// registers of a group of lanes, a wavefront at most or several wavefronts of
+// one block, NPT vectors of 16 bytes a lane; its sums go over the lanes and
+// then, by way of LDS, over the wavefronts.  Rows of odd widths are read by
+// unaligned vectors, the last one past its columns, which are left aside.
+#include "words.h"
+
+namespace gnnk {
+
+namespace {
+
+// 8-bit values are stored at any address
+typedef unsigned u2_b __attribute__((ext_vector_type(2), aligned(1)));
+typedef unsigned u1_b __attribute__((aligned(1)));
+
+// the largest of x over the aligned run of `red` lanes; every lane gets it
+__device__ __forceinline__ uint32_t run_most(uint32_t x, int red) {
+    auto with = [&](uint32_t y) { x = x > y ? x : y; };
+    if (red >= 2) with((uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, DPP_QUAD_1032, 0xF, 0xF, true));
+    if (red >= 4) with((uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, DPP_QUAD_2301, 0xF, 0xF, true));
+    if (red >= 8) with((uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, DPP_HALF_MIRROR, 0xF, 0xF, true));
+    if (red >= 16) with((uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, DPP_MIRROR, 0xF, 0xF, true));
+    if (red >= 32) with(__shfl_xor(x, 16, WAVE));
+    if (red >= 64) with(__shfl_xor(x, 32, WAVE));
+    return x;
+}
+
+// sums of N values over a row's lanes (and wavefronts); red: 16 * N floats of LDS
+template <int N, bool WIDE>
+__device__ __forceinline__ void row_totals(float* v, const AddNormArgs& A, float* red) {
+    run_totals<N>(v, WIDE ? 64 : A.L);
+    if constexpr (WIDE) {
+        const int wave = threadIdx.x >> 6, first = wave & ~(A.waves - 1);
+        __syncthreads();  // (the row before may still be read)
+        if ((threadIdx.x & 63) == 0)
+#pragma unroll
+            for (int u = 0; u < N; ++u) red[wave * N + u] = v[u];
+        __syncthreads();
+#pragma unroll
+        for (int u = 0; u < N; ++u) {
+            v[u] = 0.0f;
+            for (int k = 0; k < A.waves; ++k) v[u] += red[(first + k) * N + u];
+        }
+    }
+}
+template <bool WIDE>
+__device__ __forceinline__ uint32_t row_most(uint32_t x, const AddNormArgs& A, uint32_t* red) {
+    x = run_most(x, WIDE ? 64 : A.L);
+    if constexpr (WIDE) {
+        const int wave = threadIdx.x >> 6, first = wave & ~(A.waves - 1);
+        __syncthreads();
+        if ((threadIdx.x & 63) == 0) red[wave] = x;
+        __syncthreads();
+        x = 0;
+        for (int k = 0; k < A.waves; ++k) x = red[first + k] > x ? red[first + k] : x;
+    }
+    return x;
+}
+
+// V values as 8-bit numbers, each the nearest to t * inv; inv 0: zeros,
+// whatever t is
+template <int V, bool PART>
+__device__ __forceinline__ void put8(int8_t* p, const float* t, float inv, int n) {
+    uint32_t w[(V + 3) / 4] = {};
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        // (a magnitude that rounds past 127 steps is one of them)
+        const int q = (int)fminf(fmaxf(rintf(t[i] * inv), -127.0f), 127.0f);
+        w[i / 4] |= (uint32_t)(q & 255) << (i % 4 * 8);
+    }
+    if (inv == 0.0f)
+#pragma unroll
+        for (int i = 0; i < (V + 3) / 4; ++i) w[i] = 0;
+    if (!PART || n == V) {
+        if constexpr (V == 8) *reinterpret_cast<u2_b*>(p) = u2_b{w[0], w[1]};
+        else *reinterpret_cast<u1_b*>(p) = w[0];
+    } else {
+#pragma unroll
+        for (int i = 0; i < V; ++i)
+            if (i < n) p[i] = (int8_t)(w[i / 4] >> (i % 4 * 8));
+    }
+}
+
+// NPT vectors of V values a lane, vector p of it being number p * lanes + lane
+// of the row; PART: the last vector of a row holds fewer values than V
+template <typename T, int NPT, bool PART, bool WIDE, int MODE>
+__global__ __launch_bounds__(WIDE ? 512 : 256) void node_add_norm_kernel(AddNormArgs A) {
+    constexpr int V = 16 / sizeof(T);
+    constexpr int N = Words<T, V>::N;
+    __shared__ float red[32];
+    const int tid = threadIdx.x, TPR = WIDE ? A.waves * 64 : A.L;
+    const int lig = tid & (TPR - 1), gid = tid / TPR, per = blockDim.x / TPR;
+    const int C = A.C;
+
+    auto count = [&](int p) {  // columns of the lane's vector p
+        const int left = C - (p * TPR + lig) * V;
+        return left < 0 ? 0 : (left < V ? left : V);
+    };
+    auto get = [&](const void* base, int64_t stride, int64_t n, int p, bool ok, float* raw) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) raw[i] = 0.0f;
+        const int m = count(p), c = (p * TPR + lig) * V;
+        if (ok && m > 0) {
+            const int64_t at = n * stride + c;
+            fetch<T, V, PART>(reinterpret_cast<const T*>(base) + at, m, (A.n - 1) * stride + C - at, raw);
+        }
+    };
+    float w[NPT][N];
+    if constexpr (MODE != QUANT8) {
+        if (A.w) {
+#pragma unroll
+            for (int p = 0; p < NPT; ++p) {
+#pragma unroll
+                for (int i = 0; i < N; ++i) w[p][i] = 0.0f;
+                const int m = count(p), c = (p * TPR + lig) * V;
+                if (m > 0) fetch<T, V, PART>(reinterpret_cast<const T*>(A.w) + c, m, C - c, w[p]);
+            }
+        }
+    }
+    const int64_t step = (int64_t)gridDim.x * per;
+    float xr[NPT][N], rr[MODE == QUANT8 ? 1 : NPT][N];
+    auto ahead = [&](int64_t n) {
+#pragma unroll
+        for (int p = 0; p < NPT; ++p) {
+            get(A.x, A.x_stride, n, p, n < A.n, xr[p]);
+            if constexpr (MODE != QUANT8)
+                if (A.r) get(A.r, A.r_stride, n, p, n < A.n, rr[p]);
+        }
+    };
+    ahead((int64_t)blockIdx.x * per + gid);
+    for (int64_t n0 = (int64_t)blockIdx.x * per; n0 < A.n; n0 += step) {
+        const int64_t n = n0 + gid;
+        const bool ok = n < A.n;
+        float h[NPT][V];
+        float ss = 0.0f;
+#pragma unroll
+        for (int p = 0; p < NPT; ++p) {
+            const int m = count(p);
+            widen<T, V, PART>(xr[p], m, h[p]);
+            if constexpr (MODE != QUANT8) {
+                if (A.r) {
+                    float t[V];
+                    widen<T, V, PART>(rr[p], m, t);
+#pragma unroll
+                    for (int i = 0; i < V; ++i) h[p][i] += t[i];
+                    if (ok && m > 0 && A.sum)
+                        store_part<T, V, PART>(reinterpret_cast<T*>(A.sum) + n * A.sum_stride + (p * TPR + lig) * V,
+                                               h[p], m);
+                }
+#pragma unroll
+                for (int i = 0; i < V; ++i) ss = fmaf(h[p][i], h[p][i], ss);
+            }
+        }
+        ahead(n + step);
+        if constexpr (MODE != QUANT8) {
+            row_totals<1, WIDE>(&ss, A, red);
+            const float rn = 1.0f / sqrtf(ss * A.inv_C + A.eps);
+#pragma unroll
+            for (int p = 0; p < NPT; ++p)
+#pragma unroll
+                for (int i = 0; i < V; ++i) h[p][i] *= A.w ? rn * Words<T, V>::at(w[p], i) : rn;
+        }
+        if constexpr (MODE == ADD_NORM) {
+#pragma unroll
+            for (int p = 0; p < NPT; ++p) {
+                const int m = count(p);
+                if (ok && m > 0)
+                    store_part<T, V, PART>(reinterpret_cast<T*>(A.out) + n * A.out_stride + (p * TPR + lig) * V, h[p], m);
+            }
+        } else {
+            // the largest magnitude by its bits, where a NaN is the largest
+            uint32_t most = 0;
+#pragma unroll
+            for (int p = 0; p < NPT; ++p) {
+                const int m = count(p);
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    const uint32_t b = !PART || i < m ? __float_as_uint(h[p][i]) & 0x7FFFFFFFu : 0u;
+                    most = b > most ? b : most;
+                }
+            }
+            most = row_most<WIDE>(most, A, reinterpret_cast<uint32_t*>(red) + 16);
+            // a row of zeros has scale 0; the scale is no subnormal, whose
+            // inverse may be infinite; a row with a NaN or an infinity has
+            // scale NaN and values 0, so that what is made of it is NaN
+            const bool finite = most < 0x7F800000u;
+            float s = fmaxf(__uint_as_float(most) / 127.0f, 1.17549435e-38f);
+            const float inv = finite ? 1.0f / s : 0.0f;
+            s = !finite ? __uint_as_float(0x7FC00000u) : (most ? s : 0.0f);
+#pragma unroll
+            for (int p = 0; p < NPT; ++p) {
+                const int m = count(p);
+                if (ok && m > 0) put8<V, PART>(A.q + n * A.q_stride + (p * TPR + lig) * V, h[p], inv, m);
+            }
+            if (ok && lig == 0) A.scale[n] = s;
+        }
+    }
+}
+
+// A block takes a tile of rows: gradients of the stream row by row, and the
+// sum of gy h rn over the tile, which the next kernel adds up over the tiles.
+template <typename T, int NPT, bool PART, bool WIDE>
+__global__ __launch_bounds__(WIDE ? 512 : 256) void node_add_norm_backward_kernel(AddNormArgs A) {
+    constexpr int V = 16 / sizeof(T);
+    constexpr int N = Words<T, V>::N;
+    extern __shared__ float lds[];
+    __shared__ float red[32];
+    const int tid = threadIdx.x, TPR = WIDE ? A.waves * 64 : A.L;
+    const int lig = tid & (TPR - 1), gid = tid / TPR, per = blockDim.x / TPR;
+    const int C = A.C;
+
+    auto count = [&](int p) {
+        const int left = C - (p * TPR + lig) * V;
+        return left < 0 ? 0 : (left < V ? left : V);
+    };
+    auto get = [&](const void* base, int64_t stride, int64_t n, int p, bool ok, float* raw) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) raw[i] = 0.0f;
+        const int m = count(p), c = (p * TPR + lig) * V;
+        if (ok && m > 0) {
+            const int64_t at = n * stride + c;
+            fetch<T, V, PART>(reinterpret_cast<const T*>(base) + at, m, (A.n - 1) * stride + C - at, raw);
+        }
+    };
+    float w[NPT][N];
+#pragma unroll
+    for (int p = 0; p < NPT; ++p) {
+#pragma unroll
+        for (int i = 0; i < N; ++i) w[p][i] = 0.0f;
+        const int m = count(p), c = (p * TPR + lig) * V;
+        if (A.w && m > 0) fetch<T, V, PART>(reinterpret_cast<const T*>(A.w) + c, m, C - c, w[p]);
+    }
+    for (int64_t tile = blockIdx.x; tile < A.parts; tile += gridDim.x) {
+        const int64_t first = tile * per * A.steps;
+        float dw[NPT][V];
+#pragma unroll
+        for (int p = 0; p < NPT; ++p)
+#pragma unroll
+            for (int i = 0; i < V; ++i) dw[p][i] = 0.0f;
+
+        for (int k = 0; k < A.steps; ++k) {
+            const int64_t n = first + (int64_t)k * per + gid;
+            if (first + (int64_t)k * per >= A.n) break;
+            const bool ok = n < A.n;
+            float hr[NPT][N], gr[NPT][N], sr[NPT][N];
+#pragma unroll
+            for (int p = 0; p < NPT; ++p) {
+                get(A.x, A.x_stride, n, p, ok, hr[p]);
+                get(A.r, A.r_stride, n, p, ok, gr[p]);
+                if (A.gs) get(A.gs, A.gs_stride, n, p, ok, sr[p]);
+            }
+            float t[2] = {0.0f, 0.0f};  // sums of h^2 and of gy w h
+#pragma unroll
+            for (int p = 0; p < NPT; ++p) {
+                const int m = count(p);
+                float h[V], g[V];
+                widen<T, V, PART>(hr[p], m, h);
+                widen<T, V, PART>(gr[p], m, g);
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    t[0] = fmaf(h[i], h[i], t[0]);
+                    t[1] = fmaf(A.w ? g[i] * Words<T, V>::at(w[p], i) : g[i], h[i], t[1]);
+                }
+            }
+            row_totals<2, WIDE>(t, A, red);
+            const float rn = 1.0f / sqrtf(t[0] * A.inv_C + A.eps);
+            const float mean = rn * rn * (t[1] * A.inv_C);
+#pragma unroll
+            for (int p = 0; p < NPT; ++p) {
+                const int m = count(p);
+                float h[V], g[V], s[V];
+                widen<T, V, PART>(hr[p], m, h);
+                widen<T, V, PART>(gr[p], m, g);
+                if (A.gs) widen<T, V, PART>(sr[p], m, s);
+#pragma unroll
+                for (int i = 0; i < V; ++i) {
+                    // (a group without a row adds nothing: there rn may be infinite)
+                    if (ok) dw[p][i] = fmaf(g[i], h[i] * rn, dw[p][i]);
+                    const float gw = A.w ? g[i] * Words<T, V>::at(w[p], i) : g[i];
+                    const float d = rn * (gw - h[i] * mean);
+                    h[i] = A.gs ? s[i] + d : d;
+                }
+                if (ok && m > 0 && A.out)
+                    store_part<T, V, PART>(reinterpret_cast<T*>(A.out) + n * A.out_stride + (p * TPR + lig) * V, h, m);
+            }
+        }
+        if (!A.part) continue;
+        // the tile's sum over the block's rows side by side, in their order
+        float* const part = A.part + tile * C;
+#pragma unroll
+        for (int p = 0; p < NPT; ++p) {
+            __syncthreads();
+#pragma unroll
+            for (int i = 0; i < V; ++i) lds[i * blockDim.x + tid] = dw[p][i];
+            __syncthreads();
+            for (int q = tid; q < TPR * V; q += blockDim.x) {
+                const int i = q / TPR, l = q - i * TPR, col = (p * TPR + l) * V + i;
+                if (col >= C) continue;
+                double sum = 0.0;
+                for (int k = 0; k < per; ++k) sum += (double)lds[i * blockDim.x + k * TPR + l];
+                part[col] = (float)sum;
+            }
+        }
+    }
+}
+
+// the weight's gradient: the tiles' sums in fp64, 32 columns a workgroup, 32
+// runs of tiles side by side, each in order
+template <typename T>
+__global__ __launch_bounds__(1024) void node_add_norm_dw_kernel(AddNormArgs A) {
+    __shared__ double red[32][33];
+    const int c = threadIdx.x & 31, run = threadIdx.x >> 5;
+    const int64_t col = (int64_t)blockIdx.x * 32 + c, per = (A.parts + 31) / 32;
+    double sum = 0.0;
+    if (col < A.C) {
+        const int64_t end = (run + 1) * per < A.parts ? (run + 1) * per : A.parts;
+        constexpr int U = 8;  // loads in flight
+        for (int64_t p = run * per; p < end; p += U) {
+            float x[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) x[u] = A.part[(p + u < end ? p + u : p) * A.C + col];
+#pragma unroll
+            for (int u = 0; u < U; ++u) sum += p + u < end ? (double)x[u] : 0.0;
+        }
+    }
+    red[run][c] = sum;
+    __syncthreads();
+    if (run == 0 && col < A.C) {
+        for (int k = 1; k < 32; ++k) sum += red[k][c];
+        IO<T, 1>::store1(reinterpret_cast<T*>(A.dw) + col, (float)sum);
+    }
+}
+
+template <typename T, int NPT, bool PART, bool WIDE>
+void launch_n(const AddNormArgs& a, int mode, hipStream_t s) {
+    const dim3 grid((unsigned)a.blocks), block((unsigned)a.threads);
+    if (mode == ADD_NORM)
+        hipLaunchKernelGGL((node_add_norm_kernel<T, NPT, PART, WIDE, ADD_NORM>), grid, block, 0, s, a);
+    else if (mode == ADD_NORM8)
+        hipLaunchKernelGGL((node_add_norm_kernel<T, NPT, PART, WIDE, ADD_NORM8>), grid, block, 0, s, a);
+    else if (mode == QUANT8)
+        hipLaunchKernelGGL((node_add_norm_kernel<T, NPT, PART, WIDE, QUANT8>), grid, block, 0, s, a);
+    else
+        hipLaunchKernelGGL((node_add_norm_backward_kernel<T, NPT, PART, WIDE>), grid, block,
+                           a.part ? a.threads * 64 / sizeof(T) : 0, s, a);
+}
+
+template <typename T, int NPT>
+void launch_p(const AddNormArgs& a, int mode, hipStream_t s) {
+    const bool part = a.C % (16 / (int)sizeof(T)) != 0;
+    if (a.waves > 1) {
+        if (part) launch_n<T, NPT, true, true>(a, mode, s);
+        else launch_n<T, NPT, false, true>(a, mode, s);
+    } else {
+        if (part) launch_n<T, NPT, true, false>(a, mode, s);
+        else launch_n<T, NPT, false, false>(a, mode, s);
+    }
+}
+
+template <typename T>
+void launch_t(const AddNormArgs& a, int npt, int mode, hipStream_t s) {
+    if (a.blocks > 0) {
+        if (npt == 1) launch_p<T, 1>(a, mode, s);
+        else if (npt == 2) launch_p<T, 2>(a, mode, s);
+        else if (npt == 4) launch_p<T, 4>(a, mode, s);
+        else if constexpr (sizeof(T) == 4) launch_p<T, 8>(a, mode, s);
+    }
+    if (mode == ADD_NORM_BWD && a.part)
+        hipLaunchKernelGGL((node_add_norm_dw_kernel<T>), dim3((unsigned)((a.C + 31) / 32)), dim3(1024), 0, s, a);
+}
+
+}  // namespace
+
+hipError_t launch_node_add_norm(const AddNormArgs& a, int dtype, int npt, int mode, hipStream_t s) {
+    if (dtype == 0) launch_t<float>(a, npt, mode, s);
+    else launch_t<bf16_t>(a, npt, mode, s);
+    return hipGetLastError();
+}
+
+}  // namespace gnnk

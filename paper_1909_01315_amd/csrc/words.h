@@ -1,5 +1,6 @@
 // Rows in words and sums over neighbouring lanes, shared by the attention
-// kernels (dot products over edges, norms and rotations of their operands).
+// kernels (dot products over edges, norms and rotations of their operands) and
+// the norms of whole rows.
 #pragma once
 
 #include "device.h"
@@ -55,6 +56,70 @@ struct Words<bf16_t, VEC> {
         return (i & 1) ? bf_hi(x) : bf_lo(x);
     }
 };
+
+// V values at p in words, the first n of them the caller's (PART); all of them
+// are read where they lie within `room` values
+template <typename T, int V, bool PART>
+__device__ __forceinline__ void fetch(const T* p, int n, int64_t room, float* w) {
+    using W = Words<T, V>;
+    if (!PART || room >= V) {
+        IO<typename W::type, V>::load(reinterpret_cast<const typename W::type*>(p), w);
+    } else {
+#pragma unroll
+        for (int i = 0; i < W::N; ++i) {
+            if constexpr (W::PAIRS) {
+                const uint32_t lo = 2 * i < n ? p[2 * i] : 0, hi = 2 * i + 1 < n ? p[2 * i + 1] : 0;
+                w[i] = __uint_as_float(lo | hi << 16);
+            } else {
+                w[i] = i < n ? p[i] : 0.0f;
+            }
+        }
+    }
+}
+template <typename T, int V, bool PART>
+__device__ __forceinline__ void widen(const float* w, int n, float* t) {
+#pragma unroll
+    for (int i = 0; i < V; ++i) {
+        const float x = Words<T, V>::at(w, i);
+        t[i] = !PART || i < n ? x : 0.0f;
+    }
+}
+// V values stored; bf16 rounded two an instruction (to nearest even)
+template <typename T, int V>
+__device__ __forceinline__ void put(T* p, const float* t) {
+    if constexpr (sizeof(T) == 2 && V > 1) {
+        typedef __bf16 two __attribute__((ext_vector_type(2)));
+        uint32_t w[V / 2];
+#pragma unroll
+        for (int i = 0; i < V / 2; ++i) {
+            const two x = {(__bf16)t[2 * i], (__bf16)t[2 * i + 1]};
+            w[i] = __builtin_bit_cast(uint32_t, x);
+        }
+        if constexpr (V == 8) *reinterpret_cast<u4_h*>(p) = u4_h{w[0], w[1], w[2], w[3]};
+        else if constexpr (V == 4) *reinterpret_cast<u2_h*>(p) = u2_h{w[0], w[1]};
+        else *reinterpret_cast<u1_h*>(p) = w[0];
+    } else {
+        IO<T, V>::store(p, t);
+    }
+}
+template <typename T, int V>
+__device__ __forceinline__ void store_few(T* p, const float* t, int n) {
+    if constexpr (V == 1) {
+        if (n & 1) put<T, 1>(p, t);
+    } else {
+        if (n & V) {
+            put<T, V>(p, t);
+            store_few<T, V / 2>(p + V, t + V, n);
+        } else {
+            store_few<T, V / 2>(p, t, n);
+        }
+    }
+}
+template <typename T, int V, bool PART>
+__device__ __forceinline__ void store_part(T* p, const float* t, int n) {
+    if (!PART || n == V) put<T, V>(p, t);
+    else if constexpr (PART && V > 1) store_few<T, V / 2>(p, t, n);
+}
 
 template <int CTRL>
 __device__ __forceinline__ float dpp_f(float x) {

@@ -125,6 +125,15 @@ SYMBOLS = {
     "node_norm_rotary_backward": [ctypes.c_void_p] * 12 + [ctypes.c_float, ctypes.c_void_p, ctypes.c_size_t,
                                                            ctypes.c_void_p],
     "node_norm_rotary_work_bytes": [ctypes.c_void_p] * 5,
+    "node_add_norm": [ctypes.c_void_p] * 3 + [ctypes.c_float] + [ctypes.c_void_p] * 3,
+    "node_add_norm_i8": [ctypes.c_void_p] * 3 + [ctypes.c_float] + [ctypes.c_void_p] * 3,
+    "node_quantize": [ctypes.c_void_p] * 3,
+    "node_add_norm_backward": [ctypes.c_void_p] * 4 + [ctypes.c_float] + [ctypes.c_void_p] * 3 + [ctypes.c_size_t,
+                                                                                              ctypes.c_void_p],
+    "node_add_norm_work_bytes": [ctypes.c_void_p] * 2,
+    "weight8_bytes": [ctypes.c_int32, ctypes.c_int32, ctypes.c_void_p],
+    "weight8_pack": [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_size_t, ctypes.c_void_p],
+    "node_linear_i8": [ctypes.c_void_p] * 5,
     "graph_scratch_bytes": [ctypes.c_void_p, ctypes.c_int64, ctypes.c_int32, ctypes.c_void_p],
     "graph_attach_scratch": [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p, ctypes.c_size_t],
     "graph_scratch_captured": [ctypes.c_void_p, ctypes.c_void_p, ctypes.c_void_p],
@@ -712,6 +721,172 @@ def node_norm_rotary_backward(q, wq, grad_q, k=None, wk=None, grad_k=None, rot: 
     if dwk is not None and wk.dim() != 3:
         dwk = dwk.view(wk.shape)
     return (dq, dwq, dk, dwk) if k is not None else (dq, dwq)
+
+
+# ---------------------------------------------------------------------------
+# the residual stream between layers, and products in 8 bits
+
+# gnnk_rows8 (data, scale, rows, row_stride, cols, reserved) and gnnk_weight8
+# (packed, scale, outs, cols) as bytes
+_ROWS8 = struct.Struct("=QQqqII")
+_WEIGHT8 = struct.Struct("=QQII")
+
+
+def _rows8(q, scale):
+    """gnnk_rows8 bytes of int8 rows and their scales."""
+    if not q.is_cuda or (scale is not None and not scale.is_cuda):
+        raise ValueError("tensors must be on the GPU")
+    if q.dtype is not torch.int8 or q.dim() != 2:
+        raise TypeError("rows in 8 bits are an int8 tensor (rows, columns)")
+    rows, cols = q.shape
+    if scale is not None:
+        if scale.dtype is not torch.float32 or scale.numel() != rows or (rows > 1 and not scale.is_contiguous()):
+            raise ValueError(f"scales must be float32, contiguous, one for each of the {rows} rows")
+    stride = cols
+    if rows and cols:
+        if cols > 1 and q.stride(1) != 1:
+            raise ValueError("the columns of a row must be contiguous")
+        if rows > 1:
+            if q.stride(0) < cols:
+                raise ValueError("row stride smaller than the columns")
+            stride = q.stride(0)
+    return _ROWS8.pack(q.data_ptr(), scale.data_ptr() if scale is not None else 0, rows, stride, cols, 0)
+
+
+def _new_rows8(rows, cols, device):
+    """int8 rows whose stride is a multiple of 16 bytes, and their scales"""
+    q = torch.empty((rows, (cols + 15) & ~15), dtype=torch.int8, device=device)
+    return q if cols % 16 == 0 else q[:, :cols], torch.empty(rows, dtype=torch.float32, device=device)
+
+
+def _columns(x):
+    return x.shape[1] if x.dim() == 2 else x.shape[1] * x.shape[2]
+
+
+def _row(w):
+    """a weight or bias as one row: the elements of any contiguous shape"""
+    if w is None:
+        return None
+    if not w.is_contiguous():
+        raise ValueError("weights and biases must be contiguous")
+    return w.view(1, 1, -1)
+
+
+def node_add_norm(x, residual=None, weight=None, eps: float = 1e-6, out=None, out_sum=None, stream=None):
+    """The residual stream's sum and its norm: h = x + residual, y = weight * h / sqrt(mean(h^2) + eps) over each whole
+    row (of (rows, H, F): all heads).  weight: a row's elements in any shape, or None.  Returns (y, h), or y alone
+    without a residual.  out and out_sum may be x or residual themselves."""
+    x = _as3(x) if x.dim() != 2 else x
+    _here(x, residual, weight, out, out_sum)
+    xd = _desc(x)
+    out, od = _out(x, xd) if out is None else (out, _desc(out))
+    sd = None
+    if residual is not None:
+        out_sum, sd = _out(x, xd) if out_sum is None else (out_sum, _desc(out_sum))
+    elif out_sum is not None:
+        raise ValueError("without a residual the sum is x")
+    _check(load().node_add_norm(xd, _desc(residual), _desc(_row(weight)), eps, sd, od, _stream(stream)))
+    return (out, out_sum) if residual is not None else out
+
+
+def node_add_norm_i8(x, residual=None, weight=None, eps: float = 1e-6, out=None, scale=None, out_sum=None,
+                     stream=None):
+    """node_add_norm with y in 8 bits: (q, scale, h), or (q, scale) without a residual.  q: int8 (rows, columns), a
+    row's largest magnitude being 127, whose rows start 16 bytes apart or a multiple of it; scale: float32 (rows,);
+    scale[n] * q[n] is y.  A row with a NaN or an infinity has scale NaN and values 0."""
+    x = _as3(x) if x.dim() != 2 else x
+    _here(x, residual, weight, out, scale, out_sum)
+    xd = _desc(x)
+    if (out is None) != (scale is None):
+        raise ValueError("out and scale are given together")
+    if out is None:
+        out, scale = _new_rows8(x.shape[0], _columns(x), x.device)
+    sd = None
+    if residual is not None:
+        out_sum, sd = _out(x, xd) if out_sum is None else (out_sum, _desc(out_sum))
+    elif out_sum is not None:
+        raise ValueError("without a residual the sum is x")
+    _check(load().node_add_norm_i8(xd, _desc(residual), _desc(_row(weight)), eps, sd, _rows8(out, scale),
+                                   _stream(stream)))
+    return (out, scale, out_sum) if residual is not None else (out, scale)
+
+
+def node_quantize(x, out=None, scale=None, stream=None):
+    """The rows of x (of (rows, H, F): all heads) in 8 bits: (q, scale), as node_add_norm_i8 makes them."""
+    x = _as3(x) if x.dim() != 2 else x
+    _here(x, out, scale)
+    if (out is None) != (scale is None):
+        raise ValueError("out and scale are given together")
+    if out is None:
+        out, scale = _new_rows8(x.shape[0], _columns(x), x.device)
+    _check(load().node_quantize(_desc(x), _rows8(out, scale), _stream(stream)))
+    return out, scale
+
+
+def node_add_norm_backward(h, weight, grad_y, grad_sum=None, eps: float = 1e-6, want_x: bool = True,
+                           want_weight: bool = True, grad_x=None, stream=None):
+    """Gradients of node_add_norm from that of y and, with grad_sum, that of the sum: (dx, dweight), dx being the
+    gradient of x and of the residual.  h: the sum as node_add_norm returned it (without a residual x).  None where not
+    wanted or without a weight.  grad_x, where dx goes, may be h, grad_y or grad_sum themselves."""
+    h = _as3(h) if h.dim() != 2 else h
+    _here(h, weight, grad_y, grad_sum, grad_x)
+    hd = _desc(h)
+    gx = None
+    if grad_x is not None:
+        gx = _desc(grad_x)
+    elif want_x:
+        grad_x, gx = _out(h, hd)
+    row, dw, gw, wd = _row(weight), None, None, None
+    work, nbytes = None, 0
+    if row is not None:
+        wd = _desc(row)
+        if want_weight:
+            dw, gw = _out(row, wd)
+            need = ctypes.c_size_t(0)
+            _check(load().node_add_norm_work_bytes(hd, ctypes.byref(need)))
+            nbytes = need.value
+            if stream is None:
+                work = torch.empty(nbytes, dtype=torch.uint8, device=h.device)
+            else:
+                with torch.cuda.stream(stream):
+                    work = torch.empty(nbytes, dtype=torch.uint8, device=h.device)
+    _check(load().node_add_norm_backward(hd, wd, _desc(grad_y), _desc(grad_sum), eps, gx, gw, _ptr(work), nbytes,
+                                         _stream(stream)))
+    return grad_x, (dw.view(weight.shape) if dw is not None else None)
+
+
+class Weight8:
+    """A linear layer's weight in 8 bits, laid out for node_linear_i8: values int8 (outs, columns), scale float32
+    (outs,), scale[o] * values[o] being row o.  Both may be changed or dropped afterwards."""
+
+    def __init__(self, values: torch.Tensor, scale: torch.Tensor, stream=None):
+        _here(values, scale)
+        rows = _rows8(values, scale)
+        self.outs, self.cols = values.shape
+        need = ctypes.c_size_t(0)
+        _check(load().weight8_bytes(self.outs, self.cols, ctypes.byref(need)))
+        with torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext():
+            self.packed = torch.empty(need.value, dtype=torch.uint8, device=values.device)
+            self.scale = scale.reshape(-1).clone()
+        _check(load().weight8_pack(rows, self.packed.data_ptr(), need.value, _stream(stream)))
+        self._bytes = _WEIGHT8.pack(self.packed.data_ptr(), self.scale.data_ptr(), self.outs, self.cols)
+
+    @classmethod
+    def quantize(cls, weight: torch.Tensor, stream=None) -> "Weight8":
+        """The weight (outs, columns), float32 or bfloat16, rounded to 8 bits with a scale for each output."""
+        with torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext():
+            return cls(*node_quantize(weight.detach()))
+
+
+def node_linear_i8(weight: Weight8, q, scale, bias=None, dtype=torch.bfloat16, out=None, stream=None):
+    """Rows in 8 bits times a weight in 8 bits: out[n, o] = scale[n] * weight.scale[o] * (q[n] . values[o]) + bias[o],
+    float32 or bfloat16 (dtype, or out's).  The products' sums are exact.  bias: outs values of out's dtype.  No
+    gradient is formed."""
+    _here(weight.packed, q, scale, bias, out)
+    if out is None:
+        out = torch.empty((q.shape[0], weight.outs), dtype=dtype, device=q.device)
+    _check(load().node_linear_i8(_rows8(q, scale), weight._bytes, _desc(_row(bias)), _desc(out), _stream(stream)))
+    return out
 
 
 def dot_aggregate(g: Graph, q, k, v, bias=None, scale: float = None, out=None, stats=None, want_stats: bool = False,

@@ -1,0 +1,158 @@
+"""Products of rows and weights in 8 bits (node_linear_i8, Weight8) against
+their formula in 64 bits, on every kernel, within bounds derived in
+tests/_rows.py."""
+import pytest
+import torch
+
+from paper_1909_01315_amd import gnnk
+from _heads import close
+from _rows import BF16, F32, check_rows8, gen, norm, normal, product, spread
+
+pytestmark = pytest.mark.gpu
+
+TILES = range(8)  # 0: by the sizes
+
+
+@pytest.fixture(autouse=True)
+def reset_options():
+    yield
+    gnnk.set_option("linear8_tile", 0)
+
+
+def rows8(g, n, c, full=False):
+    q = torch.randint(-128 if full else -127, 128, (n, c), generator=g).to(torch.int8)
+    return q, (torch.rand(n, generator=g) + 0.1) * 0.01
+
+
+def check(n, k, o, dtype, tile, bias, pad=0, lead=None, seed=0, full=False):
+    gnnk.set_option("linear8_tile", tile)
+    g = gen(seed + n + 3 * k + 5 * o)
+    q, s = rows8(g, n, k, full)
+    wq, ws = rows8(g, o, k, full)
+    b = normal(g, o, dtype=dtype) if bias else None
+    weight = gnnk.Weight8(spread(wq, pad), ws.cuda())
+    got = gnnk.node_linear_i8(weight, spread(q, pad, lead), s.cuda(), bias=b.cuda() if bias else None, dtype=dtype)
+    assert got.shape == (n, o) and got.dtype is dtype
+    close(got, *product(q, s, wq, ws, b), f"{n} rows, {k} to {o} columns, tile {tile}")
+
+
+@pytest.mark.parametrize("tile", TILES)
+@pytest.mark.parametrize("n,k,o", [
+    (1, 1, 1), (1, 1024, 1536), (2, 16, 16), (3, 17, 5), (16, 64, 64), (17, 127, 65), (37, 128, 63), (5, 129, 130),
+    (64, 282, 141), (65, 376, 256), (100, 47, 47), (129, 513, 200), (257, 256, 300), (300, 1000, 129), (511, 640, 257),
+])
+def test_product(n, k, o, tile):
+    check(n, k, o, BF16, tile, bias=False)
+    check(n, k, o, F32, tile, bias=True, pad=3, lead=1)
+
+
+@pytest.mark.parametrize("tile", TILES)
+def test_rows_at_any_address(tile):
+    for pad, lead in ((1, 0), (1, 1), (5, 2), (13, 13), (16, 0), (16, 4), (2, 2)):
+        check(70, 200, 90, F32, tile, bias=False, pad=pad, lead=lead, full=True)
+
+
+@pytest.mark.parametrize("tile", TILES)
+def test_long_sums_are_exact(tile):
+    """65,536 products of the largest magnitude, whose sum is 2^30, and ones that cancel all but one."""
+    gnnk.set_option("linear8_tile", tile)
+    k = 65536
+    q = torch.full((3, k), -128, dtype=torch.int8)
+    q[1, 1::2] = 127
+    q[2] = 1
+    w = torch.full((2, k), -128, dtype=torch.int8)
+    w[1, 1::2] = 127
+    w[1, 0] = -127
+    weight = gnnk.Weight8(w.cuda(), torch.ones(2, device="cuda"))
+    got = gnnk.node_linear_i8(weight, q.cuda(), torch.ones(3, device="cuda"), dtype=F32).cpu().double()
+    want = q.double() @ w.double().t()
+    assert torch.equal(got, want.float().double())
+    assert float(got[0, 0]) == 2.0 ** 30
+
+
+def test_tiles_agree_bit_for_bit():
+    g = gen(2)
+    q, s = rows8(g, 1000, 700)
+    wq, ws = rows8(g, 500, 700)
+    weight, b = gnnk.Weight8(wq.cuda(), ws.cuda()), normal(g, 500, dtype=BF16).cuda()
+    outs = []
+    for tile in TILES:
+        gnnk.set_option("linear8_tile", tile)
+        outs.append(gnnk.node_linear_i8(weight, q.cuda(), s.cuda(), bias=b))
+    for t in outs[1:]:
+        assert torch.equal(t, outs[0])
+
+
+@pytest.mark.parametrize("tile", TILES)
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_only_the_rows_own_columns_are_written(tile, dtype):
+    gnnk.set_option("linear8_tile", tile)
+    n, k, o = 75, 130, 83
+    g = gen(4)
+    q, s = rows8(g, n, k)
+    wq, ws = rows8(g, o, k)
+    weight = gnnk.Weight8(wq.cuda(), ws.cuda())
+    buf = torch.full((n + 2, o + 7), 7.0, dtype=dtype, device="cuda")
+    own = buf[1:n + 1, 3:3 + o]
+    got = gnnk.node_linear_i8(weight, q.cuda(), s.cuda(), out=own)
+    assert got is own
+    assert torch.equal(own, gnnk.node_linear_i8(weight, q.cuda(), s.cuda(), dtype=dtype))
+    own.fill_(7.0)
+    assert bool((buf == 7.0).all())
+    heads = torch.empty((n, 1, 83), dtype=dtype, device="cuda")
+    assert torch.equal(gnnk.node_linear_i8(weight, q.cuda(), s.cuda(), out=heads).view(n, o),
+                       gnnk.node_linear_i8(weight, q.cuda(), s.cuda(), dtype=dtype))
+
+
+@pytest.mark.parametrize("tile", TILES)
+def test_rows_without_a_finite_scale_stay_alone(tile):
+    gnnk.set_option("linear8_tile", tile)
+    g = gen(9)
+    x = normal(g, 90, 100)
+    x[4, 7], x[80, 99], x[20] = float("nan"), float("inf"), 0.0
+    q, s = gnnk.node_quantize(x.cuda())
+    weight = gnnk.Weight8.quantize(normal(g, 70, 100).cuda())
+    out = gnnk.node_linear_i8(weight, q, s, dtype=F32).cpu()
+    bad = torch.isnan(out).all(1)
+    assert bad.nonzero().view(-1).tolist() == [4, 80] and bool(torch.isfinite(out[~bad]).all())
+    assert bool((out[20] == 0).all())
+
+
+def test_no_rows():
+    weight = gnnk.Weight8.quantize(torch.randn(20, 30, device="cuda"))
+    q, s = gnnk.node_quantize(torch.empty((0, 30), device="cuda"))
+    assert gnnk.node_linear_i8(weight, q, s).shape == (0, 20)
+
+
+def test_a_weight_may_change_after_it_is_laid_out():
+    g = gen(14)
+    q, s = rows8(g, 40, 96)
+    wq, ws = rows8(g, 33, 96)
+    a, b = wq.cuda(), ws.cuda()
+    weight = gnnk.Weight8(a, b)
+    want = gnnk.node_linear_i8(weight, q.cuda(), s.cuda())
+    a.zero_()
+    b.zero_()
+    assert torch.equal(gnnk.node_linear_i8(weight, q.cuda(), s.cuda()), want)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("n,k,o", [(1, 512, 768), (37, 282, 141), (300, 256, 96)])
+def test_a_layer_from_the_stream_to_its_outputs(n, k, o, dtype):
+    """Sum, norm, rows in 8 bits and product, each as the step before it left things."""
+    g = gen(n)
+    x, r = normal(g, n, k, dtype=dtype), (2 * normal(g, n, k)).to(dtype)
+    w, lw = (1 + 0.2 * normal(g, k)).to(dtype), normal(g, o, k) / k ** 0.5
+    wq, ws = gnnk.node_quantize(lw.cuda())
+    check_rows8(wq, ws, lw.double(), 0.0 * lw.double(), "weight")
+    weight = gnnk.Weight8(wq, ws)
+    q, s, h = gnnk.node_add_norm_i8(x.cuda(), r.cuda(), w.cuda(), eps=1e-6)
+    y, bound = norm(x.double() + r.double(), w.double(), 1e-6)
+    check_rows8(q, s, y, bound, "norm")
+    out = gnnk.node_linear_i8(weight, q, s)
+    close(out, *product(q, s, wq, ws, None), "product")
+    # half a step of every value and weight, products' signs at random: within a bound that counts them all alike
+    want = y @ lw.double().t()
+    step = 0.5 * s.cpu().double().view(-1, 1) * lw.double().abs().sum(1) + \
+        0.5 * ws.cpu().double() * (y.abs().sum(1, keepdim=True) + k * s.cpu().double().view(-1, 1))
+    close(out, want, step + 1e-4 * want.abs(), "layer")
