@@ -10,10 +10,11 @@
 // take it: blocks of 64 output columns and 128 of k, in them 2 steps of 64 of
 // k, 4 fragments of 16 output columns, and for each of 64 lanes 16 bytes
 // (row lane % 16 of the fragment, k from lane / 16 * 16 on); zeros past N and
-// K.  Row 4 a + i of fragment j is output column 16 a + 4 j + i of the block:
-// the weight being the instruction's first operand, a lane's results of the
-// four fragments are then 16 columns side by side of one row of the output.
-#include "device.h"
+// K.  Row 4 a + i of fragment j is output column 32 (j / 2) + 8 a + 4 (j % 2) + i
+// of the block: the weight being the instruction's first operand, a lane's
+// results of fragments 2 j and 2 j + 1 are then 8 columns side by side of one
+// row of the output, one store of bf16, and those of the four lanes of a row 32.
+#include "words.h"
 
 namespace gnnk {
 
@@ -25,6 +26,7 @@ typedef int i4_b __attribute__((ext_vector_type(4), aligned(1)));
 
 constexpr int KB = 128;             // bytes of k of a step
 constexpr int WBLOCK = 64 * KB;     // bytes of 64 output columns of a step
+constexpr int LDS_BYTES = 160 * 1024;
 
 __device__ __forceinline__ i32x4 mfma(i32x4 a, i32x4 b, i32x4 c) {
     return __builtin_amdgcn_mfma_i32_16x16x64_i8(a, b, c, 0, 0, 0);
@@ -54,29 +56,50 @@ __device__ __forceinline__ i32x4 load_x(const int8_t* row, int k, int K, const i
     return i32x4{x.x, x.y, x.z, x.w};
 }
 
-// COUNT columns of a row of the output from column n on
+// first of the four output columns that a lane holds of fragment j
+__device__ __forceinline__ int column_of(int j, int lane) { return (j >> 1) * 32 + (lane >> 4) * 8 + (j & 1) * 4; }
+
+// scales and biases of COUNT output columns from n on (those past the last one
+// are not stored)
 template <typename T, int COUNT>
-__device__ __forceinline__ void put_out(const Linear8Args& A, int64_t m, int n, const int* sum) {
-    T* const row = reinterpret_cast<T*>(A.out) + m * A.out_stride;
-    const T* const bias = reinterpret_cast<const T*>(A.bias);
-    const float s = A.xs[m];
+struct Columns {
+    float s[COUNT], b[COUNT];
+    __device__ __forceinline__ void load(const Linear8Args& A, int n) {
+        const T* const bias = reinterpret_cast<const T*>(A.bias);
+        if (n + COUNT <= A.N) {
+#pragma unroll
+            for (int i = 0; i < COUNT; i += 4) IO<float, 4>::load(A.ws + n + i, s + i);
+            if (bias)
+#pragma unroll
+                for (int i = 0; i < COUNT; i += 4) IO<T, 4>::load(bias + n + i, b + i);
+        } else {
+#pragma unroll
+            for (int i = 0; i < COUNT; ++i) {
+                const int c = n + i < A.N ? n + i : A.N - 1;
+                s[i] = A.ws[c];
+                if (bias) b[i] = IO<T, 1>::load1(bias + c);
+            }
+        }
+        if (!bias)
+#pragma unroll
+            for (int i = 0; i < COUNT; ++i) b[i] = 0.0f;
+    }
+};
+
+// COUNT columns of row m of the output from column n on
+template <typename T, int COUNT>
+__device__ __forceinline__ void put_out(const Linear8Args& A, int64_t m, int n, float xs, const Columns<T, COUNT>& c,
+                                        const int* sum) {
+    T* const p = reinterpret_cast<T*>(A.out) + m * A.out_stride + n;
     float t[COUNT];
 #pragma unroll
-    for (int i = 0; i < COUNT; ++i) {
-        const int c = n + i < A.N ? n + i : A.N - 1;
-        t[i] = (float)sum[i] * s * A.ws[c];
-        if (bias) t[i] += IO<T, 1>::load1(bias + c);
-    }
+    for (int i = 0; i < COUNT; ++i) t[i] = fmaf((float)sum[i] * xs, c.s[i], c.b[i]);
     constexpr int V = COUNT < 16 / (int)sizeof(T) ? COUNT : 16 / (int)sizeof(T);
 #pragma unroll
     for (int i = 0; i < COUNT; i += V) {
-        if (n + i + V <= A.N) {
-            IO<T, V>::store(row + n + i, t + i);
-        } else {
-#pragma unroll
-            for (int j = 0; j < V; ++j)
-                if (n + i + j < A.N) IO<T, 1>::store1(row + n + i + j, t[i + j]);
-        }
+        const int left = A.N - n - i;
+        if (left >= V) put<T, V>(p + i, t + i);
+        else if (left > 0) store_few<T, V / 2>(p + i, t + i, left);
     }
 }
 
@@ -85,6 +108,12 @@ __device__ __forceinline__ void put_out(const Linear8Args& A, int64_t m, int n, 
 struct TileArgs {
     int64_t tm, tiles, padded;
     int32_t tn, group;
+};
+
+// the panels of a weight: `width` blocks of 64 output columns each; `split`
+// wavefronts share the panel's columns of the same rows
+struct StreamArgs {
+    int32_t panels, width, split;
 };
 
 // Few rows: a block forms MI * 16 rows of NJ * 16 output columns, its
@@ -138,9 +167,13 @@ __global__ __launch_bounds__(1024) void linear8_few_kernel(Linear8Args A, int wa
         i32x4 t = sums[f * 64 + lane];
         for (int k = 1; k < waves; ++k) t += sums[(k * MI * NJ + f) * 64 + lane];
         const int64_t m = m0 + f / NJ * 16 + (lane & 15);
-        const int n = nb * 64 + (lane >> 4) * 16 + (j0 + f % NJ) * 4;
+        const int n = nb * 64 + column_of(j0 + f % NJ, lane);
         const int r[4] = {t.x, t.y, t.z, t.w};
-        if (m < A.M) put_out<T, 4>(A, m, n, r);
+        if (m < A.M && n < A.N) {
+            Columns<T, 4> c;
+            c.load(A, n);
+            put_out<T, 4>(A, m, n, A.xs[m], c, r);
+        }
     }
 }
 
@@ -235,24 +268,96 @@ __global__ __launch_bounds__(WM * WN * 64, BLOCKS) void linear8_tile_kernel(Line
             if (ks + 1 < KS) put((ks + 1) & 1);
             __syncthreads();
         }
+        float xs[MT];
 #pragma unroll
         for (int i = 0; i < MT; ++i) {
             const int64_t m = m0 + wm + i * 16 + (lane & 15);
-            if (m >= A.M) continue;
+            xs[i] = A.xs[m < A.M ? m : A.M - 1];
+        }
 #pragma unroll
-            for (int j = 0; j < NT / 4; ++j) {
-                const int n = (nb0 + wn + j) * 64 + (lane >> 4) * 16;
-                if (n >= A.N) continue;
-                int r[16];
+        for (int j = 0; j < NT; j += 2) {
+            const int n = (nb0 + wn + (j >> 2)) * 64 + column_of(j & 3, lane);
+            if (n >= A.N) continue;
+            Columns<T, 8> c;
+            c.load(A, n);
 #pragma unroll
-                for (int f = 0; f < 4; ++f) {
-                    const i32x4 v = acc[i][j * 4 + f];
-                    r[4 * f] = v.x;
-                    r[4 * f + 1] = v.y;
-                    r[4 * f + 2] = v.z;
-                    r[4 * f + 3] = v.w;
+            for (int i = 0; i < MT; ++i) {
+                const int64_t m = m0 + wm + i * 16 + (lane & 15);
+                const i32x4 u = acc[i][j], v = acc[i][j + 1];
+                const int r[8] = {u.x, u.y, u.z, u.w, v.x, v.y, v.z, v.w};
+                if (m < A.M) put_out<T, 8>(A, m, n, xs[i], c, r);
+            }
+        }
+    }
+}
+
+// Many rows of at most KS * 128 columns: a block keeps a panel of the weight
+// in LDS and its wavefronts stream rows past it, MI * 16 at a time, which they
+// read straight into registers and hold there for all of the panel's columns.
+// Nothing waits for another wavefront once the panel is there.
+template <typename T, int KS, int MI>
+__global__ __launch_bounds__(1024, 1) void linear8_stream_kernel(Linear8Args A, StreamArgs G) {
+    extern __shared__ int8_t lds[];
+    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+    // the blocks of one run of rows sit on one die, one for each panel
+    const int die = blockIdx.x & 7, at = blockIdx.x >> 3;
+    const int panel = at % G.panels;
+    const int64_t run = (int64_t)(at / G.panels) * 8 + die, runs = (int64_t)(gridDim.x >> 3) / G.panels * 8;
+    const int NB = (A.N + 63) / 64, nb0 = panel * G.width;
+    const int nbs = NB - nb0 < G.width ? NB - nb0 : G.width;  // blocks of 64 output columns
+    {
+        const i32x4* const w = reinterpret_cast<const i32x4*>(A.w + (int64_t)nb0 * KS * WBLOCK);
+        i32x4* const l = reinterpret_cast<i32x4*>(lds);
+        const int pieces = nbs * KS * (WBLOCK / 16);
+        for (int c = tid; c < pieces; c += 1024) l[c] = w[c];
+    }
+    __syncthreads();
+    const int8_t* const end = A.x + (A.M - 1) * A.x_stride + A.K;
+    const int64_t tiles = (A.M + MI * 16 - 1) / (MI * 16);
+    const int part = wave % G.split, teams = 16 / G.split;
+    for (int64_t tile = run + runs * (wave / G.split); tile < tiles; tile += runs * teams) {
+        const int64_t m0 = tile * (MI * 16);
+        const int8_t* row[MI];
+        float xs[MI];
+#pragma unroll
+        for (int i = 0; i < MI; ++i) {
+            const int64_t m = m0 + i * 16 + (lane & 15), mc = m < A.M ? m : A.M - 1;
+            row[i] = A.x + mc * A.x_stride;
+            xs[i] = A.xs[mc];
+        }
+        i32x4 x[KS * 2][MI];
+#pragma unroll
+        for (int k = 0; k < KS * 2; ++k)
+#pragma unroll
+            for (int i = 0; i < MI; ++i) {
+                const int at_k = k * 64 + (lane >> 4) * 16;
+                x[k][i] = k < KS * 2 - 2 ? load_x<false>(row[i], at_k, A.K, end) : load_x<true>(row[i], at_k, A.K, end);
+            }
+        for (int nb = part; nb < nbs; nb += G.split) {
+            const int8_t* const w = lds + nb * KS * WBLOCK + lane * 16;
+#pragma unroll
+            for (int j = 0; j < 4; j += 2) {
+                i32x4 acc[2][MI] = {};
+#pragma unroll
+                for (int k = 0; k < KS * 2; ++k)
+#pragma unroll
+                    for (int f = 0; f < 2; ++f) {
+                        const i32x4 b = *reinterpret_cast<const i32x4*>(w + k * 4096 + (j + f) * 1024);
+#pragma unroll
+                        for (int i = 0; i < MI; ++i) acc[f][i] = mfma(b, x[k][i], acc[f][i]);
+                    }
+                const int n = (nb0 + nb) * 64 + column_of(j, lane);
+                if (n < A.N) {
+                    Columns<T, 8> c;
+                    c.load(A, n);
+#pragma unroll
+                    for (int i = 0; i < MI; ++i) {
+                        const int64_t m = m0 + i * 16 + (lane & 15);
+                        const i32x4 u = acc[0][i], v = acc[1][i];
+                        const int r[8] = {u.x, u.y, u.z, u.w, v.x, v.y, v.z, v.w};
+                        if (m < A.M) put_out<T, 8>(A, m, n, xs[i], c, r);
+                    }
                 }
-                put_out<T, 16>(A, m, n, r);
             }
         }
     }
@@ -267,7 +372,7 @@ __global__ __launch_bounds__(256) void weight8_pack_kernel(const int8_t* w, int6
         const int64_t b = c >> 9;
         const int ks = (int)(b % KS);
         const int r = lane & 15, k = ks * KB + half * 64 + (lane >> 4) * 16;
-        const int64_t n = b / KS * 64 + (r >> 2) * 16 + j * 4 + (r & 3);
+        const int64_t n = b / KS * 64 + (j >> 1) * 32 + (r >> 2) * 8 + (j & 1) * 4 + (r & 3);
         uint32_t x[4] = {0, 0, 0, 0};
         if (n < N)
 #pragma unroll
@@ -297,6 +402,22 @@ void launch_few(const Linear8Args& a, int waves, hipStream_t s) {
                        waves * MI * NJ * 1024, s, a, waves);
 }
 
+template <typename T, int KS>
+void launch_stream(const Linear8Args& a, hipStream_t s) {
+    constexpr int MI = 2, CUS = 32;  // of a die
+    const int NB = (a.N + 63) / 64, most = LDS_BYTES / (KS * WBLOCK);
+    StreamArgs g;
+    g.panels = (NB + most - 1) / most;
+    if (g.panels > CUS) g.panels = CUS;  // (not reached: see launch_t)
+    g.width = (NB + g.panels - 1) / g.panels;
+    const int runs = CUS / g.panels * 8;
+    const int64_t tiles = (a.M + MI * 16 - 1) / (MI * 16);
+    g.split = 1;
+    while (g.split < 16 && g.split < g.width && tiles * g.split < runs * 8) g.split *= 2;
+    hipLaunchKernelGGL((linear8_stream_kernel<T, KS, MI>), dim3((unsigned)(runs * g.panels)), dim3(1024),
+                       g.width * KS * WBLOCK, s, a, g);
+}
+
 template <typename T>
 void launch_t(const Linear8Args& a, int way, hipStream_t s) {
     const int KS = (a.K + KB - 1) / KB, waves = KS < 16 ? KS : 16;
@@ -306,6 +427,12 @@ void launch_t(const Linear8Args& a, int way, hipStream_t s) {
     if (way == 4) return launch_tile<T, 128, 128, 2, 2, 2>(a, s);
     if (way == 5) return launch_tile<T, 256, 128, 4, 2, 1>(a, s);
     if (way == 6) return launch_tile<T, 256, 256, 2, 2, 1>(a, s);
+    if (way == 8 && KS <= 4 && a.N <= 8192) {
+        if (KS == 1) return launch_stream<T, 1>(a, s);
+        if (KS == 2) return launch_stream<T, 2>(a, s);
+        if (KS == 3) return launch_stream<T, 3>(a, s);
+        return launch_stream<T, 4>(a, s);
+    }
     if (way == 7) return launch_tile<T, 256, 256, 4, 2, 1>(a, s);
     launch_tile<T, 128, 128, 2, 2, 2>(a, s);
 }
