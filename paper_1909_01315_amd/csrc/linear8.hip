@@ -9,11 +9,12 @@
 // The weight is laid out once, in the order in which the matrix instructions
 // take it: blocks of 64 output columns and 128 of k, in them 2 steps of 64 of
 // k, 4 fragments of 16 output columns, and for each of 64 lanes 16 bytes
-// (row lane % 16 of the fragment, k from lane / 16 * 16 on); zeros past N and
-// K.  Row 4 a + i of fragment j is output column 32 (j / 2) + 8 a + 4 (j % 2) + i
-// of the block: the weight being the instruction's first operand, a lane's
-// results of fragments 2 j and 2 j + 1 are then 8 columns side by side of one
-// row of the output, one store of bf16, and those of the four lanes of a row 32.
+// (column lane % 16 of the fragment, k from lane / 16 * 16 on); zeros past N
+// and K.  Column c of fragment j is output column 4 c + j of the block: of the
+// four fragments' results a lane then holds 4 columns side by side, of 4 rows,
+// and the 16 lanes of a row write its 64 columns at once, whole lines of 128
+// bytes in bf16.  (With 64 bytes of a row a store, 16 rows at once, 262,144 rows
+// of 256 to 768 columns took 150 us, 127 of them for the stores alone.)
 #include "words.h"
 
 namespace gnnk {
@@ -27,6 +28,7 @@ typedef int i4_b __attribute__((ext_vector_type(4), aligned(1)));
 constexpr int KB = 128;             // bytes of k of a step
 constexpr int WBLOCK = 64 * KB;     // bytes of 64 output columns of a step
 constexpr int LDS_BYTES = 160 * 1024;
+constexpr int64_t PAST_CACHES = 128 << 20;  // bytes of an output that is stored past the caches
 
 __device__ __forceinline__ i32x4 mfma(i32x4 a, i32x4 b, i32x4 c) {
     return __builtin_amdgcn_mfma_i32_16x16x64_i8(a, b, c, 0, 0, 0);
@@ -56,50 +58,78 @@ __device__ __forceinline__ i32x4 load_x(const int8_t* row, int k, int K, const i
     return i32x4{x.x, x.y, x.z, x.w};
 }
 
-// first of the four output columns that a lane holds of fragment j
-__device__ __forceinline__ int column_of(int j, int lane) { return (j >> 1) * 32 + (lane >> 4) * 8 + (j & 1) * 4; }
+// four columns; NT: past the caches
+template <typename T, bool NT>
+__device__ __forceinline__ void put_four(T* p, const float* t) {
+    if constexpr (!NT) {
+        put<T, 4>(p, t);
+    } else if constexpr (sizeof(T) == 2) {
+        const bf16x2 a = {(__bf16)t[0], (__bf16)t[1]}, b = {(__bf16)t[2], (__bf16)t[3]};
+        __builtin_nontemporal_store(u2_h{__builtin_bit_cast(uint32_t, a), __builtin_bit_cast(uint32_t, b)},
+                                    reinterpret_cast<u2_h*>(p));
+    } else {
+        __builtin_nontemporal_store(f4_el{t[0], t[1], t[2], t[3]}, reinterpret_cast<f4_el*>(p));
+    }
+}
 
-// scales and biases of COUNT output columns from n on (those past the last one
-// are not stored)
-template <typename T, int COUNT>
+// The results of 16 rows and 64 output columns that the lanes of a wavefront
+// hold, four rows (lane / 16 * 4 and on) by four columns (lane % 16 * 4 and on)
+// each: scales and biases of the columns, then the rows.
+template <typename T>
 struct Columns {
-    float s[COUNT], b[COUNT];
-    __device__ __forceinline__ void load(const Linear8Args& A, int n) {
+    float s[4], b[4];
+    int n;  // the first column
+    __device__ __forceinline__ void load(const Linear8Args& A, int first, int lane) {
         const T* const bias = reinterpret_cast<const T*>(A.bias);
-        if (n + COUNT <= A.N) {
+        n = first + (lane & 15) * 4;
 #pragma unroll
-            for (int i = 0; i < COUNT; i += 4) IO<float, 4>::load(A.ws + n + i, s + i);
-            if (bias)
-#pragma unroll
-                for (int i = 0; i < COUNT; i += 4) IO<T, 4>::load(bias + n + i, b + i);
+        for (int i = 0; i < 4; ++i) s[i] = b[i] = 0.0f;
+        if (n + 4 <= A.N) {
+            IO<float, 4>::load(A.ws + n, s);
+            if (bias) IO<T, 4>::load(bias + n, b);
         } else {
 #pragma unroll
-            for (int i = 0; i < COUNT; ++i) {
-                const int c = n + i < A.N ? n + i : A.N - 1;
-                s[i] = A.ws[c];
-                if (bias) b[i] = IO<T, 1>::load1(bias + c);
+            for (int i = 0; i < 4; ++i)
+                if (n + i < A.N) {
+                    s[i] = A.ws[n + i];
+                    if (bias) b[i] = IO<T, 1>::load1(bias + n + i);
+                }
+        }
+    }
+    __device__ __forceinline__ void load_lds(const float* ls, const float* lb, int nb, int first, int lane) {
+        n = first + (lane & 15) * 4;
+        IO<float, 4>::load(ls + nb * 64 + (lane & 15) * 4, s);
+        IO<float, 4>::load(lb + nb * 64 + (lane & 15) * 4, b);
+    }
+    // row r of the lane's four, of scale xs
+    __device__ __forceinline__ void row(float xs, int r, i32x4 c0, i32x4 c1, i32x4 c2, i32x4 c3, float* t) const {
+        t[0] = fmaf((float)c0[r] * xs, s[0], b[0]);
+        t[1] = fmaf((float)c1[r] * xs, s[1], b[1]);
+        t[2] = fmaf((float)c2[r] * xs, s[2], b[2]);
+        t[3] = fmaf((float)c3[r] * xs, s[3], b[3]);
+    }
+    // rows m .. m + 3, with scales xs
+    __device__ __forceinline__ void store(const Linear8Args& A, int64_t m, const float* xs, i32x4 c0, i32x4 c1, i32x4 c2,
+                                          i32x4 c3) const {
+        T* p = reinterpret_cast<T*>(A.out) + m * A.out_stride + n;
+#pragma unroll
+        for (int r = 0; r < 4; ++r, p += A.out_stride) {
+            float t[4];
+            row(xs[r], r, c0, c1, c2, c3, t);
+            if (m + r < A.M) {
+                if (n + 4 <= A.N) put<T, 4>(p, t);
+                else if (n < A.N) store_few<T, 2>(p, t, A.N - n);
             }
         }
-        if (!bias)
-#pragma unroll
-            for (int i = 0; i < COUNT; ++i) b[i] = 0.0f;
     }
 };
-
-// COUNT columns of row m of the output from column n on
-template <typename T, int COUNT>
-__device__ __forceinline__ void put_out(const Linear8Args& A, int64_t m, int n, float xs, const Columns<T, COUNT>& c,
-                                        const int* sum) {
-    T* const p = reinterpret_cast<T*>(A.out) + m * A.out_stride + n;
-    float t[COUNT];
+// scales of rows m .. m + 3 (those past the last one are not stored)
+__device__ __forceinline__ void load_scales(const Linear8Args& A, int64_t m, float* xs) {
+    if (m + 4 <= A.M) {
+        IO<float, 4>::load(A.xs + m, xs);
+    } else {
 #pragma unroll
-    for (int i = 0; i < COUNT; ++i) t[i] = fmaf((float)sum[i] * xs, c.s[i], c.b[i]);
-    constexpr int V = COUNT < 16 / (int)sizeof(T) ? COUNT : 16 / (int)sizeof(T);
-#pragma unroll
-    for (int i = 0; i < COUNT; i += V) {
-        const int left = A.N - n - i;
-        if (left >= V) put<T, V>(p + i, t + i);
-        else if (left > 0) store_few<T, V / 2>(p + i, t + i, left);
+        for (int r = 0; r < 4; ++r) xs[r] = m + r < A.M ? A.xs[m + r] : 0.0f;
     }
 }
 
@@ -153,7 +183,7 @@ __global__ __launch_bounds__(1024) void linear8_few_kernel(Linear8Args A, int wa
 #pragma unroll
             for (int i = 0; i < MI; ++i)
 #pragma unroll
-                for (int j = 0; j < NJ; ++j) acc[i][j] = mfma(w[k][j], x[k][i], acc[i][j]);
+                for (int j = 0; j < NJ; ++j) acc[i][j] = mfma(x[k][i], w[k][j], acc[i][j]);
     };
     int ks = wave;
     for (; ks < full; ks += waves) step(ks, std::integral_constant<bool, false>());
@@ -166,14 +196,17 @@ __global__ __launch_bounds__(1024) void linear8_few_kernel(Linear8Args A, int wa
     for (int f = wave; f < MI * NJ; f += waves) {
         i32x4 t = sums[f * 64 + lane];
         for (int k = 1; k < waves; ++k) t += sums[(k * MI * NJ + f) * 64 + lane];
-        const int64_t m = m0 + f / NJ * 16 + (lane & 15);
-        const int n = nb * 64 + column_of(j0 + f % NJ, lane);
-        const int r[4] = {t.x, t.y, t.z, t.w};
-        if (m < A.M && n < A.N) {
-            Columns<T, 4> c;
-            c.load(A, n);
-            put_out<T, 4>(A, m, n, A.xs[m], c, r);
-        }
+        const int64_t m = m0 + f / NJ * 16 + (lane >> 4) * 4;
+        const int n = nb * 64 + (lane & 15) * 4 + j0 + f % NJ;
+        if (n >= A.N) continue;
+        const float s = A.ws[n], b = A.bias ? IO<T, 1>::load1(reinterpret_cast<const T*>(A.bias) + n) : 0.0f;
+        float xs[4];
+        load_scales(A, m, xs);
+#pragma unroll
+        for (int r = 0; r < 4; ++r)
+            if (m + r < A.M)
+                IO<T, 1>::store1(reinterpret_cast<T*>(A.out) + (m + r) * A.out_stride + n,
+                                 fmaf((float)t[r] * xs[r], s, b));
     }
 }
 
@@ -262,31 +295,154 @@ __global__ __launch_bounds__(WM * WN * 64, BLOCKS) void linear8_tile_kernel(Line
                 for (int j = 0; j < NT; ++j) {
                     const i32x4 w = *reinterpret_cast<const i32x4*>(wb + (j >> 2) * WBLOCK + k * 4096 + (j & 3) * 1024);
 #pragma unroll
-                    for (int i = 0; i < MT; ++i) acc[i][j] = mfma(w, x[i], acc[i][j]);
+                    for (int i = 0; i < MT; ++i) acc[i][j] = mfma(x[i], w, acc[i][j]);
                 }
             }
             if (ks + 1 < KS) put((ks + 1) & 1);
             __syncthreads();
         }
-        float xs[MT];
+        float xs[MT][4];
 #pragma unroll
-        for (int i = 0; i < MT; ++i) {
-            const int64_t m = m0 + wm + i * 16 + (lane & 15);
-            xs[i] = A.xs[m < A.M ? m : A.M - 1];
+        for (int i = 0; i < MT; ++i) load_scales(A, m0 + wm + i * 16 + (lane >> 4) * 4, xs[i]);
+#pragma unroll
+        for (int j = 0; j < NT; j += 4) {
+            Columns<T> c;
+            c.load(A, (nb0 + wn + j / 4) * 64, lane);
+#pragma unroll
+            for (int i = 0; i < MT; ++i)
+                c.store(A, m0 + wm + i * 16 + (lane >> 4) * 4, xs[i], acc[i][j], acc[i][j + 1], acc[i][j + 2],
+                        acc[i][j + 3]);
         }
+    }
+}
+
+// 16 bytes a lane from memory, at `from` + `off`, into LDS at `to` + 16 * lane
+// (one `from` and `to` for all lanes).  It counts as a load of the wavefront's
+// (vmcnt) that the compiler does not see: waits for it are written out.
+__device__ __forceinline__ void load_to_lds(const int8_t* from, uint32_t off, uint32_t to) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(off), "s"(from)
+                 : "memory");
+}
+
+// Many rows, long sums: WM by two wavefronts form BM rows of BN output columns.  Steps of 64 bytes of k pass through four LDS buffers, loaded
+// straight into LDS three steps ahead; a wavefront reads the fragments of the
+// next step while it multiplies those of this one.
+template <typename T, int BM, int BN, int WM, int BLOCKS>
+__global__ __launch_bounds__(WM * 128, BLOCKS) void linear8_deep_kernel(Linear8Args A, TileArgs G) {
+    constexpr int MT = BM / WM / 16, NT = BN / 32;
+    constexpr int STAGE = (BM + BN) * 64, XL = BM / 32 / WM, WL = BN / 32 / WM;  // bytes; loads of a wavefront
+    static_assert(NT % 4 == 0 && MT * WM * 16 == BM && XL * WM * 32 == BM && WL * WM * 32 == BN, "");
+    extern __shared__ int8_t lds[];
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) int8_t*)lds;
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
+    const int wm = (wave >> 1) * MT * 16, wn = (wave & 1) * NT / 4;  // first row, first block of 64 output columns
+    const int S = (A.K + 63) / 64, KS = (A.K + KB - 1) / KB, NB = (A.N + 63) / 64;
+
+    for (int64_t b = blockIdx.x; b < G.padded; b += gridDim.x) {
+        const int64_t t = (b & 7) * (G.padded >> 3) + (b >> 3);
+        if (t >= G.tiles) continue;
+        const int64_t group = t / ((int64_t)G.group * G.tn), in = t - group * G.group * G.tn;
+        const int64_t left = G.tm - group * G.group, high = left < G.group ? left : G.group;
+        const int64_t m0 = (group * G.group + in % high) * BM;
+        const int nb0 = (int)(in / high) * (BN / 64);
+
+        // In LDS a row of a step is 64 bytes, its pieces in the order
+        // piece ^ (row / 2 % 4): 8 rows of one piece meet in no bank
+        const int8_t* const xb = A.x + m0 * A.x_stride;
+        uint32_t xo[XL], xe[XL];  // of the last step: pieces past the row's end are any of its bytes (the weight is 0 there)
 #pragma unroll
-        for (int j = 0; j < NT; j += 2) {
-            const int n = (nb0 + wn + (j >> 2)) * 64 + column_of(j & 3, lane);
-            if (n >= A.N) continue;
-            Columns<T, 8> c;
-            c.load(A, n);
+        for (int i = 0; i < XL; ++i) {
+            const int r = (wave * XL + i) * 16 + (lane >> 2), k = ((lane & 3) ^ (r >> 1 & 3)) * 16;
+            xo[i] = (uint32_t)(m0 + r < A.M ? r : (int)(A.M - 1 - m0)) * (uint32_t)A.x_stride + k;
+            xe[i] = (S - 1) * 64 + k < A.K ? xo[i] : xo[i] - k;
+        }
+        const int8_t* wb[WL];
 #pragma unroll
-            for (int i = 0; i < MT; ++i) {
-                const int64_t m = m0 + wm + i * 16 + (lane & 15);
-                const i32x4 u = acc[i][j], v = acc[i][j + 1];
-                const int r[8] = {u.x, u.y, u.z, u.w, v.x, v.y, v.z, v.w};
-                if (m < A.M) put_out<T, 8>(A, m, n, xs[i], c, r);
+        for (int i = 0; i < WL; ++i) {
+            const int piece = wave * WL + i, nb = nb0 + piece / 4;
+            wb[i] = A.w + (int64_t)(nb < NB ? nb : NB - 1) * KS * WBLOCK + piece % 4 * 1024;
+        }
+        auto fill = [&](int s) {
+            const uint32_t to = lds0 + (s & 3) * STAGE;
+#pragma unroll
+            for (int i = 0; i < XL; ++i)
+                load_to_lds(xb + s * 64, s + 1 < S ? xo[i] : xe[i], to + (wave * XL + i) * 1024);
+#pragma unroll
+            for (int i = 0; i < WL; ++i)
+                load_to_lds(wb[i] + (int64_t)s * 4096, lane * 16, to + BM * 64 + (wave * WL + i) * 1024);
+        };
+        i32x4 acc[MT][NT] = {};
+        i32x4 x[2][MT], w[2][NT];
+        const int xr = (wm + (lane & 15)) * 64 + (((lane >> 4) ^ ((lane & 15) >> 1 & 3)) << 4);
+        const int wr = BM * 64 + wn * 4096 + lane * 16;
+        auto read = [&](int s, i32x4 (&xf)[MT], i32x4 (&wf)[NT]) {
+            const int8_t* const at = lds + (s & 3) * STAGE;
+#pragma unroll
+            for (int i = 0; i < MT; ++i) xf[i] = *reinterpret_cast<const i32x4*>(at + xr + i * 1024);
+#pragma unroll
+            for (int j = 0; j < NT; ++j) wf[j] = *reinterpret_cast<const i32x4*>(at + wr + (j >> 2) * 4096 + (j & 3) * 1024);
+        };
+        auto multiply = [&](const i32x4 (&xf)[MT], const i32x4 (&wf)[NT]) {
+#pragma unroll
+            for (int i = 0; i < MT; ++i)
+#pragma unroll
+                for (int j = 0; j < NT; ++j) acc[i][j] = mfma(xf[i], wf[j], acc[i][j]);
+        };
+        // step s: its fragments are on their way into registers; what is
+        // waited for: those, the loads of step s + 1, the other wavefronts
+        auto step = [&](int s, i32x4 (&xf)[MT], i32x4 (&wf)[NT], i32x4 (&xn)[MT], i32x4 (&wn_)[NT], auto ahead) {
+            if constexpr (ahead.value) {
+                if constexpr (XL + WL == 8) asm volatile("s_waitcnt vmcnt(16) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+                else if constexpr (XL + WL == 6) asm volatile("s_waitcnt vmcnt(12) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+                else asm volatile("s_waitcnt vmcnt(8) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+                fill(s + 4);
+            } else {
+                asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
             }
+            if (ahead.value || s + 1 < S) read(s + 1, xn, wn_);
+            multiply(xf, wf);
+        };
+        static_assert(XL + WL == 8 || XL + WL == 6 || XL + WL == 4, "");
+        constexpr std::integral_constant<bool, true> AHEAD;
+        constexpr std::integral_constant<bool, false> LAST;
+        // (the tile before is read to its end, its loads are done)
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+#pragma unroll
+        for (int s = 0; s < 4; ++s)
+            if (s < S) fill(s);
+        if (S >= 4) {
+            if constexpr (XL + WL == 8) asm volatile("s_waitcnt vmcnt(24)\n\ts_barrier" ::: "memory");
+            else if constexpr (XL + WL == 6) asm volatile("s_waitcnt vmcnt(18)\n\ts_barrier" ::: "memory");
+            else asm volatile("s_waitcnt vmcnt(12)\n\ts_barrier" ::: "memory");
+        } else {
+            asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
+        }
+        read(0, x[0], w[0]);
+        int s = 0;
+        for (; s + 5 < S; s += 2) {
+            step(s, x[0], w[0], x[1], w[1], AHEAD);
+            step(s + 1, x[1], w[1], x[0], w[0], AHEAD);
+        }
+        if (s + 4 < S) {  // S odd: one more step to load
+            step(s, x[0], w[0], x[1], w[1], AHEAD);
+            step(s + 1, x[1], w[1], x[0], w[0], LAST);
+            s += 2;
+        }
+        for (; s < S; s += 2) {
+            step(s, x[0], w[0], x[1], w[1], LAST);
+            if (s + 1 < S) step(s + 1, x[1], w[1], x[0], w[0], LAST);
+        }
+        float xs[MT][4];
+#pragma unroll
+        for (int i = 0; i < MT; ++i) load_scales(A, m0 + wm + i * 16 + (lane >> 4) * 4, xs[i]);
+#pragma unroll
+        for (int j = 0; j < NT; j += 4) {
+            Columns<T> c;
+            c.load(A, (nb0 + wn + j / 4) * 64, lane);
+#pragma unroll
+            for (int i = 0; i < MT; ++i)
+                c.store(A, m0 + wm + i * 16 + (lane >> 4) * 4, xs[i], acc[i][j], acc[i][j + 1], acc[i][j + 2],
+                        acc[i][j + 3]);
         }
     }
 }
@@ -295,10 +451,10 @@ __global__ __launch_bounds__(WM * WN * 64, BLOCKS) void linear8_tile_kernel(Line
 // in LDS and its wavefronts stream rows past it, MI * 16 at a time, which they
 // read straight into registers and hold there for all of the panel's columns.
 // Nothing waits for another wavefront once the panel is there.
-template <typename T, int KS, int MI>
-__global__ __launch_bounds__(1024, 1) void linear8_stream_kernel(Linear8Args A, StreamArgs G) {
+template <typename T, int KS, int MI, int WAVES, bool NT>
+__global__ __launch_bounds__(WAVES * 64, 1) void linear8_stream_kernel(Linear8Args A, StreamArgs G) {
     extern __shared__ int8_t lds[];
-    const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
+    const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
     // the blocks of one run of rows sit on one die, one for each panel
     const int die = blockIdx.x & 7, at = blockIdx.x >> 3;
     const int panel = at % G.panels;
@@ -309,55 +465,82 @@ __global__ __launch_bounds__(1024, 1) void linear8_stream_kernel(Linear8Args A, 
         const i32x4* const w = reinterpret_cast<const i32x4*>(A.w + (int64_t)nb0 * KS * WBLOCK);
         i32x4* const l = reinterpret_cast<i32x4*>(lds);
         const int pieces = nbs * KS * (WBLOCK / 16);
-        for (int c = tid; c < pieces; c += 1024) l[c] = w[c];
+        for (int c = tid; c < pieces; c += WAVES * 64) l[c] = w[c];
+    }
+    // scales and biases beside it: read from memory, a wavefront would wait for
+    // its own stores each time
+    float* const ls = reinterpret_cast<float*>(lds + G.width * KS * WBLOCK);
+    float* const lb = ls + G.width * 64;
+    for (int c = tid; c < nbs * 64; c += WAVES * 64) {
+        const int n = nb0 * 64 + c;
+        ls[c] = n < A.N ? A.ws[n] : 0.0f;
+        lb[c] = n < A.N && A.bias ? IO<T, 1>::load1(reinterpret_cast<const T*>(A.bias) + n) : 0.0f;
     }
     __syncthreads();
+    // a lane's place in 16 rows, 32 bits beside an address that the lanes share
+    const uint32_t xo = (uint32_t)(lane & 15) * (uint32_t)A.x_stride + (lane >> 4) * 16;
+    const uint32_t oo = ((uint32_t)(lane >> 4) * 4 * (uint32_t)A.out_stride + (lane & 15) * 4) * sizeof(T);
     const int8_t* const end = A.x + (A.M - 1) * A.x_stride + A.K;
     const int64_t tiles = (A.M + MI * 16 - 1) / (MI * 16);
-    const int part = wave % G.split, teams = 16 / G.split;
-    for (int64_t tile = run + runs * (wave / G.split); tile < tiles; tile += runs * teams) {
+    const int part = wave % G.split, teams = WAVES / G.split;
+    i32x4 x[KS * 2][MI];
+    auto load = [&](int64_t tile) {
         const int64_t m0 = tile * (MI * 16);
-        const int8_t* row[MI];
-        float xs[MI];
+        const int8_t* const base = A.x + m0 * A.x_stride;
+        if (m0 + MI * 16 < A.M && A.K % KB == 0) {
 #pragma unroll
-        for (int i = 0; i < MI; ++i) {
-            const int64_t m = m0 + i * 16 + (lane & 15), mc = m < A.M ? m : A.M - 1;
-            row[i] = A.x + mc * A.x_stride;
-            xs[i] = A.xs[mc];
-        }
-        i32x4 x[KS * 2][MI];
-#pragma unroll
-        for (int k = 0; k < KS * 2; ++k)
-#pragma unroll
-            for (int i = 0; i < MI; ++i) {
-                const int at_k = k * 64 + (lane >> 4) * 16;
-                x[k][i] = k < KS * 2 - 2 ? load_x<false>(row[i], at_k, A.K, end) : load_x<true>(row[i], at_k, A.K, end);
-            }
-        for (int nb = part; nb < nbs; nb += G.split) {
-            const int8_t* const w = lds + nb * KS * WBLOCK + lane * 16;
-#pragma unroll
-            for (int j = 0; j < 4; j += 2) {
-                i32x4 acc[2][MI] = {};
+            for (int i = 0; i < MI; ++i)
 #pragma unroll
                 for (int k = 0; k < KS * 2; ++k)
+                    x[k][i] = load_x<false>(base + i * 16 * A.x_stride + k * 64 + xo, 0, A.K, end);
+        } else {
 #pragma unroll
-                    for (int f = 0; f < 2; ++f) {
-                        const i32x4 b = *reinterpret_cast<const i32x4*>(w + k * 4096 + (j + f) * 1024);
+            for (int i = 0; i < MI; ++i) {
+                const int64_t m = m0 + i * 16 + (lane & 15);
+                const int8_t* const row = A.x + (m < A.M ? m : A.M - 1) * A.x_stride;
 #pragma unroll
-                        for (int i = 0; i < MI; ++i) acc[f][i] = mfma(b, x[k][i], acc[f][i]);
-                    }
-                const int n = (nb0 + nb) * 64 + column_of(j, lane);
-                if (n < A.N) {
-                    Columns<T, 8> c;
-                    c.load(A, n);
-#pragma unroll
-                    for (int i = 0; i < MI; ++i) {
-                        const int64_t m = m0 + i * 16 + (lane & 15);
-                        const i32x4 u = acc[0][i], v = acc[1][i];
-                        const int r[8] = {u.x, u.y, u.z, u.w, v.x, v.y, v.z, v.w};
-                        if (m < A.M) put_out<T, 8>(A, m, n, xs[i], c, r);
-                    }
+                for (int k = 0; k < KS * 2; ++k) {
+                    const int at = k * 64 + (lane >> 4) * 16;
+                    x[k][i] = k < KS * 2 - 2 ? load_x<false>(row, at, A.K, end) : load_x<true>(row, at, A.K, end);
                 }
+            }
+        }
+    };
+    const int64_t step = runs * teams;
+    int64_t tile = run + runs * (wave / G.split);
+    for (; tile < tiles; tile += step) {
+        const int64_t m0 = tile * (MI * 16);
+        float xs[MI][4];
+#pragma unroll
+        for (int i = 0; i < MI; ++i) load_scales(A, m0 + i * 16 + (lane >> 4) * 4, xs[i]);
+        load(tile);
+        for (int nb = part; nb < nbs; nb += G.split) {
+            const int8_t* const w = lds + nb * KS * WBLOCK + lane * 16;
+            i32x4 acc[4][MI] = {};
+#pragma unroll
+            for (int k = 0; k < KS * 2; ++k)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const i32x4 b = *reinterpret_cast<const i32x4*>(w + k * 4096 + j * 1024);
+#pragma unroll
+                    for (int i = 0; i < MI; ++i) acc[j][i] = mfma(x[k][i], b, acc[j][i]);
+                }
+            Columns<T> c;
+            c.load_lds(ls, lb, nb, (nb0 + nb) * 64, lane);
+            if (m0 + MI * 16 <= A.M && (nb0 + nb + 1) * 64 <= A.N) {
+                char* const base = reinterpret_cast<char*>(reinterpret_cast<T*>(A.out) + m0 * A.out_stride + (nb0 + nb) * 64);
+#pragma unroll
+                for (int i = 0; i < MI; ++i)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        float t[4];
+                        c.row(xs[i][r], r, acc[0][i], acc[1][i], acc[2][i], acc[3][i], t);
+                        put_four<T, NT>(reinterpret_cast<T*>(base + (i * 16 + r) * A.out_stride * (int64_t)sizeof(T) + oo), t);
+                    }
+            } else {
+#pragma unroll
+                for (int i = 0; i < MI; ++i)
+                    c.store(A, m0 + i * 16 + (lane >> 4) * 4, xs[i], acc[0][i], acc[1][i], acc[2][i], acc[3][i]);
             }
         }
     }
@@ -372,7 +555,7 @@ __global__ __launch_bounds__(256) void weight8_pack_kernel(const int8_t* w, int6
         const int64_t b = c >> 9;
         const int ks = (int)(b % KS);
         const int r = lane & 15, k = ks * KB + half * 64 + (lane >> 4) * 16;
-        const int64_t n = b / KS * 64 + (j >> 1) * 32 + (r >> 2) * 8 + (j & 1) * 4 + (r & 3);
+        const int64_t n = b / KS * 64 + r * 4 + j;
         uint32_t x[4] = {0, 0, 0, 0};
         if (n < N)
 #pragma unroll
@@ -395,6 +578,19 @@ void launch_tile(const Linear8Args& a, hipStream_t s) {
                        2 * (BM + BN) * KB, s, a, g);
 }
 
+template <typename T, int BM, int BN, int WM, int BLOCKS>
+void launch_deep(const Linear8Args& a, hipStream_t s) {
+    TileArgs g;
+    g.tm = (a.M + BM - 1) / BM;
+    g.tn = (a.N + BN - 1) / BN;
+    g.tiles = g.tm * g.tn;
+    g.padded = (g.tiles + 7) / 8 * 8;
+    g.group = 8;
+    const int64_t blocks = g.padded < (1 << 20) ? g.padded : 1 << 20;
+    hipLaunchKernelGGL((linear8_deep_kernel<T, BM, BN, WM, BLOCKS>), dim3((unsigned)blocks), dim3(WM * 128), 4 * (BM + BN) * 64, s,
+                       a, g);
+}
+
 template <typename T, int MI, int NJ>
 void launch_few(const Linear8Args& a, int waves, hipStream_t s) {
     const int64_t blocks = ((a.M + MI * 16 - 1) / (MI * 16)) * ((a.N + 63) / 64 * (4 / NJ));
@@ -402,10 +598,10 @@ void launch_few(const Linear8Args& a, int waves, hipStream_t s) {
                        waves * MI * NJ * 1024, s, a, waves);
 }
 
-template <typename T, int KS>
+template <typename T, int KS, int MI, int WAVES, bool NT>
 void launch_stream(const Linear8Args& a, hipStream_t s) {
-    constexpr int MI = 2, CUS = 32;  // of a die
-    const int NB = (a.N + 63) / 64, most = LDS_BYTES / (KS * WBLOCK);
+    constexpr int CUS = 32;  // of a die
+    const int NB = (a.N + 63) / 64, most = LDS_BYTES / (KS * WBLOCK + 512);
     StreamArgs g;
     g.panels = (NB + most - 1) / most;
     if (g.panels > CUS) g.panels = CUS;  // (not reached: see launch_t)
@@ -413,27 +609,54 @@ void launch_stream(const Linear8Args& a, hipStream_t s) {
     const int runs = CUS / g.panels * 8;
     const int64_t tiles = (a.M + MI * 16 - 1) / (MI * 16);
     g.split = 1;
-    while (g.split < 16 && g.split < g.width && tiles * g.split < runs * 8) g.split *= 2;
-    hipLaunchKernelGGL((linear8_stream_kernel<T, KS, MI>), dim3((unsigned)(runs * g.panels)), dim3(1024),
-                       g.width * KS * WBLOCK, s, a, g);
+    while (WAVES % (g.split * 2) == 0 && g.split < g.width && tiles * g.split < runs * WAVES / 2) g.split *= 2;
+    hipLaunchKernelGGL((linear8_stream_kernel<T, KS, MI, WAVES, NT>), dim3((unsigned)(runs * g.panels)),
+                       dim3(WAVES * 64), g.width * (KS * WBLOCK + 512), s, a, g);
+}
+
+template <typename T, int MI, int WAVES, bool NT>
+void launch_streams(const Linear8Args& a, hipStream_t s) {
+    const int KS = (a.K + KB - 1) / KB;
+    if (KS == 1) return launch_stream<T, 1, MI, WAVES, NT>(a, s);
+    if (KS == 2) return launch_stream<T, 2, MI, WAVES, NT>(a, s);
+    if (KS == 3) return launch_stream<T, 3, MI, WAVES, NT>(a, s);
+    return launch_stream<T, 4, MI, WAVES, NT>(a, s);
+}
+
+enum Tile { AUTO, FEW, TILE64, TILE128X64, TILE128, DEEP256, DEEP128, TILE256, STREAM, STREAM_PAST };
+
+Tile choose(const Linear8Args& a, int out_bytes, bool pieces, bool streams) {
+    if (a.M <= 64) return FEW;
+    if (streams) return a.M * a.N * out_bytes > PAST_CACHES ? STREAM_PAST : STREAM;
+    if (!pieces) return TILE128;
+    return ((a.M + 255) / 256) * ((a.N + 255) / 256) >= 192 ? DEEP256 : DEEP128;
 }
 
 template <typename T>
-void launch_t(const Linear8Args& a, int way, hipStream_t s) {
+void launch_t(const Linear8Args& a, int tile, hipStream_t s) {
     const int KS = (a.K + KB - 1) / KB, waves = KS < 16 ? KS : 16;
-    if (way ? way == 1 : a.M <= 64) return a.M > 16 ? launch_few<T, 4, 1>(a, waves, s) : launch_few<T, 1, 1>(a, waves, s);
-    if (way == 2) return launch_tile<T, 64, 64, 2, 1, 2>(a, s);
-    if (way == 3) return launch_tile<T, 128, 64, 4, 1, 2>(a, s);
-    if (way == 4) return launch_tile<T, 128, 128, 2, 2, 2>(a, s);
-    if (way == 5) return launch_tile<T, 256, 128, 4, 2, 1>(a, s);
-    if (way == 6) return launch_tile<T, 256, 256, 2, 2, 1>(a, s);
-    if (way == 8 && KS <= 4 && a.N <= 8192) {
-        if (KS == 1) return launch_stream<T, 1>(a, s);
-        if (KS == 2) return launch_stream<T, 2>(a, s);
-        if (KS == 3) return launch_stream<T, 3>(a, s);
-        return launch_stream<T, 4>(a, s);
+    // 16-byte pieces that lie within a row; rows that fit a wavefront's registers
+    const bool pieces = a.K % 16 == 0 && a.x_stride % 16 == 0 && a.x_stride < (1 << 24) && ((uintptr_t)a.x & 15) == 0;
+    const bool streams = KS <= 4 && a.N <= 8192 && a.x_stride < (1 << 24) && a.out_stride < (1 << 24);
+    switch (tile ? tile : choose(a, sizeof(T), pieces, streams)) {
+        case FEW: return a.M > 16 ? launch_few<T, 4, 1>(a, waves, s) : launch_few<T, 1, 1>(a, waves, s);
+        case TILE64: return launch_tile<T, 64, 64, 2, 1, 2>(a, s);
+        case TILE128X64: return launch_tile<T, 128, 64, 4, 1, 2>(a, s);
+        case TILE256: return launch_tile<T, 256, 256, 4, 2, 1>(a, s);
+        case DEEP256:
+            if (pieces) return launch_deep<T, 256, 256, 4, 1>(a, s);
+            break;
+        case DEEP128:
+            if (pieces) return launch_deep<T, 128, 128, 2, 2>(a, s);
+            break;
+        case STREAM:
+            if (streams) return launch_streams<T, 1, 16, false>(a, s);
+            break;
+        case STREAM_PAST:
+            if (streams) return launch_streams<T, 1, 16, true>(a, s);
+            break;
+        default: break;
     }
-    if (way == 7) return launch_tile<T, 256, 256, 4, 2, 1>(a, s);
     launch_tile<T, 128, 128, 2, 2, 2>(a, s);
 }
 
