@@ -324,126 +324,173 @@ __device__ __forceinline__ void load_to_lds(const int8_t* from, uint32_t off, ui
                  : "memory");
 }
 
-// Many rows, long sums: WM by two wavefronts form BM rows of BN output columns.  Steps of 64 bytes of k pass through four LDS buffers, loaded
-// straight into LDS three steps ahead; a wavefront reads the fragments of the
-// next step while it multiplies those of this one.
-template <typename T, int BM, int BN, int WM, int BLOCKS>
+// Many rows, long sums: WM by two wavefronts form BM rows of BN output columns,
+// one tile after another.  Steps of 128 bytes of k, whole lines, are loaded
+// straight into one of two LDS buffers while the one before is multiplied; a
+// wavefront reads the fragments of half a step while it multiplies those of the
+// half before.  The next tile's first two steps load while a tile is stored.
+template <typename T, int BM, int BN, int WM, int BLOCKS, bool NT_OUT>
 __global__ __launch_bounds__(WM * 128, BLOCKS) void linear8_deep_kernel(Linear8Args A, TileArgs G) {
     constexpr int MT = BM / WM / 16, NT = BN / 32;
-    constexpr int STAGE = (BM + BN) * 64, XL = BM / 32 / WM, WL = BN / 32 / WM;  // bytes; loads of a wavefront
-    static_assert(NT % 4 == 0 && MT * WM * 16 == BM && XL * WM * 32 == BM && WL * WM * 32 == BN, "");
+    constexpr int STAGE = (BM + BN) * KB, XL = BM / 16 / WM, WL = BN / 16 / WM;  // bytes; loads of a wavefront
+    static_assert(NT % 4 == 0 && MT * WM * 16 == BM && XL * WM * 16 == BM && WL * WM * 16 == BN, "");
+    static_assert(BM == BN && BM + BN == WM * 128, "a thread holds one column's scale or one row's");
     extern __shared__ int8_t lds[];
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) int8_t*)lds;
+    float* const ls = reinterpret_cast<float*>(lds + 2 * STAGE);  // scales, biases of columns, scales of rows
+    float* const lb = ls + BN;
+    float* const lx = lb + BN;
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
     const int wm = (wave >> 1) * MT * 16, wn = (wave & 1) * NT / 4;  // first row, first block of 64 output columns
-    const int S = (A.K + 63) / 64, KS = (A.K + KB - 1) / KB, NB = (A.N + 63) / 64;
+    const int S = (A.K + KB - 1) / KB, NB = (A.N + 63) / 64;
 
-    for (int64_t b = blockIdx.x; b < G.padded; b += gridDim.x) {
+    // In LDS a row of a step is 128 bytes, its pieces in the order
+    // piece ^ (row % 8): 8 rows of one piece meet in no bank
+    const int piece = ((lane & 7) ^ (lane >> 3)) * 16;
+    // (pieces past the row's end are any of its bytes: the weight is 0 there)
+    const int past = (S - 1) * KB + piece < A.K ? 0 : piece;
+    const int xr = (wm + (lane & 15)) * KB, wr = BM * KB + wn * WBLOCK + lane * 16;
+
+    int64_t m0 = 0;
+    int nb0 = 0;
+    const int8_t* xb = nullptr;
+    uint32_t xo[XL];
+    float scale = 0.0f, bias = 0.0f;
+    // the tile of number b: its place, its scales; false past the last one
+    auto begin = [&](int64_t b) {
+        // blocks are dealt to the eight dies in turn: each gets a run of tiles
         const int64_t t = (b & 7) * (G.padded >> 3) + (b >> 3);
-        if (t >= G.tiles) continue;
+        if (b >= G.padded || t >= G.tiles) return false;
         const int64_t group = t / ((int64_t)G.group * G.tn), in = t - group * G.group * G.tn;
         const int64_t left = G.tm - group * G.group, high = left < G.group ? left : G.group;
-        const int64_t m0 = (group * G.group + in % high) * BM;
-        const int nb0 = (int)(in / high) * (BN / 64);
-
-        // In LDS a row of a step is 64 bytes, its pieces in the order
-        // piece ^ (row / 2 % 4): 8 rows of one piece meet in no bank
-        const int8_t* const xb = A.x + m0 * A.x_stride;
-        uint32_t xo[XL], xe[XL];  // of the last step: pieces past the row's end are any of its bytes (the weight is 0 there)
+        m0 = (group * G.group + in % high) * BM;
+        nb0 = (int)(in / high) * (BN / 64);
+        xb = A.x + m0 * A.x_stride;
 #pragma unroll
         for (int i = 0; i < XL; ++i) {
-            const int r = (wave * XL + i) * 16 + (lane >> 2), k = ((lane & 3) ^ (r >> 1 & 3)) * 16;
-            xo[i] = (uint32_t)(m0 + r < A.M ? r : (int)(A.M - 1 - m0)) * (uint32_t)A.x_stride + k;
-            xe[i] = (S - 1) * 64 + k < A.K ? xo[i] : xo[i] - k;
+            const int r = (wave * XL + i) * 8 + (lane >> 3);
+            xo[i] = (uint32_t)(m0 + r < A.M ? r : (int)(A.M - 1 - m0)) * (uint32_t)A.x_stride + piece;
         }
-        const int8_t* wb[WL];
-#pragma unroll
-        for (int i = 0; i < WL; ++i) {
-            const int piece = wave * WL + i, nb = nb0 + piece / 4;
-            wb[i] = A.w + (int64_t)(nb < NB ? nb : NB - 1) * KS * WBLOCK + piece % 4 * 1024;
+        if (tid < BN) {
+            const int n = nb0 * 64 + tid, c = n < A.N ? n : A.N - 1;
+            scale = A.ws[c];
+            bias = A.bias ? IO<T, 1>::load1(reinterpret_cast<const T*>(A.bias) + c) : 0.0f;
+        } else {
+            const int64_t m = m0 + tid - BN;
+            scale = A.xs[m < A.M ? m : A.M - 1];
         }
-        auto fill = [&](int s) {
-            const uint32_t to = lds0 + (s & 3) * STAGE;
+        return true;
+    };
+    // loads `first` to `last` of a wavefront's for step s
+    auto fill = [&](int s, int first, int last) {
+        const uint32_t to = lds0 + (s & 1) * STAGE;
+        const int off = s + 1 < S ? 0 : past;
 #pragma unroll
-            for (int i = 0; i < XL; ++i)
-                load_to_lds(xb + s * 64, s + 1 < S ? xo[i] : xe[i], to + (wave * XL + i) * 1024);
-#pragma unroll
-            for (int i = 0; i < WL; ++i)
-                load_to_lds(wb[i] + (int64_t)s * 4096, lane * 16, to + BM * 64 + (wave * WL + i) * 1024);
-        };
-        i32x4 acc[MT][NT] = {};
-        i32x4 x[2][MT], w[2][NT];
-        const int xr = (wm + (lane & 15)) * 64 + (((lane >> 4) ^ ((lane & 15) >> 1 & 3)) << 4);
-        const int wr = BM * 64 + wn * 4096 + lane * 16;
-        auto read = [&](int s, i32x4 (&xf)[MT], i32x4 (&wf)[NT]) {
-            const int8_t* const at = lds + (s & 3) * STAGE;
-#pragma unroll
-            for (int i = 0; i < MT; ++i) xf[i] = *reinterpret_cast<const i32x4*>(at + xr + i * 1024);
-#pragma unroll
-            for (int j = 0; j < NT; ++j) wf[j] = *reinterpret_cast<const i32x4*>(at + wr + (j >> 2) * 4096 + (j & 3) * 1024);
-        };
-        auto multiply = [&](const i32x4 (&xf)[MT], const i32x4 (&wf)[NT]) {
-#pragma unroll
-            for (int i = 0; i < MT; ++i)
-#pragma unroll
-                for (int j = 0; j < NT; ++j) acc[i][j] = mfma(xf[i], wf[j], acc[i][j]);
-        };
-        // step s: its fragments are on their way into registers; what is
-        // waited for: those, the loads of step s + 1, the other wavefronts
-        auto step = [&](int s, i32x4 (&xf)[MT], i32x4 (&wf)[NT], i32x4 (&xn)[MT], i32x4 (&wn_)[NT], auto ahead) {
-            if constexpr (ahead.value) {
-                if constexpr (XL + WL == 8) asm volatile("s_waitcnt vmcnt(16) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-                else if constexpr (XL + WL == 6) asm volatile("s_waitcnt vmcnt(12) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-                else asm volatile("s_waitcnt vmcnt(8) lgkmcnt(0)\n\ts_barrier" ::: "memory");
-                fill(s + 4);
+        for (int l = 0; l < XL + WL; ++l) {
+            if (l < first || l >= last) continue;
+            if (l < XL) {
+                load_to_lds(xb + s * KB, xo[l < XL ? l : 0] - off, to + (wave * XL + l) * 1024);
             } else {
-                asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+                const int part = wave * WL + l - XL, nb = nb0 + part / 8;
+                load_to_lds(A.w + ((int64_t)(nb < NB ? nb : NB - 1) * S + s) * WBLOCK + part % 8 * 1024, lane * 16,
+                            to + BM * KB + part * 1024);
             }
-            if (ahead.value || s + 1 < S) read(s + 1, xn, wn_);
-            multiply(xf, wf);
-        };
-        static_assert(XL + WL == 8 || XL + WL == 6 || XL + WL == 4, "");
-        constexpr std::integral_constant<bool, true> AHEAD;
-        constexpr std::integral_constant<bool, false> LAST;
-        // (the tile before is read to its end, its loads are done)
+        }
+    };
+    i32x4 x[2][MT], w[2][NT];
+    i32x4 acc[MT][NT];
+    // part of the fragments of half a step: four of the weight's, or the rows'
+    constexpr int PARTS = NT / 4 + 1;
+    auto read = [&](int s, int half, int part) {
+        const int8_t* const at = lds + (s & 1) * STAGE;
+        if (part < NT / 4) {
+#pragma unroll
+            for (int j = 0; j < 4; ++j)
+                w[half][part * 4 + j] = *reinterpret_cast<const i32x4*>(at + wr + half * 4096 + part * WBLOCK + j * 1024);
+        } else {
+            const int p = ((half * 4 + (lane >> 4)) ^ (lane & 7)) << 4;
+#pragma unroll
+            for (int i = 0; i < MT; ++i) x[half][i] = *reinterpret_cast<const i32x4*>(at + xr + p + i * 16 * KB);
+        }
+    };
+    // half a step; the fragments of the next half, of step `rs`, and the loads
+    // of step `fs` (negative: none) are issued between its products, lest they
+    // hold them up
+    auto half_step = [&](int half, int rs, int fs) {
+#pragma unroll
+        for (int i = 0; i < MT; ++i) {
+#pragma unroll
+            for (int j = 0; j < NT; ++j) acc[i][j] = mfma(x[half][i], w[half][j], acc[i][j]);
+            __builtin_amdgcn_sched_barrier(0);
+            if (rs >= 0 && i < PARTS) read(rs, half ^ 1, i);
+            if (fs >= 0) fill(fs, i * (XL + WL) / MT, (i + 1) * (XL + WL) / MT);
+            __builtin_amdgcn_sched_barrier(0);
+        }
+    };
+
+    int64_t b = blockIdx.x;
+    if (!begin(b)) return;
+    fill(0, 0, XL + WL);
+    if (S > 1) fill(1, 0, XL + WL);
+    for (bool more = true; more;) {
+        if (tid < BN) {
+            ls[tid] = scale;
+            lb[tid] = bias;
+        } else {
+            lx[tid - BN] = scale;
+        }
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
 #pragma unroll
-        for (int s = 0; s < 4; ++s)
-            if (s < S) fill(s);
-        if (S >= 4) {
-            if constexpr (XL + WL == 8) asm volatile("s_waitcnt vmcnt(24)\n\ts_barrier" ::: "memory");
-            else if constexpr (XL + WL == 6) asm volatile("s_waitcnt vmcnt(18)\n\ts_barrier" ::: "memory");
-            else asm volatile("s_waitcnt vmcnt(12)\n\ts_barrier" ::: "memory");
-        } else {
-            asm volatile("s_waitcnt vmcnt(0)\n\ts_barrier" ::: "memory");
+        for (int i = 0; i < MT; ++i)
+#pragma unroll
+            for (int j = 0; j < NT; ++j) acc[i][j] = i32x4{0, 0, 0, 0};
+#pragma unroll
+        for (int p = 0; p < PARTS; ++p) read(0, 0, p);
+        for (int s = 0; s + 1 < S; ++s) {
+            half_step(0, s, -1);
+            // the loads of step s + 1 are there, and step s is read to its end
+            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+            half_step(1, s + 1, s + 2 < S ? s + 2 : -1);
         }
-        read(0, x[0], w[0]);
-        int s = 0;
-        for (; s + 5 < S; s += 2) {
-            step(s, x[0], w[0], x[1], w[1], AHEAD);
-            step(s + 1, x[1], w[1], x[0], w[0], AHEAD);
+        half_step(0, S - 1, -1);
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        const int64_t m = m0 + wm;
+        const int nb = nb0 + wn;
+        b += gridDim.x;
+        more = begin(b);
+        if (more) {
+            fill(0, 0, XL + WL);
+            if (S > 1) fill(1, 0, XL + WL);
         }
-        if (s + 4 < S) {  // S odd: one more step to load
-            step(s, x[0], w[0], x[1], w[1], AHEAD);
-            step(s + 1, x[1], w[1], x[0], w[0], LAST);
-            s += 2;
-        }
-        for (; s < S; s += 2) {
-            step(s, x[0], w[0], x[1], w[1], LAST);
-            if (s + 1 < S) step(s + 1, x[1], w[1], x[0], w[0], LAST);
-        }
+        half_step(1, -1, -1);
+
+        const uint32_t oo = ((uint32_t)(lane >> 4) * 4 * (uint32_t)A.out_stride + (lane & 15) * 4) * sizeof(T);
         float xs[MT][4];
 #pragma unroll
-        for (int i = 0; i < MT; ++i) load_scales(A, m0 + wm + i * 16 + (lane >> 4) * 4, xs[i]);
+        for (int i = 0; i < MT; ++i) IO<float, 4>::load(lx + wm + i * 16 + (lane >> 4) * 4, xs[i]);
 #pragma unroll
         for (int j = 0; j < NT; j += 4) {
             Columns<T> c;
-            c.load(A, (nb0 + wn + j / 4) * 64, lane);
+            c.load_lds(ls, lb, wn + j / 4, (nb + j / 4) * 64, lane);
+            if (m + MT * 16 <= A.M && (nb + j / 4 + 1) * 64 <= A.N) {
+                char* const base = reinterpret_cast<char*>(reinterpret_cast<T*>(A.out) + m * A.out_stride + (nb + j / 4) * 64);
 #pragma unroll
-            for (int i = 0; i < MT; ++i)
-                c.store(A, m0 + wm + i * 16 + (lane >> 4) * 4, xs[i], acc[i][j], acc[i][j + 1], acc[i][j + 2],
-                        acc[i][j + 3]);
+                for (int i = 0; i < MT; ++i)
+#pragma unroll
+                    for (int r = 0; r < 4; ++r) {
+                        float t[4];
+                        c.row(xs[i][r], r, acc[i][j], acc[i][j + 1], acc[i][j + 2], acc[i][j + 3], t);
+                        put_four<T, NT_OUT>(reinterpret_cast<T*>(base + (i * 16 + r) * A.out_stride * (int64_t)sizeof(T) + oo), t);
+                    }
+            } else {
+#pragma unroll
+                for (int i = 0; i < MT; ++i)
+                    c.store(A, m + i * 16 + (lane >> 4) * 4, xs[i], acc[i][j], acc[i][j + 1], acc[i][j + 2],
+                            acc[i][j + 3]);
+            }
         }
+        // (the scales are read to their end)
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
     }
 }
 
@@ -578,7 +625,7 @@ void launch_tile(const Linear8Args& a, hipStream_t s) {
                        2 * (BM + BN) * KB, s, a, g);
 }
 
-template <typename T, int BM, int BN, int WM, int BLOCKS>
+template <typename T, int BM, int BN, int WM, int BLOCKS, bool NT_OUT>
 void launch_deep(const Linear8Args& a, hipStream_t s) {
     TileArgs g;
     g.tm = (a.M + BM - 1) / BM;
@@ -586,9 +633,9 @@ void launch_deep(const Linear8Args& a, hipStream_t s) {
     g.tiles = g.tm * g.tn;
     g.padded = (g.tiles + 7) / 8 * 8;
     g.group = 8;
-    const int64_t blocks = g.padded < (1 << 20) ? g.padded : 1 << 20;
-    hipLaunchKernelGGL((linear8_deep_kernel<T, BM, BN, WM, BLOCKS>), dim3((unsigned)blocks), dim3(WM * 128), 4 * (BM + BN) * 64, s,
-                       a, g);
+    const int64_t blocks = g.padded < 256 * BLOCKS ? g.padded : 256 * BLOCKS;
+    hipLaunchKernelGGL((linear8_deep_kernel<T, BM, BN, WM, BLOCKS, NT_OUT>), dim3((unsigned)blocks), dim3(WM * 128),
+                       2 * (BM + BN) * KB + (BM + 2 * BN) * 4, s, a, g);
 }
 
 template <typename T, int MI, int NJ>
@@ -636,7 +683,8 @@ template <typename T>
 void launch_t(const Linear8Args& a, int tile, hipStream_t s) {
     const int KS = (a.K + KB - 1) / KB, waves = KS < 16 ? KS : 16;
     // 16-byte pieces that lie within a row; rows that fit a wavefront's registers
-    const bool pieces = a.K % 16 == 0 && a.x_stride % 16 == 0 && a.x_stride < (1 << 24) && ((uintptr_t)a.x & 15) == 0;
+    const bool pieces = a.K % 16 == 0 && a.x_stride % 16 == 0 && ((uintptr_t)a.x & 15) == 0 && a.x_stride < (1 << 24) &&
+                        a.out_stride < (1 << 24);
     const bool streams = KS <= 4 && a.N <= 8192 && a.x_stride < (1 << 24) && a.out_stride < (1 << 24);
     switch (tile ? tile : choose(a, sizeof(T), pieces, streams)) {
         case FEW: return a.M > 16 ? launch_few<T, 4, 1>(a, waves, s) : launch_few<T, 1, 1>(a, waves, s);
@@ -644,10 +692,10 @@ void launch_t(const Linear8Args& a, int tile, hipStream_t s) {
         case TILE128X64: return launch_tile<T, 128, 64, 4, 1, 2>(a, s);
         case TILE256: return launch_tile<T, 256, 256, 4, 2, 1>(a, s);
         case DEEP256:
-            if (pieces) return launch_deep<T, 256, 256, 4, 1>(a, s);
+            if (pieces) return launch_deep<T, 256, 256, 4, 1, false>(a, s);
             break;
         case DEEP128:
-            if (pieces) return launch_deep<T, 128, 128, 2, 2>(a, s);
+            if (pieces) return launch_deep<T, 128, 128, 2, 2, false>(a, s);
             break;
         case STREAM:
             if (streams) return launch_streams<T, 1, 16, false>(a, s);
