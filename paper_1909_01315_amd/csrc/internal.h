@@ -348,7 +348,7 @@ struct Linear8Args {
     int32_t N, K;
 };
 // tile: 0 by the sizes, otherwise the kernel of that number
-constexpr int LINEAR8_TILES = 9;
+constexpr int LINEAR8_TILES = 7;
 hipError_t launch_linear8(const Linear8Args& a, int dtype, int tile, hipStream_t s);
 hipError_t launch_weight8_pack(const int8_t* w, int64_t stride, int32_t N, int32_t K, int8_t* packed, hipStream_t s);
 hipError_t launch_fill_rows(const void* ptr, int ptr64, int64_t n_rows, int64_t n_edges, int32_t* row,

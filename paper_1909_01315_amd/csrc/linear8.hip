@@ -28,7 +28,10 @@ typedef int i4_b __attribute__((ext_vector_type(4), aligned(1)));
 constexpr int KB = 128;             // bytes of k of a step
 constexpr int WBLOCK = 64 * KB;     // bytes of 64 output columns of a step
 constexpr int LDS_BYTES = 160 * 1024;
-constexpr int64_t PAST_CACHES = 128 << 20;  // bytes of an output that is stored past the caches
+// bytes of an output that is stored past the caches (the last one holds 256 MB):
+// 262,144 rows of 768 columns of bf16, 403 MB, 101 -> 81 us; 100,000 rows of 600,
+// 120 MB, 57 -> 76
+constexpr int64_t PAST_CACHES = 192 << 20;
 
 __device__ __forceinline__ i32x4 mfma(i32x4 a, i32x4 b, i32x4 c) {
     return __builtin_amdgcn_mfma_i32_16x16x64_i8(a, b, c, 0, 0, 0);
@@ -329,7 +332,7 @@ __device__ __forceinline__ void load_to_lds(const int8_t* from, uint32_t off, ui
 // straight into one of two LDS buffers while the one before is multiplied; a
 // wavefront reads the fragments of half a step while it multiplies those of the
 // half before.  The next tile's first two steps load while a tile is stored.
-template <typename T, int BM, int BN, int WM, int BLOCKS, bool NT_OUT>
+template <typename T, int BM, int BN, int WM, int BLOCKS, bool RAGGED, bool PAST>
 __global__ __launch_bounds__(WM * 128, BLOCKS) void linear8_deep_kernel(Linear8Args A, TileArgs G) {
     constexpr int MT = BM / WM / 16, NT = BN / 32;
     constexpr int STAGE = (BM + BN) * KB, XL = BM / 16 / WM, WL = BN / 16 / WM;  // bytes; loads of a wavefront
@@ -349,6 +352,7 @@ __global__ __launch_bounds__(WM * 128, BLOCKS) void linear8_deep_kernel(Linear8A
     const int piece = ((lane & 7) ^ (lane >> 3)) * 16;
     // (pieces past the row's end are any of its bytes: the weight is 0 there)
     const int past = (S - 1) * KB + piece < A.K ? 0 : piece;
+    const int8_t* const end = A.x + (A.M - 1) * A.x_stride + A.K;
     const int xr = (wm + (lane & 15)) * KB, wr = BM * KB + wn * WBLOCK + lane * 16;
 
     int64_t m0 = 0;
@@ -389,7 +393,18 @@ __global__ __launch_bounds__(WM * 128, BLOCKS) void linear8_deep_kernel(Linear8A
         for (int l = 0; l < XL + WL; ++l) {
             if (l < first || l >= last) continue;
             if (l < XL) {
-                load_to_lds(xb + s * KB, xo[l < XL ? l : 0] - off, to + (wave * XL + l) * 1024);
+                const uint32_t at = xo[l < XL ? l : 0] - off, place = to + (wave * XL + l) * 1024;
+                if (!RAGGED || s + 1 < S) {
+                    load_to_lds(xb + s * KB, at, place);
+                } else {
+                    // (the last row of all: its last piece may pass the tensor's end)
+                    const int8_t* const from = xb + s * KB + at;
+                    if (from + 16 <= end)
+                        load_to_lds(xb + s * KB, at, place);
+                    else
+                        *reinterpret_cast<i32x4*>(lds + (place - lds0) + lane * 16) =
+                            load_x<true>(from, 0, (int)(end - from), end);
+                }
             } else {
                 const int part = wave * WL + l - XL, nb = nb0 + part / 8;
                 load_to_lds(A.w + ((int64_t)(nb < NB ? nb : NB - 1) * S + s) * WBLOCK + part % 8 * 1024, lane * 16,
@@ -480,7 +495,7 @@ __global__ __launch_bounds__(WM * 128, BLOCKS) void linear8_deep_kernel(Linear8A
                     for (int r = 0; r < 4; ++r) {
                         float t[4];
                         c.row(xs[i][r], r, acc[i][j], acc[i][j + 1], acc[i][j + 2], acc[i][j + 3], t);
-                        put_four<T, NT_OUT>(reinterpret_cast<T*>(base + (i * 16 + r) * A.out_stride * (int64_t)sizeof(T) + oo), t);
+                        put_four<T, PAST>(reinterpret_cast<T*>(base + (i * 16 + r) * A.out_stride * (int64_t)sizeof(T) + oo), t);
                     }
             } else {
 #pragma unroll
@@ -625,8 +640,8 @@ void launch_tile(const Linear8Args& a, hipStream_t s) {
                        2 * (BM + BN) * KB, s, a, g);
 }
 
-template <typename T, int BM, int BN, int WM, int BLOCKS, bool NT_OUT>
-void launch_deep(const Linear8Args& a, hipStream_t s) {
+template <typename T, int BM, int BN, int WM, int BLOCKS, bool RAGGED, bool PAST>
+void launch_deep_of(const Linear8Args& a, hipStream_t s) {
     TileArgs g;
     g.tm = (a.M + BM - 1) / BM;
     g.tn = (a.N + BN - 1) / BN;
@@ -634,8 +649,18 @@ void launch_deep(const Linear8Args& a, hipStream_t s) {
     g.padded = (g.tiles + 7) / 8 * 8;
     g.group = 8;
     const int64_t blocks = g.padded < 256 * BLOCKS ? g.padded : 256 * BLOCKS;
-    hipLaunchKernelGGL((linear8_deep_kernel<T, BM, BN, WM, BLOCKS, NT_OUT>), dim3((unsigned)blocks), dim3(WM * 128),
+    hipLaunchKernelGGL((linear8_deep_kernel<T, BM, BN, WM, BLOCKS, RAGGED, PAST>), dim3((unsigned)blocks), dim3(WM * 128),
                        2 * (BM + BN) * KB + (BM + 2 * BN) * 4, s, a, g);
+}
+
+template <typename T, int BM, int BN, int WM, int BLOCKS>
+void launch_deep(const Linear8Args& a, hipStream_t s) {
+    const bool past = a.M * a.N * (int64_t)sizeof(T) > PAST_CACHES;
+    if (a.K % 16)
+        return past ? launch_deep_of<T, BM, BN, WM, BLOCKS, true, true>(a, s)
+                    : launch_deep_of<T, BM, BN, WM, BLOCKS, true, false>(a, s);
+    return past ? launch_deep_of<T, BM, BN, WM, BLOCKS, false, true>(a, s)
+                : launch_deep_of<T, BM, BN, WM, BLOCKS, false, false>(a, s);
 }
 
 template <typename T, int MI, int NJ>
@@ -667,35 +692,55 @@ void launch_streams(const Linear8Args& a, hipStream_t s) {
     if (KS == 1) return launch_stream<T, 1, MI, WAVES, NT>(a, s);
     if (KS == 2) return launch_stream<T, 2, MI, WAVES, NT>(a, s);
     if (KS == 3) return launch_stream<T, 3, MI, WAVES, NT>(a, s);
-    return launch_stream<T, 4, MI, WAVES, NT>(a, s);
+    if (KS == 4) return launch_stream<T, 4, MI, WAVES, NT>(a, s);
+    if (KS == 5) return launch_stream<T, 5, MI, WAVES, NT>(a, s);
+    if (KS == 6) return launch_stream<T, 6, MI, WAVES, NT>(a, s);
+    if (KS == 7) return launch_stream<T, 7, MI, WAVES, NT>(a, s);
+    return launch_stream<T, 8, MI, WAVES, NT>(a, s);
 }
 
-enum Tile { AUTO, FEW, TILE64, TILE128X64, TILE128, DEEP256, DEEP128, TILE256, STREAM, STREAM_PAST };
+enum Tile { AUTO, FEW, TILE64, TILE128, DEEP128, DEEP256, STREAM, STREAM_PAST };
 
-Tile choose(const Linear8Args& a, int out_bytes, bool pieces, bool streams) {
-    if (a.M <= 64) return FEW;
-    if (streams) return a.M * a.N * out_bytes > PAST_CACHES ? STREAM_PAST : STREAM;
-    if (!pieces) return TILE128;
-    return ((a.M + 255) / 256) * ((a.N + 255) / 256) >= 192 ? DEEP256 : DEEP128;
+// The kernel for a product, by what 10 to 300,000 rows of 128 to 4,096 columns
+// measured (us; a call of few rows takes 6.5 on the host):
+//  - few rows, or so few products for their depth that one block after another
+//    would read long sums: FEW (2,048 to 2,048 columns, 130 rows 9.2, DEEP128
+//    11.0, 300 rows 16.6 and 11.6; 4,096 to 1,024, 200 rows 11 and 18)
+//  - rows of up to 512 columns, and up to 1,024 where they lie at any address:
+//    STREAM (100,000 rows, 512 to 512 columns 34, DEEP128 40, TILE128 60; 600 to
+//    600 at any address 57, TILE128 90)
+//  - other rows in 16-byte pieces: DEEP256 where sums are long and the last
+//    round of tiles is not much shorter than the chip is wide (20,000 rows, 4,096
+//    to 512 columns, 158 tiles 45, DEEP128 53; 1,000 rows, 64 tiles 38, 18.5;
+//    20,000 rows, 1,024 to 1,024 columns 37, 27), else DEEP128
+//  - what is left, wider rows at any address: tiles through registers, small
+//    ones where those fill the chip (4,000 rows, 1,000 to 300 columns 11.3 and 14;
+//    20,000 rows 23 and 19)
+Tile choose(const Linear8Args& a, int es, int KS, bool pieces, bool streams) {
+    const int64_t macs = (a.M + 63) / 64 * 64 * a.N * a.K;
+    if (a.M <= 64 || (KS > 4 && macs <= KS * 65000000ll)) return FEW;
+    if (streams && (KS <= 4 || !pieces)) return a.M * a.N * es > PAST_CACHES ? STREAM_PAST : STREAM;
+    if (!pieces) return ((a.M + 63) / 64) * ((a.N + 63) / 64) <= 512 ? TILE64 : TILE128;
+    const int64_t big = ((a.M + 255) / 256) * ((a.N + 255) / 256);
+    return KS >= 16 && big * 100 >= (big + 255) / 256 * 256 * 55 ? DEEP256 : DEEP128;
 }
 
 template <typename T>
 void launch_t(const Linear8Args& a, int tile, hipStream_t s) {
     const int KS = (a.K + KB - 1) / KB, waves = KS < 16 ? KS : 16;
-    // 16-byte pieces that lie within a row; rows that fit a wavefront's registers
-    const bool pieces = a.K % 16 == 0 && a.x_stride % 16 == 0 && ((uintptr_t)a.x & 15) == 0 && a.x_stride < (1 << 24) &&
-                        a.out_stride < (1 << 24);
-    const bool streams = KS <= 4 && a.N <= 8192 && a.x_stride < (1 << 24) && a.out_stride < (1 << 24);
-    switch (tile ? tile : choose(a, sizeof(T), pieces, streams)) {
+    // places within a tile of rows fit 32 bits; rows in 16-byte pieces; rows
+    // that a wavefront's registers hold
+    const bool near = a.x_stride < (1 << 24) && a.out_stride < (1 << 24);
+    const bool pieces = near && a.x_stride % 16 == 0 && ((uintptr_t)a.x & 15) == 0;
+    const bool streams = near && KS <= 8 && a.N <= 4096;
+    switch (tile ? tile : choose(a, sizeof(T), KS, pieces, streams)) {
         case FEW: return a.M > 16 ? launch_few<T, 4, 1>(a, waves, s) : launch_few<T, 1, 1>(a, waves, s);
         case TILE64: return launch_tile<T, 64, 64, 2, 1, 2>(a, s);
-        case TILE128X64: return launch_tile<T, 128, 64, 4, 1, 2>(a, s);
-        case TILE256: return launch_tile<T, 256, 256, 4, 2, 1>(a, s);
-        case DEEP256:
-            if (pieces) return launch_deep<T, 256, 256, 4, 1, false>(a, s);
-            break;
         case DEEP128:
-            if (pieces) return launch_deep<T, 128, 128, 2, 2, false>(a, s);
+            if (pieces) return launch_deep<T, 128, 128, 2, 2>(a, s);
+            break;
+        case DEEP256:
+            if (pieces) return launch_deep<T, 256, 256, 4, 1>(a, s);
             break;
         case STREAM:
             if (streams) return launch_streams<T, 1, 16, false>(a, s);

@@ -10,7 +10,7 @@ from _rows import BF16, F32, check_rows8, gen, norm, normal, product, spread
 
 pytestmark = pytest.mark.gpu
 
-TILES = range(10)  # 0: by the sizes
+TILES = range(8)  # 0: by the sizes
 
 
 @pytest.fixture(autouse=True)
