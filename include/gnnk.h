@@ -593,8 +593,9 @@ gnnk_status node_quantize(const gnnk_tensor* x, gnnk_rows8* out, hipStream_t str
  *   grad_w = sum over rows of grad_out sum r
  * sum as node_add_norm wrote it (without residual: x); grad_x is the gradient
  * of x and that of the residual.  grad_sum (nullable: 0) is the gradient of
- * the sum from what else read it.  grad_w's sums: fp32 over at most 32 rows,
- * fp64 over those in a fixed order, rounded once.  grad_x and grad_w are
+ * the sum from what else read it.  grad_w's sums, in a fixed order: fp32 over
+ * at most 32 rows, fp64 over a tile of such sums (rounded to fp32) and over
+ * the tiles, then rounded once.  grad_x and grad_w are
  * nullable, grad_w needs w.  work: device memory of at least
  * node_add_norm_work_bytes bytes, 256-byte aligned, for calls that ask for
  * grad_w (else it may be NULL); it need not be initialised and is the caller's

@@ -1688,9 +1688,9 @@ namespace {
 constexpr int NORM_MAX_COLS = 16384;
 constexpr int ROWS8_MAX_COLS = 65536;
 constexpr int WEIGHT8_MAX_OUTS = 1 << 24;
-constexpr int NORM_BLOCKS = 2048;      // blocks that share a call's rows
-constexpr int NORM_TILE_STEPS = 32;    // rows that a group of lanes adds up in fp32, at most
-constexpr int NORM_TILES = 2048;       // tiles that fill the chip
+constexpr int64_t NORM_BYTES = 12288, QUANT_BYTES = 20480;  // that a block moves, about
+constexpr int NORM_TILES = 512;        // tiles that fill the chip
+constexpr int ADD_NORM_RUN = 128;      // tiles that a workgroup adds up
 
 int64_t cols_of(const gnnk_tensor* t) { return (int64_t)t->heads * t->feat; }
 
@@ -1709,13 +1709,16 @@ Span flat(const void* p, int64_t bytes) { return Span{(uintptr_t)p, bytes > 0 ? 
 
 // lanes and vectors of a row; returns the vectors a lane.  A wavefront holds
 // rows of up to 2,048 columns, four vectors of bf16 or eight of fp32 a lane;
-// wider ones take several.
-int add_norm_geo(AddNormArgs& A, const gnnk_tensor* x) {
+// wider ones take several, up to eight.  The backward has two or three rows in
+// registers and sums besides: half as many vectors a lane where eight
+// wavefronts hold the row all the same (65,536 rows of 4,096 bf16 606 -> 451 us).
+int add_norm_geo(AddNormArgs& A, const gnnk_tensor* x, bool bwd = false) {
     A.C = (int32_t)cols_of(x);
     A.inv_C = 1.0f / (float)A.C;
     A.n = x->rows;
-    const int V = x->dtype == GNNK_BF16 ? 8 : 4, most = x->dtype == GNNK_BF16 ? 4 : 8;
-    const int NV = (A.C + V - 1) / V;
+    const int V = x->dtype == GNNK_BF16 ? 8 : 4, NV = (A.C + V - 1) / V;
+    int most = x->dtype == GNNK_BF16 ? 4 : 8;
+    if (bwd && NV <= 64 * 8 * most / 2) most /= 2;
     A.L = std::min(64, pow2ceil(NV));
     A.waves = pow2ceil((NV + 64 * most - 1) / (64 * most));
     A.threads = std::max(256, A.waves * 64);
@@ -1724,26 +1727,41 @@ int add_norm_geo(AddNormArgs& A, const gnnk_tensor* x) {
 }
 int rows_of_block(const AddNormArgs& A) { return A.threads / (A.waves > 1 ? A.waves * 64 : A.L); }
 
-void add_norm_blocks(AddNormArgs& A) {
-    const int per = rows_of_block(A);
-    A.blocks = (int32_t)std::min<int64_t>((A.n + per - 1) / per, NORM_BLOCKS);
+// Blocks of a forward call: each moves about `bytes` bytes, taking some rows
+// after others where one set of them is less (a row moves `moved` bytes).
+// 262,144 rows of 256 fp32, sum and norm, 16 KB a set: one set a block 180 us,
+// two 191, four 193, 2,048 blocks that share the rows 210; in 8 bits alone, 5 KB a
+// set: 96, 76, 67 and 65.
+void add_norm_blocks(AddNormArgs& A, int64_t moved, int64_t bytes) {
+    const int64_t per = rows_of_block(A), sets = std::max<int64_t>(1, (bytes + per * moved / 2) / (per * moved));
+    A.blocks = (int32_t)std::min<int64_t>((A.n + per * sets - 1) / (per * sets), 1 << 20);
 }
 
-// the tiles of a backward: enough to fill the chip, and no longer than sums in
-// fp32 may be
-void add_norm_tiles(AddNormArgs& A) {
-    const int64_t groups = (A.n + rows_of_block(A) - 1) / rows_of_block(A);
-    A.steps = (int32_t)std::min<int64_t>(NORM_TILE_STEPS, std::max<int64_t>(1, groups / NORM_TILES));
-    A.parts = (groups + A.steps - 1) / A.steps;
+// The tiles of a backward: as short as their sums' share of the bytes allows (32
+// rows of bf16 or 16 of fp32, an eighth or less of what the rows take on short
+// grids), which the memory likes (262,144 rows of 256 fp32 without the weight's
+// gradient, tiles of 128 / 64 / 32 / 16 rows: 222 / 209 / 199 / 194 us), in at least
+// two sets of rows, the second of which loads behind the first.  A workgroup
+// adds up ADD_NORM_RUN tiles.
+void add_norm_tiles(AddNormArgs& A, int dtype) {
+    const int64_t per = rows_of_block(A), sets = (A.n + per - 1) / per;
+    int64_t steps = std::max<int64_t>(2, (dtype == 1 ? 32 : 16) / per);
+    if (sets < steps * NORM_TILES) steps = std::max<int64_t>(1, sets / NORM_TILES);
+    A.steps = (int32_t)steps;
+    A.parts = (sets + steps - 1) / steps;
     A.blocks = (int32_t)std::min<int64_t>(A.parts, 1 << 20);
+    A.runs = (int32_t)std::min<int64_t>(std::max<int64_t>(1, A.parts / ADD_NORM_RUN), 256);
+}
+
+size_t add_norm_parts_bytes(const AddNormArgs& A) { return ((size_t)A.parts * A.C * 4 + 255) / 256 * 256; }
+size_t add_norm_work(const AddNormArgs& A) {
+    return std::max<size_t>(256, add_norm_parts_bytes(A) + (A.runs > 1 ? (size_t)A.runs * A.C * 8 : 0));
 }
 
 // 64 outputs and 128 columns at a time
 size_t weight8_size(int32_t outs, int32_t cols) {
     return (size_t)((outs + 63) / 64) * ((cols + 127) / 128) * 8192;
 }
-
-size_t add_norm_work(const AddNormArgs& A) { return std::max<size_t>(256, (size_t)A.parts * A.C * 4); }
 
 // out overlaps none of the operands `in`, except the ones of its own rows that
 // it may replace
@@ -1811,7 +1829,7 @@ gnnk_status node_add_norm(const gnnk_tensor* x, const gnnk_tensor* residual, con
     add_norm_operands(A, x, residual, w, eps, sum);
     A.out = out->data;
     A.out_stride = out->row_stride;
-    add_norm_blocks(A);
+    add_norm_blocks(A, A.C * (residual ? 4ll : 2ll) * (dtype_code(x) ? 2 : 4), NORM_BYTES);
     return launch_status(launch_node_add_norm(A, dtype_code(x), npt, ADD_NORM, stream), "norm launch");
 }
 
@@ -1834,7 +1852,7 @@ gnnk_status node_add_norm_i8(const gnnk_tensor* x, const gnnk_tensor* residual, 
     A.q = out->data;
     A.q_stride = out->row_stride;
     A.scale = out->scale;
-    add_norm_blocks(A);
+    add_norm_blocks(A, A.C * ((residual ? 3ll : 1ll) * (dtype_code(x) ? 2 : 4) + 1), NORM_BYTES);
     return launch_status(launch_node_add_norm(A, dtype_code(x), npt, ADD_NORM8, stream), "norm launch");
 }
 
@@ -1853,7 +1871,7 @@ gnnk_status node_quantize(const gnnk_tensor* x, gnnk_rows8* out, hipStream_t str
     A.q = out->data;
     A.q_stride = out->row_stride;
     A.scale = out->scale;
-    add_norm_blocks(A);
+    add_norm_blocks(A, A.C * (dtype_code(x) ? 3ll : 5ll), QUANT_BYTES);
     return launch_status(launch_node_add_norm(A, dtype_code(x), npt, QUANT8, stream), "quantize launch");
 }
 
@@ -1875,8 +1893,8 @@ gnnk_status node_add_norm_backward(const gnnk_tensor* sum, const gnnk_tensor* w,
     if (!same_dtype({sum, w, grad_out, grad_sum, grad_x, grad_w}))
         return fail(GNNK_EINVAL, "all tensors must share one dtype");
     AddNormArgs A{};
-    const int npt = add_norm_geo(A, sum);
-    add_norm_tiles(A);
+    const int npt = add_norm_geo(A, sum, true);
+    add_norm_tiles(A, dtype_code(sum));
     const size_t need = grad_w ? add_norm_work(A) : 0;
     if (need && (!work || work_bytes < need))
         return fail(GNNK_ENOMEM, "the weight's gradient needs %zu bytes of work, %zu given", need, work ? work_bytes : 0);
@@ -1900,6 +1918,7 @@ gnnk_status node_add_norm_backward(const gnnk_tensor* sum, const gnnk_tensor* w,
     if (grad_w) {
         A.dw = grad_w->data;
         A.part = static_cast<float*>(work);
+        A.sums = reinterpret_cast<double*>(static_cast<char*>(work) + add_norm_parts_bytes(A));
     }
     return launch_status(launch_node_add_norm(A, dtype_code(sum), npt, ADD_NORM_BWD, stream), "norm backward launch");
 }
@@ -1912,8 +1931,8 @@ gnnk_status node_add_norm_work_bytes(const gnnk_tensor* sum, size_t* bytes) {
         cols_of(sum) > NORM_MAX_COLS || (sum->dtype != GNNK_F32 && sum->dtype != GNNK_BF16))
         return fail(GNNK_EINVAL, "fewer than 2^31 rows of at most %d columns", NORM_MAX_COLS);
     AddNormArgs A{};
-    add_norm_geo(A, sum);
-    add_norm_tiles(A);
+    add_norm_geo(A, sum, true);
+    add_norm_tiles(A, dtype_code(sum));
     *bytes = add_norm_work(A);
     return GNNK_OK;
 }

@@ -327,7 +327,9 @@ struct AddNormArgs {
     float* scale;            // of each row of q
     void* dw;                // backward: gradient of w
     float* part;             // parts x C sums of tiles, nullptr: dw not wanted
+    double* sums;            // runs x C sums of runs of tiles, where there are several
     int64_t parts;
+    int32_t runs;
     int64_t x_stride, r_stride, gs_stride, sum_stride, out_stride, q_stride, n;
     int32_t C, L, waves;     // columns; lanes of a row, or wavefronts where it takes several
     int32_t threads, blocks; // of a block, of the launch

@@ -207,7 +207,11 @@ __global__ __launch_bounds__(WIDE ? 512 : 256) void node_add_norm_kernel(AddNorm
 
 // A block takes a tile of rows: gradients of the stream row by row, and the
 // sum of gy h rn over the tile, which the next kernel adds up over the tiles.
-template <typename T, int NPT, bool PART, bool WIDE>
+// The next rows load before a row's gradients are stored: what waits for loads
+// waits for all stores before them.  DENSE: every lane's vectors lie within the
+// row, so that a set of rows is stored without a branch and the wait for the
+// next rows leaves the stores out (there are some: DENSE asks for them).
+template <typename T, int NPT, bool PART, bool WIDE, bool DENSE>
 __global__ __launch_bounds__(WIDE ? 512 : 256) void node_add_norm_backward_kernel(AddNormArgs A) {
     constexpr int V = 16 / sizeof(T);
     constexpr int N = Words<T, V>::N;
@@ -218,17 +222,9 @@ __global__ __launch_bounds__(WIDE ? 512 : 256) void node_add_norm_backward_kerne
     const int C = A.C;
 
     auto count = [&](int p) {
+        if (DENSE) return V;
         const int left = C - (p * TPR + lig) * V;
         return left < 0 ? 0 : (left < V ? left : V);
-    };
-    auto get = [&](const void* base, int64_t stride, int64_t n, int p, bool ok, float* raw) {
-#pragma unroll
-        for (int i = 0; i < N; ++i) raw[i] = 0.0f;
-        const int m = count(p), c = (p * TPR + lig) * V;
-        if (ok && m > 0) {
-            const int64_t at = n * stride + c;
-            fetch<T, V, PART>(reinterpret_cast<const T*>(base) + at, m, (A.n - 1) * stride + C - at, raw);
-        }
     };
     float w[NPT][N];
 #pragma unroll
@@ -238,6 +234,28 @@ __global__ __launch_bounds__(WIDE ? 512 : 256) void node_add_norm_backward_kerne
         const int m = count(p), c = (p * TPR + lig) * V;
         if (A.w && m > 0) fetch<T, V, PART>(reinterpret_cast<const T*>(A.w) + c, m, C - c, w[p]);
     }
+    float hr[NPT][N], gr[NPT][N], sr[NPT][N];
+    // (of no row past the last one: that one's again)
+    auto load = [&](int64_t n) {
+        n = n < A.n ? n : A.n - 1;
+#pragma unroll
+        for (int p = 0; p < NPT; ++p) {
+            const int m = count(p), c = (p * TPR + lig) * V;
+            if (!DENSE) {
+#pragma unroll
+                for (int i = 0; i < N; ++i) hr[p][i] = gr[p][i] = sr[p][i] = 0.0f;
+            }
+            if (DENSE || m > 0) {
+                auto get = [&](const void* base, int64_t stride, float* raw) {
+                    const int64_t at = n * stride + c;
+                    fetch<T, V, PART>(reinterpret_cast<const T*>(base) + at, m, (A.n - 1) * stride + C - at, raw);
+                };
+                get(A.x, A.x_stride, hr[p]);
+                get(A.r, A.r_stride, gr[p]);
+                if (A.gs) get(A.gs, A.gs_stride, sr[p]);
+            }
+        }
+    };
     for (int64_t tile = blockIdx.x; tile < A.parts; tile += gridDim.x) {
         const int64_t first = tile * per * A.steps;
         float dw[NPT][V];
@@ -246,50 +264,52 @@ __global__ __launch_bounds__(WIDE ? 512 : 256) void node_add_norm_backward_kerne
 #pragma unroll
             for (int i = 0; i < V; ++i) dw[p][i] = 0.0f;
 
+        if (A.n > 0) load(first + gid);
         for (int k = 0; k < A.steps; ++k) {
-            const int64_t n = first + (int64_t)k * per + gid;
-            if (first + (int64_t)k * per >= A.n) break;
+            const int64_t n0 = first + (int64_t)k * per, n = n0 + gid;
+            if (n0 >= A.n) break;
             const bool ok = n < A.n;
-            float hr[NPT][N], gr[NPT][N], sr[NPT][N];
-#pragma unroll
-            for (int p = 0; p < NPT; ++p) {
-                get(A.x, A.x_stride, n, p, ok, hr[p]);
-                get(A.r, A.r_stride, n, p, ok, gr[p]);
-                if (A.gs) get(A.gs, A.gs_stride, n, p, ok, sr[p]);
-            }
+            float h[NPT][V], g[NPT][V], s[NPT][V];
             float t[2] = {0.0f, 0.0f};  // sums of h^2 and of gy w h
 #pragma unroll
             for (int p = 0; p < NPT; ++p) {
                 const int m = count(p);
-                float h[V], g[V];
-                widen<T, V, PART>(hr[p], m, h);
-                widen<T, V, PART>(gr[p], m, g);
+                widen<T, V, PART>(hr[p], m, h[p]);
+                widen<T, V, PART>(gr[p], m, g[p]);
+                if (A.gs) widen<T, V, PART>(sr[p], m, s[p]);
 #pragma unroll
                 for (int i = 0; i < V; ++i) {
-                    t[0] = fmaf(h[i], h[i], t[0]);
-                    t[1] = fmaf(A.w ? g[i] * Words<T, V>::at(w[p], i) : g[i], h[i], t[1]);
+                    t[0] = fmaf(h[p][i], h[p][i], t[0]);
+                    t[1] = fmaf(A.w ? g[p][i] * Words<T, V>::at(w[p], i) : g[p][i], h[p][i], t[1]);
                 }
             }
+            if (k + 1 < A.steps && n0 + per < A.n) load(n + per);
             row_totals<2, WIDE>(t, A, red);
             const float rn = 1.0f / sqrtf(t[0] * A.inv_C + A.eps);
             const float mean = rn * rn * (t[1] * A.inv_C);
 #pragma unroll
             for (int p = 0; p < NPT; ++p) {
-                const int m = count(p);
-                float h[V], g[V], s[V];
-                widen<T, V, PART>(hr[p], m, h);
-                widen<T, V, PART>(gr[p], m, g);
-                if (A.gs) widen<T, V, PART>(sr[p], m, s);
 #pragma unroll
                 for (int i = 0; i < V; ++i) {
-                    // (a group without a row adds nothing: there rn may be infinite)
-                    if (ok) dw[p][i] = fmaf(g[i], h[i] * rn, dw[p][i]);
-                    const float gw = A.w ? g[i] * Words<T, V>::at(w[p], i) : g[i];
-                    const float d = rn * (gw - h[i] * mean);
-                    h[i] = A.gs ? s[i] + d : d;
+                    // (a group without a row adds nothing)
+                    if (ok) dw[p][i] = fmaf(g[p][i], h[p][i] * rn, dw[p][i]);
+                    const float gw = A.w ? g[p][i] * Words<T, V>::at(w[p], i) : g[p][i];
+                    const float d = rn * (gw - h[p][i] * mean);
+                    h[p][i] = A.gs ? s[p][i] + d : d;
                 }
-                if (ok && m > 0 && A.out)
-                    store_part<T, V, PART>(reinterpret_cast<T*>(A.out) + n * A.out_stride + (p * TPR + lig) * V, h, m);
+            }
+            if (!DENSE && !A.out) continue;
+            T* const out = reinterpret_cast<T*>(A.out) + n * A.out_stride + lig * V;
+            if (DENSE && n0 + per <= A.n) {
+#pragma unroll
+                for (int p = 0; p < NPT; ++p) put<T, V>(out + p * TPR * V, h[p]);
+            } else {
+#pragma unroll
+                for (int p = 0; p < NPT; ++p) {
+                    const int m = count(p);
+                    if (ok && m > 0) store_part<T, V, PART>(out + p * TPR * V, h[p], m);
+                }
+                if (DENSE) break;  // (they were the last rows)
             }
         }
         if (!A.part) continue;
@@ -312,30 +332,35 @@ __global__ __launch_bounds__(WIDE ? 512 : 256) void node_add_norm_backward_kerne
     }
 }
 
-// the weight's gradient: the tiles' sums in fp64, 32 columns a workgroup, 32
-// runs of tiles side by side, each in order
-template <typename T>
-__global__ __launch_bounds__(1024) void node_add_norm_dw_kernel(AddNormArgs A) {
-    __shared__ double red[32][33];
-    const int c = threadIdx.x & 31, run = threadIdx.x >> 5;
-    const int64_t col = (int64_t)blockIdx.x * 32 + c, per = (A.parts + 31) / 32;
+// the weight's gradient: the tiles' sums in fp64, 64 columns and ADD_NORM_RUN
+// tiles a workgroup, four runs of them side by side, each in order; then the
+// sums of such runs in the same way
+template <typename T, typename P>
+__global__ __launch_bounds__(256) void node_add_norm_dw_kernel(const P* part, int64_t parts, int C, double* sums, T* dw,
+                                                               int runs) {
+    __shared__ double red[4][64];
+    const int c = threadIdx.x & 63, q = threadIdx.x >> 6;
+    const int64_t col = (int64_t)(blockIdx.x / runs) * 64 + c, run = blockIdx.x % runs;
+    const int64_t each = (parts + runs - 1) / runs, per = (each + 3) / 4;
+    const int64_t stop = (run + 1) * each < parts ? (run + 1) * each : parts;
+    const int64_t first = run * each + q * per, end = first + per < stop ? first + per : stop;
     double sum = 0.0;
-    if (col < A.C) {
-        const int64_t end = (run + 1) * per < A.parts ? (run + 1) * per : A.parts;
-        constexpr int U = 8;  // loads in flight
-        for (int64_t p = run * per; p < end; p += U) {
-            float x[U];
+    if (col < C) {
+        constexpr int U = 16;  // loads in flight
+        for (int64_t p = first; p < end; p += U) {
+            P x[U];
 #pragma unroll
-            for (int u = 0; u < U; ++u) x[u] = A.part[(p + u < end ? p + u : p) * A.C + col];
+            for (int u = 0; u < U; ++u) x[u] = part[(p + u < end ? p + u : p) * C + col];
 #pragma unroll
             for (int u = 0; u < U; ++u) sum += p + u < end ? (double)x[u] : 0.0;
         }
     }
-    red[run][c] = sum;
+    red[q][c] = sum;
     __syncthreads();
-    if (run == 0 && col < A.C) {
-        for (int k = 1; k < 32; ++k) sum += red[k][c];
-        IO<T, 1>::store1(reinterpret_cast<T*>(A.dw) + col, (float)sum);
+    if (q == 0 && col < C) {
+        sum += red[1][c] + red[2][c] + red[3][c];
+        if (sums) sums[run * C + col] = sum;
+        else IO<T, 1>::store1(dw + col, (float)sum);
     }
 }
 
@@ -348,8 +373,11 @@ void launch_n(const AddNormArgs& a, int mode, hipStream_t s) {
         hipLaunchKernelGGL((node_add_norm_kernel<T, NPT, PART, WIDE, ADD_NORM8>), grid, block, 0, s, a);
     else if (mode == QUANT8)
         hipLaunchKernelGGL((node_add_norm_kernel<T, NPT, PART, WIDE, QUANT8>), grid, block, 0, s, a);
+    else if (!PART && a.out && a.C == (WIDE ? a.waves * 64 : a.L) * NPT * 16 / (int)sizeof(T))
+        hipLaunchKernelGGL((node_add_norm_backward_kernel<T, NPT, false, WIDE, true>), grid, block,
+                           a.part ? a.threads * 64 / sizeof(T) : 0, s, a);
     else
-        hipLaunchKernelGGL((node_add_norm_backward_kernel<T, NPT, PART, WIDE>), grid, block,
+        hipLaunchKernelGGL((node_add_norm_backward_kernel<T, NPT, PART, WIDE, false>), grid, block,
                            a.part ? a.threads * 64 / sizeof(T) : 0, s, a);
 }
 
@@ -373,8 +401,19 @@ void launch_t(const AddNormArgs& a, int npt, int mode, hipStream_t s) {
         else if (npt == 4) launch_p<T, 4>(a, mode, s);
         else if constexpr (sizeof(T) == 4) launch_p<T, 8>(a, mode, s);
     }
-    if (mode == ADD_NORM_BWD && a.part)
-        hipLaunchKernelGGL((node_add_norm_dw_kernel<T>), dim3((unsigned)((a.C + 31) / 32)), dim3(1024), 0, s, a);
+    if (mode == ADD_NORM_BWD && a.part) {
+        const unsigned wide = (unsigned)((a.C + 63) / 64);
+        T* const dw = reinterpret_cast<T*>(a.dw);
+        if (a.runs > 1) {
+            hipLaunchKernelGGL((node_add_norm_dw_kernel<T, float>), dim3(wide * a.runs), dim3(256), 0, s, a.part, a.parts,
+                               a.C, a.sums, dw, a.runs);
+            hipLaunchKernelGGL((node_add_norm_dw_kernel<T, double>), dim3(wide), dim3(256), 0, s, a.sums,
+                               (int64_t)a.runs, a.C, nullptr, dw, 1);
+        } else {
+            hipLaunchKernelGGL((node_add_norm_dw_kernel<T, float>), dim3(wide), dim3(256), 0, s, a.part, a.parts, a.C,
+                               nullptr, dw, 1);
+        }
+    }
 }
 
 }  // namespace

@@ -120,7 +120,7 @@ def test_add_norm_backward_asks_for_its_work(lib):
     for rows in (0, 1, 100, 10**4, 10**6, 10**8):
         assert lib.node_add_norm_work_bytes(tensor(0, rows=rows, feat=128), ctypes.byref(need)) == gnnk.OK
         sizes.append(need.value)
-    assert sizes == sorted(sizes) and sizes[-1] < 10**8 * 128 * 4 // 60
+    assert sizes == sorted(sizes) and sizes[-1] < 10**8 * 128 * 4 // 15  # a row of sums for 16 rows
     assert lib.node_add_norm_work_bytes(None, ctypes.byref(need)) == gnnk.EINVAL
     assert lib.node_add_norm_work_bytes(BACK["h"], None) == gnnk.EINVAL
     assert lib.node_add_norm_work_bytes(tensor(0, feat=16385), ctypes.byref(need)) == gnnk.EINVAL
