@@ -753,23 +753,31 @@ def _rows8(q, scale):
     return _ROWS8.pack(q.data_ptr(), scale.data_ptr() if scale is not None else 0, rows, stride, cols, 0)
 
 
-def _new_rows8(rows, cols, device):
-    """int8 rows whose stride is a multiple of 16 bytes, and their scales"""
-    q = torch.empty((rows, (cols + 15) & ~15), dtype=torch.int8, device=device)
-    return q if cols % 16 == 0 else q[:, :cols], torch.empty(rows, dtype=torch.float32, device=device)
+_CODES = {torch.float32: F32, torch.bfloat16: BF16}
+
+
+def _flat(t, rows=None):
+    """_desc of a tensor whose rows are whole: a contiguous one of two dimensions, or all of one as `rows` = 1 row,
+    without a look at its strides (0.5 us instead of 1.3)"""
+    if t is None:
+        return None
+    dt = _CODES.get(t.dtype)
+    if dt is None or not t.is_cuda or not t.is_contiguous() or (rows is None and t.dim() != 2):
+        if rows is not None and t.is_cuda and not t.is_contiguous():
+            raise ValueError("weights and biases must be contiguous")
+        return _desc(t if rows is None else t.reshape(1, 1, -1))
+    cols = t.numel() if rows is not None else t.shape[1]
+    return _TENSOR.pack(t.data_ptr(), rows or t.shape[0], 1, cols & 0xFFFFFFFF, cols, dt, 0)
+
+
+def _new_rows8(x, rows, cols):
+    """int8 rows whose stride is a multiple of 16 bytes, and their scales, on x's device"""
+    q = x.new_empty((rows, (cols + 15) & ~15), dtype=torch.int8)
+    return q if cols % 16 == 0 else q[:, :cols], x.new_empty((rows,), dtype=torch.float32)
 
 
 def _columns(x):
     return x.shape[1] if x.dim() == 2 else x.shape[1] * x.shape[2]
-
-
-def _row(w):
-    """a weight or bias as one row: the elements of any contiguous shape"""
-    if w is None:
-        return None
-    if not w.is_contiguous():
-        raise ValueError("weights and biases must be contiguous")
-    return w.view(1, 1, -1)
 
 
 def node_add_norm(x, residual=None, weight=None, eps: float = 1e-6, out=None, out_sum=None, stream=None):
@@ -778,14 +786,14 @@ def node_add_norm(x, residual=None, weight=None, eps: float = 1e-6, out=None, ou
     without a residual.  out and out_sum may be x or residual themselves."""
     x = _as3(x) if x.dim() != 2 else x
     _here(x, residual, weight, out, out_sum)
-    xd = _desc(x)
+    xd = _flat(x)
     out, od = _out(x, xd) if out is None else (out, _desc(out))
     sd = None
     if residual is not None:
         out_sum, sd = _out(x, xd) if out_sum is None else (out_sum, _desc(out_sum))
     elif out_sum is not None:
         raise ValueError("without a residual the sum is x")
-    _check(load().node_add_norm(xd, _desc(residual), _desc(_row(weight)), eps, sd, od, _stream(stream)))
+    _check(load().node_add_norm(xd, _flat(residual), _flat(weight, 1), eps, sd, od, _stream(stream)))
     return (out, out_sum) if residual is not None else out
 
 
@@ -796,17 +804,17 @@ def node_add_norm_i8(x, residual=None, weight=None, eps: float = 1e-6, out=None,
     scale[n] * q[n] is y.  A row with a NaN or an infinity has scale NaN and values 0."""
     x = _as3(x) if x.dim() != 2 else x
     _here(x, residual, weight, out, scale, out_sum)
-    xd = _desc(x)
+    xd = _flat(x)
     if (out is None) != (scale is None):
         raise ValueError("out and scale are given together")
     if out is None:
-        out, scale = _new_rows8(x.shape[0], _columns(x), x.device)
+        out, scale = _new_rows8(x, x.shape[0], _columns(x))
     sd = None
     if residual is not None:
         out_sum, sd = _out(x, xd) if out_sum is None else (out_sum, _desc(out_sum))
     elif out_sum is not None:
         raise ValueError("without a residual the sum is x")
-    _check(load().node_add_norm_i8(xd, _desc(residual), _desc(_row(weight)), eps, sd, _rows8(out, scale),
+    _check(load().node_add_norm_i8(xd, _flat(residual), _flat(weight, 1), eps, sd, _rows8(out, scale),
                                    _stream(stream)))
     return (out, scale, out_sum) if residual is not None else (out, scale)
 
@@ -818,8 +826,8 @@ def node_quantize(x, out=None, scale=None, stream=None):
     if (out is None) != (scale is None):
         raise ValueError("out and scale are given together")
     if out is None:
-        out, scale = _new_rows8(x.shape[0], _columns(x), x.device)
-    _check(load().node_quantize(_desc(x), _rows8(out, scale), _stream(stream)))
+        out, scale = _new_rows8(x, x.shape[0], _columns(x))
+    _check(load().node_quantize(_flat(x), _rows8(out, scale), _stream(stream)))
     return out, scale
 
 
@@ -830,18 +838,17 @@ def node_add_norm_backward(h, weight, grad_y, grad_sum=None, eps: float = 1e-6, 
     wanted or without a weight.  grad_x, where dx goes, may be h, grad_y or grad_sum themselves."""
     h = _as3(h) if h.dim() != 2 else h
     _here(h, weight, grad_y, grad_sum, grad_x)
-    hd = _desc(h)
+    hd = _flat(h)
     gx = None
     if grad_x is not None:
         gx = _desc(grad_x)
     elif want_x:
         grad_x, gx = _out(h, hd)
-    row, dw, gw, wd = _row(weight), None, None, None
+    dw, gw, wd = None, None, _flat(weight, 1)
     work, nbytes = None, 0
-    if row is not None:
-        wd = _desc(row)
+    if weight is not None:
         if want_weight:
-            dw, gw = _out(row, wd)
+            dw, gw = _out(weight, wd)
             need = ctypes.c_size_t(0)
             _check(load().node_add_norm_work_bytes(hd, ctypes.byref(need)))
             nbytes = need.value
@@ -850,9 +857,9 @@ def node_add_norm_backward(h, weight, grad_y, grad_sum=None, eps: float = 1e-6, 
             else:
                 with torch.cuda.stream(stream):
                     work = torch.empty(nbytes, dtype=torch.uint8, device=h.device)
-    _check(load().node_add_norm_backward(hd, wd, _desc(grad_y), _desc(grad_sum), eps, gx, gw, _ptr(work), nbytes,
+    _check(load().node_add_norm_backward(hd, wd, _flat(grad_y), _flat(grad_sum), eps, gx, gw, _ptr(work), nbytes,
                                          _stream(stream)))
-    return grad_x, (dw.view(weight.shape) if dw is not None else None)
+    return grad_x, dw
 
 
 class Weight8:
@@ -883,9 +890,10 @@ def node_linear_i8(weight: Weight8, q, scale, bias=None, dtype=torch.bfloat16, o
     float32 or bfloat16 (dtype, or out's).  The products' sums are exact.  bias: outs values of out's dtype.  No
     gradient is formed."""
     _here(weight.packed, q, scale, bias, out)
+    xd = _rows8(q, scale)
     if out is None:
-        out = torch.empty((q.shape[0], weight.outs), dtype=dtype, device=q.device)
-    _check(load().node_linear_i8(_rows8(q, scale), weight._bytes, _desc(_row(bias)), _desc(out), _stream(stream)))
+        out = q.new_empty((q.shape[0], weight.outs), dtype=dtype)
+    _check(load().node_linear_i8(xd, weight._bytes, _flat(bias, 1), _flat(out), _stream(stream)))
     return out
 
 
