@@ -17,8 +17,12 @@ the aggregation layers of the paper's experiments built from them:
                 summed with 1/in-degree-per-relation weights
   DotAttentionConv  multi-head attention by dot products of queries and keys,
                 normed per head and turned by the nodes' positions
+  AddNorm       the residual stream between layers: the sum and its norm
+  Linear8, DotAttentionConv8  the forms for inference with weights and rows in
+                8 bits
 
-Dense projections (the node-wise update) are ordinary torch layers.  Graph
+Dense projections (the node-wise update) are ordinary torch layers, but for
+those in 8 bits.  Graph
 handles come from gnnk.Graph; the caller keeps them alive while tensors that
 depend on them are in use.
 """
@@ -206,6 +210,33 @@ class _DotAggregate(torch.autograd.Function):
         return (None, *(view(t, x) for t, x in zip(grads, (q, k, v, bias))), None)
 
 
+class _AddNorm(torch.autograd.Function):
+    """node_add_norm; the backward reads the sum, and gives its operands one
+    gradient."""
+
+    @staticmethod
+    def forward(ctx, x, residual, weight, eps):
+        ctx.eps = eps
+        if residual is None:
+            ctx.save_for_backward(x, weight)
+            return gnnk.node_add_norm(x, None, weight, eps=eps)
+        y, h = gnnk.node_add_norm(x, residual, weight, eps=eps)
+        ctx.save_for_backward(h, weight)
+        ctx.set_materialize_grads(False)
+        return y, h
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, gy, gh=None):
+        h, weight = ctx.saved_tensors
+        nf = ctx.needs_input_grad
+        if gy is None:  # the norm was not used
+            return gh if nf[0] else None, gh if nf[1] else None, None, None
+        dx, dw = gnnk.node_add_norm_backward(h, weight, _c(gy), grad_sum=_c(gh), eps=ctx.eps, want_x=nf[0] or nf[1],
+                                             want_weight=nf[2])
+        return dx if nf[0] else None, dx if nf[1] else None, dw, None
+
+
 # ---------------------------------------------------------------------------
 # functional API (same names and argument order as the C ABI)
 
@@ -252,6 +283,12 @@ def norm_rotary(q, wq=None, k=None, wk=None, rot=None, pos_q=None, pos_k=None, e
     positions (rot None: none).  Returns both, or the queries alone without keys."""
     _fixed(pos_q, pos_k)
     return _NormRotary.apply(_c(q), _c(wq), _c(k), _c(wk), rot, pos_q, pos_k, float(eps))
+
+
+def add_norm(x, residual=None, weight=None, eps: float = 1e-6):
+    """Differentiable sum and norm of the residual stream: (y, h) with h = x + residual and y = weight * h /
+    sqrt(mean(h^2) + eps) over whole rows; y alone without a residual."""
+    return _AddNorm.apply(_c(x), _c(residual), _c(weight), float(eps))
 
 
 def dot_aggregate(g, q, k, v, bias=None, scale: float = None):
@@ -399,6 +436,97 @@ class DotAttentionConv(torch.nn.Module):
         elif rot is not None:
             q, k = rotary(rot, q, pos_q), rotary(rot, k, pos)
         return dot_aggregate(g, q, k, v, bias)
+
+
+class AddNorm(torch.nn.Module):
+    """The residual stream between two layers: (y, h) with h = x + residual,
+    which the next layer adds to, and y, h's rows divided by their root mean
+    square, which it reads.  Without a residual (the first layer) h is x."""
+
+    def __init__(self, feats: int, eps: float = 1e-6):
+        super().__init__()
+        self.weight = torch.nn.Parameter(torch.ones(feats))
+        self.eps = eps
+
+    def forward(self, x, residual=None):
+        if residual is None:
+            return add_norm(x, None, self.weight, self.eps), x
+        return add_norm(x, residual, self.weight, self.eps)
+
+    def rows8(self, x, residual=None):
+        """(q, scale, h): the norm in 8 bits, for Linear8 and DotAttentionConv8 (no gradients)"""
+        _no_gradient(x, residual, self.weight)
+        if residual is None:
+            return (*gnnk.node_add_norm_i8(x, None, self.weight, eps=self.eps), x)
+        return gnnk.node_add_norm_i8(x, residual, self.weight, eps=self.eps)
+
+
+def _no_gradient(*tensors):
+    """The forms in 8 bits form no gradient: refuse to drop one that is asked for."""
+    if torch.is_grad_enabled() and any(t is not None and t.requires_grad for t in tensors):
+        raise ValueError("no gradient is formed in 8 bits: call it under torch.no_grad()")
+
+
+def _rows8(x):
+    """(q, scale) of rows in 8 bits, or of a tensor whose rows are rounded to them here"""
+    if isinstance(x, tuple):
+        return x[:2]
+    _no_gradient(x)
+    return gnnk.node_quantize(x)
+
+
+class Linear8(torch.nn.Module):
+    """A linear layer for inference with its weight in 8 bits, a scale for each
+    output: of a tensor, whose rows are rounded to 8 bits with a scale each, or
+    of rows that are (q, scale) already.  The result is of the type of the
+    weight that it was made from, or `dtype`."""
+
+    def __init__(self, weight: torch.Tensor, bias: torch.Tensor = None, dtype=None):
+        super().__init__()
+        self.dtype = dtype or weight.dtype
+        self.weight = gnnk.Weight8.quantize(weight)
+        self.bias = bias.detach().to(self.dtype).contiguous() if bias is not None else None
+
+    @classmethod
+    def of(cls, linear: torch.nn.Linear, dtype=None) -> "Linear8":
+        return cls(linear.weight, linear.bias, dtype)
+
+    def forward(self, x):
+        return gnnk.node_linear_i8(self.weight, *_rows8(x), bias=self.bias, dtype=self.dtype)
+
+
+class DotAttentionConv8(torch.nn.Module):
+    """A DotAttentionConv for inference with its projections in 8 bits, keys and
+    values (and queries, where every source is a destination) in one product.
+    The nodes' features are a tensor or rows in 8 bits, (q, scale), as
+    AddNorm.rows8 leaves them."""
+
+    def __init__(self, conv: DotAttentionConv, dtype=None):
+        super().__init__()
+        self.H, self.K, self.F, self.eps = conv.H, conv.K, conv.F, conv.eps
+        self.dtype = dtype or conv.fc_q.weight.dtype
+        both = torch.cat([conv.fc_q.weight, conv.fc_k.weight, conv.fc_v.weight])
+        self.fc = Linear8(both, dtype=self.dtype)
+        self.fc_q = Linear8(conv.fc_q.weight, dtype=self.dtype)
+        self.fc_kv = Linear8(both[self.H * self.F:], dtype=self.dtype)
+        weight = lambda w: w.detach().to(self.dtype) if w is not None else None
+        self.norm_q, self.norm_k, self.rotary = weight(conv.norm_q), weight(conv.norm_k), conv.rotary
+
+    def forward(self, g, x, pos=None, bias=None):
+        x8, scale = _rows8(x)
+        if g.num_dst == x8.shape[0]:
+            q, k, v = self.fc((x8, scale)).split([self.H * self.F, self.K * self.F, self.K * self.F], 1)
+        else:
+            q = self.fc_q((x8[: g.num_dst], scale[: g.num_dst]))
+            k, v = self.fc_kv((x8, scale)).split(self.K * self.F, 1)
+        q, k, v = q.unflatten(1, (self.H, self.F)), k.unflatten(1, (self.K, self.F)), v.unflatten(1, (self.K, self.F))
+        rot = self.rotary(x8.device)
+        pos_q = pos[: g.num_dst] if pos is not None else None
+        if self.norm_q is not None:
+            q, k = gnnk.node_norm_rotary(q, self.norm_q, k, self.norm_k, rot=rot, pos_q=pos_q, pos_k=pos, eps=self.eps)
+        elif rot is not None:
+            q, k = gnnk.node_rotary(rot, q, pos_q), gnnk.node_rotary(rot, k, pos)
+        return gnnk.dot_aggregate(g, q, k, v, bias=bias)
 
 
 def rel_norm(etype, dst, num_rels: int, num_dst: int):

@@ -1,0 +1,262 @@
+"""The residual stream and products in 8 bits as a program runs them: the
+autograd form against differences and its operators, the layers as exactly the
+chains of their operators, replays, streams and long strides."""
+import pytest
+import torch
+
+from paper_1909_01315_amd import gnnk, nn
+from _heads import U32, close
+from _rows import BF16, F32, check_rows8, gen, norm, normal, product
+from test_gpu_attention_layer import graph
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(autouse=True)
+def reset_options():
+    yield
+    gnnk.set_option("linear8_tile", 0)
+
+
+def test_gradients_match_differences():
+    """Gradients of nn.add_norm against central differences of its 64-bit form along random directions."""
+    g = gen(31)
+    n, c, eps = 14, 37, 1e-4
+    xs = [normal(g, n, c), normal(g, n, c), 1 + 0.2 * normal(g, c)]
+    cy, ch = normal(g, n, c), normal(g, n, c)
+    leaves = [t.cuda().requires_grad_(True) for t in xs]
+    y, h = nn.add_norm(*leaves, eps=eps)
+    ((y * cy.cuda()).sum() + (h * ch.cuda()).sum()).backward()
+
+    def value(ts):
+        s = ts[0] + ts[1]
+        return (s / torch.sqrt((s * s).mean(1, keepdim=True) + eps) * ts[2] * cy.double()).sum() + (s * ch.double()).sum()
+
+    for i, t in enumerate(xs):
+        d = normal(g, *t.shape).double()
+        step = 1e-5
+        at = lambda k: value([u.double() + (k * step * d if j == i else 0.0) for j, u in enumerate(xs)])
+        want = float((at(1) - at(-1)) / (2 * step))
+        grad = leaves[i].grad.double().cpu()
+        # fp32 gradients, at most 300 u of each term, h's rounding among them; differences exact to step^2
+        assert abs(float((grad * d).sum()) - want) <= \
+            300 * U32 * float((grad.abs() * d.abs()).sum()) + 1e-6 * (1 + abs(want)), i
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_autograd_gives_the_operators_gradients(dtype):
+    g = gen(33)
+    n, c = 200, 96
+    x, r, cy, ch = (normal(g, n, c, dtype=dtype).cuda() for _ in range(4))
+    w = (1 + 0.2 * normal(g, c)).to(dtype).cuda()
+    layer = nn.AddNorm(c, eps=1e-5).cuda().to(dtype)
+    with torch.no_grad():
+        layer.weight.copy_(w)
+    y0, h0 = gnnk.node_add_norm(x, r, w, eps=1e-5)
+    both = gnnk.node_add_norm_backward(h0, w, cy, grad_sum=ch, eps=1e-5)
+    norm_only = gnnk.node_add_norm_backward(h0, w, cy, eps=1e-5)
+    for use, (dx, dw) in (("both", both), ("norm", norm_only), ("sum", (ch, None))):
+        a, b = x.clone().requires_grad_(True), r.clone().requires_grad_(True)
+        layer.weight.grad = None
+        y, h = layer(a, b)
+        assert torch.equal(y, y0) and torch.equal(h, h0)
+        terms = {"both": (y * cy).sum() + (h * ch).sum(), "norm": (y * cy).sum(), "sum": (h * ch).sum()}
+        terms[use].backward()
+        assert torch.equal(a.grad, dx) and torch.equal(b.grad, dx), use
+        assert (layer.weight.grad is None) if dw is None else torch.equal(layer.weight.grad, dw), use
+    # the residual alone asks for a gradient; x is the residual; no residual
+    b = r.clone().requires_grad_(True)
+    y, h = nn.add_norm(x, b, w, eps=1e-5)
+    (y * cy).sum().backward()
+    assert torch.equal(b.grad, norm_only[0])
+    a = x.clone().requires_grad_(True)
+    y, h = nn.add_norm(a, a, w)
+    (y * cy).sum().backward()
+    one, _ = gnnk.node_add_norm_backward(h.detach(), w, cy)
+    assert torch.equal(a.grad, one + one)
+    a = x.clone().requires_grad_(True)
+    y, h = layer(a)
+    assert h is a
+    (y * cy).sum().backward()
+    assert torch.equal(a.grad, gnnk.node_add_norm_backward(x, w, cy, eps=1e-5)[0])
+
+
+def test_second_derivatives_and_gradients_in_8_bits_are_refused():
+    x = torch.randn(5, 16, device="cuda", requires_grad=True)
+    y, h = nn.add_norm(x, x)
+    (d,) = torch.autograd.grad((y ** 2).sum(), x, create_graph=True)
+    with pytest.raises(RuntimeError):
+        (d ** 2).sum().backward()
+    lin = nn.Linear8.of(torch.nn.Linear(16, 8).cuda())
+    stream = nn.AddNorm(16).cuda()
+    for call in (lambda: lin(x), lambda: stream.rows8(x), lambda: stream.rows8(x.detach())):
+        with pytest.raises(ValueError, match="gradient"):
+            call()
+    with torch.no_grad():
+        assert lin(x).shape == (5, 8) and stream.rows8(x)[2] is x
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_linear8_is_the_chain(dtype):
+    torch.manual_seed(5)
+    linear = torch.nn.Linear(70, 50).cuda().to(dtype)
+    layer = nn.Linear8.of(linear)
+    x = normal(gen(2), 33, 70, dtype=dtype).cuda()
+    wq, ws = gnnk.node_quantize(linear.weight.detach())
+    check_rows8(wq, ws, linear.weight.detach().cpu().double(), 0 * linear.weight.detach().cpu().double(), "weight")
+    q, s = gnnk.node_quantize(x)
+    out = layer(x)
+    assert out.dtype is dtype and torch.equal(out, layer((q, s)))
+    close(out, *product(q, s, wq, ws, linear.bias.detach()), "layer")
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("n_src,n_dst", [(90, 60), (80, 80)])
+@pytest.mark.parametrize("H,K,F,pairs,qk_norm", [(4, 2, 20, (3, 4), True), (8, 8, 16, (8,), False), (6, 1, 47, None, True)])
+def test_attention_in_8_bits_is_the_chain(H, K, F, pairs, qk_norm, n_src, n_dst, dtype):
+    """From the stream to the attention's output: sum and norm in 8 bits, projections, norms and rotations, attention."""
+    gr, dst = graph(n_src, n_dst, 1200, 71)
+    g = gen(73)
+    torch.manual_seed(7)
+    D = 48
+    conv = nn.DotAttentionConv(D, F, H, kv_heads=K, qk_norm=qk_norm, axis_pairs=pairs).cuda().to(dtype)
+    conv8 = nn.DotAttentionConv8(conv)
+    stream = nn.AddNorm(D).cuda().to(dtype)
+    x, r = normal(g, n_src, D, dtype=dtype).cuda(), normal(g, n_src, D, dtype=dtype).cuda()
+    pos = (normal(g, n_src, len(pairs)) * 10).cuda() if pairs else None
+    with torch.no_grad():
+        q8, s8, h = stream.rows8(x, r)
+        out = conv8(gr, (q8, s8), pos)
+        assert torch.equal(out, conv8(gr, (q8, s8, h), pos))
+        parts = []
+        for fc in (conv.fc_q, conv.fc_k, conv.fc_v):
+            weight = gnnk.Weight8.quantize(fc.weight)
+            parts.append(gnnk.node_linear_i8(weight, q8, s8, dtype=dtype))
+        q, k, v = parts[0][:n_dst].view(-1, H, F), parts[1].view(-1, K, F), parts[2].view(-1, K, F)
+        rot = conv.rotary(x.device)
+        pq = pos[:n_dst] if pairs else None
+        if qk_norm:
+            q, k = gnnk.node_norm_rotary(q, conv.norm_q, k, conv.norm_k, rot=rot, pos_q=pq, pos_k=pos, eps=conv.eps)
+        elif rot is not None:
+            q, k = gnnk.node_rotary(rot, q, pq), gnnk.node_rotary(rot, k, pos)
+        assert torch.equal(out, gnnk.dot_aggregate(gr, q, k, v))
+        y = gnnk.node_quantize(out)  # all heads of a node are one row
+        assert y[0].shape == (n_dst, H * F)
+        last = nn.Linear8(torch.randn(D, H * F, device="cuda").to(dtype))
+        assert torch.equal(last(out), last(y)) and last(out).shape == (n_dst, D)
+
+
+def run_all(t):
+    """every operator once, on the tensors of `t`"""
+    y, h = gnnk.node_add_norm(t["x"], t["r"], t["w"])
+    dx, dw = gnnk.node_add_norm_backward(h, t["w"], t["g"], grad_sum=t["r"])
+    q, s, h8 = gnnk.node_add_norm_i8(t["x"], t["r"], t["w"])
+    out = gnnk.node_linear_i8(t["weight"], q, s, bias=t["b"])
+    q2, s2 = gnnk.node_quantize(out)
+    return [y, h, dx, dw, q, s, h8, out, q2, s2, gnnk.node_linear_i8(t["weight2"], q2, s2, dtype=F32)]
+
+
+def tensors(seed, n, c, o, dtype):
+    g = gen(seed)
+    t = {k: normal(g, n, c, dtype=dtype).cuda() for k in "xrg"}
+    t["w"] = (1 + 0.1 * normal(g, c)).to(dtype).cuda()
+    t["b"] = normal(g, o, dtype=BF16).cuda()
+    t["weight"] = gnnk.Weight8.quantize(normal(g, o, c).cuda())
+    t["weight2"] = gnnk.Weight8.quantize(normal(g, 40, o).cuda())
+    return t
+
+
+@pytest.mark.parametrize("n,c,o,dtype", [(1, 512, 768, BF16), (5000, 256, 384, F32), (3000, 2048, 2048, BF16),
+                                         (2000, 282, 141, F32)])
+def test_replays_on_another_stream_equal_eager(n, c, o, dtype):
+    t = tensors(41, n, c, o, dtype)
+    eager = [x.clone() for x in run_all(t)]
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        run_all(t)
+    torch.cuda.current_stream().wait_stream(side)
+    captured = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(captured, stream=side):
+        outs = run_all(t)
+    for _ in range(3):
+        for x in outs:
+            x.fill_(77)
+        captured.replay()
+        torch.cuda.synchronize()
+        for a, b in zip(outs, eager):
+            assert torch.equal(a, b)
+        _ = (t["x"] * 2).sum().item()
+
+
+def test_calls_on_several_streams_at_once():
+    ts = [tensors(50 + i, 4000 + 100 * i, 512, 512, BF16) for i in range(3)]
+    want = [[x.clone() for x in run_all(t)] for t in ts]
+    torch.cuda.synchronize()
+    streams = [torch.cuda.Stream() for _ in ts]
+    for _ in range(4):
+        got = []
+        for t, s in zip(ts, streams):
+            with torch.cuda.stream(s):
+                got.append(run_all(t))
+        torch.cuda.synchronize()
+        for a, b in zip(got, want):
+            assert all(torch.equal(x, y) for x, y in zip(a, b))
+
+
+def test_the_stream_argument():
+    """Calls given a stream run there, also what they allocate for themselves."""
+    t = tensors(61, 3000, 300, 200, F32)
+    want = run_all(t)
+    wq = torch.randn(64, 300, device="cuda")
+    torch.cuda.synchronize()
+    side = torch.cuda.Stream()
+    for _ in range(3):
+        with torch.cuda.stream(side):  # (outputs belong to the stream)
+            outs = {k: torch.empty_like(v) for k, v in zip(("y", "h", "dx"), want)}
+        y, h = gnnk.node_add_norm(t["x"], t["r"], t["w"], out=outs["y"], out_sum=outs["h"], stream=side)
+        dx, dw = gnnk.node_add_norm_backward(h, t["w"], t["g"], grad_sum=t["r"], grad_x=outs["dx"], stream=side)
+        weight = gnnk.Weight8.quantize(wq, stream=side)
+        torch.cuda.synchronize()
+        assert torch.equal(y, want[0]) and torch.equal(h, want[1]) and torch.equal(dx, want[2])
+        assert torch.equal(dw, want[3])
+        assert torch.equal(weight.packed, gnnk.Weight8.quantize(wq).packed)
+
+
+@pytest.mark.parametrize("tile", range(8))
+def test_places_past_32_bits(tile):
+    """Rows so far apart that their places in bytes and in elements pass 2^32."""
+    gnnk.set_option("linear8_tile", tile)
+    n, k, o, apart = 70000, 200, 70, 65536
+    big = torch.empty(n * apart, dtype=torch.int8, device="cuda").view(n, apart)  # 4.6 GB
+    q = big[:, 16:16 + k]
+    near = torch.randint(-127, 128, (n, k), dtype=torch.int8, device="cuda")
+    q.copy_(near)
+    s = torch.rand(n, device="cuda") + 0.5
+    weight = gnnk.Weight8.quantize(torch.randn(o, k, device="cuda"))
+    want = gnnk.node_linear_i8(weight, near, s)
+    assert torch.equal(gnnk.node_linear_i8(weight, q, s), want)
+    out = big.view(torch.bfloat16)[:, 200:200 + o]  # behind the rows read
+    assert torch.equal(gnnk.node_linear_i8(weight, q, s, out=out), want)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_norms_past_32_bits(dtype):
+    n, c, apart = 70000, 100, 65536 // (2 if dtype is F32 else 1)
+    big = torch.empty((n, apart), dtype=dtype, device="cuda")  # 9.2 GB
+    g = gen(3)
+    x, r, gy = (normal(g, n, c, dtype=dtype).cuda() for _ in range(3))
+    w = torch.ones(c, dtype=dtype)
+    far = [big[:, 16 + i * 200: 16 + i * 200 + c] for i in range(6)]
+    for t, v in zip(far, (x, r, gy)):
+        t.copy_(v)
+    y, h = gnnk.node_add_norm(x, r, w.cuda())
+    yf, hf = gnnk.node_add_norm(far[0], far[1], w.cuda(), out=far[3], out_sum=far[4])
+    assert torch.equal(yf, y) and torch.equal(hf, h)
+    dx, dw = gnnk.node_add_norm_backward(h, w.cuda(), gy, grad_sum=r)
+    dxf, dwf = gnnk.node_add_norm_backward(far[4], w.cuda(), far[2], grad_sum=far[1], grad_x=far[5])
+    assert torch.equal(dxf, dx) and torch.equal(dwf, dw)
+    q, s = gnnk.node_quantize(x)
+    qf, sf = gnnk.node_quantize(far[0], out=big.view(torch.int8)[:, 8000:8000 + c], scale=torch.empty_like(s))
+    assert torch.equal(qf, q) and torch.equal(sf, s)
