@@ -1688,7 +1688,7 @@ namespace {
 constexpr int NORM_MAX_COLS = 16384;
 constexpr int ROWS8_MAX_COLS = 65536;
 constexpr int WEIGHT8_MAX_OUTS = 1 << 24;
-constexpr int64_t NORM_BYTES = 12288, QUANT_BYTES = 20480;  // that a block moves, about
+constexpr int64_t NORM_BYTES = 20480;  // that a block moves, about
 constexpr int NORM_TILES = 512;        // tiles that fill the chip
 constexpr int ADD_NORM_RUN = 128;      // tiles that a workgroup adds up
 
@@ -1712,14 +1712,18 @@ Span flat(const void* p, int64_t bytes) { return Span{(uintptr_t)p, bytes > 0 ? 
 // wider ones take several, up to eight.  The backward has two or three rows in
 // registers and sums besides: half as many vectors a lane where eight
 // wavefronts hold the row all the same (65,536 rows of 4,096 bf16 606 -> 451 us).
-int add_norm_geo(AddNormArgs& A, const gnnk_tensor* x, bool bwd = false) {
+// Rows in 8 bits without a norm, of which a lane has little to load, lie in 16 or
+// 32 lanes where there are rows enough (262,144 of 256 fp32 71 -> 59 us, 232,965
+// of 512 bf16 76 -> 64).
+int add_norm_geo(AddNormArgs& A, const gnnk_tensor* x, AddNormMode mode) {
     A.C = (int32_t)cols_of(x);
     A.inv_C = 1.0f / (float)A.C;
     A.n = x->rows;
     const int V = x->dtype == GNNK_BF16 ? 8 : 4, NV = (A.C + V - 1) / V;
     int most = x->dtype == GNNK_BF16 ? 4 : 8;
-    if (bwd && NV <= 64 * 8 * most / 2) most /= 2;
-    A.L = std::min(64, pow2ceil(NV));
+    if (mode == ADD_NORM_BWD && NV <= 64 * 8 * most / 2) most /= 2;
+    const bool narrow = mode == QUANT8 && A.n >= 4096;
+    A.L = std::min(narrow && NV <= 16 * most ? 16 : narrow && NV <= 32 * most ? 32 : 64, pow2ceil(NV));
     A.waves = pow2ceil((NV + 64 * most - 1) / (64 * most));
     A.threads = std::max(256, A.waves * 64);
     const int lanes = A.waves > 1 ? A.waves * 64 : A.L;
@@ -1727,13 +1731,13 @@ int add_norm_geo(AddNormArgs& A, const gnnk_tensor* x, bool bwd = false) {
 }
 int rows_of_block(const AddNormArgs& A) { return A.threads / (A.waves > 1 ? A.waves * 64 : A.L); }
 
-// Blocks of a forward call: each moves about `bytes` bytes, taking some rows
+// Blocks of a forward call: each moves about NORM_BYTES, taking some rows
 // after others where one set of them is less (a row moves `moved` bytes).
 // 262,144 rows of 256 fp32, sum and norm, 16 KB a set: one set a block 180 us,
 // two 191, four 193, 2,048 blocks that share the rows 210; in 8 bits alone, 5 KB a
 // set: 96, 76, 67 and 65.
-void add_norm_blocks(AddNormArgs& A, int64_t moved, int64_t bytes) {
-    const int64_t per = rows_of_block(A), sets = std::max<int64_t>(1, (bytes + per * moved / 2) / (per * moved));
+void add_norm_blocks(AddNormArgs& A, int64_t moved) {
+    const int64_t per = rows_of_block(A), sets = std::max<int64_t>(1, (NORM_BYTES + per * moved / 2) / (per * moved));
     A.blocks = (int32_t)std::min<int64_t>((A.n + per * sets - 1) / (per * sets), 1 << 20);
 }
 
@@ -1825,11 +1829,11 @@ gnnk_status node_add_norm(const gnnk_tensor* x, const gnnk_tensor* residual, con
         return fail(GNNK_EINVAL, "an output overlaps an operand or the other one");
     if (x->rows == 0) return GNNK_OK;
     AddNormArgs A{};
-    const int npt = add_norm_geo(A, x);
+    const int npt = add_norm_geo(A, x, ADD_NORM);
     add_norm_operands(A, x, residual, w, eps, sum);
     A.out = out->data;
     A.out_stride = out->row_stride;
-    add_norm_blocks(A, A.C * (residual ? 4ll : 2ll) * (dtype_code(x) ? 2 : 4), NORM_BYTES);
+    add_norm_blocks(A, A.C * (residual ? 4ll : 2ll) * (dtype_code(x) ? 2 : 4));
     return launch_status(launch_node_add_norm(A, dtype_code(x), npt, ADD_NORM, stream), "norm launch");
 }
 
@@ -1847,12 +1851,12 @@ gnnk_status node_add_norm_i8(const gnnk_tensor* x, const gnnk_tensor* residual, 
         return fail(GNNK_EINVAL, "an output overlaps an operand or another one");
     if (x->rows == 0) return GNNK_OK;
     AddNormArgs A{};
-    const int npt = add_norm_geo(A, x);
+    const int npt = add_norm_geo(A, x, ADD_NORM8);
     add_norm_operands(A, x, residual, w, eps, sum);
     A.q = out->data;
     A.q_stride = out->row_stride;
     A.scale = out->scale;
-    add_norm_blocks(A, A.C * ((residual ? 3ll : 1ll) * (dtype_code(x) ? 2 : 4) + 1), NORM_BYTES);
+    add_norm_blocks(A, A.C * ((residual ? 3ll : 1ll) * (dtype_code(x) ? 2 : 4) + 1));
     return launch_status(launch_node_add_norm(A, dtype_code(x), npt, ADD_NORM8, stream), "norm launch");
 }
 
@@ -1866,12 +1870,12 @@ gnnk_status node_quantize(const gnnk_tensor* x, gnnk_rows8* out, hipStream_t str
         return fail(GNNK_EINVAL, "an output overlaps an operand or another one");
     if (x->rows == 0) return GNNK_OK;
     AddNormArgs A{};
-    const int npt = add_norm_geo(A, x);
+    const int npt = add_norm_geo(A, x, QUANT8);
     add_norm_operands(A, x, nullptr, nullptr, 0.0f, nullptr);
     A.q = out->data;
     A.q_stride = out->row_stride;
     A.scale = out->scale;
-    add_norm_blocks(A, A.C * (dtype_code(x) ? 3ll : 5ll), QUANT_BYTES);
+    add_norm_blocks(A, A.C * (dtype_code(x) ? 3ll : 5ll));
     return launch_status(launch_node_add_norm(A, dtype_code(x), npt, QUANT8, stream), "quantize launch");
 }
 
@@ -1893,7 +1897,7 @@ gnnk_status node_add_norm_backward(const gnnk_tensor* sum, const gnnk_tensor* w,
     if (!same_dtype({sum, w, grad_out, grad_sum, grad_x, grad_w}))
         return fail(GNNK_EINVAL, "all tensors must share one dtype");
     AddNormArgs A{};
-    const int npt = add_norm_geo(A, sum, true);
+    const int npt = add_norm_geo(A, sum, ADD_NORM_BWD);
     add_norm_tiles(A, dtype_code(sum));
     const size_t need = grad_w ? add_norm_work(A) : 0;
     if (need && (!work || work_bytes < need))
@@ -1931,7 +1935,7 @@ gnnk_status node_add_norm_work_bytes(const gnnk_tensor* sum, size_t* bytes) {
         cols_of(sum) > NORM_MAX_COLS || (sum->dtype != GNNK_F32 && sum->dtype != GNNK_BF16))
         return fail(GNNK_EINVAL, "fewer than 2^31 rows of at most %d columns", NORM_MAX_COLS);
     AddNormArgs A{};
-    add_norm_geo(A, sum, true);
+    add_norm_geo(A, sum, ADD_NORM_BWD);
     add_norm_tiles(A, dtype_code(sum));
     *bytes = add_norm_work(A);
     return GNNK_OK;
