@@ -104,6 +104,23 @@ struct Columns {
         IO<float, 4>::load(ls + nb * 64 + (lane & 15) * 4, s);
         IO<float, 4>::load(lb + nb * 64 + (lane & 15) * 4, b);
     }
+    // scales from LDS (those of the 64 columns at ls), biases from memory
+    __device__ __forceinline__ void load_mixed(const Linear8Args& A, const float* ls, int first, int lane) {
+        n = first + (lane & 15) * 4;
+        IO<float, 4>::load(ls + (lane & 15) * 4, s);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) b[i] = 0.0f;
+        if (A.bias) {
+            const T* const bias = reinterpret_cast<const T*>(A.bias);
+            if (n + 4 <= A.N) {
+                IO<T, 4>::load(bias + n, b);
+            } else {
+#pragma unroll
+                for (int i = 0; i < 4; ++i)
+                    if (n + i < A.N) b[i] = IO<T, 1>::load1(bias + n + i);
+            }
+        }
+    }
     // row r of the lane's four, of scale xs
     __device__ __forceinline__ void row(float xs, int r, i32x4 c0, i32x4 c1, i32x4 c2, i32x4 c3, float* t) const {
         t[0] = fmaf((float)c0[r] * xs, s[0], b[0]);
@@ -327,6 +344,12 @@ __device__ __forceinline__ void load_to_lds(const int8_t* from, uint32_t off, ui
                  : "memory");
 }
 
+// the same of 4 bytes a lane, at `to` + 4 * lane
+__device__ __forceinline__ void load_word_to_lds(const void* from, uint32_t off, uint32_t to) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(to), "v"(off), "s"(from)
+                 : "memory");
+}
+
 // Many rows, long sums: WM by two wavefronts form BM rows of BN output columns,
 // one tile after another.  Steps of 128 bytes of k, whole lines, are loaded
 // straight into one of two LDS buffers while the one before is multiplied; a
@@ -337,12 +360,10 @@ __global__ __launch_bounds__(WM * 128, BLOCKS) void linear8_deep_kernel(Linear8A
     constexpr int MT = BM / WM / 16, NT = BN / 32;
     constexpr int STAGE = (BM + BN) * KB, XL = BM / 16 / WM, WL = BN / 16 / WM;  // bytes; loads of a wavefront
     static_assert(NT % 4 == 0 && MT * WM * 16 == BM && XL * WM * 16 == BM && WL * WM * 16 == BN, "");
-    static_assert(BM == BN && BM + BN == WM * 128, "a thread holds one column's scale or one row's");
+    static_assert(BM == BN && BM + BN == WM * 128, "a lane loads one column's scale or one row's");
     extern __shared__ int8_t lds[];
     const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) int8_t*)lds;
-    float* const ls = reinterpret_cast<float*>(lds + 2 * STAGE);  // scales, biases of columns, scales of rows
-    float* const lb = ls + BN;
-    float* const lx = lb + BN;
+    float* const scales = reinterpret_cast<float*>(lds + 2 * STAGE);  // of columns and rows, for tiles in turn
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
     const int wm = (wave >> 1) * MT * 16, wn = (wave & 1) * NT / 4;  // first row, first block of 64 output columns
     const int S = (A.K + KB - 1) / KB, NB = (A.N + 63) / 64;
@@ -355,35 +376,44 @@ __global__ __launch_bounds__(WM * 128, BLOCKS) void linear8_deep_kernel(Linear8A
     const int8_t* const end = A.x + (A.M - 1) * A.x_stride + A.K;
     const int xr = (wm + (lane & 15)) * KB, wr = BM * KB + wn * WBLOCK + lane * 16;
 
-    int64_t m0 = 0;
-    int nb0 = 0;
-    const int8_t* xb = nullptr;
-    uint32_t xo[XL];
-    float scale = 0.0f, bias = 0.0f;
-    // the tile of number b: its place, its scales; false past the last one
-    auto begin = [&](int64_t b) {
+    struct Place {
+        int64_t m0;
+        int nb0;
+        bool there;
+    };
+    // the place of tile number b; none past the last one
+    auto place = [&](int64_t b) {
         // blocks are dealt to the eight dies in turn: each gets a run of tiles
         const int64_t t = (b & 7) * (G.padded >> 3) + (b >> 3);
-        if (b >= G.padded || t >= G.tiles) return false;
-        const int64_t group = t / ((int64_t)G.group * G.tn), in = t - group * G.group * G.tn;
-        const int64_t left = G.tm - group * G.group, high = left < G.group ? left : G.group;
-        m0 = (group * G.group + in % high) * BM;
-        nb0 = (int)(in / high) * (BN / 64);
+        if (b >= G.padded || t >= G.tiles) return Place{0, 0, false};
+        const int64_t group = t / ((int64_t)G.group * G.tn);
+        const int in = (int)(t - group * G.group * G.tn);
+        const int64_t left = G.tm - group * G.group;
+        const int high = left < G.group ? (int)left : G.group;
+        return Place{(group * G.group + in % high) * BM, in / high * (BN / 64), true};
+    };
+    int64_t m0;
+    int nb0;
+    const int8_t* xb;
+    uint32_t xo[XL];
+    // go on to the tile at p; its scales load into LDS
+    auto begin = [&](const Place& p, int turn) {
+        m0 = p.m0;
+        nb0 = p.nb0;
         xb = A.x + m0 * A.x_stride;
 #pragma unroll
         for (int i = 0; i < XL; ++i) {
             const int r = (wave * XL + i) * 8 + (lane >> 3);
             xo[i] = (uint32_t)(m0 + r < A.M ? r : (int)(A.M - 1 - m0)) * (uint32_t)A.x_stride + piece;
         }
-        if (tid < BN) {
-            const int n = nb0 * 64 + tid, c = n < A.N ? n : A.N - 1;
-            scale = A.ws[c];
-            bias = A.bias ? IO<T, 1>::load1(reinterpret_cast<const T*>(A.bias) + c) : 0.0f;
+        const uint32_t to = lds0 + 2 * STAGE + turn * (BM + BN) * 4 + wave * 256;
+        if (wave < WM) {
+            const int n = nb0 * 64 + tid;
+            load_word_to_lds(A.ws, (n < A.N ? n : A.N - 1) * 4, to);
         } else {
-            const int64_t m = m0 + tid - BN;
-            scale = A.xs[m < A.M ? m : A.M - 1];
+            const int r = tid - BN;
+            load_word_to_lds(A.xs + m0, (m0 + r < A.M ? r : (int)(A.M - 1 - m0)) * 4, to);
         }
-        return true;
     };
     // loads `first` to `last` of a wavefront's for step s
     auto fill = [&](int s, int first, int last) {
@@ -444,17 +474,21 @@ __global__ __launch_bounds__(WM * 128, BLOCKS) void linear8_deep_kernel(Linear8A
     };
 
     int64_t b = blockIdx.x;
-    if (!begin(b)) return;
+    Place at = place(b);
+    if (!at.there) return;
+    begin(at, 0);
     fill(0, 0, XL + WL);
     if (S > 1) fill(1, 0, XL + WL);
-    for (bool more = true; more;) {
-        if (tid < BN) {
-            ls[tid] = scale;
-            lb[tid] = bias;
-        } else {
-            lx[tid - BN] = scale;
-        }
-        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    bool drained = true;
+    for (int turn = 0; at.there; turn ^= 1) {
+        // the first step is there; what may be on its way: the second one, and
+        // the stores of a whole tile before
+        if (drained || S == 1)
+            asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        else
+            asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(XL + WL + MT * NT < 63 ? XL + WL + MT * NT : 63) : "memory");
+        b += gridDim.x;
+        at = place(b);
 #pragma unroll
         for (int i = 0; i < MT; ++i)
 #pragma unroll
@@ -471,23 +505,28 @@ __global__ __launch_bounds__(WM * 128, BLOCKS) void linear8_deep_kernel(Linear8A
         asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
         const int64_t m = m0 + wm;
         const int nb = nb0 + wn;
-        b += gridDim.x;
-        more = begin(b);
-        if (more) {
+        if (at.there) {
+            begin(at, turn ^ 1);
             fill(0, 0, XL + WL);
             if (S > 1) fill(1, 0, XL + WL);
         }
         half_step(1, -1, -1);
 
+        const float* const ls = scales + turn * (BM + BN);
         const uint32_t oo = ((uint32_t)(lane >> 4) * 4 * (uint32_t)A.out_stride + (lane & 15) * 4) * sizeof(T);
         float xs[MT][4];
 #pragma unroll
-        for (int i = 0; i < MT; ++i) IO<float, 4>::load(lx + wm + i * 16 + (lane >> 4) * 4, xs[i]);
+        for (int i = 0; i < MT; ++i) IO<float, 4>::load(ls + BN + wm + i * 16 + (lane >> 4) * 4, xs[i]);
+        Columns<T> cols[NT / 4];
+#pragma unroll
+        for (int j = 0; j < NT / 4; ++j) cols[j].load_mixed(A, ls + (wn + j) * 64, (nb + j) * 64, lane);
+        // (of a whole tile: a store for each four sums)
+        const bool whole = m + MT * 16 <= A.M && (nb + NT / 4) * 64 <= A.N;
+        drained = !whole;
 #pragma unroll
         for (int j = 0; j < NT; j += 4) {
-            Columns<T> c;
-            c.load_lds(ls, lb, wn + j / 4, (nb + j / 4) * 64, lane);
-            if (m + MT * 16 <= A.M && (nb + j / 4 + 1) * 64 <= A.N) {
+            const Columns<T>& c = cols[j / 4];
+            if (whole) {
                 char* const base = reinterpret_cast<char*>(reinterpret_cast<T*>(A.out) + m * A.out_stride + (nb + j / 4) * 64);
 #pragma unroll
                 for (int i = 0; i < MT; ++i)
@@ -504,8 +543,6 @@ __global__ __launch_bounds__(WM * 128, BLOCKS) void linear8_deep_kernel(Linear8A
                             acc[i][j + 3]);
             }
         }
-        // (the scales are read to their end)
-        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
     }
 }
 
@@ -650,7 +687,7 @@ void launch_deep_of(const Linear8Args& a, hipStream_t s) {
     g.group = 8;
     const int64_t blocks = g.padded < 256 * BLOCKS ? g.padded : 256 * BLOCKS;
     hipLaunchKernelGGL((linear8_deep_kernel<T, BM, BN, WM, BLOCKS, RAGGED, PAST>), dim3((unsigned)blocks), dim3(WM * 128),
-                       2 * (BM + BN) * KB + (BM + 2 * BN) * 4, s, a, g);
+                       2 * (BM + BN) * KB + 2 * (BM + BN) * 4, s, a, g);
 }
 
 template <typename T, int BM, int BN, int WM, int BLOCKS>
