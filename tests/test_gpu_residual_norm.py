@@ -195,3 +195,16 @@ def test_weight_gradient_of_many_rows_is_the_same_every_time():
         dx, bx, terms, tb = norm_gradients(x.double(), w.double(), gy.double(), None, 1e-6)
         close(first[1], terms.sum(0), tb.sum(0), "dw")
         close(first[0], dx, bx, "dx")
+
+
+def test_the_sum_may_be_left_out():
+    """The C call takes a residual without keeping the sum."""
+    g, x, r, w = inputs(60, 100, F32, 2)
+    xd, rd, wd = x.cuda(), r.cuda(), w.cuda()
+    y, _ = gnnk.node_add_norm(xd, rd, wd)
+    q, s, _ = gnnk.node_add_norm_i8(xd, rd, wd)
+    y1, q1, s1 = torch.empty_like(y), torch.empty_like(q), torch.empty_like(s)
+    d, lib, stream = gnnk._desc, gnnk.load(), torch.cuda.current_stream().cuda_stream
+    assert lib.node_add_norm(d(xd), d(rd), d(wd.view(1, 1, -1)), 1e-6, None, d(y1), stream) == gnnk.OK
+    assert lib.node_add_norm_i8(d(xd), d(rd), d(wd.view(1, 1, -1)), 1e-6, None, gnnk._rows8(q1, s1), stream) == gnnk.OK
+    assert torch.equal(y1, y) and torch.equal(q1, q) and torch.equal(s1, s)
