@@ -153,6 +153,20 @@ __device__ __forceinline__ void load_scales(const Linear8Args& A, int64_t m, flo
     }
 }
 
+// 16 bytes a lane from memory, at `from` + `off`, into LDS at `to` + 16 * lane
+// (one `from` and `to` for all lanes).  It counts as a load of the wavefront's
+// (vmcnt) that the compiler does not see: waits for it are written out.
+__device__ __forceinline__ void load_to_lds(const int8_t* from, uint32_t off, uint32_t to) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(off), "s"(from)
+                 : "memory");
+}
+
+// the same of 4 bytes a lane, at `to` + 4 * lane
+__device__ __forceinline__ void load_word_to_lds(const void* from, uint32_t off, uint32_t to) {
+    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(to), "v"(off), "s"(from)
+                 : "memory");
+}
+
 // the tiles of a product: tm by tn, `group` of rows side by side; padded to
 // eight equal runs
 struct TileArgs {
@@ -334,20 +348,6 @@ __global__ __launch_bounds__(WM * WN * 64, BLOCKS) void linear8_tile_kernel(Line
                         acc[i][j + 3]);
         }
     }
-}
-
-// 16 bytes a lane from memory, at `from` + `off`, into LDS at `to` + 16 * lane
-// (one `from` and `to` for all lanes).  It counts as a load of the wavefront's
-// (vmcnt) that the compiler does not see: waits for it are written out.
-__device__ __forceinline__ void load_to_lds(const int8_t* from, uint32_t off, uint32_t to) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(off), "s"(from)
-                 : "memory");
-}
-
-// the same of 4 bytes a lane, at `to` + 4 * lane
-__device__ __forceinline__ void load_word_to_lds(const void* from, uint32_t off, uint32_t to) {
-    asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dword %1, %2" ::"s"(to), "v"(off), "s"(from)
-                 : "memory");
 }
 
 // Many rows, long sums: WM by two wavefronts form BM rows of BN output columns,
@@ -560,12 +560,9 @@ __global__ __launch_bounds__(WAVES * 64, 1) void linear8_stream_kernel(Linear8Ar
     const int64_t run = (int64_t)(at / G.panels) * 8 + die, runs = (int64_t)(gridDim.x >> 3) / G.panels * 8;
     const int NB = (A.N + 63) / 64, nb0 = panel * G.width;
     const int nbs = NB - nb0 < G.width ? NB - nb0 : G.width;  // blocks of 64 output columns
-    {
-        const i32x4* const w = reinterpret_cast<const i32x4*>(A.w + (int64_t)nb0 * KS * WBLOCK);
-        i32x4* const l = reinterpret_cast<i32x4*>(lds);
-        const int pieces = nbs * KS * (WBLOCK / 16);
-        for (int c = tid; c < pieces; c += WAVES * 64) l[c] = w[c];
-    }
+    const uint32_t lds0 = (uint32_t)(uintptr_t)(__attribute__((address_space(3))) int8_t*)lds;
+    for (int c = wave; c < nbs * KS * (WBLOCK / 1024); c += WAVES)
+        load_to_lds(A.w + (int64_t)nb0 * KS * WBLOCK + c * 1024, lane * 16, lds0 + c * 1024);
     // scales and biases beside it: read from memory, a wavefront would wait for
     // its own stores each time
     float* const ls = reinterpret_cast<float*>(lds + G.width * KS * WBLOCK);
@@ -575,7 +572,6 @@ __global__ __launch_bounds__(WAVES * 64, 1) void linear8_stream_kernel(Linear8Ar
         ls[c] = n < A.N ? A.ws[n] : 0.0f;
         lb[c] = n < A.N && A.bias ? IO<T, 1>::load1(reinterpret_cast<const T*>(A.bias) + n) : 0.0f;
     }
-    __syncthreads();
     // a lane's place in 16 rows, 32 bits beside an address that the lanes share
     const uint32_t xo = (uint32_t)(lane & 15) * (uint32_t)A.x_stride + (lane >> 4) * 16;
     const uint32_t oo = ((uint32_t)(lane >> 4) * 4 * (uint32_t)A.out_stride + (lane & 15) * 4) * sizeof(T);
@@ -583,10 +579,14 @@ __global__ __launch_bounds__(WAVES * 64, 1) void linear8_stream_kernel(Linear8Ar
     const int64_t tiles = (A.M + MI * 16 - 1) / (MI * 16);
     const int part = wave % G.split, teams = WAVES / G.split;
     i32x4 x[KS * 2][MI];
+    float xs[MI][4];
     auto load = [&](int64_t tile) {
         const int64_t m0 = tile * (MI * 16);
+#pragma unroll
+        for (int i = 0; i < MI; ++i) load_scales(A, m0 + i * 16 + (lane >> 4) * 4, xs[i]);
         const int8_t* const base = A.x + m0 * A.x_stride;
-        if (m0 + MI * 16 < A.M && A.K % KB == 0) {
+        if (base + (MI * 16 - 1) * A.x_stride + KS * KB <= end) {
+            // (what follows a row's end counts for nothing, and lies in the tensor)
 #pragma unroll
             for (int i = 0; i < MI; ++i)
 #pragma unroll
@@ -607,12 +607,11 @@ __global__ __launch_bounds__(WAVES * 64, 1) void linear8_stream_kernel(Linear8Ar
     };
     const int64_t step = runs * teams;
     int64_t tile = run + runs * (wave / G.split);
-    for (; tile < tiles; tile += step) {
+    if (tile < tiles) load(tile);
+    // the panel is there
+    asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    while (tile < tiles) {
         const int64_t m0 = tile * (MI * 16);
-        float xs[MI][4];
-#pragma unroll
-        for (int i = 0; i < MI; ++i) load_scales(A, m0 + i * 16 + (lane >> 4) * 4, xs[i]);
-        load(tile);
         for (int nb = part; nb < nbs; nb += G.split) {
             const int8_t* const w = lds + nb * KS * WBLOCK + lane * 16;
             i32x4 acc[4][MI] = {};
@@ -642,6 +641,8 @@ __global__ __launch_bounds__(WAVES * 64, 1) void linear8_stream_kernel(Linear8Ar
                     c.store(A, m0 + i * 16 + (lane >> 4) * 4, xs[i], acc[0][i], acc[1][i], acc[2][i], acc[3][i]);
             }
         }
+        tile += step;
+        if (tile < tiles) load(tile);
     }
 }
 
