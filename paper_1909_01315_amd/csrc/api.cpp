@@ -1690,7 +1690,8 @@ constexpr int ROWS8_MAX_COLS = 65536;
 constexpr int WEIGHT8_MAX_OUTS = 1 << 24;
 constexpr int64_t NORM_BYTES = 20480;  // that a block moves, about
 constexpr int NORM_TILES = 512;        // tiles that fill the chip
-constexpr int ADD_NORM_RUN = 128;      // tiles that a workgroup adds up
+constexpr int ADD_NORM_ONCE = 4096;    // tiles that one launch adds up, and tiles that a workgroup of two
+constexpr int ADD_NORM_RUN = 512;      // launches does
 
 int64_t cols_of(const gnnk_tensor* t) { return (int64_t)t->heads * t->feat; }
 
@@ -1741,20 +1742,19 @@ void add_norm_blocks(AddNormArgs& A, int64_t moved) {
     A.blocks = (int32_t)std::min<int64_t>((A.n + per * sets - 1) / (per * sets), 1 << 20);
 }
 
-// The tiles of a backward: as short as their sums' share of the bytes allows (32
-// rows of bf16 or 16 of fp32, an eighth or less of what the rows take on short
-// grids), which the memory likes (262,144 rows of 256 fp32 without the weight's
+// The tiles of a backward: as short as their sums' share of the bytes allows (16
+// rows, or 32 of many rows of bf16, 3 to 6%; fewer only to fill the chip), which
+// the memory likes (262,144 rows of 256 fp32 without the weight's
 // gradient, tiles of 128 / 64 / 32 / 16 rows: 222 / 209 / 199 / 194 us), in at least
-// two sets of rows, the second of which loads behind the first.  A workgroup
-// adds up ADD_NORM_RUN tiles.
+// two sets of rows, the second of which loads behind the first.
 void add_norm_tiles(AddNormArgs& A, int dtype) {
     const int64_t per = rows_of_block(A), sets = (A.n + per - 1) / per;
-    int64_t steps = std::max<int64_t>(2, (dtype == 1 ? 32 : 16) / per);
+    int64_t steps = std::max<int64_t>(2, (dtype == 1 && sets * per >= 32 * NORM_TILES * 4 ? 32 : 16) / per);
     if (sets < steps * NORM_TILES) steps = std::max<int64_t>(1, sets / NORM_TILES);
     A.steps = (int32_t)steps;
     A.parts = (sets + steps - 1) / steps;
     A.blocks = (int32_t)std::min<int64_t>(A.parts, 1 << 20);
-    A.runs = (int32_t)std::min<int64_t>(std::max<int64_t>(1, A.parts / ADD_NORM_RUN), 256);
+    A.runs = A.parts <= ADD_NORM_ONCE ? 1 : (int32_t)std::min<int64_t>(A.parts / ADD_NORM_RUN, 256);
 }
 
 size_t add_norm_parts_bytes(const AddNormArgs& A) { return ((size_t)A.parts * A.C * 4 + 255) / 256 * 256; }

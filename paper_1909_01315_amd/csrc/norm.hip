@@ -332,16 +332,19 @@ __global__ __launch_bounds__(WIDE ? 512 : 256) void node_add_norm_backward_kerne
     }
 }
 
-// the weight's gradient: the tiles' sums in fp64, 64 columns and ADD_NORM_RUN
-// tiles a workgroup, four runs of them side by side, each in order; then the
-// sums of such runs in the same way
-template <typename T, typename P>
-__global__ __launch_bounds__(256) void node_add_norm_dw_kernel(const P* part, int64_t parts, int C, double* sums, T* dw,
-                                                               int runs) {
-    __shared__ double red[4][64];
-    const int c = threadIdx.x & 63, q = threadIdx.x >> 6;
-    const int64_t col = (int64_t)(blockIdx.x / runs) * 64 + c, run = blockIdx.x % runs;
-    const int64_t each = (parts + runs - 1) / runs, per = (each + 3) / 4;
+// the weight's gradient: the tiles' sums in fp64, COLS columns and a run of
+// tiles a workgroup, 1,024 / COLS parts of it side by side, each in order, then
+// the parts in order; of several runs their sums, which a second launch adds up.
+// One launch where it can be: 1,250 tiles of 282 columns, 16 columns a workgroup,
+// 6.6 us; in runs of 512 tiles, 64 columns a workgroup, and a second launch 10
+template <typename T, typename P, int COLS>
+__global__ __launch_bounds__(1024) void node_add_norm_dw_kernel(const P* part, int64_t parts, int C, double* sums, T* dw,
+                                                                int runs) {
+    constexpr int SUB = 1024 / COLS;
+    __shared__ double red[SUB][COLS + 1];
+    const int c = threadIdx.x % COLS, q = threadIdx.x / COLS;
+    const int64_t col = (int64_t)(blockIdx.x / runs) * COLS + c, run = blockIdx.x % runs;
+    const int64_t each = (parts + runs - 1) / runs, per = (each + SUB - 1) / SUB;
     const int64_t stop = (run + 1) * each < parts ? (run + 1) * each : parts;
     const int64_t first = run * each + q * per, end = first + per < stop ? first + per : stop;
     double sum = 0.0;
@@ -357,8 +360,14 @@ __global__ __launch_bounds__(256) void node_add_norm_dw_kernel(const P* part, in
     }
     red[q][c] = sum;
     __syncthreads();
+    if (q < 4) {
+        for (int k = 1; k < SUB / 4; ++k) sum = (k == 1 ? red[q * (SUB / 4)][c] : sum) + red[q * (SUB / 4) + k][c];
+    }
+    __syncthreads();
+    if (q < 4) red[q][c] = sum;
+    __syncthreads();
     if (q == 0 && col < C) {
-        sum += red[1][c] + red[2][c] + red[3][c];
+        sum = red[0][c] + red[1][c] + red[2][c] + red[3][c];
         if (sums) sums[run * C + col] = sum;
         else IO<T, 1>::store1(dw + col, (float)sum);
     }
@@ -402,16 +411,16 @@ void launch_t(const AddNormArgs& a, int npt, int mode, hipStream_t s) {
         else if constexpr (sizeof(T) == 4) launch_p<T, 8>(a, mode, s);
     }
     if (mode == ADD_NORM_BWD && a.part) {
-        const unsigned wide = (unsigned)((a.C + 63) / 64);
+        const unsigned wide = (unsigned)((a.C + 63) / 64), narrow = (unsigned)((a.C + 15) / 16);
         T* const dw = reinterpret_cast<T*>(a.dw);
         if (a.runs > 1) {
-            hipLaunchKernelGGL((node_add_norm_dw_kernel<T, float>), dim3(wide * a.runs), dim3(256), 0, s, a.part, a.parts,
-                               a.C, a.sums, dw, a.runs);
-            hipLaunchKernelGGL((node_add_norm_dw_kernel<T, double>), dim3(wide), dim3(256), 0, s, a.sums,
+            hipLaunchKernelGGL((node_add_norm_dw_kernel<T, float, 64>), dim3(wide * a.runs), dim3(1024), 0, s, a.part,
+                               a.parts, a.C, a.sums, dw, a.runs);
+            hipLaunchKernelGGL((node_add_norm_dw_kernel<T, double, 16>), dim3(narrow), dim3(1024), 0, s, a.sums,
                                (int64_t)a.runs, a.C, nullptr, dw, 1);
         } else {
-            hipLaunchKernelGGL((node_add_norm_dw_kernel<T, float>), dim3(wide), dim3(256), 0, s, a.part, a.parts, a.C,
-                               nullptr, dw, 1);
+            hipLaunchKernelGGL((node_add_norm_dw_kernel<T, float, 16>), dim3(narrow), dim3(1024), 0, s, a.part, a.parts,
+                               a.C, nullptr, dw, 1);
         }
     }
 }
