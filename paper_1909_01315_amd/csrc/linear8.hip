@@ -61,6 +61,19 @@ __device__ __forceinline__ i32x4 load_x(const int8_t* row, int k, int K, const i
     return i32x4{x.x, x.y, x.z, x.w};
 }
 
+// The same of any address, from the five words that hold the 16 bytes: loads at
+// addresses that are no multiple of 4 take twice as long (100,000 rows of 282 to
+// 128 columns 18 -> 14 us, of 1,001 to 512 111 -> 90; through tiles they wait for
+// less, 1,501 to 1,500 384 -> 505).  Reads up to 3 bytes before and 4 after.
+__device__ __forceinline__ i32x4 load_shifted(const int8_t* p) {
+    const uint32_t by = (uint32_t)(uintptr_t)p & 3;
+    const uint32_t* const w = reinterpret_cast<const uint32_t*>(p - by);
+    const i4_el a = *reinterpret_cast<const i4_el*>(w);
+    const uint32_t b = w[4];
+    return i32x4{(int)__builtin_amdgcn_alignbyte(a.y, a.x, by), (int)__builtin_amdgcn_alignbyte(a.z, a.y, by),
+                 (int)__builtin_amdgcn_alignbyte(a.w, a.z, by), (int)__builtin_amdgcn_alignbyte(b, a.w, by)};
+}
+
 // four columns; NT: past the caches
 template <typename T, bool NT>
 __device__ __forceinline__ void put_four(T* p, const float* t) {
@@ -550,7 +563,7 @@ __global__ __launch_bounds__(WM * 128, BLOCKS) void linear8_deep_kernel(Linear8A
 // in LDS and its wavefronts stream rows past it, MI * 16 at a time, which they
 // read straight into registers and hold there for all of the panel's columns.
 // Nothing waits for another wavefront once the panel is there.
-template <typename T, int KS, int MI, int WAVES, bool NT>
+template <typename T, int KS, int MI, int WAVES, bool NT, bool SHIFT>
 __global__ __launch_bounds__(WAVES * 64, 1) void linear8_stream_kernel(Linear8Args A, StreamArgs G) {
     extern __shared__ int8_t lds[];
     const int tid = threadIdx.x, wave = __builtin_amdgcn_readfirstlane(tid >> 6), lane = tid & 63;
@@ -585,13 +598,14 @@ __global__ __launch_bounds__(WAVES * 64, 1) void linear8_stream_kernel(Linear8Ar
 #pragma unroll
         for (int i = 0; i < MI; ++i) load_scales(A, m0 + i * 16 + (lane >> 4) * 4, xs[i]);
         const int8_t* const base = A.x + m0 * A.x_stride;
-        if (base + (MI * 16 - 1) * A.x_stride + KS * KB <= end) {
+        if (base + (MI * 16 - 1) * A.x_stride + KS * KB + (SHIFT ? 4 : 0) <= end && (!SHIFT || tile > 0)) {
             // (what follows a row's end counts for nothing, and lies in the tensor)
 #pragma unroll
             for (int i = 0; i < MI; ++i)
 #pragma unroll
                 for (int k = 0; k < KS * 2; ++k)
-                    x[k][i] = load_x<false>(base + i * 16 * A.x_stride + k * 64 + xo, 0, A.K, end);
+                    x[k][i] = SHIFT ? load_shifted(base + i * 16 * A.x_stride + k * 64 + xo)
+                                    : load_x<false>(base + i * 16 * A.x_stride + k * 64 + xo, 0, A.K, end);
         } else {
 #pragma unroll
             for (int i = 0; i < MI; ++i) {
@@ -708,7 +722,7 @@ void launch_few(const Linear8Args& a, int waves, hipStream_t s) {
                        waves * MI * NJ * 1024, s, a, waves);
 }
 
-template <typename T, int KS, int MI, int WAVES, bool NT>
+template <typename T, int KS, int MI, int WAVES, bool NT, bool SHIFT>
 void launch_stream(const Linear8Args& a, hipStream_t s) {
     constexpr int CUS = 32;  // of a die
     const int NB = (a.N + 63) / 64, most = LDS_BYTES / (KS * WBLOCK + 512);
@@ -720,21 +734,27 @@ void launch_stream(const Linear8Args& a, hipStream_t s) {
     const int64_t tiles = (a.M + MI * 16 - 1) / (MI * 16);
     g.split = 1;
     while (WAVES % (g.split * 2) == 0 && g.split < g.width && tiles * g.split < runs * WAVES / 2) g.split *= 2;
-    hipLaunchKernelGGL((linear8_stream_kernel<T, KS, MI, WAVES, NT>), dim3((unsigned)(runs * g.panels)),
+    hipLaunchKernelGGL((linear8_stream_kernel<T, KS, MI, WAVES, NT, SHIFT>), dim3((unsigned)(runs * g.panels)),
                        dim3(WAVES * 64), g.width * (KS * WBLOCK + 512), s, a, g);
+}
+
+template <typename T, int MI, int WAVES, bool NT, bool SHIFT>
+void launch_streams_of(const Linear8Args& a, hipStream_t s) {
+    const int KS = (a.K + KB - 1) / KB;
+    if (KS == 1) return launch_stream<T, 1, MI, WAVES, NT, SHIFT>(a, s);
+    if (KS == 2) return launch_stream<T, 2, MI, WAVES, NT, SHIFT>(a, s);
+    if (KS == 3) return launch_stream<T, 3, MI, WAVES, NT, SHIFT>(a, s);
+    if (KS == 4) return launch_stream<T, 4, MI, WAVES, NT, SHIFT>(a, s);
+    if (KS == 5) return launch_stream<T, 5, MI, WAVES, NT, SHIFT>(a, s);
+    if (KS == 6) return launch_stream<T, 6, MI, WAVES, NT, SHIFT>(a, s);
+    if (KS == 7) return launch_stream<T, 7, MI, WAVES, NT, SHIFT>(a, s);
+    return launch_stream<T, 8, MI, WAVES, NT, SHIFT>(a, s);
 }
 
 template <typename T, int MI, int WAVES, bool NT>
 void launch_streams(const Linear8Args& a, hipStream_t s) {
-    const int KS = (a.K + KB - 1) / KB;
-    if (KS == 1) return launch_stream<T, 1, MI, WAVES, NT>(a, s);
-    if (KS == 2) return launch_stream<T, 2, MI, WAVES, NT>(a, s);
-    if (KS == 3) return launch_stream<T, 3, MI, WAVES, NT>(a, s);
-    if (KS == 4) return launch_stream<T, 4, MI, WAVES, NT>(a, s);
-    if (KS == 5) return launch_stream<T, 5, MI, WAVES, NT>(a, s);
-    if (KS == 6) return launch_stream<T, 6, MI, WAVES, NT>(a, s);
-    if (KS == 7) return launch_stream<T, 7, MI, WAVES, NT>(a, s);
-    return launch_stream<T, 8, MI, WAVES, NT>(a, s);
+    if ((a.x_stride | (int64_t)(uintptr_t)a.x) & 3) return launch_streams_of<T, MI, WAVES, NT, true>(a, s);
+    launch_streams_of<T, MI, WAVES, NT, false>(a, s);
 }
 
 enum Tile { AUTO, FEW, TILE64, TILE128, DEEP128, DEEP256, STREAM, STREAM_PAST };
@@ -743,42 +763,43 @@ enum Tile { AUTO, FEW, TILE64, TILE128, DEEP128, DEEP256, STREAM, STREAM_PAST };
 // measured (us; a call of few rows takes 6.5 on the host):
 //  - few rows, or so few products for their depth that one block after another
 //    would read long sums: FEW (2,048 to 2,048 columns, 130 rows 9.2, DEEP128
-//    11.0, 300 rows 16.6 and 11.6; 4,096 to 1,024, 200 rows 11 and 18)
-//  - rows of up to 512 columns, and up to 1,024 where they lie at any address:
-//    STREAM (100,000 rows, 512 to 512 columns 34, DEEP128 40, TILE128 60; 600 to
-//    600 at any address 57, TILE128 90)
-//  - other rows in 16-byte pieces: DEEP256 where sums are long and the last
+//    11.0, 300 rows 16.6 and 11.6; 4,096 to 1,024, 200 rows 11 and 18; at addresses
+//    that are no whole words half as many: 3,001 to 1,000, 400 rows 31, TILE64 19)
+//  - rows of up to 512 columns, and up to 1,024 where they do not start on 16
+//    bytes: STREAM (100,000 rows, 512 to 512 columns 34, DEEP128 40, TILE128 60;
+//    600 to 512 in rows of 600 bytes 47, 53, 72; 1,024 to 512 73, 68, 92)
+//  - other rows that start on whole words: DEEP256 where sums are long and the last
 //    round of tiles is not much shorter than the chip is wide (20,000 rows, 4,096
 //    to 512 columns, 158 tiles 45, DEEP128 53; 1,000 rows, 64 tiles 38, 18.5;
 //    20,000 rows, 1,024 to 1,024 columns 37, 27), else DEEP128
 //  - what is left, wider rows at any address: tiles through registers, small
 //    ones where those fill the chip (4,000 rows, 1,000 to 300 columns 11.3 and 14;
 //    20,000 rows 23 and 19)
-Tile choose(const Linear8Args& a, int es, int KS, bool pieces, bool streams) {
+Tile choose(const Linear8Args& a, int es, int KS, bool words, bool lines, bool streams) {
     const int64_t macs = (a.M + 63) / 64 * 64 * a.N * a.K;
-    if (a.M <= 64 || (KS > 4 && macs <= KS * 65000000ll)) return FEW;
-    if (streams && (KS <= 4 || !pieces)) return a.M * a.N * es > PAST_CACHES ? STREAM_PAST : STREAM;
-    if (!pieces) return ((a.M + 63) / 64) * ((a.N + 63) / 64) <= 512 ? TILE64 : TILE128;
+    if (a.M <= 64 || (KS > 4 && macs <= KS * (words ? 65000000ll : 30000000ll))) return FEW;
+    if (streams && (KS <= 4 || !lines)) return a.M * a.N * es > PAST_CACHES ? STREAM_PAST : STREAM;
+    if (!words) return ((a.M + 63) / 64) * ((a.N + 63) / 64) <= 512 ? TILE64 : TILE128;
     const int64_t big = ((a.M + 255) / 256) * ((a.N + 255) / 256);
-    return KS >= 16 && big * 100 >= (big + 255) / 256 * 256 * 55 ? DEEP256 : DEEP128;
+    return KS >= 16 && a.N > 256 && big * 100 >= (big + 255) / 256 * 256 * 55 ? DEEP256 : DEEP128;
 }
 
 template <typename T>
 void launch_t(const Linear8Args& a, int tile, hipStream_t s) {
     const int KS = (a.K + KB - 1) / KB, waves = KS < 16 ? KS : 16;
-    // places within a tile of rows fit 32 bits; rows in 16-byte pieces; rows
-    // that a wavefront's registers hold
+    // places within a tile of rows fit 32 bits; rows that start on whole words, as
+    // loads into LDS take them, or on 16 bytes; rows that a wavefront's registers hold
     const bool near = a.x_stride < (1 << 24) && a.out_stride < (1 << 24);
-    const bool pieces = near && a.x_stride % 16 == 0 && ((uintptr_t)a.x & 15) == 0;
-    const bool streams = near && KS <= 8 && a.N <= 4096;
-    switch (tile ? tile : choose(a, sizeof(T), KS, pieces, streams)) {
+    const int64_t place = a.x_stride | (int64_t)(uintptr_t)a.x;
+    const bool words = near && place % 4 == 0, lines = place % 16 == 0, streams = near && KS <= 8 && a.N <= 4096;
+    switch (tile ? tile : choose(a, sizeof(T), KS, words, lines, streams)) {
         case FEW: return a.M > 16 ? launch_few<T, 4, 1>(a, waves, s) : launch_few<T, 1, 1>(a, waves, s);
         case TILE64: return launch_tile<T, 64, 64, 2, 1, 2>(a, s);
         case DEEP128:
-            if (pieces) return launch_deep<T, 128, 128, 2, 2>(a, s);
+            if (words) return launch_deep<T, 128, 128, 2, 2>(a, s);
             break;
         case DEEP256:
-            if (pieces) return launch_deep<T, 256, 256, 4, 1>(a, s);
+            if (words) return launch_deep<T, 256, 256, 4, 1>(a, s);
             break;
         case STREAM:
             if (streams) return launch_streams<T, 1, 16, false>(a, s);
