@@ -32,9 +32,10 @@
  *    node_rotary, node_norm_rotary and node_add_norm in place).
  *  - Edge tensors are indexed by edge id.  Node tensors by node id.
  *  - Index ranges are not checked on the compute path; use graph_validate.
- *  - All floating-point tensors of one call share one dtype.  Sums and dot
- *    products accumulate in fp64 and are rounded once to the output dtype
- *    (bf16 outputs: to fp32, then to bf16 round-to-nearest-even).
+ *  - All floating-point tensors of one call share one dtype (scales of 8-bit
+ *    rows are fp32).  Sums and dot products accumulate in fp64 and are rounded
+ *    once to the output dtype (bf16 outputs: to fp32, then to bf16
+ *    round-to-nearest-even), unless a call says otherwise.
  *  - Rows of any width: a sum over the features of a message (DOT, or the
  *    gradient of an operand broadcast over features) wider than one pass of a
  *    wavefront (64 lanes of 4 fp32 or 8 bf16 values) adds its passes in fp64
@@ -645,6 +646,12 @@ gnnk_status node_linear_i8(const gnnk_rows8* x, const gnnk_weight8* w, const gnn
  *                 whole batches of it: 0 (default) two where a batch holds
  *                 64 or more edges (16 or more lane groups), else one;
  *                 otherwise 1-8 (results do not depend on it)
+ *   "linear8_tile" kernel of node_linear_i8: 0 (default) by the sizes and
+ *                 addresses; otherwise 1 for few rows, 2 and 3 tiles of 64 and
+ *                 of 128, 4 and 5 deep tiles of 128 and of 256, 6 and 7 rows
+ *                 that stream past a panel of the weight, 7 with stores past
+ *                 the caches; tiles of 128 where a call does not allow the one
+ *                 asked for (results do not depend on it)
  *   "order_edges" at graph creation: edges from which a build orders its
  *                 segments by the neighbours they cover and may list rows by
  *                 neighbour: 0 (default) 2^20, otherwise 1 to 2^31 - 2^16 - 1

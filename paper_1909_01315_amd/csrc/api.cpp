@@ -1691,7 +1691,7 @@ constexpr int WEIGHT8_MAX_OUTS = 1 << 24;
 constexpr int64_t NORM_BYTES = 20480;  // that a block moves, about
 constexpr int NORM_TILES = 512;        // tiles that fill the chip
 constexpr int ADD_NORM_ONCE = 4096;    // tiles that one launch adds up, and tiles that a workgroup of two
-constexpr int ADD_NORM_RUN = 512;      // launches does
+constexpr int ADD_NORM_RUN = 256;      // launches does
 
 int64_t cols_of(const gnnk_tensor* t) { return (int64_t)t->heads * t->feat; }
 

@@ -15,6 +15,19 @@
 // and the 16 lanes of a row write its 64 columns at once, whole lines of 128
 // bytes in bf16.  (With 64 bytes of a row a store, 16 rows at once, 262,144 rows
 // of 256 to 768 columns took 150 us, 127 of them for the stores alone.)
+//
+// Four kernels, for what bounds a product (choose() has the rule).  What they
+// measured, rows x columns to outputs, results in bf16:
+//   few     1 x 1,024 to 1,536 3.8 us, 37 x 2,048 to 2,048 6.6: a launch, one
+//           chain of loads and the join of its wavefronts
+//   stream  262,144 x 256 to 768 81 us (5.8 TB/s; a fill of the output alone 59),
+//           232,965 x 512 to 512 83 (4.3 TB/s, rows read once a panel), 20,011 x
+//           282 to 141 of fp32 8.4
+//   deep    16,384 x 4,096 to 4,096 208 us when the chip is cool (2.64 POP/s), 229
+//           without a pause (2.40; the vector and LDS work aside, the matrix
+//           instructions alone take 130 at the 4.2 POP/s that random bytes allow)
+//   tile    100,000 x 1,501 to 1,500 430 us (1.05 POP/s), at addresses that loads
+//           into LDS do not take
 #include "words.h"
 
 namespace gnnk {

