@@ -18,7 +18,7 @@
 //
 // Four kernels, for what bounds a product (choose() has the rule).  What they
 // measured, rows x columns to outputs, results in bf16:
-//   few     1 x 1,024 to 1,536 3.8 us, 37 x 2,048 to 2,048 6.6: a launch, one
+//   few     1 x 1,024 to 1,536 3.2 us, 37 x 2,048 to 2,048 6.4: a launch, one
 //           chain of loads and the join of its wavefronts
 //   stream  262,144 x 256 to 768 81 us (5.8 TB/s; a fill of the output alone 59),
 //           232,965 x 512 to 512 83 (4.3 TB/s, rows read once a panel), 20,011 x
@@ -214,8 +214,8 @@ __global__ __launch_bounds__(1024) void linear8_few_kernel(Linear8Args A, int wa
     extern __shared__ i32x4 sums[];
     const int wave = threadIdx.x >> 6, lane = threadIdx.x & 63;
     constexpr int PER = 4 / NJ;  // blocks that share 64 output columns, NJ fragments each
-    const unsigned nbs = (unsigned)((A.N + 63) / 64) * PER, b = blockIdx.x % nbs;
-    const int nb = b / PER, j0 = b % PER * NJ;
+    const unsigned nbs = (unsigned)((A.N + 63) / 64) * PER, at = blockIdx.x % nbs;
+    const int nb = at / PER, j0 = at % PER * NJ;
     const int64_t m0 = (int64_t)(blockIdx.x / nbs) * MI * 16;
     const int KS = (A.K + KB - 1) / KB, full = A.K / KB;
     const int8_t* const wp = A.w + (int64_t)nb * KS * WBLOCK + j0 * 1024 + lane * 16;
@@ -225,6 +225,18 @@ __global__ __launch_bounds__(1024) void linear8_few_kernel(Linear8Args A, int wa
     for (int i = 0; i < MI; ++i) {
         const int64_t m = m0 + i * 16 + (lane & 15);
         row[i] = A.x + (m < A.M ? m : A.M - 1) * A.x_stride;
+    }
+    // a wavefront that joins the sums of a fragment reads its scales first, while it
+    // waits for its rows (37 rows of 2,048 to 2,048 columns in a captured graph 5.7 ->
+    // 5.5 us, one of 4,096 to 4,096 4.1 -> 3.7)
+    const int f = wave, n = nb * 64 + (lane & 15) * 4 + j0 + f % NJ;
+    const int64_t m = m0 + f / NJ * 16 + (lane >> 4) * 4;
+    float xs[4], s = 0.0f, b = 0.0f;
+    if (f < MI * NJ) {
+        const int c = n < A.N ? n : A.N - 1;
+        load_scales(A, m, xs);
+        s = A.ws[c];
+        if (A.bias) b = IO<T, 1>::load1(reinterpret_cast<const T*>(A.bias) + c);
     }
     i32x4 acc[MI][NJ] = {};
     auto step = [&](int ks, auto tail) {
@@ -253,20 +265,22 @@ __global__ __launch_bounds__(1024) void linear8_few_kernel(Linear8Args A, int wa
 #pragma unroll
         for (int j = 0; j < NJ; ++j) sums[((wave * MI + i) * NJ + j) * 64 + lane] = acc[i][j];
     __syncthreads();
-    for (int f = wave; f < MI * NJ; f += waves) {
+    auto join = [&](int f, int64_t m, int n, const float* xs, float s, float b) {
         i32x4 t = sums[f * 64 + lane];
         for (int k = 1; k < waves; ++k) t += sums[(k * MI * NJ + f) * 64 + lane];
-        const int64_t m = m0 + f / NJ * 16 + (lane >> 4) * 4;
-        const int n = nb * 64 + (lane & 15) * 4 + j0 + f % NJ;
-        if (n >= A.N) continue;
-        const float s = A.ws[n], b = A.bias ? IO<T, 1>::load1(reinterpret_cast<const T*>(A.bias) + n) : 0.0f;
-        float xs[4];
-        load_scales(A, m, xs);
+        if (n >= A.N) return;
 #pragma unroll
         for (int r = 0; r < 4; ++r)
             if (m + r < A.M)
-                IO<T, 1>::store1(reinterpret_cast<T*>(A.out) + (m + r) * A.out_stride + n,
-                                 fmaf((float)t[r] * xs[r], s, b));
+                IO<T, 1>::store1(reinterpret_cast<T*>(A.out) + (m + r) * A.out_stride + n, fmaf((float)t[r] * xs[r], s, b));
+    };
+    if (f < MI * NJ) join(f, m, n, xs, s, b);
+    // (fewer wavefronts than fragments: short rows)
+    for (int g = f + waves; g < MI * NJ; g += waves) {
+        const int n = nb * 64 + (lane & 15) * 4 + j0 + g % NJ, c = n < A.N ? n : A.N - 1;
+        const int64_t m = m0 + g / NJ * 16 + (lane >> 4) * 4;
+        load_scales(A, m, xs);
+        join(g, m, n, xs, A.ws[c], A.bias ? IO<T, 1>::load1(reinterpret_cast<const T*>(A.bias) + c) : 0.0f);
     }
 }
 

@@ -16,7 +16,7 @@
 // and normed in 178 us (6.0 TB/s read and written), 65,536 of 4,096 bf16 in 368
 // (5.8), 232,965 of 512 bf16 with the norm in 8 bits in 139 (6.0), 100,000 of 376
 // fp32 to 8 bits in 34 (5.6).  The backward reads three rows for one that it
-// writes: 210 us and 12 for the weight's gradient on the first (5.1).  Rows of
+// writes: 210 us and 11 for the weight's gradient on the first (5.1).  Rows of
 // 282 bf16, which start on no vector, are bound by instructions and by the short
 // grid: 20,011 of them 13 us, backward 17 and 5.  One row: 2.4 us.
 //
