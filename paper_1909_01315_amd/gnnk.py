@@ -868,7 +868,7 @@ def node_add_norm_backward(h, weight, grad_y, grad_sum=None, eps: float = 1e-6, 
 
 class Weight8:
     """A linear layer's weight in 8 bits, laid out for node_linear_i8: values int8 (outs, columns), scale float32
-    (outs,), scale[o] * values[o] being row o.  Both may be changed or dropped afterwards."""
+    (outs,), scale[o] * values[o] being row o.  Both may be changed or dropped afterwards; it may be copied and pickled."""
 
     def __init__(self, values: torch.Tensor, scale: torch.Tensor, stream=None):
         _here(values, scale)
@@ -877,10 +877,24 @@ class Weight8:
         need = ctypes.c_size_t(0)
         _check(load().weight8_bytes(self.outs, self.cols, ctypes.byref(need)))
         with torch.cuda.stream(stream) if stream is not None else contextlib.nullcontext():
-            self.packed = torch.empty(need.value, dtype=torch.uint8, device=values.device)
-            self.scale = scale.reshape(-1).clone()
-        _check(load().weight8_pack(rows, self.packed.data_ptr(), need.value, _stream(stream)))
-        self._bytes = _WEIGHT8.pack(self.packed.data_ptr(), self.scale.data_ptr(), self.outs, self.cols)
+            self._packed = torch.empty(need.value, dtype=torch.uint8, device=values.device)
+            self._scale = scale.reshape(-1).clone()
+        _check(load().weight8_pack(rows, self._packed.data_ptr(), need.value, _stream(stream)))
+        self._bind()
+
+    # its tensors stay: the descriptor holds their addresses, and a copy has its own
+    packed = property(lambda self: self._packed)
+    scale = property(lambda self: self._scale)
+
+    def _bind(self):
+        self._bytes = _WEIGHT8.pack(self._packed.data_ptr(), self._scale.data_ptr(), self.outs, self.cols)
+
+    def __getstate__(self):
+        return {k: v for k, v in self.__dict__.items() if k != "_bytes"}
+
+    def __setstate__(self, state):
+        self.__dict__.update(state)
+        self._bind()
 
     @classmethod
     def quantize(cls, weight: torch.Tensor, stream=None) -> "Weight8":
@@ -893,7 +907,7 @@ def node_linear_i8(weight: Weight8, q, scale, bias=None, dtype=torch.bfloat16, o
     """Rows in 8 bits times a weight in 8 bits: out[n, o] = scale[n] * weight.scale[o] * (q[n] . values[o]) + bias[o],
     float32 or bfloat16 (dtype, or out's).  The products' sums are exact.  bias: outs values of out's dtype.  No
     gradient is formed."""
-    _here(weight.packed, q, scale, bias, out)
+    _here(weight._packed, q, scale, bias, out)
     xd = _rows8(q, scale)
     if out is None:
         out = q.new_empty((q.shape[0], weight.outs), dtype=dtype)

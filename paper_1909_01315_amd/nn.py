@@ -470,6 +470,7 @@ def _no_gradient(*tensors):
 def _rows8(x):
     """(q, scale) of rows in 8 bits, or of a tensor whose rows are rounded to them here"""
     if isinstance(x, tuple):
+        _no_gradient(x[1])
         return x[:2]
     _no_gradient(x)
     return gnnk.node_quantize(x)
@@ -479,7 +480,8 @@ class Linear8(torch.nn.Module):
     """A linear layer for inference with its weight in 8 bits, a scale for each
     output: of a tensor, whose rows are rounded to 8 bits with a scale each, or
     of rows that are (q, scale) already.  The result is of the type of the
-    weight that it was made from, or `dtype`."""
+    weight that it was made from, or `dtype`.  It has no parameters: it is made
+    anew from a weight that changes, and copied and pickled whole."""
 
     def __init__(self, weight: torch.Tensor, bias: torch.Tensor = None, dtype=None):
         super().__init__()
@@ -514,6 +516,7 @@ class DotAttentionConv8(torch.nn.Module):
 
     def forward(self, g, x, pos=None, bias=None):
         x8, scale = _rows8(x)
+        _no_gradient(bias)
         if g.num_dst == x8.shape[0]:
             q, k, v = self.fc((x8, scale)).split([self.H * self.F, self.K * self.F, self.K * self.F], 1)
         else:

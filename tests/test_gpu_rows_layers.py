@@ -1,6 +1,9 @@
 """The residual stream and products in 8 bits as a program runs them: the
 autograd form against differences and its operators, the layers as exactly the
 chains of their operators, replays, streams and long strides."""
+import copy
+import io
+
 import pytest
 import torch
 
@@ -260,3 +263,46 @@ def test_norms_past_32_bits(dtype):
     q, s = gnnk.node_quantize(x)
     qf, sf = gnnk.node_quantize(far[0], out=big.view(torch.int8)[:, 8000:8000 + c], scale=torch.empty_like(s))
     assert torch.equal(qf, q) and torch.equal(sf, s)
+
+
+def test_a_copied_layer_keeps_its_weight():
+    g = gen(41)
+    w, x = normal(g, 70, 130).cuda(), normal(g, 9, 130).cuda()
+    layer = nn.Linear8(w, torch.ones(70, device="cuda"))
+    want = layer(x)
+    buf = io.BytesIO()
+    torch.save(layer, buf)
+    buf.seek(0)
+    copies = [copy.copy(layer.weight), copy.deepcopy(layer).weight, torch.load(buf, weights_only=False).weight]
+    layer.weight.packed.zero_()
+    for k, c in enumerate(copies):
+        t = gnnk.node_linear_i8(c, *gnnk.node_quantize(x), bias=layer.bias, dtype=F32)
+        assert torch.equal(t, want if k else torch.ones_like(want))  # (a shallow copy shares it)
+    with pytest.raises(AttributeError):
+        layer.weight.scale = layer.weight.scale * 2
+    layer.weight.scale.mul_(2)
+
+
+def test_gradients_of_a_bias_are_not_dropped():
+    conv = nn.DotAttentionConv8(nn.DotAttentionConv(32, 8, 2).cuda())
+    gr, _ = graph(40, 40, 300, 5)
+    x = normal(gen(42), 40, 32).cuda()
+    bias = torch.zeros(gr.num_edges, 2, 1, device="cuda", requires_grad=True)
+    with pytest.raises(ValueError, match="gradient"):
+        conv(gr, x, bias=bias)
+    q, s = gnnk.node_quantize(x)
+    with pytest.raises(ValueError, match="gradient"):
+        conv(gr, (q, s.requires_grad_(True)))
+    with torch.no_grad():
+        assert conv(gr, (q, s), bias=bias).shape == (40, 2, 8)
+
+
+def test_the_two_gradients_are_tensors_of_their_own():
+    g = gen(43)
+    for use in range(3):
+        a, b = (normal(g, 6, 32).cuda().requires_grad_(True) for _ in range(2))
+        y, h = nn.add_norm(a, b, torch.ones(32, device="cuda"))
+        (y.sum() if use == 0 else h.sum() if use == 1 else (y * h).sum()).backward()
+        want = b.grad.clone()
+        a.grad.add_(1)
+        assert torch.equal(b.grad, want)
