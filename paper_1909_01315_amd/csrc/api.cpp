@@ -1713,9 +1713,16 @@ Span flat(const void* p, int64_t bytes) { return Span{(uintptr_t)p, bytes > 0 ? 
 // wider ones take several, up to eight.  The backward has two or three rows in
 // registers and sums besides: half as many vectors a lane where eight
 // wavefronts hold the row all the same (65,536 rows of 4,096 bf16 606 -> 451 us).
-// Rows in 8 bits without a norm, of which a lane has little to load, lie in 16 or
-// 32 lanes where there are rows enough (262,144 of 256 fp32 71 -> 59 us, 232,965
-// of 512 bf16 76 -> 64).
+// Three vectors a lane where four would leave a quarter of them idle (100,000 of
+// 1,500 bf16 to 8 bits 107 -> 92 us, with the norm 289 -> 236).  Where there are
+// rows enough, rows lie in fewer lanes if
+//  - they are rounded to 8 bits without a norm, of which a lane has little to load:
+//    16 or 32 lanes of up to four vectors (262,144 of 256 fp32 71 -> 59 us, 232,965
+//    of 512 bf16 76 -> 64);
+//  - a wavefront's lanes would idle: 16 or 32 lanes of three vectors, in 8 bits
+//    (200,000 of 320 bf16 with the norm 100 -> 81 us; of 512, 64 vectors, 145 in 64
+//    lanes and 148 in 16), and at any address (300,000 of 282 bf16 157 -> 140;
+//    200,000 of 640, whose rows are whole vectors, 177 -> 183: those stay).
 int add_norm_geo(AddNormArgs& A, const gnnk_tensor* x, AddNormMode mode) {
     A.C = (int32_t)cols_of(x);
     A.inv_C = 1.0f / (float)A.C;
@@ -1723,12 +1730,19 @@ int add_norm_geo(AddNormArgs& A, const gnnk_tensor* x, AddNormMode mode) {
     const int V = x->dtype == GNNK_BF16 ? 8 : 4, NV = (A.C + V - 1) / V;
     int most = x->dtype == GNNK_BF16 ? 4 : 8;
     if (mode == ADD_NORM_BWD && NV <= 64 * 8 * most / 2) most /= 2;
-    const bool narrow = mode == QUANT8 && A.n >= 4096;
-    A.L = std::min(narrow && NV <= 16 * most ? 16 : narrow && NV <= 32 * most ? 32 : 64, pow2ceil(NV));
+    A.L = std::min(64, pow2ceil(NV));
+    if (A.n >= 4096 && mode != ADD_NORM_BWD) {
+        if ((NV > 32 && NV <= 48) || (NV > 64 && NV <= 96)) {
+            if (mode != ADD_NORM || A.C % V) A.L = NV <= 48 ? 16 : 32;
+        } else if (mode == QUANT8) {
+            A.L = std::min(NV <= 64 ? 16 : NV <= 128 ? 32 : 64, A.L);
+        }
+    }
     A.waves = pow2ceil((NV + 64 * most - 1) / (64 * most));
     A.threads = std::max(256, A.waves * 64);
     const int lanes = A.waves > 1 ? A.waves * 64 : A.L;
-    return pow2ceil((NV + lanes - 1) / lanes);
+    const int npt = (NV + lanes - 1) / lanes;
+    return npt == 3 ? 3 : pow2ceil(npt);
 }
 int rows_of_block(const AddNormArgs& A) { return A.threads / (A.waves > 1 ? A.waves * 64 : A.L); }
 

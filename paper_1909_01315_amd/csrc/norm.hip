@@ -390,18 +390,25 @@ __global__ __launch_bounds__(1024) void node_add_norm_dw_kernel(const P* part, i
 template <typename T, int NPT, bool PART, bool WIDE>
 void launch_n(const AddNormArgs& a, int mode, hipStream_t s) {
     const dim3 grid((unsigned)a.blocks), block((unsigned)a.threads);
-    if (mode == ADD_NORM)
-        hipLaunchKernelGGL((node_add_norm_kernel<T, NPT, PART, WIDE, ADD_NORM>), grid, block, 0, s, a);
-    else if (mode == ADD_NORM8)
-        hipLaunchKernelGGL((node_add_norm_kernel<T, NPT, PART, WIDE, ADD_NORM8>), grid, block, 0, s, a);
-    else if (mode == QUANT8)
-        hipLaunchKernelGGL((node_add_norm_kernel<T, NPT, PART, WIDE, QUANT8>), grid, block, 0, s, a);
-    else if (!PART && a.out && a.C == (WIDE ? a.waves * 64 : a.L) * NPT * 16 / (int)sizeof(T))
-        hipLaunchKernelGGL((node_add_norm_backward_kernel<T, NPT, false, WIDE, true>), grid, block,
-                           a.part ? a.threads * 64 / sizeof(T) : 0, s, a);
-    else
-        hipLaunchKernelGGL((node_add_norm_backward_kernel<T, NPT, PART, WIDE, false>), grid, block,
-                           a.part ? a.threads * 64 / sizeof(T) : 0, s, a);
+    // a lane holds up to 2 MOST vectors, in the backward MOST; of several
+    // wavefronts more than half of that, but for the widest rows of a backward
+    constexpr int MOST = (int)sizeof(T);
+    if constexpr (!WIDE || NPT > MOST) {
+        if (mode == ADD_NORM)
+            hipLaunchKernelGGL((node_add_norm_kernel<T, NPT, PART, WIDE, ADD_NORM>), grid, block, 0, s, a);
+        else if (mode == ADD_NORM8)
+            hipLaunchKernelGGL((node_add_norm_kernel<T, NPT, PART, WIDE, ADD_NORM8>), grid, block, 0, s, a);
+        else if (mode == QUANT8)
+            hipLaunchKernelGGL((node_add_norm_kernel<T, NPT, PART, WIDE, QUANT8>), grid, block, 0, s, a);
+    }
+    if constexpr (WIDE ? NPT > MOST / 2 : NPT <= MOST) {
+        if (mode != ADD_NORM_BWD) return;
+        const size_t lds = a.part ? a.threads * 64 / sizeof(T) : 0;
+        if (!PART && a.out && a.C == (WIDE ? a.waves * 64 : a.L) * NPT * 16 / (int)sizeof(T))
+            hipLaunchKernelGGL((node_add_norm_backward_kernel<T, NPT, false, WIDE, true>), grid, block, lds, s, a);
+        else
+            hipLaunchKernelGGL((node_add_norm_backward_kernel<T, NPT, PART, WIDE, false>), grid, block, lds, s, a);
+    }
 }
 
 template <typename T, int NPT>
@@ -421,6 +428,7 @@ void launch_t(const AddNormArgs& a, int npt, int mode, hipStream_t s) {
     if (a.blocks > 0) {
         if (npt == 1) launch_p<T, 1>(a, mode, s);
         else if (npt == 2) launch_p<T, 2>(a, mode, s);
+        else if (npt == 3) launch_p<T, 3>(a, mode, s);
         else if (npt == 4) launch_p<T, 4>(a, mode, s);
         else if constexpr (sizeof(T) == 4) launch_p<T, 8>(a, mode, s);
     }

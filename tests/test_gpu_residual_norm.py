@@ -208,3 +208,17 @@ def test_the_sum_may_be_left_out():
     assert lib.node_add_norm(d(xd), d(rd), d(wd.view(1, 1, -1)), 1e-6, None, d(y1), stream) == gnnk.OK
     assert lib.node_add_norm_i8(d(xd), d(rd), d(wd.view(1, 1, -1)), 1e-6, None, gnnk._rows8(q1, s1), stream) == gnnk.OK
     assert torch.equal(y1, y) and torch.equal(q1, q) and torch.equal(s1, s)
+
+
+# rows enough to lie in fewer lanes, of three vectors each
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("n,c", [(4096, 141), (4100, 160), (4097, 282), (5000, 380), (4099, 640), (4096, 768), (4110, 769)])
+def test_many_rows_in_few_lanes(n, c, dtype):
+    test_norm(n, c, dtype)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("n,c", [(50, 600), (40, 1200), (31, 1501), (12, 2500), (7, 5001), (3, 12000)])
+def test_three_vectors_a_lane(n, c, dtype):
+    test_norm(n, c, dtype)
+    test_gradients(n, c, dtype)
