@@ -83,16 +83,18 @@ __device__ __forceinline__ uint32_t row_most(uint32_t x, const AddNormArgs& A, u
 // whatever t is
 template <int V, bool PART>
 __device__ __forceinline__ void put8(int8_t* p, const float* t, float inv, int n) {
-    uint32_t w[(V + 3) / 4] = {};
+    // beside 1.5 * 2^23 a float's last bit is 1: the sum is rounded to a whole number,
+    // ties to even, whose lowest byte is its lowest byte (no magnitude passes 127
+    // steps by more than the roundings of s and inv, 2^-23 of it)
+    uint32_t b[V], w[V / 4];
 #pragma unroll
-    for (int i = 0; i < V; ++i) {
-        // (a magnitude that rounds past 127 steps is one of them)
-        const int q = (int)fminf(fmaxf(rintf(t[i] * inv), -127.0f), 127.0f);
-        w[i / 4] |= (uint32_t)(q & 255) << (i % 4 * 8);
+    for (int i = 0; i < V; ++i) b[i] = __float_as_uint(fmaf(t[i], inv, 12582912.0f));
+#pragma unroll
+    for (int i = 0; i < V / 4; ++i) {
+        const uint32_t lo = __builtin_amdgcn_perm(b[i * 4 + 1], b[i * 4], 0x0C0C0400u);
+        const uint32_t hi = __builtin_amdgcn_perm(b[i * 4 + 3], b[i * 4 + 2], 0x04000C0Cu);
+        w[i] = inv == 0.0f ? 0u : lo | hi;
     }
-    if (inv == 0.0f)
-#pragma unroll
-        for (int i = 0; i < (V + 3) / 4; ++i) w[i] = 0;
     if (!PART || n == V) {
         if constexpr (V == 8) *reinterpret_cast<u2_b*>(p) = u2_b{w[0], w[1]};
         else *reinterpret_cast<u1_b*>(p) = w[0];
