@@ -106,7 +106,11 @@ __device__ __forceinline__ void put8(int8_t* p, const float* t, float inv, int n
 }
 
 // NPT vectors of V values a lane, vector p of it being number p * lanes + lane
-// of the row; PART: the last vector of a row holds fewer values than V
+// of the row; PART: the last vector of a row holds fewer values than V.  The
+// first `full_of` vectors of each lane are whole ones of the row (there are as
+// many vectors a lane as it takes, but for eight, which stand for five to eight).
+constexpr int full_of(int npt) { return npt <= 4 ? npt - 1 : 0; }
+
 template <typename T, int NPT, bool PART, bool WIDE, int MODE>
 __global__ __launch_bounds__(WIDE ? 512 : 256) void node_add_norm_kernel(AddNormArgs A) {
     constexpr int V = 16 / sizeof(T);
@@ -117,6 +121,7 @@ __global__ __launch_bounds__(WIDE ? 512 : 256) void node_add_norm_kernel(AddNorm
     const int C = A.C;
 
     auto count = [&](int p) {  // columns of the lane's vector p
+        if (p < full_of(NPT)) return V;
         const int left = C - (p * TPR + lig) * V;
         return left < 0 ? 0 : (left < V ? left : V);
     };
@@ -126,7 +131,9 @@ __global__ __launch_bounds__(WIDE ? 512 : 256) void node_add_norm_kernel(AddNorm
         const int m = count(p), c = (p * TPR + lig) * V;
         if (ok && m > 0) {
             const int64_t at = n * stride + c;
-            fetch<T, V, PART>(reinterpret_cast<const T*>(base) + at, m, (A.n - 1) * stride + C - at, raw);
+            const T* const from = reinterpret_cast<const T*>(base) + at;
+            if (p < full_of(NPT)) fetch<T, V, false>(from, V, 0, raw);
+            else fetch<T, V, PART>(from, m, (A.n - 1) * stride + C - at, raw);
         }
     };
     float w[NPT][N];
@@ -238,7 +245,7 @@ __global__ __launch_bounds__(WIDE ? 512 : 256) void node_add_norm_backward_kerne
     const int C = A.C;
 
     auto count = [&](int p) {
-        if (DENSE) return V;
+        if (DENSE || p < full_of(NPT)) return V;
         const int left = C - (p * TPR + lig) * V;
         return left < 0 ? 0 : (left < V ? left : V);
     };
@@ -264,7 +271,9 @@ __global__ __launch_bounds__(WIDE ? 512 : 256) void node_add_norm_backward_kerne
             if (DENSE || m > 0) {
                 auto get = [&](const void* base, int64_t stride, float* raw) {
                     const int64_t at = n * stride + c;
-                    fetch<T, V, PART>(reinterpret_cast<const T*>(base) + at, m, (A.n - 1) * stride + C - at, raw);
+                    const T* const from = reinterpret_cast<const T*>(base) + at;
+                    if (p < full_of(NPT)) fetch<T, V, false>(from, V, 0, raw);
+                    else fetch<T, V, PART>(from, m, (A.n - 1) * stride + C - at, raw);
                 };
                 get(A.x, A.x_stride, hr[p]);
                 get(A.r, A.r_stride, gr[p]);
