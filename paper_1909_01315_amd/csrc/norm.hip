@@ -34,6 +34,7 @@ namespace {
 // 8-bit values are stored at any address
 typedef unsigned u2_b __attribute__((ext_vector_type(2), aligned(1)));
 typedef unsigned u1_b __attribute__((aligned(1)));
+typedef unsigned short u1s_b __attribute__((aligned(1)));
 
 // the largest of x over the aligned run of `red` lanes; every lane gets it
 __device__ __forceinline__ uint32_t run_most(uint32_t x, int red) {
@@ -82,7 +83,7 @@ __device__ __forceinline__ uint32_t row_most(uint32_t x, const AddNormArgs& A, u
 // V values as 8-bit numbers, each the nearest to t * inv; inv 0: zeros,
 // whatever t is
 template <int V, bool PART>
-__device__ __forceinline__ void put8(int8_t* p, const float* t, float inv, int n) {
+__device__ __forceinline__ void put8(int8_t* p, const float* t, float inv, int n, int tail) {
     // beside 1.5 * 2^23 a float's last bit is 1: the sum is rounded to a whole number,
     // ties to even, whose lowest byte is its lowest byte (no magnitude passes 127
     // steps by more than the roundings of s and inv, 2^-23 of it)
@@ -99,10 +100,26 @@ __device__ __forceinline__ void put8(int8_t* p, const float* t, float inv, int n
         if constexpr (V == 8) *reinterpret_cast<u2_b*>(p) = u2_b{w[0], w[1]};
         else *reinterpret_cast<u1_b*>(p) = w[0];
     } else {
-#pragma unroll
-        for (int i = 0; i < V; ++i)
-            if (i < n) p[i] = (int8_t)(w[i / 4] >> (i % 4 * 8));
+        uint32_t x = w[0];
+        if (V == 8 && (tail & 4)) {
+            *reinterpret_cast<u1_b*>(p) = x;
+            p += 4;
+            x = w[V / 4 - 1];
+        }
+        if (tail & 2) {
+            *reinterpret_cast<u1s_b*>(p) = (uint16_t)x;
+            p += 2;
+            x >>= 16;
+        }
+        if (tail & 1) *p = (int8_t)x;
     }
+}
+// a lane's vector of a row: its `n` columns, V or the last vector's, `tail`,
+// the same in all lanes
+template <typename T, int V, bool PART>
+__device__ __forceinline__ void store_row(T* p, const float* t, int n, int tail) {
+    if (!PART || n == V) put<T, V>(p, t);
+    else if constexpr (PART) store_few<T, V / 2>(p, t, tail);
 }
 
 // NPT vectors of V values a lane, vector p of it being number p * lanes + lane
@@ -118,7 +135,7 @@ __global__ __launch_bounds__(WIDE ? 512 : 256) void node_add_norm_kernel(AddNorm
     __shared__ float red[32];
     const int tid = threadIdx.x, TPR = WIDE ? A.waves * 64 : A.L;
     const int lig = tid & (TPR - 1), gid = tid / TPR, per = blockDim.x / TPR;
-    const int C = A.C;
+    const int C = A.C, tail = C & (V - 1);
 
     auto count = [&](int p) {  // columns of the lane's vector p
         if (p < full_of(NPT)) return V;
@@ -175,8 +192,8 @@ __global__ __launch_bounds__(WIDE ? 512 : 256) void node_add_norm_kernel(AddNorm
 #pragma unroll
                     for (int i = 0; i < V; ++i) h[p][i] += t[i];
                     if (ok && m > 0 && A.sum)
-                        store_part<T, V, PART>(reinterpret_cast<T*>(A.sum) + n * A.sum_stride + (p * TPR + lig) * V,
-                                               h[p], m);
+                        store_row<T, V, PART>(reinterpret_cast<T*>(A.sum) + n * A.sum_stride + (p * TPR + lig) * V,
+                                              h[p], m, tail);
                 }
 #pragma unroll
                 for (int i = 0; i < V; ++i) ss = fmaf(h[p][i], h[p][i], ss);
@@ -196,7 +213,8 @@ __global__ __launch_bounds__(WIDE ? 512 : 256) void node_add_norm_kernel(AddNorm
             for (int p = 0; p < NPT; ++p) {
                 const int m = count(p);
                 if (ok && m > 0)
-                    store_part<T, V, PART>(reinterpret_cast<T*>(A.out) + n * A.out_stride + (p * TPR + lig) * V, h[p], m);
+                    store_row<T, V, PART>(reinterpret_cast<T*>(A.out) + n * A.out_stride + (p * TPR + lig) * V, h[p], m,
+                                          tail);
             }
         } else {
             // the largest magnitude by its bits, where a NaN is the largest
@@ -221,7 +239,7 @@ __global__ __launch_bounds__(WIDE ? 512 : 256) void node_add_norm_kernel(AddNorm
 #pragma unroll
             for (int p = 0; p < NPT; ++p) {
                 const int m = count(p);
-                if (ok && m > 0) put8<V, PART>(A.q + n * A.q_stride + (p * TPR + lig) * V, h[p], inv, m);
+                if (ok && m > 0) put8<V, PART>(A.q + n * A.q_stride + (p * TPR + lig) * V, h[p], inv, m, tail);
             }
             if (ok && lig == 0) A.scale[n] = s;
         }
@@ -242,7 +260,7 @@ __global__ __launch_bounds__(WIDE ? 512 : 256) void node_add_norm_backward_kerne
     __shared__ float red[32];
     const int tid = threadIdx.x, TPR = WIDE ? A.waves * 64 : A.L;
     const int lig = tid & (TPR - 1), gid = tid / TPR, per = blockDim.x / TPR;
-    const int C = A.C;
+    const int C = A.C, tail = C & (V - 1);
 
     auto count = [&](int p) {
         if (DENSE || p < full_of(NPT)) return V;
@@ -332,7 +350,7 @@ __global__ __launch_bounds__(WIDE ? 512 : 256) void node_add_norm_backward_kerne
 #pragma unroll
                 for (int p = 0; p < NPT; ++p) {
                     const int m = count(p);
-                    if (ok && m > 0) store_part<T, V, PART>(out + p * TPR * V, h[p], m);
+                    if (ok && m > 0) store_row<T, V, PART>(out + p * TPR * V, h[p], m, tail);
                 }
                 if (DENSE) break;  // (they were the last rows)
             }
