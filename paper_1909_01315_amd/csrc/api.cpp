@@ -1719,10 +1719,13 @@ Span flat(const void* p, int64_t bytes) { return Span{(uintptr_t)p, bytes > 0 ? 
 //  - they are rounded to 8 bits without a norm, of which a lane has little to load:
 //    16 or 32 lanes of up to four vectors (262,144 of 256 fp32 71 -> 59 us, 232,965
 //    of 512 bf16 76 -> 64);
-//  - a wavefront's lanes would idle: 16 or 32 lanes of three vectors, in 8 bits
-//    (200,000 of 320 bf16 with the norm 100 -> 81 us; of 512, 64 vectors, 145 in 64
-//    lanes and 148 in 16), and at any address (300,000 of 282 bf16 157 -> 140;
-//    200,000 of 640, whose rows are whole vectors, 177 -> 183: those stay).
+//  - lanes would idle: 8, 16 or 32 of three vectors, in 8 bits (200,000 of 320 bf16
+//    with the norm 100 -> 81 us; of 512, 64 vectors, 145 in 64 lanes and 148 in 16)
+//    and at any address (300,000 of 150 bf16 86 -> 77; 200,000 of 640, whose rows are
+//    whole vectors, 177 -> 183: those stay);
+//  - most lanes would hold a row's last vector, whose columns are checked, and no
+//    other: 32 of two vectors (200,000 of 501 bf16 163 -> 146, with the norm in 8
+//    bits 172 -> 144, backward 175 -> 171).
 int add_norm_geo(AddNormArgs& A, const gnnk_tensor* x, AddNormMode mode) {
     A.C = (int32_t)cols_of(x);
     A.inv_C = 1.0f / (float)A.C;
@@ -1731,12 +1734,13 @@ int add_norm_geo(AddNormArgs& A, const gnnk_tensor* x, AddNormMode mode) {
     int most = x->dtype == GNNK_BF16 ? 4 : 8;
     if (mode == ADD_NORM_BWD && NV <= 64 * 8 * most / 2) most /= 2;
     A.L = std::min(64, pow2ceil(NV));
-    if (A.n >= 4096 && mode != ADD_NORM_BWD) {
-        if ((NV > 32 && NV <= 48) || (NV > 64 && NV <= 96)) {
-            if (mode != ADD_NORM || A.C % V) A.L = NV <= 48 ? 16 : 32;
-        } else if (mode == QUANT8) {
-            A.L = std::min(NV <= 64 ? 16 : NV <= 128 ? 32 : 64, A.L);
-        }
+    if (A.n >= 4096) {
+        const bool any = A.C % V != 0;
+        const int three = NV > 16 && NV <= 24 ? 8 : NV > 32 && NV <= 48 ? 16 : NV > 64 && NV <= 96 ? 32 : 0;
+        if (mode == ADD_NORM_BWD) A.L = any && NV > 32 && NV <= 64 ? 32 : A.L;
+        else if (three && (mode != ADD_NORM || any)) A.L = three;
+        else if (mode == QUANT8) A.L = std::min(NV <= 64 ? 16 : NV <= 128 ? 32 : 64, A.L);
+        else if (any && NV > 48 && NV <= 64) A.L = 32;
     }
     A.waves = pow2ceil((NV + 64 * most - 1) / (64 * most));
     A.threads = std::max(256, A.waves * 64);

@@ -222,3 +222,10 @@ def test_many_rows_in_few_lanes(n, c, dtype):
 def test_three_vectors_a_lane(n, c, dtype):
     test_norm(n, c, dtype)
     test_gradients(n, c, dtype)
+
+
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("n,c", [(4101, 80), (4096, 95), (4100, 191), (4097, 225), (4099, 129), (4105, 401), (4096, 511)])
+def test_many_rows_of_any_address(n, c, dtype):
+    test_norm(n, c, dtype)
+    test_gradients(n, c, dtype)
