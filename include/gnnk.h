@@ -579,10 +579,12 @@ gnnk_status node_add_norm(const gnnk_tensor* x, const gnnk_tensor* residual, con
 
 /* The same with the norm in 8 bits: with y = w * sum / sqrt(mean(sum^2) + eps),
  * in fp32, row by row
- *   scale = max |y| / 127,  q = y / scale rounded to the nearest (ties to even)
- * A row of zeros has scale 0, no other one a scale below 2^-126; a row with a
- * NaN or an infinity has scale NaN and values 0, so that products with it are
- * NaN.  out->data past its columns is left as it was. */
+ *   scale = max |y| / 127,  q = 127 y / max |y| rounded to the nearest (ties to even)
+ * Of bf16 values that is exact; an fp32 quotient up to 2^-23 of itself below or
+ * at halfway between two numbers may go to the larger one.  A row of zeros has
+ * scale 0, no other one a scale below 2^-126 (q = y / scale, where it would be);
+ * a row with a NaN or an infinity has scale NaN and values 0, so that products
+ * with it are NaN.  out->data past its columns is left as it was. */
 gnnk_status node_add_norm_i8(const gnnk_tensor* x, const gnnk_tensor* residual, const gnnk_tensor* w, float eps,
                              gnnk_tensor* sum, gnnk_rows8* out, hipStream_t stream);
 

@@ -3,7 +3,7 @@
 // backward, and rows in 8 bits (after the norm, or as they are).
 //
 //   h = x + r,  rn = 1 / sqrt(mean(h^2) + eps),  y = h rn w
-//   s = max |y| / 127,  q = round(y / s)
+//   s = max |y| / 127,  q = round(127 y / max |y|)
 //   dx = gh + rn (gy w - h rn^2 mean(gy w h)),  dw = sum over rows of gy h rn
 //
 // A pure stream: every row is read once and written once.  A row lies in the
@@ -87,7 +87,7 @@ template <int V, bool PART>
 __device__ __forceinline__ void put8(int8_t* p, const float* t, float inv, int n, int tail) {
     // beside 1.5 * 2^23 a float's last bit is 1: the sum is rounded to a whole number,
     // ties to even, whose lowest byte is its lowest byte (no magnitude passes 127
-    // steps by more than the roundings of s and inv, 2^-23 of it)
+    // steps by more than what inv is off by, 2^-23 of it)
     uint32_t b[V], w[V / 4];
 #pragma unroll
     for (int i = 0; i < V; ++i) b[i] = __float_as_uint(fmaf(t[i], inv, 12582912.0f));
@@ -234,8 +234,16 @@ __global__ __launch_bounds__(WIDE ? 512 : 256) void node_add_norm_kernel(AddNorm
             // inverse may be infinite; a row with a NaN or an infinity has
             // scale NaN and values 0, so that what is made of it is NaN
             const bool finite = most < 0x7F800000u;
-            float s = fmaxf(__uint_as_float(most) / 127.0f, 1.17549435e-38f);
-            const float inv = finite ? 1.0f / s : 0.0f;
+            const float top = __uint_as_float(most);
+            float s = fmaxf(top / 127.0f, 0x1p-126f);
+            // values are rounded in one step from their product with the inverse, 127 / top.
+            // It is off by at most 2^-23 of itself and never too small: half the largest
+            // value, common in bf16, is a tie of 63.5 steps and goes to 64, the even one.
+            // (1 / s, off either way, sent half of these to 63.)  Other ties among bf16
+            // values are only where top is 127 times a power of two, whose inverse is exact
+            float inv = 127.0f / top;
+            if (fmaf(inv, top, -127.0f) < 0.0f) inv = __uint_as_float(__float_as_uint(inv) + 1);
+            inv = finite ? fminf(inv, 0x1p126f) : 0.0f;
             s = !finite ? __uint_as_float(0x7FC00000u) : (most ? s : 0.0f);
 #pragma unroll
             for (int p = 0; p < NPT; ++p) {

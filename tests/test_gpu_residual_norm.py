@@ -171,6 +171,35 @@ def test_ties_go_to_the_even_number():
     assert q[0].tolist() == [127, 0, 2, 2, 0, -2, -2, 126]
 
 
+@pytest.mark.parametrize("n,c", [(700, 33), (5000, 376), (200, 2048), (6, 5001)])
+def test_halves_of_the_largest_magnitude_go_to_the_even_number(n, c):
+    """127 x / max |x| rounded to the nearest, ties to even.  Of values of 8 significant bits it is either a tie or 2^-16 of
+    itself away from one, more than the 2^-23 by which the inverse of the step may be off: the numbers are those of the exact
+    quotient, which 64 bits round to no tie that it is not.  (Half the largest magnitude is 63.5 steps.)"""
+    g = gen(n)
+    x = normal(g, n, c, dtype=BF16)
+    x[:, 1], x[:, 3] = 0.0, 0.0
+    half = x.abs().amax(1) / 2
+    x[:, 1], x[n // 2:, 3] = half, -half[n // 2:]
+    v = x.double()
+    want = torch.round(127.0 * v / v.abs().amax(1, keepdim=True))
+    assert bool((want[:, 1] == 64).all()) and bool((want[n // 2:, 3] == -64).all())
+    for dtype in (BF16, F32):
+        assert torch.equal(gnnk.node_quantize(x.to(dtype).cuda())[0].cpu().double(), want), dtype
+
+
+@pytest.mark.parametrize("n,c", [(700, 33), (5000, 376), (200, 2048)])
+def test_numbers_of_fp32_rows(n, c):
+    """The nearest to 127 x / max |x|, but for quotients up to 2^-23 of themselves below halfway, which may go up."""
+    x = normal(gen(n + 1), n, c)
+    v = x.double()
+    v = 127.0 * v / v.abs().amax(1, keepdim=True)
+    q = gnnk.node_quantize(x.cuda())[0].cpu().double()
+    # (64 bits: the quotient, and what it is compared with, are off by 2^-52 of themselves)
+    up = torch.round(v * (1 + 2.0 ** -23 + 2.0 ** -50))
+    assert bool(((q == torch.round(v)) | (q == up)).all())
+
+
 def test_no_rows():
     for dtype in (F32, BF16):
         x, w = torch.empty((0, 40), dtype=dtype, device="cuda"), torch.ones(40, dtype=dtype, device="cuda")
