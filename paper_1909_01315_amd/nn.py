@@ -516,7 +516,7 @@ class DotAttentionConv8(torch.nn.Module):
 
     def forward(self, g, x, pos=None, bias=None):
         x8, scale = _rows8(x)
-        _no_gradient(bias)
+        _no_gradient(pos, bias)
         if g.num_dst == x8.shape[0]:
             q, k, v = self.fc((x8, scale)).split([self.H * self.F, self.K * self.F, self.K * self.F], 1)
         else:

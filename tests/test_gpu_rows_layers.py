@@ -297,6 +297,18 @@ def test_gradients_of_a_bias_are_not_dropped():
         assert conv(gr, (q, s), bias=bias).shape == (40, 2, 8)
 
 
+@pytest.mark.parametrize("qk_norm", [True, False])
+def test_gradients_of_positions_are_not_dropped(qk_norm):
+    conv = nn.DotAttentionConv8(nn.DotAttentionConv(32, 8, 2, qk_norm=qk_norm, axis_pairs=(2, 1)).cuda())
+    gr, _ = graph(40, 40, 300, 5)
+    x, pos = normal(gen(44), 40, 32).cuda(), normal(gen(45), 40, 2).cuda()
+    want = conv(gr, x, pos)
+    with pytest.raises(ValueError, match="gradient"):
+        conv(gr, x, pos.requires_grad_(True))
+    with torch.no_grad():
+        assert torch.equal(conv(gr, x, pos), want)
+
+
 def test_the_two_gradients_are_tensors_of_their_own():
     g = gen(43)
     for use in range(3):
