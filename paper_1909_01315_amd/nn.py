@@ -487,7 +487,7 @@ class Linear8(torch.nn.Module):
         super().__init__()
         self.dtype = dtype or weight.dtype
         self.weight = gnnk.Weight8.quantize(weight)
-        self.bias = bias.detach().to(self.dtype).contiguous() if bias is not None else None
+        self.bias = bias.detach().to(self.dtype, copy=True).contiguous() if bias is not None else None
 
     @classmethod
     def of(cls, linear: torch.nn.Linear, dtype=None) -> "Linear8":
@@ -511,7 +511,7 @@ class DotAttentionConv8(torch.nn.Module):
         self.fc = Linear8(both, dtype=self.dtype)
         self.fc_q = Linear8(conv.fc_q.weight, dtype=self.dtype)
         self.fc_kv = Linear8(both[self.H * self.F:], dtype=self.dtype)
-        weight = lambda w: w.detach().to(self.dtype) if w is not None else None
+        weight = lambda w: w.detach().to(self.dtype, copy=True) if w is not None else None
         self.norm_q, self.norm_k, self.rotary = weight(conv.norm_q), weight(conv.norm_k), conv.rotary
 
     def forward(self, g, x, pos=None, bias=None):

@@ -309,6 +309,22 @@ def test_gradients_of_positions_are_not_dropped(qk_norm):
         assert torch.equal(conv(gr, x, pos), want)
 
 
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_layers_in_8_bits_stay_as_they_were_made(dtype):
+    """What a later step does to the layers that they were made from changes nothing in them."""
+    torch.manual_seed(11)
+    linear = torch.nn.Linear(48, 30).cuda().to(dtype)
+    conv = nn.DotAttentionConv(48, 16, 2, axis_pairs=(4, 4)).cuda().to(dtype)
+    layer, conv8 = nn.Linear8.of(linear), nn.DotAttentionConv8(conv)
+    gr, _ = graph(70, 50, 600, 6)
+    x, pos = normal(gen(46), 70, 48, dtype=dtype).cuda(), normal(gen(47), 70, 2).cuda()
+    want = layer(x), conv8(gr, x, pos)
+    with torch.no_grad():
+        for p in [*linear.parameters(), *conv.parameters()]:
+            p.mul_(3.0).add_(1.0)
+    assert torch.equal(layer(x), want[0]) and torch.equal(conv8(gr, x, pos), want[1])
+
+
 def test_the_two_gradients_are_tensors_of_their_own():
     g = gen(43)
     for use in range(3):
