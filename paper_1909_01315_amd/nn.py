@@ -512,7 +512,10 @@ class DotAttentionConv8(torch.nn.Module):
         self.fc_q = Linear8(conv.fc_q.weight, dtype=self.dtype)
         self.fc_kv = Linear8(both[self.H * self.F:], dtype=self.dtype)
         weight = lambda w: w.detach().to(self.dtype, copy=True) if w is not None else None
-        self.norm_q, self.norm_k, self.rotary = weight(conv.norm_q), weight(conv.norm_k), conv.rotary
+        self.norm_q, self.norm_k = weight(conv.norm_q), weight(conv.norm_k)
+        self.axis_pairs, self.base, self.interleaved, self._rotary = conv.axis_pairs, conv.base, conv.interleaved, {}
+
+    rotary = DotAttentionConv.rotary
 
     def forward(self, g, x, pos=None, bias=None):
         x8, scale = _rows8(x)

@@ -2,7 +2,9 @@
 autograd form against differences and its operators, the layers as exactly the
 chains of their operators, replays, streams and long strides."""
 import copy
+import gc
 import io
+import weakref
 
 import pytest
 import torch
@@ -323,6 +325,26 @@ def test_layers_in_8_bits_stay_as_they_were_made(dtype):
         for p in [*linear.parameters(), *conv.parameters()]:
             p.mul_(3.0).add_(1.0)
     assert torch.equal(layer(x), want[0]) and torch.equal(conv8(gr, x, pos), want[1])
+
+
+def test_layers_in_8_bits_hold_nothing_of_the_layers_they_were_made_from():
+    conv = nn.DotAttentionConv(512, 64, 8, axis_pairs=(16, 16)).cuda()
+    conv8 = nn.DotAttentionConv8(conv)
+    gr, _ = graph(40, 40, 300, 5)
+    x, pos = normal(gen(48), 40, 512).cuda(), normal(gen(49), 40, 2).cuda()
+    want = conv8(gr, x, pos)
+    ref = weakref.ref(conv)
+    floats = sum(p.numel() * p.element_size() for p in conv.parameters())
+    del conv
+    gc.collect()
+    assert ref() is None
+    buf = io.BytesIO()
+    torch.save(conv8, buf)
+    # the projections are kept twice, once joined, a quarter of their floats each
+    assert buf.tell() < 0.6 * floats
+    buf.seek(0)
+    for other in (copy.deepcopy(conv8), torch.load(buf, weights_only=False)):
+        assert torch.equal(other(gr, x, pos), want)
 
 
 def test_the_two_gradients_are_tensors_of_their_own():
