@@ -156,3 +156,43 @@ def test_a_layer_from_the_stream_to_its_outputs(n, k, o, dtype):
     step = 0.5 * s.cpu().double().view(-1, 1) * lw.double().abs().sum(1) + \
         0.5 * ws.cpu().double() * (y.abs().sum(1, keepdim=True) + k * s.cpu().double().view(-1, 1))
     close(out, want, step + 1e-4 * want.abs(), "layer")
+
+
+def many_tiles(n, k, o, dtype, tiles, bias, step):
+    """Kernels `tiles` on more tiles than their blocks hold at once, rows of a stride that is a multiple of `step` bytes:
+    three times the same bits as tiles through registers, whose first, last and some other rows are checked."""
+    g = torch.Generator(device="cuda")
+    g.manual_seed(n + k + o)
+    whole = lambda *shape: torch.randint(-128, 128, shape, generator=g, device="cuda", dtype=torch.int8)
+    scales = lambda m: torch.rand(m, generator=g, device="cuda") * 0.01 + 0.001
+    q, s, wq, ws = whole(n, (k + step - 1) // step * step)[:, :k], scales(n), whole(o, k), scales(o)
+    b = torch.randn(o, generator=g, device="cuda").to(dtype) if bias else None
+    weight = gnnk.Weight8(wq, ws)
+    gnnk.set_option("linear8_tile", 3)
+    want = gnnk.node_linear_i8(weight, q, s, bias=b, dtype=dtype)
+    at = torch.cat([torch.arange(40), torch.arange(n - 300, n), torch.randint(0, n, (60,))]).cuda()
+    close(want[at], *product(q[at], s[at], wq, ws, b.cpu() if bias else None), "tiles through registers")
+    for tile in tiles:
+        gnnk.set_option("linear8_tile", tile)
+        for _ in range(3):
+            out = torch.full_like(want, float("nan"))
+            gnnk.node_linear_i8(weight, q, s, bias=b, out=out)
+            assert torch.equal(out, want), (tile, int((out != want).sum()))
+
+
+# 41,041 rows to 1,030 outputs are 2,889 tiles of 128, 512 of them at once, or 805 of 256, 256 at once; the last of
+# rows and of outputs are no whole ones.  One, two, three and eight steps; last steps of 2 and 15 bytes, of whole
+# vectors and of others; rows that start on words and on vectors
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("bias", [False, True])
+@pytest.mark.parametrize("k,step", [(128, 16), (100, 4), (130, 4), (143, 16), (250, 4), (256, 16), (300, 4), (384, 4), (1000, 16),
+                                    (1001, 4)])
+def test_deep_tiles_one_after_another(k, step, bias, dtype):
+    many_tiles(41041, k, 1030, dtype, (4, 5), bias, step)
+
+
+# outputs of more than 192 MB, which these kernels store past the caches
+@pytest.mark.parametrize("n,k,o,dtype", [(100003, 257, 1027, BF16), (50021, 512, 1030, F32)])
+def test_large_outputs(n, k, o, dtype):
+    assert n * o * (4 if dtype is F32 else 2) > 192 << 20
+    many_tiles(n, k, o, dtype, (4, 5, 6, 7), True, 4)
