@@ -181,7 +181,9 @@ __device__ __forceinline__ void load_scales(const Linear8Args& A, int64_t m, flo
 
 // 16 bytes a lane from memory, at `from` + `off`, into LDS at `to` + 16 * lane
 // (one `from` and `to` for all lanes).  It counts as a load of the wavefront's
-// (vmcnt) that the compiler does not see: waits for it are written out.
+// (vmcnt) that the compiler does not see: waits for it are written out.  It
+// writes m0, which the compiler reserves and so does not take as a clobber; its
+// own code for these kernels has no instruction that reads or writes m0.
 __device__ __forceinline__ void load_to_lds(const int8_t* from, uint32_t off, uint32_t to) {
     asm volatile("s_mov_b32 m0, %0\n\ts_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"s"(to), "v"(off), "s"(from)
                  : "memory");
