@@ -56,10 +56,11 @@ def test_rows_of_one_length(H, K, F, dtype, n):
     gr = gnnk.Graph.from_coo(src, dst, n, n)
     q, z = (torch.randn((n, H, F), generator=g).to(dtype).cuda() for _ in range(2))
     k, v = (torch.randn((n, K, F), generator=g).to(dtype).cuda() for _ in range(2))
-    graphs = []
+    graphs, kept = [], []
     for deg in (-1, 8, 32):  # the library's choice, wavefronts, lane groups
         gnnk.set_option("small_deg", deg)
         out, stats = gnnk.dot_aggregate(gr, q, k, v, want_stats=True)
+        kept.append((out, stats))  # (the captured calls hold their addresses)
         graphs.append(captured(lambda: gnnk.dot_aggregate(gr, q, k, v, out=out, stats=stats)))
         graphs.append(captured(lambda: gnnk.dot_aggregate_backward(gr, q, k, v, out, stats, z)))
     t = best(graphs)
