@@ -570,10 +570,12 @@ typedef struct {
  * The norm is that of the whole row, all heads, and of the sum before it is
  * rounded.  x, residual (nullable: none, then sum must be NULL), sum (nullable)
  * and out are of one shape and dtype, at most 16,384 columns, fewer than 2^31
- * rows; w (nullable: all ones) is one row.  The sum of a row's squares is fp32;
- * eps >= 0.  sum or out may be x or residual itself (the same rows at the same
- * address); no output may overlap an operand or the other output otherwise.
- * Errors: GNNK_EINVAL on shapes, dtypes and overlaps. */
+ * rows; w (nullable: all ones) is one row.  The sum of a row's squares is fp32,
+ * in an order that depends on its columns and on whether the call has 4,096 rows
+ * or more, not on the row's place; eps >= 0.  sum or out may be x or residual
+ * itself (the same rows at the same address); no output may overlap an operand
+ * or the other output otherwise.  Errors: GNNK_EINVAL on shapes, dtypes and
+ * overlaps. */
 gnnk_status node_add_norm(const gnnk_tensor* x, const gnnk_tensor* residual, const gnnk_tensor* w, float eps,
                           gnnk_tensor* sum, gnnk_tensor* out, hipStream_t stream);
 

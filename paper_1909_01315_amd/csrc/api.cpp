@@ -1714,8 +1714,8 @@ Span flat(const void* p, int64_t bytes) { return Span{(uintptr_t)p, bytes > 0 ? 
 // registers and sums besides: half as many vectors a lane where eight
 // wavefronts hold the row all the same (65,536 rows of 4,096 bf16 606 -> 451 us).
 // Three vectors a lane where four would leave a quarter of them idle (100,000 of
-// 1,500 bf16 to 8 bits 107 -> 92 us, with the norm 289 -> 236).  Where there are
-// rows enough, rows lie in fewer lanes if
+// 1,500 bf16 to 8 bits 107 -> 92 us, with the norm 289 -> 236).  From 4,096 rows
+// on, rows lie in fewer lanes if
 //  - they are rounded to 8 bits without a norm, of which a lane has little to load:
 //    16 or 32 lanes of up to four vectors (262,144 of 256 fp32 71 -> 59 us, 232,965
 //    of 512 bf16 76 -> 64);
@@ -1726,6 +1726,11 @@ Span flat(const void* p, int64_t bytes) { return Span{(uintptr_t)p, bytes > 0 ? 
 //  - most lanes would hold a row's last vector, whose columns are checked, and no
 //    other: 32 of two vectors (200,000 of 501 bf16 163 -> 146, with the norm in 8
 //    bits 172 -> 144, backward 175 -> 171).
+// At the border both sides are a few us apart at most: with and without, 4,096 rows
+// of 501 bf16 5.4 and 5.8 us, backward 5.5 and 6.1, 1,000 rows 4.3 and 4.1, 4.5 and
+// 4.1; of 256 fp32 to 8 bits 2.9 and 4.1, 1,000 rows 2.8 and 4.0; of 282 bf16 with
+// the norm in 8 bits 5.2 and 7.7, 1,000 rows 4.9 and 6.7.  (In 8 bits fewer lanes
+// gain at any count.)
 int add_norm_geo(AddNormArgs& A, const gnnk_tensor* x, AddNormMode mode) {
     A.C = (int32_t)cols_of(x);
     A.inv_C = 1.0f / (float)A.C;

@@ -23,9 +23,10 @@
 //   stream  262,144 x 256 to 768 81 us (5.8 TB/s; a fill of the output alone 59),
 //           232,965 x 512 to 512 83 (4.3 TB/s, rows read once a panel), 20,011 x
 //           282 to 141 of fp32 8.4
-//   deep    16,384 x 4,096 to 4,096 208 us when the chip is cool (2.64 POP/s), 229
-//           without a pause (2.40; the vector and LDS work aside, the matrix
-//           instructions alone take 130 at the 4.2 POP/s that random bytes allow)
+//   deep    16,384 x 4,096 to 4,096 212 us (2.6 POP/s), 229 to 239 where rows lie
+//           4,096 bytes apart; x 2,048 124, x 8,192 396: 1.4 us a tile and step,
+//           of which the matrix instructions alone take 1.02 (4.2 POP/s on random
+//           bytes, 4.9 on zeros), and 8 us a tile besides, its stores among them
 //   tile    100,000 x 1,501 to 1,500 430 us (1.05 POP/s), at addresses that loads
 //           into LDS do not take
 #include "words.h"
@@ -524,7 +525,9 @@ __global__ __launch_bounds__(WM * 128, BLOCKS) void linear8_deep_kernel(Linear8A
     bool drained = true;
     for (int turn = 0; at.there; turn ^= 1) {
         // the first step is there; what may be on its way: the second one, and
-        // the stores of a whole tile before
+        // the stores of a whole tile before, one for each four sums.  (Of a last
+        // step that load_x reads there may be fewer loads, but it waits for its
+        // own, and so for all before them)
         if (drained || S == 1)
             asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
         else
@@ -756,8 +759,7 @@ void launch_stream(const Linear8Args& a, hipStream_t s) {
     constexpr int CUS = 32;  // of a die
     const int NB = (a.N + 63) / 64, most = LDS_BYTES / (KS * WBLOCK + 512);
     StreamArgs g;
-    g.panels = (NB + most - 1) / most;
-    if (g.panels > CUS) g.panels = CUS;  // (not reached: see launch_t)
+    g.panels = (NB + most - 1) / most;  // (at most CUS: of 64 blocks at least two a panel)
     g.width = (NB + g.panels - 1) / g.panels;
     const int runs = CUS / g.panels * 8;
     const int64_t tiles = (a.M + MI * 16 - 1) / (MI * 16);

@@ -17,9 +17,12 @@
 // (5.8), 232,965 of 512 bf16 with the norm in 8 bits in 139 (6.0), 100,000 of 376
 // fp32 to 8 bits in 34 (5.6).  The backward reads three rows for one that it
 // writes: 210 us and 11 for the weight's gradient on the first (5.1).  Rows of
-// 282 bf16, which start on no vector, are bound by instructions too: 300,000 of
-// them 129 us (5.2 TB/s), with the norm in 8 bits 127 (4.7), backward 165 (4.1);
-// 20,011 of them, a short grid, 12 us, backward 17 and 5.  One row: 2.4 us.
+// 282 bf16, which start on no vector, are slower: 300,000 of them 129 us (5.2
+// TB/s), with the norm in 8 bits 127 (4.7), backward 165 (4.1).  What bounds them
+// is not shown: 0.58, 0.76 and 0.92 vector instructions in a SIMD's four cycles,
+// at 3.7, 3.6 and 2.8 wavefronts a SIMD, where rows of 288, whole vectors, issue
+// 0.87, 0.70 and 1.23 at 7.2, 3.6 and 4.6.  20,011 of them, a short grid, 12 us,
+// backward 17 and 5.  One row: 2.4 us.
 //
 // Sums over a row are fp32, over at most 32 terms a lane and then pairs of
 // lanes; the gradient of the weight is a sum over all rows, fp32 within a lane's

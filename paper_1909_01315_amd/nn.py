@@ -480,8 +480,9 @@ class Linear8(torch.nn.Module):
     """A linear layer for inference with its weight in 8 bits, a scale for each
     output: of a tensor, whose rows are rounded to 8 bits with a scale each, or
     of rows that are (q, scale) already.  The result is of the type of the
-    weight that it was made from, or `dtype`.  It has no parameters: it is made
-    anew from a weight that changes, and copied and pickled whole."""
+    weight that it was made from, or `dtype`.  It has no parameters and no
+    buffers: it is made anew from a weight that changes, on the device of that
+    weight, where it stays (`to` moves nothing), and copied and pickled whole."""
 
     def __init__(self, weight: torch.Tensor, bias: torch.Tensor = None, dtype=None):
         super().__init__()
@@ -501,7 +502,9 @@ class DotAttentionConv8(torch.nn.Module):
     """A DotAttentionConv for inference with its projections in 8 bits, keys and
     values (and queries, where every source is a destination) in one product.
     The nodes' features are a tensor or rows in 8 bits, (q, scale), as
-    AddNorm.rows8 leaves them."""
+    AddNorm.rows8 leaves them.  It is a copy of the layer's weights as they
+    are, on their device, and holds them twice: in one product for graphs
+    whose sources are their destinations, in two for others."""
 
     def __init__(self, conv: DotAttentionConv, dtype=None):
         super().__init__()
